@@ -10,8 +10,10 @@ import tempfile
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libtessel_hip.so")
-SOURCES = ["tessel_kernels.hip", "tessel_wide.hip", "tessel_graph.hip", "tessel_mail.hip", "tessel_api.cpp"]
-HEADERS = ["tessel_device.h", "tessel_common.h", os.path.join("..", "..", "include", "tessel.h")]
+SOURCES = ["tessel_kernels.hip", "tessel_wide.hip", "tessel_graph.hip", "tessel_mail.hip", "tessel_api.cpp",
+           "tessel_attention.hip", "tessel_norm.hip", "tessel_checkpoint.hip", "tessel_weight.hip", "tessel_block_api.cpp"]
+HEADERS = ["tessel_device.h", "tessel_common.h", os.path.join("..", "..", "include", "tessel.h"),
+           "tessel_block.h", "tessel_tile.h", "tessel_rows.h", os.path.join("..", "..", "include", "tessel_block_ops.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",

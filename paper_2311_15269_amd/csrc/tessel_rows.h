@@ -1,0 +1,88 @@
+// Rows of values of the three element types, eight at a time, and activation checkpoints.  (Included by kernel sources only.)
+#pragma once
+#include "tessel_block.h"
+#include "tessel_tile.h"
+
+namespace tessel {
+
+constexpr int kGroup = TESSEL_CHECKPOINT_GROUP;
+
+// Eight neighbouring values.  Rows of an odd number of channels start anywhere, so the loads and stores ask for no more than the
+// element's alignment (the memory path takes 16 bytes at any address).
+template <typename T> struct Eight {
+    typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+};
+
+// values col .. col + 7 of a row of `channels`, zeros behind its end
+template <typename T>
+__device__ __forceinline__ void load8(float *v, const T *row, int col, int channels)
+{
+    if (col + 8 <= channels) {
+        const typename Eight<T>::type w = *(const typename Eight<T>::type *)(row + col);
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = (float)w[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = col + j < channels ? (float)row[col + j] : 0.0f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *row, const float *v, int col, int channels)
+{
+    if (col + 8 <= channels) {
+        typename Eight<T>::type w;
+#pragma unroll
+        for (int j = 0; j < 8; j++) w[j] = (T)v[j];
+        *(typename Eight<T>::type *)(row + col) = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            if (col + j < channels) row[col + j] = (T)v[j];
+    }
+}
+
+// exponents of a checkpoint as they are held, e + 127: the least of a type, and the one at which 64 2^e leaves its range
+template <typename T> __device__ __forceinline__ constexpr uint32_t least_exponent() { return __is_same(T, f16) ? 103u : 1u; }
+template <typename T> __device__ __forceinline__ constexpr uint32_t top_exponent() { return __is_same(T, f16) ? 137u : 249u; }
+
+// Eight lanes hold a group of 64 channels, eight each: its exponent (0: not finite), and this lane's values as bytes.
+template <typename T>
+__device__ __forceinline__ uint32_t hold8(const float *v, uint2 &bytes)
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 8; j++) most = max(most, __float_as_uint(v[j]) & 0x7FFFFFFFu);          // (as whole numbers: NaN is above infinity)
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    // most = 2^E m with 1 <= m < 2: 2^(E - 6) if m < 127.5 / 64 (its upper mantissa bits are not all ones), else the next
+    uint32_t e = (most >> 23) + ((most & 0x7F0000u) == 0x7F0000u ? 1u : 0u);
+    e = max(e, least_exponent<T>() + 6u) - 6u;
+    const bool finite = most < 0x7F800000u;
+    const float by = __uint_as_float((254u - e) << 23), limit = e >= top_exponent<T>() ? 63.0f : 127.0f;
+    bytes = make_uint2(0, 0);
+    if (finite) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int q = (int)fminf(fmaxf(rintf(v[j] * by), -limit), limit);
+            (j < 4 ? bytes.x : bytes.y) |= (uint32_t)(q & 255) << (8 * (j & 3));
+        }
+    }
+    return finite ? e : 0u;
+}
+
+// the values of eight bytes under an exponent
+__device__ __forceinline__ void held8(float *v, uint2 bytes, uint32_t e)
+{
+    const float by = e == 0u ? __uint_as_float(0x7FC00000u) : __uint_as_float(e << 23);
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = (float)(int8_t)((j < 4 ? bytes.x : bytes.y) >> (8 * (j & 3))) * by;
+}
+
+inline int launched(hipError_t e)
+{
+    if (e != hipSuccess) (void)hipGetLastError();
+    return (int)e;
+}
+
+}  // namespace tessel

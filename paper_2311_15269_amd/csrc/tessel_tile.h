@@ -1,0 +1,91 @@
+// Matrix tiles of the block operators: element types, matrix instructions, layouts in LDS.  (Included by kernel sources only.)
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace tessel {
+
+typedef __bf16   bf16;
+typedef _Float16 f16;
+typedef short    short4v __attribute__((ext_vector_type(4)));
+typedef short    short8v __attribute__((ext_vector_type(8)));
+typedef float    float4v __attribute__((ext_vector_type(4)));
+typedef float    float16v __attribute__((ext_vector_type(16)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4v lds_short4v;
+
+// Eight values of a type, as one operand of a matrix instruction.
+template <typename T> struct Vec8;
+template <> struct Vec8<bf16> { typedef bf16 type __attribute__((ext_vector_type(8))); };
+template <> struct Vec8<f16> { typedef f16 type __attribute__((ext_vector_type(8))); };
+
+// c += a b, 32 x 16 times 16 x 32.  a: lane holds row lane % 32, columns 8 (lane / 32) + 0..7; b: column lane % 32, rows
+// 8 (lane / 32) + 0..7; c: column lane % 32, register i row 8 (i / 4) + 4 (lane / 32) + i % 4.
+template <typename T>
+__device__ __forceinline__ float16v mma(uint4v a, uint4v b, float16v c)
+{
+    typedef typename Vec8<T>::type V;
+    if constexpr (__is_same(T, bf16))
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+}
+
+// two values rounded to the nearest, as one word
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float x, float y)
+{
+    typedef T V __attribute__((ext_vector_type(2)));
+    V v = {(T)x, (T)y};
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// Registers 8 s .. 8 s + 7 of a product's c as the b operand of the next product: the summed index of that operand's
+// slot (lane / 32, j) is then 16 s + 8 (j / 4) + 4 (lane / 32) + j % 4, and its a operand is read in the same order.
+template <typename T>
+__device__ __forceinline__ uint4v operand(const float16v &c, int s)
+{
+    uint4v r;
+#pragma unroll
+    for (int j = 0; j < 4; j++) r[j] = pack2<T>(c[8 * s + 2 * j], c[8 * s + 2 * j + 1]);
+    return r;
+}
+
+// A tile of rows of W values (2 bytes each) in LDS, rows packed, chunks of 16 bytes of a row swapped so that both ways
+// of reading touch all banks: 16 rows at one column (row operands), and 4 rows x 32 columns (transposing reads).
+template <int W>
+__device__ __forceinline__ int chunk_at(int row, int chunk)          // in chunks of 16 bytes
+{
+    if constexpr (W == 128) return row * 16 + (chunk ^ ((row & 3) << 2 | (row >> 2 & 3)));
+    else return row * 8 + (chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3)));
+}
+
+// a operand of 32 rows from `row`, columns 16 s .. 16 s + 15 (also a b operand of 32 columns, for a tile that holds columns as rows)
+template <int W>
+__device__ __forceinline__ uint4v row_operand(const uint4v *tile, int row, int s)
+{
+    const int lane = threadIdx.x & 63;
+    return tile[chunk_at<W>(row + (lane & 31), 2 * s + (lane >> 5))];
+}
+
+// a operand whose rows are the tile's columns 32 b .. 32 b + 31 and whose summed index are the tile's rows row .. row + 15 in
+// the order of operand(): two transposing reads, of which each group of 16 lanes takes 4 rows x 16 columns.
+template <int W>
+__device__ __forceinline__ uint4v column_operand(const uint4v *tile, int row, int b)
+{
+    const int lane = threadIdx.x & 63, i = lane & 15;
+    const int r = row + 4 * (lane >> 5) + (i >> 2);
+    const int chunk = 4 * b + 2 * (lane >> 4 & 1) + (i >> 1 & 1);
+    const char *p = (const char *)tile;
+    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(p + 16 * chunk_at<W>(r, chunk) + 8 * (i & 1)));
+    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(p + 16 * chunk_at<W>(r + 8, chunk) + 8 * (i & 1)));
+    return __builtin_bit_cast(uint4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// the other half-wave's value of the same column
+__device__ __forceinline__ float other_half(float x)
+{
+    return __shfl_xor(x, 32);
+}
+
+}  // namespace tessel

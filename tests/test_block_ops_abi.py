@@ -1,0 +1,220 @@
+"""include/tessel_block_ops.h: every declared symbol is exported and bound, and what the library refuses before it touches a GPU.
+No GPU, no compute calls."""
+import ctypes as C
+import os
+import re
+
+import pytest
+
+from paper_2311_15269_amd import binding, block_ops as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, INVALID, TOOBIG, WORKSPACE, UNSUPPORTED = 0, -1, -4, -5, -9
+
+
+def test_library_exports_every_declared_symbol():
+    text = open(os.path.join(ROOT, "include", "tessel_block_ops.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = sorted(set(re.findall(r"\b(tessel_[a-z_]+)\s*\(", text)))
+    assert names == sorted(B.EXPORTS)
+    lib = B._library()
+    for name in names:
+        assert getattr(lib, name) is not None
+
+
+def packing(lengths, total=None):
+    array = (C.c_int32 * max(1, len(lengths)))(*lengths)
+    h = C.c_void_p()
+    rc = B._library().tessel_packing_create(array, len(lengths), sum(lengths) if total is None else total, C.byref(h))
+    return rc, h
+
+
+def test_packing_checks_its_lengths():
+    lib = B._library()
+    for lengths, total, code in (([], 0, OK), ([], 5, OK), ([0, 0], 0, OK), ([3, 0, 4], 9, OK), ([3, -1], 9, INVALID), ([3, 4], 6, INVALID),
+                                 ([1], -1, INVALID), ([1], 1 << 31, TOOBIG)):
+        rc, h = packing(lengths, total)
+        assert rc == code, (lengths, total)
+        assert bool(h.value) == (code == OK)
+        if rc == OK:
+            n = C.c_size_t()
+            assert lib.tessel_packing_table_bytes(h, C.byref(n)) == OK and n.value >= 16
+            lib.tessel_packing_destroy(h)
+    assert lib.tessel_packing_create(None, 2, 4, C.byref(C.c_void_p())) == INVALID
+    assert lib.tessel_packing_create(None, 0, 4, None) == INVALID
+    assert lib.tessel_packing_bind(None, 256, 64, None) == INVALID
+    # 300 sequences of 129 tokens (two tiles each), 130 tokens behind them (two more): 16 bytes a tile
+    rc, h = packing([129] * 300, 129 * 300 + 130)
+    n = C.c_size_t()
+    assert lib.tessel_packing_table_bytes(h, C.byref(n)) == OK and n.value == 602 * 16
+    assert lib.tessel_packing_bind(h, None, n.value, None) == WORKSPACE
+    assert lib.tessel_packing_bind(h, 256 + 8, n.value, None) == WORKSPACE
+    assert lib.tessel_packing_bind(h, 256, n.value - 1, None) == WORKSPACE
+    lib.tessel_packing_destroy(h)
+
+
+AT = 1 << 20          # an aligned address that no call below reads
+
+
+def attention(**change):
+    def heads(n):
+        return B.Heads(AT, n * 64, 64)
+    a = B.Attention(type=0, heads=4, kv_heads=2, dim=64, scale=0.125, q=heads(4), k=heads(2), v=heads(2), o=heads(4), lse=AT, d_o=heads(4),
+                    dq=heads(4), dk=heads(2), dv=heads(2))
+    for name, value in change.items():
+        setattr(a, name, value)
+    return a
+
+
+@pytest.mark.parametrize("change, code", [
+    ({}, WORKSPACE),                                            # valid; the packing is not bound
+    ({"type": 2}, UNSUPPORTED), ({"type": 7}, UNSUPPORTED), ({"dim": 60}, UNSUPPORTED), ({"dim": 136}, UNSUPPORTED), ({"dim": 0}, INVALID),
+    ({"heads": 0}, INVALID), ({"kv_heads": 3}, INVALID), ({"kv_heads": 0}, INVALID), ({"kv_heads": 8}, INVALID),
+    ({"scale": 0.0}, INVALID), ({"scale": -1.0}, INVALID), ({"scale": float("nan")}, INVALID), ({"scale": float("inf")}, INVALID),
+    ({"q": B.Heads(None, 256, 64)}, INVALID), ({"q": B.Heads(AT + 8, 256, 64)}, INVALID), ({"k": B.Heads(AT, 132, 64)}, INVALID),
+    ({"v": B.Heads(AT, -128, 64)}, INVALID), ({"v": B.Heads(AT, 128, 4)}, INVALID), ({"k": B.Heads(AT, 0, 0)}, WORKSPACE),
+    ({"o": B.Heads(AT, 32, 64)}, INVALID), ({"o": B.Heads(AT, 256, 32)}, INVALID), ({"lse": None}, INVALID), ({"heads": 1 << 30, "kv_heads": 1}, TOOBIG),
+])
+def test_attention_forward_refuses(change, code):
+    rc, h = packing([5, 300])
+    lib = B._library()
+    a = attention(**change)
+    assert lib.tessel_attention_forward(h, C.byref(a), None) == code
+    lib.tessel_packing_destroy(h)
+
+
+@pytest.mark.parametrize("change, code", [
+    ({}, WORKSPACE), ({"type": 2}, UNSUPPORTED), ({"d_o": B.Heads(AT + 2, 256, 64)}, INVALID), ({"dq": B.Heads(AT, 8, 64)}, INVALID),
+    ({"dk": B.Heads(None, 128, 64)}, INVALID), ({"dv": B.Heads(AT, 128, 8)}, INVALID), ({"d_o": B.Heads(AT, 0, 0)}, WORKSPACE), ({"lse": 0}, INVALID),
+])
+def test_attention_backward_refuses(change, code):
+    rc, h = packing([5, 300])
+    lib = B._library()
+    a = attention(**change)
+    assert lib.tessel_attention_backward(h, C.byref(a), AT, 1 << 30, None) == code
+    n = C.c_size_t()
+    if code == WORKSPACE:
+        assert lib.tessel_attention_backward_workspace_bytes(h, C.byref(a), C.byref(n)) == OK and n.value >= 4 * 4 * 305
+    assert lib.tessel_attention_backward_workspace_bytes(h, C.byref(a), None) == INVALID
+    lib.tessel_packing_destroy(h)
+
+
+def test_attention_over_no_tokens_does_nothing():
+    rc, h = packing([0, 0])
+    a = attention(q=B.Heads(None, 0, 0))
+    assert B._library().tessel_attention_forward(h, C.byref(a), None) == OK
+    assert B._library().tessel_attention_backward(h, C.byref(a), None, 0, None) == OK
+    assert B._library().tessel_attention_forward(None, C.byref(a), None) == INVALID
+    assert B._library().tessel_attention_forward(h, None, None) == INVALID
+    B._library().tessel_packing_destroy(h)
+
+
+def norm(**change):
+    r = B.Rows(AT, 100)
+    a = B.ResidualNorm(type=0, gate_kind=0, tokens=7, channels=100, scale=1.0, eps=1e-6, x=r, y=r, pre=AT, post=AT, stats=AT, r=r, h=r, dr=r, dh=r,
+                       dx=r, dy=r, dgate=r, dpre=AT, dpost=AT, dgate_channel=AT)
+    for name, value in change.items():
+        setattr(a, name, value)
+    return a
+
+
+@pytest.mark.parametrize("change, code", [
+    ({"type": 3}, UNSUPPORTED), ({"channels": 0}, INVALID), ({"channels": 16385}, TOOBIG), ({"tokens": -1}, INVALID), ({"tokens": 1 << 31}, TOOBIG),
+    ({"gate_kind": 3}, INVALID), ({"gate_kind": 1}, INVALID), ({"gate_kind": 2}, INVALID), ({"eps": -1e-6}, INVALID),
+    ({"eps": float("nan")}, INVALID), ({"scale": float("inf")}, INVALID), ({"pre": None}, INVALID), ({"pre": AT + 2}, INVALID),
+    ({"post": AT + 1}, INVALID), ({"x": B.Rows(None, 100)}, INVALID), ({"y": B.Rows(AT + 1, 100)}, INVALID), ({"x": B.Rows(AT, -100)}, INVALID),
+    ({"r": B.Rows(AT, 99)}, INVALID), ({"h": B.Rows(None, 100)}, INVALID), ({"stats": None}, INVALID), ({"type": 2, "x": B.Rows(AT + 2, 100)}, INVALID),
+])
+def test_norm_forward_refuses(change, code):
+    a = norm(**change)
+    assert B._library().tessel_residual_norm_forward(C.byref(a), None) == code
+
+
+@pytest.mark.parametrize("change, code", [
+    ({"dr": B.Rows(None, 100)}, INVALID), ({"dh": B.Rows(AT + 1, 100)}, INVALID), ({"dx": B.Rows(AT, 50)}, INVALID), ({"dy": B.Rows(None, 0)}, INVALID),
+    ({"dpre": None}, INVALID), ({"dpost": None}, INVALID), ({"gate_kind": 1, "gate": B.Rows(AT, 0), "dgate_channel": None}, INVALID),
+    ({"gate_kind": 2, "gate": B.Rows(AT, 100), "dgate": B.Rows(AT, 1)}, INVALID), ({"type": -1}, UNSUPPORTED), ({}, WORKSPACE),
+])
+def test_norm_backward_refuses(change, code):
+    a = norm(**change)
+    lib = B._library()
+    assert lib.tessel_residual_norm_backward(C.byref(a), None, 0, None) == code
+    n = C.c_size_t()
+    assert lib.tessel_residual_norm_backward_workspace_bytes(C.byref(a), C.byref(n)) == OK
+    if code == WORKSPACE:
+        assert lib.tessel_residual_norm_backward(C.byref(a), AT, n.value - 1, None) == WORKSPACE
+        assert lib.tessel_residual_norm_backward(C.byref(a), AT + 4, n.value, None) == WORKSPACE
+
+
+def kept(**change):
+    c = B.CheckpointDesc(AT, AT, 128, 2, 9, 100, 0)
+    for name, value in change.items():
+        setattr(c, name, value)
+    return c
+
+
+BAD_CHECKPOINTS = [
+    ({"type": 4}, UNSUPPORTED), ({"tokens": -1}, INVALID), ({"channels": 0}, INVALID), ({"values": None}, INVALID), ({"values": AT + 8}, INVALID),
+    ({"exponents": None}, INVALID), ({"value_stride": 120}, INVALID), ({"value_stride": 64}, INVALID), ({"exponent_stride": 1}, INVALID),
+    ({"tokens": 1 << 31}, TOOBIG), ({"tokens": (1 << 31) - 1, "channels": 64}, TOOBIG),
+]
+
+
+@pytest.mark.parametrize("change, code", BAD_CHECKPOINTS)
+def test_checkpoint_calls_refuse(change, code):
+    lib = B._library()
+    c, good, x = kept(**change), kept(), B.Rows(AT, 100)
+    assert lib.tessel_checkpoint_store(C.byref(c), C.byref(x), None) == code
+    assert lib.tessel_checkpoint_restore(C.byref(c), C.byref(x), None) == code
+    assert lib.tessel_gated_forward(0, C.byref(x), C.byref(x), C.byref(x), C.byref(good), C.byref(c), None) == code
+    assert lib.tessel_gated_backward(0, C.byref(x), C.byref(c), C.byref(good), C.byref(x), C.byref(x), None, None) == code
+    a = B.WeightGrad(x=c, dy=x, outputs=100, dw=AT, dw_stride=100)
+    assert lib.tessel_weight_gradient(C.byref(a), AT, 1 << 40, None) == code
+
+
+def test_rows_and_gates_are_checked():
+    lib = B._library()
+    c, x = kept(), B.Rows(AT, 100)
+    for bad in (B.Rows(None, 100), B.Rows(AT + 1, 100), B.Rows(AT, -4)):
+        assert lib.tessel_checkpoint_store(C.byref(c), C.byref(bad), None) == INVALID
+        assert lib.tessel_checkpoint_restore(C.byref(c), C.byref(bad), None) == INVALID
+        assert lib.tessel_gated_forward(1, C.byref(x), C.byref(bad), C.byref(x), C.byref(c), C.byref(c), None) == INVALID
+        assert lib.tessel_gated_backward(1, C.byref(x), C.byref(c), C.byref(c), C.byref(x), C.byref(bad), None, None) == INVALID
+    narrow = B.Rows(AT, 99)
+    assert lib.tessel_checkpoint_restore(C.byref(c), C.byref(narrow), None) == INVALID
+    assert lib.tessel_gated_forward(1, C.byref(x), C.byref(x), C.byref(narrow), C.byref(c), C.byref(c), None) == INVALID
+    assert lib.tessel_gated_backward(1, C.byref(x), C.byref(c), C.byref(c), C.byref(x), C.byref(x), C.byref(narrow), None) == INVALID
+    assert lib.tessel_gated_forward(2, C.byref(x), C.byref(x), C.byref(x), C.byref(c), C.byref(c), None) == INVALID
+    for other in (kept(tokens=8), kept(channels=101), kept(type=1)):
+        assert lib.tessel_gated_forward(0, C.byref(x), C.byref(x), C.byref(x), C.byref(c), C.byref(other), None) == INVALID
+    empty = kept(tokens=0, values=None, exponents=None)
+    none = B.Rows(None, 0)
+    assert lib.tessel_checkpoint_store(C.byref(empty), C.byref(none), None) == OK
+    assert lib.tessel_gated_forward(0, C.byref(none), C.byref(none), C.byref(none), C.byref(empty), C.byref(empty), None) == OK
+
+
+@pytest.mark.parametrize("change, code", [
+    ({"outputs": 0}, INVALID), ({"dw": None}, INVALID), ({"dw": AT + 2}, INVALID), ({"dw_stride": 99}, INVALID), ({"dy": B.Rows(None, 50)}, INVALID),
+    ({"x": kept(type=2)}, UNSUPPORTED), ({"x": kept(tokens=4096)}, WORKSPACE),
+])
+def test_weight_gradient_refuses(change, code):
+    a = B.WeightGrad(x=kept(), dy=B.Rows(AT, 50), outputs=50, dw=AT, dw_stride=100)
+    for name, value in change.items():
+        setattr(a, name, value)
+    lib = B._library()
+    assert lib.tessel_weight_gradient(C.byref(a), None, 0, None) == code
+    if code == WORKSPACE:
+        n = C.c_size_t()
+        assert lib.tessel_weight_gradient_workspace_bytes(C.byref(a), C.byref(n)) == OK and n.value > 0
+        assert lib.tessel_weight_gradient(C.byref(a), AT, n.value - 1, None) == WORKSPACE
+
+
+def test_binding_refuses_what_it_can_see():
+    import torch
+    with pytest.raises(binding.TesselError):
+        B.checkpoint(torch.zeros(2, 64))                        # not on the GPU
+    with pytest.raises(binding.TesselError):
+        B._act("relu")
+    with pytest.raises(binding.TesselError) as e:
+        B._type(torch.zeros(1, dtype=torch.float64))
+    assert e.value.code == UNSUPPORTED
