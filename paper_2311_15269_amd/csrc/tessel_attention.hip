@@ -35,30 +35,6 @@ __device__ __forceinline__ const T *row_of(const tessel_heads &h, int64_t token,
 
 __device__ __forceinline__ uint4v load16(const void *p) { return *(const uint4v *)p; }
 
-// One tile of 64 rows x W on its way to LDS: global -> registers (fetch), registers -> LDS (put).  Rows from `rows` on and columns from
-// dim on are zeros.
-template <typename T, int W>
-struct Stage {
-    static constexpr int kChunks = W / 8, kPer = 64 * kChunks / kThreads;
-    uint4v v[kPer];
-    __device__ __forceinline__ void fetch(const T *base, int64_t stride, int rows, int dim)
-    {
-#pragma unroll
-        for (int i = 0; i < kPer; i++) {
-            const int n = threadIdx.x + i * kThreads, r = n / kChunks, c = n % kChunks;
-            v[i] = r < rows && 8 * c < dim ? load16(base + r * stride + 8 * c) : uint4v{0, 0, 0, 0};
-        }
-    }
-    __device__ __forceinline__ void put(uint4v *tile) const
-    {
-#pragma unroll
-        for (int i = 0; i < kPer; i++) {
-            const int n = threadIdx.x + i * kThreads;
-            tile[chunk_at<W>(n / kChunks, n % kChunks)] = v[i];
-        }
-    }
-};
-
 // the operand of this lane's row straight from memory: columns 16 s + 8 (lane / 32) + 0..7
 template <typename T, int W>
 __device__ __forceinline__ void fetch_rows(uint4v *v, const T *row, bool valid, int dim)
@@ -97,10 +73,19 @@ __device__ void clear_rows(const tessel_heads &h, int begin, int rows, int head,
         *(uint4v *)((T *)row_of<T>(h, begin + n / chunks, head) + 8 * (n % chunks)) = uint4v{0, 0, 0, 0};
 }
 
+// Zeros into tiles that will not be filled whole: heads narrower than the tile, or fewer rows than the tiles hold.
+template <int N, int W>
+__device__ __forceinline__ void clear_tiles(uint4v (*tiles)[64 * W / 8], int rows, int dim)
+{
+    if (dim == W && rows >= 128) return;
+    for (int n = threadIdx.x; n < N * 64 * W / 8; n += kThreads) tiles[0][n] = uint4v{0, 0, 0, 0};
+    __syncthreads();
+}
+
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
 {
-    __shared__ uint4v keys[64 * W / 8], values[64 * W / 8];
+    __shared__ uint4v buffers[4][64 * W / 8];
     int t, head;
     work_of(l.a.heads, t, head);
     const AttendTile tile = l.tiles[t];
@@ -124,17 +109,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
     const float by = l.a.scale * kLog2e, slack = 8.0f / by;
 
     const T *kp = row_of<T>(l.a.k, tile.begin, kv), *vp = row_of<T>(l.a.v, tile.begin, kv);
-    Stage<T, W> ks, vs;
-    ks.fetch(kp, l.a.k.token_stride, last, dim);
-    vs.fetch(vp, l.a.v.token_stride, last, dim);
-    for (int k0 = 0; k0 < last; k0 += 64) {
-        __syncthreads();
-        ks.put(keys);
-        vs.put(values);
-        __syncthreads();
+    clear_tiles<4, W>(buffers, last, dim);
+    Copy<T, W>::start(buffers[0], kp, l.a.k.token_stride, last, dim);
+    Copy<T, W>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
+    for (int k0 = 0, turn = 0; k0 < last; k0 += 64, turn ^= 2) {
+        const uint4v *keys = buffers[turn], *values = buffers[turn + 1];
+        __syncthreads();                                         // (this tile has arrived, and all are done with the one before)
         if (k0 + 64 < last) {
-            ks.fetch(kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
-            vs.fetch(vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
+            Copy<T, W>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
+            Copy<T, W>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
         }
         if (k0 > wfirst + 31) continue;
         float16v s[2] = {};
@@ -282,7 +265,7 @@ __device__ __forceinline__ float gradient_scale(const AttendLaunch &l)
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 {
-    __shared__ uint4v keys[64 * W / 8], values[64 * W / 8];
+    __shared__ uint4v buffers[4][64 * W / 8];
     int t, head;
     work_of(l.a.heads, t, head);
     const AttendTile tile = l.tiles[t];
@@ -308,17 +291,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     float16v dq[W / 32] = {};
 
     const T *kp = row_of<T>(l.a.k, tile.begin, kv), *vp = row_of<T>(l.a.v, tile.begin, kv);
-    Stage<T, W> ks, vs;
-    ks.fetch(kp, l.a.k.token_stride, last, dim);
-    vs.fetch(vp, l.a.v.token_stride, last, dim);
-    for (int k0 = 0; k0 < last; k0 += 64) {
-        __syncthreads();
-        ks.put(keys);
-        vs.put(values);
+    clear_tiles<4, W>(buffers, last, dim);
+    Copy<T, W>::start(buffers[0], kp, l.a.k.token_stride, last, dim);
+    Copy<T, W>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
+    for (int k0 = 0, turn = 0; k0 < last; k0 += 64, turn ^= 2) {
+        const uint4v *keys = buffers[turn], *values = buffers[turn + 1];
         __syncthreads();
         if (k0 + 64 < last) {
-            ks.fetch(kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
-            vs.fetch(vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
+            Copy<T, W>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
+            Copy<T, W>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
         }
 #pragma unroll
         for (int b = 0; b < 2; b++) {
@@ -354,8 +335,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
 {
-    __shared__ uint4v queries[64 * W / 8], grads[64 * W / 8];
-    __shared__ float4v lses[16], deltas[16];
+    __shared__ uint4v buffers[4][64 * W / 8];
+    __shared__ float4v numbers[2][2][16];                        // log-sums and deltas of a tile's queries
     int t, kv;
     work_of(l.a.kv_heads, t, kv);
     const AttendTile tile = l.tiles[t];
@@ -379,54 +360,57 @@ __global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
     const float by = l.a.scale * kLog2e;
     float16v dk[W / 32] = {}, dv[W / 32] = {};
 
-    for (int head = kv * shared; head < (kv + 1) * shared; head++) {
-        const T *qp = row_of<T>(l.a.q, tile.begin, head), *gp = row_of<T>(l.a.d_o, tile.begin, head);
-        const float *lp = l.a.lse + head * l.tokens + tile.begin, *dp = l.delta + head * l.tokens + tile.begin;
-        for (int q0 = first; q0 < tile.length; q0 += 64) {
-            Stage<T, W> qs, gs;
-            qs.fetch(qp + q0 * l.a.q.token_stride, l.a.q.token_stride, tile.length - q0, dim);
-            gs.fetch(gp + q0 * l.a.d_o.token_stride, l.a.d_o.token_stride, tile.length - q0, dim);
-            float row = 0;
-            if (threadIdx.x < 128) {
-                const int r = q0 + (threadIdx.x & 63);
-                row = r < tile.length ? (threadIdx.x < 64 ? lp[r] * kLog2e : dp[r]) : 0.0f;
+    // the tiles of all heads that share these keys, one behind the other
+    const int tiles = (tile.length - first + 63) / 64;
+    float number = 0;                                            // (on its way to LDS, one tile ahead)
+    auto fetch = [&](int n, int turn) {
+        const int head = kv * shared + n / tiles, q0 = first + n % tiles * 64, rows = tile.length - q0;
+        Copy<T, W>::start(buffers[2 * turn], row_of<T>(l.a.q, tile.begin + q0, head), l.a.q.token_stride, rows, dim);
+        Copy<T, W>::start(buffers[2 * turn + 1], row_of<T>(l.a.d_o, tile.begin + q0, head), l.a.d_o.token_stride, rows, dim);
+        if (threadIdx.x < 128) {
+            const int64_t at = head * l.tokens + tile.begin + q0 + min((int)threadIdx.x & 63, rows - 1);
+            number = threadIdx.x < 64 ? l.a.lse[at] * kLog2e : l.delta[at];
+        }
+    };
+    clear_tiles<4, W>(buffers, tile.length - first, dim);
+    fetch(0, 0);
+    for (int n = 0; n < tiles * shared; n++) {
+        const int turn = n & 1, q0 = first + n % tiles * 64;
+        const uint4v *queries = buffers[2 * turn], *grads = buffers[2 * turn + 1];
+        const float4v *lses = numbers[turn][0], *deltas = numbers[turn][1];
+        if (threadIdx.x < 128) ((float *)numbers[turn])[threadIdx.x] = number;
+        __syncthreads();
+        if (n + 1 < tiles * shared) fetch(n + 1, turn ^ 1);
+#pragma unroll
+        for (int b = 0; b < 2; b++) {
+            if (q0 + 32 * b + 31 < wfirst) continue;
+            float16v s = {}, d = {};
+#pragma unroll
+            for (int n = 0; n < W / 16; n++) {
+                s = mma<T>(row_operand<W>(queries, 32 * b, n), k[n], s);
+                d = mma<T>(row_operand<W>(grads, 32 * b, n), v[n], d);
             }
-            __syncthreads();
-            qs.put(queries);
-            gs.put(grads);
-            if (threadIdx.x < 128) (threadIdx.x < 64 ? (float *)lses : (float *)deltas)[threadIdx.x & 63] = row;
-            __syncthreads();
+            const bool edge = q0 + 32 * b < wfirst + 31 || q0 + 32 * b + 32 > tile.length;
 #pragma unroll
-            for (int b = 0; b < 2; b++) {
-                if (q0 + 32 * b + 31 < wfirst) continue;
-                float16v s = {}, d = {};
+            for (int i = 0; i < 4; i++) {
+                const float4v lse = lses[8 * b + 2 * i + half], delta = deltas[8 * b + 2 * i + half];
 #pragma unroll
-                for (int n = 0; n < W / 16; n++) {
-                    s = mma<T>(row_operand<W>(queries, 32 * b, n), k[n], s);
-                    d = mma<T>(row_operand<W>(grads, 32 * b, n), v[n], d);
+                for (int j = 0; j < 4; j++) {
+                    const int query = q0 + 32 * b + 8 * i + 4 * half + j;
+                    float p = __builtin_amdgcn_exp2f(s[4 * i + j] * by - lse[j]);
+                    float e = p * (d[4 * i + j] - delta[j]) * grow;
+                    if (edge && (query < key || query >= tile.length)) p = e = 0.0f;
+                    s[4 * i + j] = p;
+                    d[4 * i + j] = e;
                 }
-                const bool edge = q0 + 32 * b < wfirst + 31 || q0 + 32 * b + 32 > tile.length;
+            }
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float4v lse = lses[8 * b + 2 * i + half], delta = deltas[8 * b + 2 * i + half];
+            for (int n = 0; n < 2; n++) {
+                const uint4v p = operand<T>(s, n), e = operand<T>(d, n);
 #pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const int query = q0 + 32 * b + 8 * i + 4 * half + j;
-                        float p = __builtin_amdgcn_exp2f(s[4 * i + j] * by - lse[j]);
-                        float e = p * (d[4 * i + j] - delta[j]) * grow;
-                        if (edge && (query < key || query >= tile.length)) p = e = 0.0f;
-                        s[4 * i + j] = p;
-                        d[4 * i + j] = e;
-                    }
-                }
-#pragma unroll
-                for (int n = 0; n < 2; n++) {
-                    const uint4v p = operand<T>(s, n), e = operand<T>(d, n);
-#pragma unroll
-                    for (int c = 0; c < W / 32; c++) {
-                        dv[c] = mma<T>(column_operand<W>(grads, 32 * b + 16 * n, c), p, dv[c]);
-                        dk[c] = mma<T>(column_operand<W>(queries, 32 * b + 16 * n, c), e, dk[c]);
-                    }
+                for (int c = 0; c < W / 32; c++) {
+                    dv[c] = mma<T>(column_operand<W>(grads, 32 * b + 16 * n, c), p, dv[c]);
+                    dk[c] = mma<T>(column_operand<W>(queries, 32 * b + 16 * n, c), e, dk[c]);
                 }
             }
         }

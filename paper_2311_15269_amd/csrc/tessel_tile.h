@@ -82,6 +82,32 @@ __device__ __forceinline__ uint4v column_operand(const uint4v *tile, int row, in
     return __builtin_bit_cast(uint4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+typedef __attribute__((address_space(3))) uint4v lds_uint4v;
+typedef __attribute__((address_space(1))) const uint4v global_uint4v;
+
+// A tile of 64 rows x W on its way from memory straight to LDS by a workgroup of 256, without passing registers: a wave's
+// instruction fills 1 KB of LDS from its start on, so the lanes pick the chunks of their rows in the order of chunk_at.  Rows from
+// `rows` on and columns from dim on are left as they are in LDS.
+template <typename T, int W>
+struct Copy {
+    static constexpr int kChunks = W / 8, kRows = 256 / kChunks, kPer = 64 / kRows;       // (kRows: 16 or 32, after which chunk_at repeats)
+    __device__ __forceinline__ static void start(uint4v *tile, const T *base, int64_t stride, int rows, int dim)
+    {
+        const int r = threadIdx.x / kChunks, c = (threadIdx.x % kChunks) ^ (chunk_at<W>(r, 0) % kChunks);
+        const T *p = base + r * stride + 8 * c;
+        lds_uint4v *to = (lds_uint4v *)(tile + __builtin_amdgcn_readfirstlane(threadIdx.x & ~63));
+        if (rows >= 64 && dim == W) {
+#pragma unroll
+            for (int i = 0; i < kPer; i++) __builtin_amdgcn_global_load_lds((global_uint4v *)(p + i * kRows * stride), to + i * 256, 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; i++)
+                if (r + i * kRows < rows && 8 * c < dim)
+                    __builtin_amdgcn_global_load_lds((global_uint4v *)(p + i * kRows * stride), to + i * 256, 16, 0, 0);
+        }
+    }
+};
+
 // the other half-wave's value of the same column
 __device__ __forceinline__ float other_half(float x)
 {
