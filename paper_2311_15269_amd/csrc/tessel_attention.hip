@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
     Copy<T, W>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
     for (int k0 = 0, turn = 0; k0 < last; k0 += 64, turn ^= 2) {
         const uint4v *keys = buffers[turn], *values = buffers[turn + 1];
-        __syncthreads();                                         // (this tile has arrived, and all are done with the one before)
+        copies_arrive();                                         // (this tile has arrived, and all are done with the one before)
         if (k0 + 64 < last) {
             Copy<T, W>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
             Copy<T, W>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     Copy<T, W>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
     for (int k0 = 0, turn = 0; k0 < last; k0 += 64, turn ^= 2) {
         const uint4v *keys = buffers[turn], *values = buffers[turn + 1];
-        __syncthreads();
+        copies_arrive();
         if (k0 + 64 < last) {
             Copy<T, W>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
             Copy<T, W>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
@@ -332,11 +332,93 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     for (int b = 0; b < W / 32; b++) put_rows<T>(out, dq[b], b, back, dim);
 }
 
+// Keeps accumulators where they are from one tile to the next (the compiler else moves them to other registers and back in every tile),
+// and gives the last product the time that it takes to write them.
+template <int W>
+__device__ __forceinline__ void keep_sums(float16v *x, float16v *y)
+{
+    asm volatile("s_nop 15");
+#pragma unroll
+    for (int c = 0; c < W / 32; c++) asm volatile("" : "+a"(x[c]), "+a"(y[c]));
+}
+
+// What a wave of the kernel below does with a tile of 64 queries, its 32 keys against the queries' two blocks of 32.  Four phases of W / 16
+// steps of two products each: the scores and dp = do v of block 0, those of block 1, the sums into dv and dk of block 0, those of block 1.  The
+// exponentials of block 0 are worked out between the products of the second phase, those of block 1 in the third: with one wave on a
+// SIMD (two accumulators of 32 x W leave no room for more) nothing else would run beside the matrix unit.  LDS is read two steps ahead.
+template <typename T, int W, bool EDGE>
+__device__ __forceinline__ void dkv_tile(const uint4v *queries, const uint4v *grads, const float4v *lses, const float4v *deltas, const uint4v *k,
+                                         const uint4v *v, float16v *dk, float16v *dv, float by, float grow, int before)
+{
+    constexpr int S = W / 16, E = 16 / S;                        // steps a phase, values of a block a step
+    const int half = threadIdx.x >> 5 & 1;
+    uint4v f[4 * S][2];
+    float16v s[2], d[2];
+    uint4v p[2][2], e[2][2];
+    auto read = [&](int t) {
+        if (t >= 4 * S) return;
+        const int b = t / S & 1, n = t % S;
+        if (t < 2 * S) {
+            f[t][0] = row_operand<W>(queries, 32 * b, n);
+            f[t][1] = row_operand<W>(grads, 32 * b, n);
+        } else {
+            const int row = 32 * b + 16 * (n / (W / 32)), c = n % (W / 32);
+            f[t][0] = column_operand<W>(queries, row, c);
+            f[t][1] = column_operand<W>(grads, row, c);
+        }
+    };
+    // the sums of the first products start from what is taken off them
+    auto start = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float4v x = lses[8 * b + 2 * i + half], y = deltas[8 * b + 2 * i + half];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                s[b][4 * i + j] = x[j];
+                d[b][4 * i + j] = y[j];
+            }
+        }
+    };
+    start(0);
+    read(0);
+    read(1);
+#pragma unroll
+    for (int t = 0; t < 4 * S; t++) {
+        const int phase = t / S, n = t % S;
+        read(t + 2);
+        if (t == S - 1) start(1);
+        if (phase < 2) {
+            s[phase] = mma<T>(f[t][0], k[n], s[phase]);
+            d[phase] = mma<T>(f[t][1], v[n], d[phase]);
+        } else {
+            const int b = phase - 2, c = n % (W / 32), h = n / (W / 32);
+            dk[c] = mma<T>(f[t][0], e[b][h], dk[c]);
+            dv[c] = mma<T>(f[t][1], p[b][h], dv[c]);
+        }
+        if (phase == 1 || phase == 2) {
+            const int b = phase - 1;
+#pragma unroll
+            for (int i = n * E; i < (n + 1) * E; i++) {
+                float x = __builtin_amdgcn_exp2f(s[b][i] * by);
+                if (EDGE && 32 * b + 8 * (i / 4) + i % 4 < before) x = 0.0f;
+                d[b][i] *= __is_same(T, f16) ? x * grow : x;
+                s[b][i] = x;
+                if (i % 8 == 7) {
+                    p[b][i / 8] = operand<T>(s[b], i / 8);
+                    e[b][i / 8] = operand<T>(d[b], i / 8);
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    keep_sums<W>(dk, dv);
+}
+
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
 {
     __shared__ uint4v buffers[4][64 * W / 8];
-    __shared__ float4v numbers[2][2][16];                        // log-sums and deltas of a tile's queries
+    __shared__ float4v numbers[2][2][16];                        // - log-sum / scale and - delta of a tile's queries
     int t, kv;
     work_of(l.a.kv_heads, t, kv);
     const AttendTile tile = l.tiles[t];
@@ -348,7 +430,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
     }
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
     // (the tile with the most keys before it has the fewest queries behind it: the order of falling work is turned round)
-    const int first = (tile.tiles - 1 - tile.tile) * kAttendRows, wfirst = first + 32 * wave, key = wfirst + (lane & 31);
+    const int first = (tile.tiles - 1 - tile.tile) * kAttendRows, key = first + 32 * wave + (lane & 31);
     const int64_t token = tile.begin + key;
     const bool valid = key < tile.length;
     const int shared = l.a.heads / l.a.kv_heads;
@@ -361,58 +443,37 @@ __global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
     float16v dk[W / 32] = {}, dv[W / 32] = {};
 
     // the tiles of all heads that share these keys, one behind the other
-    const int tiles = (tile.length - first + 63) / 64;
+    const int tiles = (tile.length - first + 63) / 64, edges = min(tiles, kAttendRows / 64), all = tiles * shared;
     float number = 0;                                            // (on its way to LDS, one tile ahead)
-    auto fetch = [&](int n, int turn) {
+    auto fetch = [&](int n) {
         const int head = kv * shared + n / tiles, q0 = first + n % tiles * 64, rows = tile.length - q0;
-        Copy<T, W>::start(buffers[2 * turn], row_of<T>(l.a.q, tile.begin + q0, head), l.a.q.token_stride, rows, dim);
-        Copy<T, W>::start(buffers[2 * turn + 1], row_of<T>(l.a.d_o, tile.begin + q0, head), l.a.d_o.token_stride, rows, dim);
+        uint4v (*to)[64 * W / 8] = buffers + 2 * (n & 1);
+        Copy<T, W>::start(to[0], row_of<T>(l.a.q, tile.begin + q0, head), l.a.q.token_stride, rows, dim);
+        Copy<T, W>::start(to[1], row_of<T>(l.a.d_o, tile.begin + q0, head), l.a.d_o.token_stride, rows, dim);
         if (threadIdx.x < 128) {
-            const int64_t at = head * l.tokens + tile.begin + q0 + min((int)threadIdx.x & 63, rows - 1);
-            number = threadIdx.x < 64 ? l.a.lse[at] * kLog2e : l.delta[at];
+            const int r = threadIdx.x & 63;
+            const int64_t at = head * l.tokens + tile.begin + q0 + r;
+            // (queries behind the sequence's end: a probability of nought)
+            if (threadIdx.x < 64) number = r < rows ? -l.a.lse[at] / l.a.scale : -INFINITY;
+            else number = r < rows ? -l.delta[at] : 0.0f;
         }
     };
+    auto next = [&](int n) {
+        if (threadIdx.x < 128) ((float *)numbers[n & 1])[threadIdx.x] = number;
+        copies_arrive();                                         // (tile n has arrived, and all are done with the one before)
+        if (n + 1 < all) fetch(n + 1);
+    };
     clear_tiles<4, W>(buffers, tile.length - first, dim);
-    fetch(0, 0);
-    for (int n = 0; n < tiles * shared; n++) {
-        const int turn = n & 1, q0 = first + n % tiles * 64;
-        const uint4v *queries = buffers[2 * turn], *grads = buffers[2 * turn + 1];
-        const float4v *lses = numbers[turn][0], *deltas = numbers[turn][1];
-        if (threadIdx.x < 128) ((float *)numbers[turn])[threadIdx.x] = number;
-        __syncthreads();
-        if (n + 1 < tiles * shared) fetch(n + 1, turn ^ 1);
-#pragma unroll
-        for (int b = 0; b < 2; b++) {
-            if (q0 + 32 * b + 31 < wfirst) continue;
-            float16v s = {}, d = {};
-#pragma unroll
-            for (int n = 0; n < W / 16; n++) {
-                s = mma<T>(row_operand<W>(queries, 32 * b, n), k[n], s);
-                d = mma<T>(row_operand<W>(grads, 32 * b, n), v[n], d);
-            }
-            const bool edge = q0 + 32 * b < wfirst + 31 || q0 + 32 * b + 32 > tile.length;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const float4v lse = lses[8 * b + 2 * i + half], delta = deltas[8 * b + 2 * i + half];
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const int query = q0 + 32 * b + 8 * i + 4 * half + j;
-                    float p = __builtin_amdgcn_exp2f(s[4 * i + j] * by - lse[j]);
-                    float e = p * (d[4 * i + j] - delta[j]) * grow;
-                    if (edge && (query < key || query >= tile.length)) p = e = 0.0f;
-                    s[4 * i + j] = p;
-                    d[4 * i + j] = e;
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < 2; n++) {
-                const uint4v p = operand<T>(s, n), e = operand<T>(d, n);
-#pragma unroll
-                for (int c = 0; c < W / 32; c++) {
-                    dv[c] = mma<T>(column_operand<W>(grads, 32 * b + 16 * n, c), p, dv[c]);
-                    dk[c] = mma<T>(column_operand<W>(queries, 32 * b + 16 * n, c), e, dk[c]);
-                }
-            }
+    fetch(0);
+    for (int n = 0; n < all;) {
+        for (int i = 0; i < edges; i++, n++) {
+            next(n);
+            dkv_tile<T, W, true>(buffers[2 * (n & 1)], buffers[2 * (n & 1) + 1], numbers[n & 1][0], numbers[n & 1][1], k, v, dk, dv, by, grow,
+                                 32 * wave + (lane & 31) - 64 * i - 4 * half);
+        }
+        for (int i = edges; i < tiles; i++, n++) {
+            next(n);
+            dkv_tile<T, W, false>(buffers[2 * (n & 1)], buffers[2 * (n & 1) + 1], numbers[n & 1][0], numbers[n & 1][1], k, v, dk, dv, by, grow, 0);
         }
     }
     if (!valid) return;

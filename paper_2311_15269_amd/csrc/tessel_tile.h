@@ -108,6 +108,14 @@ struct Copy {
     }
 };
 
+// Waits until this wave's copies are in LDS, then for the other waves.  (A barrier alone waits for no copy: what goes from memory
+// to LDS counts as a load from memory.)
+__device__ __forceinline__ void copies_arrive()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 // the other half-wave's value of the same column
 __device__ __forceinline__ float other_half(float x)
 {
