@@ -69,23 +69,23 @@ template <typename T>
 __device__ void clear_rows(const tessel_heads &h, int begin, int rows, int head, int dim)
 {
     const int chunks = dim / 8;
-    for (int n = threadIdx.x; n < rows * chunks; n += kThreads)
+    for (int n = threadIdx.x; n < rows * chunks; n += blockDim.x)
         *(uint4v *)((T *)row_of<T>(h, begin + n / chunks, head) + 8 * (n % chunks)) = uint4v{0, 0, 0, 0};
 }
 
 // Zeros into tiles that will not be filled whole: heads narrower than the tile, or fewer rows than the tiles hold.
-template <int N, int W>
+template <int N, int W, int THREADS = kThreads>
 __device__ __forceinline__ void clear_tiles(uint4v (*tiles)[64 * W / 8], int rows, int dim)
 {
     if (dim == W && rows >= 128) return;
-    for (int n = threadIdx.x; n < N * 64 * W / 8; n += kThreads) tiles[0][n] = uint4v{0, 0, 0, 0};
+    for (int n = threadIdx.x; n < N * 64 * W / 8; n += THREADS) tiles[0][n] = uint4v{0, 0, 0, 0};
     __syncthreads();
 }
 
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
 {
-    __shared__ uint4v buffers[4][64 * W / 8];
+    __shared__ __attribute__((aligned(256))) uint4v buffers[4][64 * W / 8];
     int t, head;
     work_of(l.a.heads, t, head);
     const AttendTile tile = l.tiles[t];
@@ -109,22 +109,23 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
     const float by = l.a.scale * kLog2e, slack = 8.0f / by;
 
     const T *kp = row_of<T>(l.a.k, tile.begin, kv), *vp = row_of<T>(l.a.v, tile.begin, kv);
+    Reader<W> at;
     clear_tiles<4, W>(buffers, last, dim);
-    Copy<T, W>::start(buffers[0], kp, l.a.k.token_stride, last, dim);
-    Copy<T, W>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
+    Copy<T, W, kThreads>::start(buffers[0], kp, l.a.k.token_stride, last, dim);
+    Copy<T, W, kThreads>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
     for (int k0 = 0, turn = 0; k0 < last; k0 += 64, turn ^= 2) {
-        const uint4v *keys = buffers[turn], *values = buffers[turn + 1];
+        const lds_tile *keys = (const lds_tile *)buffers[turn], *values = (const lds_tile *)buffers[turn + 1];
         copies_arrive();                                         // (this tile has arrived, and all are done with the one before)
         if (k0 + 64 < last) {
-            Copy<T, W>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
-            Copy<T, W>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
+            Copy<T, W, kThreads>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
+            Copy<T, W, kThreads>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
         }
         if (k0 > wfirst + 31) continue;
         float16v s[2] = {};
 #pragma unroll
         for (int b = 0; b < 2; b++)
 #pragma unroll
-            for (int n = 0; n < W / 16; n++) s[b] = mma<T>(row_operand<W>(keys, 32 * b, n), q[n], s[b]);
+            for (int n = 0; n < W / 16; n++) s[b] = mma<T>(at.rows(keys, 32 * b, n), q[n], s[b]);
         if (k0 + 63 > wfirst) {
 #pragma unroll
             for (int b = 0; b < 2; b++)
@@ -147,19 +148,19 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
 #pragma unroll
             for (int b = 0; b < W / 32; b++) o[b] *= shrink;
         }
-        const float at = m == -INFINITY ? 0.0f : m * by;
+        const float off = m == -INFINITY ? 0.0f : m * by;
 #pragma unroll
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int i = 0; i < 16; i++) {
-                s[b][i] = __builtin_amdgcn_exp2f(s[b][i] * by - at);
+                s[b][i] = __builtin_amdgcn_exp2f(s[b][i] * by - off);
                 sum += s[b][i];
             }
 #pragma unroll
         for (int n = 0; n < 4; n++) {
             const uint4v p = operand<T>(s[n / 2], n % 2);
 #pragma unroll
-            for (int b = 0; b < W / 32; b++) o[b] = mma<T>(column_operand<W>(values, 16 * n, b), p, o[b]);
+            for (int b = 0; b < W / 32; b++) o[b] = mma<T>(at.columns(values, 16 * n, b), p, o[b]);
         }
     }
     sum += other_half(sum);
@@ -265,7 +266,7 @@ __device__ __forceinline__ float gradient_scale(const AttendLaunch &l)
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 {
-    __shared__ uint4v buffers[4][64 * W / 8];
+    __shared__ __attribute__((aligned(256))) uint4v buffers[4][64 * W / 8];
     int t, head;
     work_of(l.a.heads, t, head);
     const AttendTile tile = l.tiles[t];
@@ -291,15 +292,16 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     float16v dq[W / 32] = {};
 
     const T *kp = row_of<T>(l.a.k, tile.begin, kv), *vp = row_of<T>(l.a.v, tile.begin, kv);
+    Reader<W> at;
     clear_tiles<4, W>(buffers, last, dim);
-    Copy<T, W>::start(buffers[0], kp, l.a.k.token_stride, last, dim);
-    Copy<T, W>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
+    Copy<T, W, kThreads>::start(buffers[0], kp, l.a.k.token_stride, last, dim);
+    Copy<T, W, kThreads>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
     for (int k0 = 0, turn = 0; k0 < last; k0 += 64, turn ^= 2) {
-        const uint4v *keys = buffers[turn], *values = buffers[turn + 1];
+        const lds_tile *keys = (const lds_tile *)buffers[turn], *values = (const lds_tile *)buffers[turn + 1];
         copies_arrive();
         if (k0 + 64 < last) {
-            Copy<T, W>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
-            Copy<T, W>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
+            Copy<T, W, kThreads>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
+            Copy<T, W, kThreads>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
         }
 #pragma unroll
         for (int b = 0; b < 2; b++) {
@@ -307,8 +309,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
             float16v s = {}, d = {};
 #pragma unroll
             for (int n = 0; n < W / 16; n++) {
-                s = mma<T>(row_operand<W>(keys, 32 * b, n), q[n], s);
-                d = mma<T>(row_operand<W>(values, 32 * b, n), g[n], d);
+                s = mma<T>(at.rows(keys, 32 * b, n), q[n], s);
+                d = mma<T>(at.rows(values, 32 * b, n), g[n], d);
             }
             const bool edge = k0 + 32 * b + 31 > wfirst;
 #pragma unroll
@@ -321,7 +323,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
             for (int n = 0; n < 2; n++) {
                 const uint4v p = operand<T>(s, n);
 #pragma unroll
-                for (int c = 0; c < W / 32; c++) dq[c] = mma<T>(column_operand<W>(keys, 32 * b + 16 * n, c), p, dq[c]);
+                for (int c = 0; c < W / 32; c++) dq[c] = mma<T>(at.columns(keys, 32 * b + 16 * n, c), p, dq[c]);
             }
         }
     }
@@ -332,92 +334,82 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     for (int b = 0; b < W / 32; b++) put_rows<T>(out, dq[b], b, back, dim);
 }
 
-// Keeps accumulators where they are from one tile to the next (the compiler else moves them to other registers and back in every tile),
-// and gives the last product the time that it takes to write them.
-template <int W>
-__device__ __forceinline__ void keep_sums(float16v *x, float16v *y)
-{
-    asm volatile("s_nop 15");
-#pragma unroll
-    for (int c = 0; c < W / 32; c++) asm volatile("" : "+a"(x[c]), "+a"(y[c]));
-}
-
-// What a wave of the kernel below does with a tile of 64 queries, its 32 keys against the queries' two blocks of 32.  Four phases of W / 16
-// steps of two products each: the scores and dp = do v of block 0, those of block 1, the sums into dv and dk of block 0, those of block 1.  The
-// exponentials of block 0 are worked out between the products of the second phase, those of block 1 in the third: with one wave on a
-// SIMD (two accumulators of 32 x W leave no room for more) nothing else would run beside the matrix unit.  LDS is read two steps ahead.
+// What a wave of the kernel below does with a block of 32 queries and its 32 keys.  LDS is read one step ahead of the products.
 template <typename T, int W, bool EDGE>
-__device__ __forceinline__ void dkv_tile(const uint4v *queries, const uint4v *grads, const float4v *lses, const float4v *deltas, const uint4v *k,
-                                         const uint4v *v, float16v *dk, float16v *dv, float by, float grow, int before)
+__device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_tile *grads, int row, Reader<W> at, const float4v *lses, const float4v *deltas, const uint4v *k,
+                                          const uint4v *values, float16v *dk, float16v *dv, float by, float grow, int before)
 {
-    constexpr int S = W / 16, E = 16 / S;                        // steps a phase, values of a block a step
+    constexpr int S = W / 16;                                    // steps a phase, two products each
     const int half = threadIdx.x >> 5 & 1;
-    uint4v f[4 * S][2];
-    float16v s[2], d[2];
-    uint4v p[2][2], e[2][2];
+    at.hold();
+    uint4v f[2 * S][2], v[S];
+    float16v s, d;
+    uint4v p[2], e[2];
     auto read = [&](int t) {
-        if (t >= 4 * S) return;
-        const int b = t / S & 1, n = t % S;
-        if (t < 2 * S) {
-            f[t][0] = row_operand<W>(queries, 32 * b, n);
-            f[t][1] = row_operand<W>(grads, 32 * b, n);
-        } else {
-            const int row = 32 * b + 16 * (n / (W / 32)), c = n % (W / 32);
-            f[t][0] = column_operand<W>(queries, row, c);
-            f[t][1] = column_operand<W>(grads, row, c);
+        if (t < S) {
+            f[t][0] = at.rows(queries, row, t);
+            f[t][1] = at.rows(grads, row, t);
+            v[t] = values[64 * t];
+        } else if (t < 2 * S) {
+            const int n = t - S, h = n / (W / 32), c = n % (W / 32);
+            f[t][0] = at.columns(queries, row + 16 * h, c);
+            f[t][1] = at.columns(grads, row + 16 * h, c);
         }
     };
-    // the sums of the first products start from what is taken off them
-    auto start = [&](int b) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const float4v x = lses[8 * b + 2 * i + half], y = deltas[8 * b + 2 * i + half];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                s[b][4 * i + j] = x[j];
-                d[b][4 * i + j] = y[j];
-            }
-        }
-    };
-    start(0);
     read(0);
+    // the sums of the first products start from what is taken off them
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const float4v x = lses[row / 4 + 2 * i + half], y = deltas[row / 4 + 2 * i + half];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            s[4 * i + j] = x[j];
+            d[4 * i + j] = y[j];
+        }
+    }
     read(1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int t = 0; t < 4 * S; t++) {
-        const int phase = t / S, n = t % S;
-        read(t + 2);
-        if (t == S - 1) start(1);
-        if (phase < 2) {
-            s[phase] = mma<T>(f[t][0], k[n], s[phase]);
-            d[phase] = mma<T>(f[t][1], v[n], d[phase]);
-        } else {
-            const int b = phase - 2, c = n % (W / 32), h = n / (W / 32);
-            dk[c] = mma<T>(f[t][0], e[b][h], dk[c]);
-            dv[c] = mma<T>(f[t][1], p[b][h], dv[c]);
-        }
-        if (phase == 1 || phase == 2) {
-            const int b = phase - 1;
-#pragma unroll
-            for (int i = n * E; i < (n + 1) * E; i++) {
-                float x = __builtin_amdgcn_exp2f(s[b][i] * by);
-                if (EDGE && 32 * b + 8 * (i / 4) + i % 4 < before) x = 0.0f;
-                d[b][i] *= __is_same(T, f16) ? x * grow : x;
-                s[b][i] = x;
-                if (i % 8 == 7) {
-                    p[b][i / 8] = operand<T>(s[b], i / 8);
-                    e[b][i / 8] = operand<T>(d[b], i / 8);
-                }
-            }
-        }
+    for (int t = 0; t < S; t++) {
+        if (t + 2 < S) read(t + 2);
+        s = mma<T>(f[t][0], k[t], s);
+        d = mma<T>(f[t][1], v[t], d);
         __builtin_amdgcn_sched_barrier(0);
     }
-    keep_sums<W>(dk, dv);
+    read(S);
+    read(S + 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        float x = __builtin_amdgcn_exp2f(s[i] * by);
+        if (EDGE && 8 * (i / 4) + i % 4 < before) x = 0.0f;
+        d[i] *= __is_same(T, f16) ? x * grow : x;
+        s[i] = x;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        p[h] = operand<T>(s, h);
+        e[h] = operand<T>(d, h);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = S; t < 2 * S; t++) {
+        const int n = t - S, h = n / (W / 32), c = n % (W / 32);
+        read(t + 2);
+        dk[c] = mma<T>(f[t][0], e[h], dk[c]);
+        dv[c] = mma<T>(f[t][1], p[h], dv[c]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
+constexpr int kDkvThreads = 512;
+
+// Eight waves: the first four take the tile's first 32 queries, the others the last 32, each 32 of the workgroup's 128 keys; two
+// waves on a SIMD, so that one's exponentials run beside the other's products.  At the end the second four hand their sums to the first.
 template <typename T, int W>
-__global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
+__global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch l)
 {
-    __shared__ uint4v buffers[4][64 * W / 8];
+    __shared__ __attribute__((aligned(256))) uint4v buffers[4][64 * W / 8], values[128 * W / 8];
     __shared__ float4v numbers[2][2][16];                        // - log-sum / scale and - delta of a tile's queries
     int t, kv;
     work_of(l.a.kv_heads, t, kv);
@@ -428,7 +420,7 @@ __global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
         clear_rows<T>(l.a.dv, tile.begin, -tile.length, kv, dim);
         return;
     }
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+    const int wave = threadIdx.x >> 6 & 3, row = threadIdx.x >> 8 << 5, lane = threadIdx.x & 63, half = lane >> 5;
     // (the tile with the most keys before it has the fewest queries behind it: the order of falling work is turned round)
     const int first = (tile.tiles - 1 - tile.tile) * kAttendRows, key = first + 32 * wave + (lane & 31);
     const int64_t token = tile.begin + key;
@@ -439,17 +431,20 @@ __global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
     uint4v k[W / 16], v[W / 16];
     fetch_rows<T, W>(k, row_of<T>(l.a.k, token, kv), valid, dim);
     fetch_rows<T, W>(v, row_of<T>(l.a.v, token, kv), valid, dim);
+    uint4v *const mine = values + wave * (W / 16 * 64) + lane;   // (registers hold the keys' operands; the values' lie in LDS as the lanes need them)
+#pragma unroll
+    for (int n = 0; n < W / 16; n++) mine[64 * n] = v[n];        // (both waves of these keys: the same)
     const float by = l.a.scale * kLog2e;
     float16v dk[W / 32] = {}, dv[W / 32] = {};
 
     // the tiles of all heads that share these keys, one behind the other
-    const int tiles = (tile.length - first + 63) / 64, edges = min(tiles, kAttendRows / 64), all = tiles * shared;
+    const int tiles = (tile.length - first + 63) / 64, all = tiles * shared;
     float number = 0;                                            // (on its way to LDS, one tile ahead)
     auto fetch = [&](int n) {
         const int head = kv * shared + n / tiles, q0 = first + n % tiles * 64, rows = tile.length - q0;
         uint4v (*to)[64 * W / 8] = buffers + 2 * (n & 1);
-        Copy<T, W>::start(to[0], row_of<T>(l.a.q, tile.begin + q0, head), l.a.q.token_stride, rows, dim);
-        Copy<T, W>::start(to[1], row_of<T>(l.a.d_o, tile.begin + q0, head), l.a.d_o.token_stride, rows, dim);
+        Copy<T, W, kDkvThreads>::start(to[0], row_of<T>(l.a.q, tile.begin + q0, head), l.a.q.token_stride, rows, dim);
+        Copy<T, W, kDkvThreads>::start(to[1], row_of<T>(l.a.d_o, tile.begin + q0, head), l.a.d_o.token_stride, rows, dim);
         if (threadIdx.x < 128) {
             const int r = threadIdx.x & 63;
             const int64_t at = head * l.tokens + tile.begin + q0 + r;
@@ -458,39 +453,50 @@ __global__ __launch_bounds__(kThreads, 1) void attend_dkv_kernel(AttendLaunch l)
             else number = r < rows ? -l.delta[at] : 0.0f;
         }
     };
-    auto next = [&](int n) {
+    const Reader<W> at;
+    clear_tiles<4, W, kDkvThreads>(buffers, tile.length - first, dim);
+    fetch(0);
+    for (int n = 0; n < all; n++) {
         if (threadIdx.x < 128) ((float *)numbers[n & 1])[threadIdx.x] = number;
         copies_arrive();                                         // (tile n has arrived, and all are done with the one before)
         if (n + 1 < all) fetch(n + 1);
-    };
-    clear_tiles<4, W>(buffers, tile.length - first, dim);
-    fetch(0);
-    for (int n = 0; n < all;) {
-        for (int i = 0; i < edges; i++, n++) {
-            next(n);
-            dkv_tile<T, W, true>(buffers[2 * (n & 1)], buffers[2 * (n & 1) + 1], numbers[n & 1][0], numbers[n & 1][1], k, v, dk, dv, by, grow,
-                                 32 * wave + (lane & 31) - 64 * i - 4 * half);
-        }
-        for (int i = edges; i < tiles; i++, n++) {
-            next(n);
-            dkv_tile<T, W, false>(buffers[2 * (n & 1)], buffers[2 * (n & 1) + 1], numbers[n & 1][0], numbers[n & 1][1], k, v, dk, dv, by, grow, 0);
-        }
+        const lds_tile *queries = (const lds_tile *)buffers[2 * (n & 1)], *grads = (const lds_tile *)buffers[2 * (n & 1) + 1];
+        const float4v *lses = numbers[n & 1][0], *deltas = numbers[n & 1][1];
+        const int before = 32 * wave - n % tiles * 64 - row;     // (this block's queries of which the wave's first key is ahead)
+        if (before > 31) continue;
+        if (before > -32) dkv_block<T, W, true>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, before + (lane & 31) - 4 * half);
+        else dkv_block<T, W, false>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, 0);
     }
-    if (!valid) return;
+    float4v *sums = (float4v *)buffers + wave * (W / 32 * 4 * 64) + lane;
     const float back = l.a.scale / grow;
-    T *dkp = (T *)row_of<T>(l.a.dk, token, kv), *dvp = (T *)row_of<T>(l.a.dv, token, kv);
 #pragma unroll
-    for (int b = 0; b < W / 32; b++) {
-        put_rows<T>(dkp, dk[b], b, back, dim);
-        put_rows<T>(dvp, dv[b], b, 1.0f, dim);
+    for (int x = 0; x < 2; x++) {
+        float16v *c = x == 0 ? dk : dv;
+        __syncthreads();
+        if (row != 0) {
+#pragma unroll
+            for (int b = 0; b < W / 32; b++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) sums[(4 * b + i) * 64] = float4v{c[b][4 * i], c[b][4 * i + 1], c[b][4 * i + 2], c[b][4 * i + 3]};
+        }
+        __syncthreads();
+        if (row == 0 && valid) {
+            T *to = (T *)row_of<T>(x == 0 ? l.a.dk : l.a.dv, token, kv);
+#pragma unroll
+            for (int b = 0; b < W / 32; b++) {
+#pragma unroll
+                for (int i = 0; i < 16; i++) c[b][i] += sums[(4 * b + i / 4) * 64][i % 4];
+                put_rows<T>(to, c[b], b, x == 0 ? back : 1.0f, dim);
+            }
+        }
     }
 }
 
-static int launch(const void *kernel, int64_t blocks, const AttendLaunch &l, void *stream)
+static int launch(const void *kernel, int64_t blocks, const AttendLaunch &l, void *stream, int threads = kThreads)
 {
     AttendLaunch copy = l;
     void *args[] = {&copy};
-    const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)blocks), dim3(kThreads), args, 0, (hipStream_t)stream);
+    const hipError_t e = hipLaunchKernel(kernel, dim3((unsigned)blocks), dim3(threads), args, 0, (hipStream_t)stream);
     if (e != hipSuccess) (void)hipGetLastError();
     return (int)e;
 }
@@ -507,7 +513,7 @@ int launch_attend(const AttendLaunch &l, void *stream)
 int launch_attend_backward(const AttendLaunch &l, void *stream)
 {
     int e = launch(ATTEND_KERNEL(attend_delta_kernel), kAmaxParts, l, stream);
-    if (e == 0) e = launch(ATTEND_KERNEL(attend_dkv_kernel), (int64_t)l.num_tiles * l.a.kv_heads, l, stream);
+    if (e == 0) e = launch(ATTEND_KERNEL(attend_dkv_kernel), (int64_t)l.num_tiles * l.a.kv_heads, l, stream, kDkvThreads);
     if (e == 0) e = launch(ATTEND_KERNEL(attend_dq_kernel), (int64_t)l.num_tiles * l.a.heads, l, stream);
     return e;
 }

@@ -51,7 +51,7 @@ __device__ __forceinline__ uint4v operand(const float16v &c, int s)
     return r;
 }
 
-// A tile of rows of W values (2 bytes each) in LDS, rows packed, chunks of 16 bytes of a row swapped so that both ways
+// A tile of rows of W values (2 bytes each) in LDS (its start: a multiple of 256 bytes), rows packed, chunks of 16 bytes of a row swapped so that both ways
 // of reading touch all banks: 16 rows at one column (row operands), and 4 rows x 32 columns (transposing reads).
 template <int W>
 __device__ __forceinline__ int chunk_at(int row, int chunk)          // in chunks of 16 bytes
@@ -60,37 +60,48 @@ __device__ __forceinline__ int chunk_at(int row, int chunk)          // in chunk
     else return row * 8 + (chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3)));
 }
 
-// a operand of 32 rows from `row`, columns 16 s .. 16 s + 15 (also a b operand of 32 columns, for a tile that holds columns as rows)
-template <int W>
-__device__ __forceinline__ uint4v row_operand(const uint4v *tile, int row, int s)
-{
-    const int lane = threadIdx.x & 63;
-    return tile[chunk_at<W>(row + (lane & 31), 2 * s + (lane >> 5))];
-}
-
-// a operand whose rows are the tile's columns 32 b .. 32 b + 31 and whose summed index are the tile's rows row .. row + 15 in
-// the order of operand(): two transposing reads, of which each group of 16 lanes takes 4 rows x 16 columns.
-template <int W>
-__device__ __forceinline__ uint4v column_operand(const uint4v *tile, int row, int b)
-{
-    const int lane = threadIdx.x & 63, i = lane & 15;
-    const int r = row + 4 * (lane >> 5) + (i >> 2);
-    const int chunk = 4 * b + 2 * (lane >> 4 & 1) + (i >> 1 & 1);
-    const char *p = (const char *)tile;
-    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(p + 16 * chunk_at<W>(r, chunk) + 8 * (i & 1)));
-    const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(p + 16 * chunk_at<W>(r + 8, chunk) + 8 * (i & 1)));
-    return __builtin_bit_cast(uint4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
 typedef __attribute__((address_space(3))) uint4v lds_uint4v;
+typedef __attribute__((address_space(3))) const uint4v lds_tile;
+
+// Where a lane reads operands from a tile in LDS: two byte addresses, from which those of all operands come by one exclusive or and a
+// constant offset (the swaps of chunk_at are exclusive ors too, and tiles start at multiples of 256 bytes).  hold() keeps the
+// compiler from working the addresses of a loop out before it and keeping them all in registers.
+template <int W>
+struct Reader {
+    uint32_t r, c;
+    __device__ __forceinline__ Reader()
+    {
+        const int lane = threadIdx.x & 63, i = lane & 15, row = 4 * (lane >> 5) + (i >> 2);
+        r = 16 * chunk_at<W>(lane & 31, lane >> 5);
+        c = 16 * chunk_at<W>(row, 2 * (lane >> 4 & 1) + (i >> 1 & 1)) + 8 * (i & 1);
+    }
+    __device__ __forceinline__ void hold() { asm volatile("" : "+v"(r), "+v"(c)); }
+    // a operand of the tile's rows row .. row + 31 (row: a multiple of 16), columns 16 s .. 16 s + 15; also a b operand, for a tile that
+    // holds columns as rows
+    __device__ __forceinline__ uint4v rows(const lds_tile *tile, int row, int s) const
+    {
+        return *(const lds_tile *)((uint32_t)(uintptr_t)tile + (r ^ (32 * s)) + row * 2 * W);
+    }
+    // a operand whose rows are the tile's columns 32 b .. 32 b + 31 and whose summed index are the tile's rows row .. row + 15 (row: a
+    // multiple of 16) in the order of operand(): two transposing reads, of which each group of 16 lanes takes 4 rows x 16 columns.
+    __device__ __forceinline__ uint4v columns(const lds_tile *tile, int row, int b) const
+    {
+        const uint32_t at = (uint32_t)(uintptr_t)tile + row * 2 * W;
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(at + (c ^ (64 * b))));
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(at + 8 * 2 * W + (c ^ (64 * b + 32))));
+        return __builtin_bit_cast(uint4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
 typedef __attribute__((address_space(1))) const uint4v global_uint4v;
 
-// A tile of 64 rows x W on its way from memory straight to LDS by a workgroup of 256, without passing registers: a wave's
+// A tile of 64 rows x W on its way from memory straight to LDS by all threads of a workgroup, without passing registers: a wave's
 // instruction fills 1 KB of LDS from its start on, so the lanes pick the chunks of their rows in the order of chunk_at.  Rows from
 // `rows` on and columns from dim on are left as they are in LDS.
-template <typename T, int W>
+template <typename T, int W, int THREADS>
 struct Copy {
-    static constexpr int kChunks = W / 8, kRows = 256 / kChunks, kPer = 64 / kRows;       // (kRows: 16 or 32, after which chunk_at repeats)
+    static constexpr int kChunks = W / 8, kRows = THREADS / kChunks, kPer = 64 / kRows;
+    static_assert(kRows % 16 == 0, "the order of chunks repeats after 16 rows");
     __device__ __forceinline__ static void start(uint4v *tile, const T *base, int64_t stride, int rows, int dim)
     {
         const int r = threadIdx.x / kChunks, c = (threadIdx.x % kChunks) ^ (chunk_at<W>(r, 0) % kChunks);
@@ -98,12 +109,12 @@ struct Copy {
         lds_uint4v *to = (lds_uint4v *)(tile + __builtin_amdgcn_readfirstlane(threadIdx.x & ~63));
         if (rows >= 64 && dim == W) {
 #pragma unroll
-            for (int i = 0; i < kPer; i++) __builtin_amdgcn_global_load_lds((global_uint4v *)(p + i * kRows * stride), to + i * 256, 16, 0, 0);
+            for (int i = 0; i < kPer; i++) __builtin_amdgcn_global_load_lds((global_uint4v *)(p + i * kRows * stride), to + i * THREADS, 16, 0, 0);
         } else {
 #pragma unroll
             for (int i = 0; i < kPer; i++)
                 if (r + i * kRows < rows && 8 * c < dim)
-                    __builtin_amdgcn_global_load_lds((global_uint4v *)(p + i * kRows * stride), to + i * 256, 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((global_uint4v *)(p + i * kRows * stride), to + i * THREADS, 16, 0, 0);
         }
     }
 };

@@ -87,12 +87,13 @@ struct HeldStage {
 template <typename T>
 __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightLaunch l)
 {
-    __shared__ uint4v rows[kSteps * kTile / 8], columns[kSteps * kTile / 8];
+    __shared__ __attribute__((aligned(256))) uint4v rows[kSteps * kTile / 8], columns[kSteps * kTile / 8];
     const tessel_weight_grad &a = l.a;
     const int n0 = blockIdx.x / l.tiles_c * kTile, c0 = blockIdx.x % l.tiles_c * kTile;
     const int64_t begin = blockIdx.y * l.per, end = min(begin + l.per, a.x.tokens);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
     const int wn = wave >> 1, wc = wave & 1;
+    const Reader<128> at;
     float16v acc[2][2] = {};
     DyStage<T> ds;
     HeldStage<T> hs;
@@ -110,8 +111,8 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightLaunch l)
             uint4v x[2], y[2];
 #pragma unroll
             for (int b = 0; b < 2; b++) {
-                x[b] = column_operand<128>(rows, 16 * s, 2 * wn + b);
-                y[b] = column_operand<128>(columns, 16 * s, 2 * wc + b);
+                x[b] = at.columns((const lds_tile *)rows, 16 * s, 2 * wn + b);
+                y[b] = at.columns((const lds_tile *)columns, 16 * s, 2 * wc + b);
             }
 #pragma unroll
             for (int i = 0; i < 2; i++)
