@@ -57,6 +57,18 @@ class WeightGrad(C.Structure):
                 ("dw_stride", C.c_int64)]
 
 
+def _flat(struct):
+    """The same layout with the fields of the structures inside side by side: one call fills it, which is most of what a small call costs
+    on the host."""
+    fields = []
+    for name, kind in struct._fields_:
+        fields += [(name + "_" + n, k) for n, k in kind._fields_] if issubclass(kind, C.Structure) else [(name, kind)]
+    flat = type("Flat" + struct.__name__, (C.Structure,), {"_fields_": fields})
+    assert C.sizeof(flat) == C.sizeof(struct)
+    return flat
+
+
+_FlatAttention, _FlatNorm, _FlatWeight = _flat(Attention), _flat(ResidualNorm), _flat(WeightGrad)
 _lib = None
 
 
@@ -70,34 +82,41 @@ def _library():
         lib.tessel_packing_destroy.restype = None
         lib.tessel_packing_table_bytes.argtypes = [ptr, size]
         lib.tessel_packing_bind.argtypes = [ptr, ptr, C.c_size_t, ptr]
-        lib.tessel_attention_forward.argtypes = [ptr, C.POINTER(Attention), ptr]
-        lib.tessel_attention_backward_workspace_bytes.argtypes = [ptr, C.POINTER(Attention), size]
-        lib.tessel_attention_backward.argtypes = [ptr, C.POINTER(Attention), ptr, C.c_size_t, ptr]
-        lib.tessel_residual_norm_forward.argtypes = [C.POINTER(ResidualNorm), ptr]
-        lib.tessel_residual_norm_backward_workspace_bytes.argtypes = [C.POINTER(ResidualNorm), size]
-        lib.tessel_residual_norm_backward.argtypes = [C.POINTER(ResidualNorm), ptr, C.c_size_t, ptr]
+        # (structures by address: the nested ones above and their flat twins alike)
+        lib.tessel_attention_forward.argtypes = [ptr, ptr, ptr]
+        lib.tessel_attention_backward_workspace_bytes.argtypes = [ptr, ptr, size]
+        lib.tessel_attention_backward.argtypes = [ptr, ptr, ptr, C.c_size_t, ptr]
+        lib.tessel_residual_norm_forward.argtypes = [ptr, ptr]
+        lib.tessel_residual_norm_backward_workspace_bytes.argtypes = [ptr, size]
+        lib.tessel_residual_norm_backward.argtypes = [ptr, ptr, C.c_size_t, ptr]
         for f in (lib.tessel_checkpoint_store, lib.tessel_checkpoint_restore):
-            f.argtypes = [C.POINTER(CheckpointDesc), C.POINTER(Rows), ptr]
-        lib.tessel_gated_forward.argtypes = [C.c_int] + [C.POINTER(Rows)] * 3 + [C.POINTER(CheckpointDesc)] * 2 + [ptr]
-        lib.tessel_gated_backward.argtypes = [C.c_int, C.POINTER(Rows)] + [C.POINTER(CheckpointDesc)] * 2 + [C.POINTER(Rows)] * 3 + [ptr]
-        lib.tessel_weight_gradient_workspace_bytes.argtypes = [C.POINTER(WeightGrad), size]
-        lib.tessel_weight_gradient.argtypes = [C.POINTER(WeightGrad), ptr, C.c_size_t, ptr]
+            f.argtypes = [ptr, ptr, ptr]
+        lib.tessel_gated_forward.argtypes = [C.c_int] + [ptr] * 6
+        lib.tessel_gated_backward.argtypes = [C.c_int] + [ptr] * 7
+        lib.tessel_weight_gradient_workspace_bytes.argtypes = [ptr, size]
+        lib.tessel_weight_gradient.argtypes = [ptr, ptr, C.c_size_t, ptr]
         _lib = lib
     return _lib
 
 
 def _stream(t):
     import torch
-    return torch.cuda.current_stream(t.device).cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream(t.device).cuda_stream if raw is None else raw(t.get_device())
 
 
 def _refuse(text):
     raise binding.TesselError(E_INVALID_ARG, text)
 
 
+_TYPES = {}
+
+
 def _type(t):
     import torch
-    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(t.dtype)
+    if not _TYPES:
+        _TYPES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
+    code = _TYPES.get(t.dtype)
     if code is None:
         raise binding.TesselError(E_UNSUPPORTED, "no operator for tensors of type %s" % t.dtype)
     return code
@@ -105,28 +124,33 @@ def _type(t):
 
 def _same(like, shape, *tensors):
     """all on the GPU of `like`, of its type and of this shape"""
+    dtype, at = like.dtype, like.get_device()
     for t in tensors:
-        if not t.is_cuda or t.device != like.device or t.dtype != like.dtype or tuple(t.shape) != tuple(shape):
+        if not t.is_cuda or t.dtype is not dtype or t.shape != shape or t.get_device() != at:
             _refuse("expected a %s tensor of shape %s on %s, got %s %s on %s" % (like.dtype, tuple(shape), like.device, t.dtype, tuple(t.shape), t.device))
 
 
 def _heads(t):
-    """a [tokens, heads, dim] tensor; one whose last dimension is not contiguous, or whose strides or start are not multiples of
-    16 bytes, is refused"""
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    """a [tokens, heads, dim] tensor: start and strides.  One whose last dimension is not contiguous, or whose strides or start are not
+    multiples of 16 bytes, is refused."""
+    n, heads, dim = t.shape
+    token, head, last = t.stride()
+    if last != 1 and dim > 1:
         _refuse("the last dimension has to be contiguous")
-    return Heads(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2], t.stride(1) if t.shape[1] > 1 else t.shape[2])
+    return t.data_ptr(), token if n > 1 else heads * dim, head if heads > 1 else dim
 
 
 def _rows(t):
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        _refuse("expected [tokens, channels] with contiguous channels, got strides %s" % (t.stride(),))
-    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    """a [tokens, channels] tensor: start and stride"""
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
+        _refuse("expected [tokens, channels] with contiguous channels, got strides %s" % (stride,))
+    return t.data_ptr(), stride[0] if t.shape[0] > 1 else t.shape[1]
 
 
 def _vector(t, channels, like):
     import torch
-    if t.dtype != torch.float32 or tuple(t.shape) != (channels,) or (channels > 1 and t.stride(0) != 1) or t.device != like.device:
+    if t.dtype is not torch.float32 or t.shape != (channels,) or (channels > 1 and t.stride(0) != 1) or t.get_device() != like.get_device():
         _refuse("expected %d contiguous 32-bit numbers on %s, got %s %s" % (channels, like.device, t.dtype, tuple(t.shape)))
     return t.data_ptr()
 
@@ -166,42 +190,42 @@ class Packing:
         except Exception:       # interpreter shutdown
             pass
 
-    def _describe(self, q, k, v, scale):
+    def _describe(self, q, k, v, scale, stream):
         import torch
         if q.dim() != 3 or k.dim() != 3 or q.device != self._table.device:
             _refuse("expected [tokens, heads, dim] on %s" % self._table.device)
-        heads, dim = q.shape[1], q.shape[2]
+        heads, kv_heads, dim = q.shape[1], k.shape[1], q.shape[2]
         _same(q, (self.tokens, heads, dim), q)
-        _same(q, (self.tokens, k.shape[1], dim), k, v)
-        scale = 1 / math.sqrt(max(1, dim)) if scale is None else scale
-        if _stream(q) != self._made_on:                     # (the table must not be given away while that stream still reads it)
+        _same(q, (self.tokens, kv_heads, dim), k, v)
+        if stream != self._made_on:                         # (the table must not be given away while that stream still reads it)
             self._table.record_stream(torch.cuda.current_stream(q.device))
-        return Attention(type=_type(q), heads=heads, kv_heads=k.shape[1], dim=dim, scale=scale, q=_heads(q), k=_heads(k), v=_heads(v))
+        return (_type(q), heads, kv_heads, dim, 1 / math.sqrt(max(1, dim)) if scale is None else scale, *_heads(q), *_heads(k), *_heads(v))
 
     def attention(self, q, k, v, scale=None):
         """tessel_attention_forward: q [tokens, heads, dim], k and v [tokens, kv_heads, dim] -> (o like q, lse [heads, tokens])"""
         import torch
-        a = self._describe(q, k, v, scale)
+        stream = _stream(q)
+        described = self._describe(q, k, v, scale, stream)
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(q.shape[1], self.tokens, dtype=torch.float32, device=q.device)
-        a.o, a.lse = _heads(o), lse.data_ptr()
-        binding._check(_library().tessel_attention_forward(self._h, C.byref(a), _stream(q)))
+        lse = torch.empty((q.shape[1], self.tokens), dtype=torch.float32, device=q.device)
+        a = _FlatAttention(*described, *_heads(o), lse.data_ptr())
+        binding._check(_library().tessel_attention_forward(self._h, C.byref(a), stream))
         return o, lse
 
     def attention_backward(self, d_o, q, k, v, o, lse, scale=None):
         """tessel_attention_backward: (dq, dk, dv) from the gradient of o and what the forward call took and gave"""
         import torch
-        lib = _library()
-        a = self._describe(q, k, v, scale)
+        lib, stream = _library(), _stream(q)
+        described = self._describe(q, k, v, scale, stream)
         _same(q, q.shape, d_o, o)
-        if lse.dtype != torch.float32 or tuple(lse.shape) != (q.shape[1], self.tokens) or not lse.is_contiguous() or lse.device != q.device:
+        if lse.dtype is not torch.float32 or lse.shape != (q.shape[1], self.tokens) or not lse.is_contiguous() or lse.get_device() != q.get_device():
             _refuse("lse is not what the forward call gave")
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        a.o, a.lse, a.d_o, a.dq, a.dk, a.dv = _heads(o), lse.data_ptr(), _heads(d_o), _heads(dq), _heads(dk), _heads(dv)
+        a = _FlatAttention(*described, *_heads(o), lse.data_ptr(), *_heads(d_o), *_heads(dq), *_heads(dk), *_heads(dv))
         n = C.c_size_t()
         binding._check(lib.tessel_attention_backward_workspace_bytes(self._h, C.byref(a), C.byref(n)))
         ws = _workspace(n.value, q)
-        binding._check(lib.tessel_attention_backward(self._h, C.byref(a), ws.data_ptr(), ws.numel(), _stream(q)))
+        binding._check(lib.tessel_attention_backward(self._h, C.byref(a), ws.data_ptr(), ws.numel(), stream))
         return dq, dk, dv
 
 
@@ -210,26 +234,25 @@ def _describe_norm(x, y, pre, post, gate, scale, eps):
         _refuse("expected [tokens, channels]")
     _same(x, x.shape, x, y)
     n, c = x.shape
-    a = ResidualNorm(type=_type(x), tokens=n, channels=c, scale=scale, eps=eps, x=_rows(x), y=_rows(y), pre=_vector(pre, c, x),
-                     post=None if post is None else _vector(post, c, x))
     if gate is None:
-        a.gate_kind = GATE_NONE
+        kind, at = GATE_NONE, (None, 0)
     elif gate.dim() == 1:
-        a.gate_kind, a.gate = GATE_CHANNEL, Rows(_vector(gate, c, x), 0)
+        kind, at = GATE_CHANNEL, (_vector(gate, c, x), 0)
     else:
         _same(x, x.shape, gate)
-        a.gate_kind, a.gate = GATE_TOKEN, _rows(gate)
-    return a
+        kind, at = GATE_TOKEN, _rows(gate)
+    return (_type(x), kind, n, c, scale, eps, *_rows(x), *_rows(y), *at, _vector(pre, c, x), None if post is None else _vector(post, c, x))
 
 
 def residual_norm(x, y, pre, post=None, gate=None, scale=1.0, eps=1e-6):
     """tessel_residual_norm_forward: (r, h, stats) with r = scale x + gate n(y, post), h = n(r, pre).  post None: y itself; gate:
     None, [channels] in 32 bits or [tokens, channels] like x."""
     import torch
-    a = _describe_norm(x, y, pre, post, gate, scale, eps)
-    r, h = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(2))
-    stats = torch.empty(2, x.shape[0], dtype=torch.float32, device=x.device)
-    a.r, a.h, a.stats = _rows(r), _rows(h), stats.data_ptr()
+    described = _describe_norm(x, y, pre, post, gate, scale, eps)
+    shape, dtype, device = x.shape, x.dtype, x.device
+    r, h = torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)
+    stats = torch.empty((2, shape[0]), dtype=torch.float32, device=device)
+    a = _FlatNorm(*described, stats.data_ptr(), r.data_ptr(), shape[1], h.data_ptr(), shape[1])
     binding._check(_library().tessel_residual_norm_forward(C.byref(a), _stream(x)))
     return r, h, stats
 
@@ -239,27 +262,30 @@ def residual_norm_backward(dr, dh, x, y, stats, pre, post=None, gate=None, scale
     dgate) of earlier micro-batches, to which the parameters' gradients are added (dgate: of a gate for the channels)."""
     import torch
     lib = _library()
-    a = _describe_norm(x, y, pre, post, gate, scale, 0.0)
-    _same(x, x.shape, dr, dh)
-    if stats.dtype != torch.float32 or tuple(stats.shape) != (2, x.shape[0]) or not stats.is_contiguous() or stats.device != x.device:
+    described = _describe_norm(x, y, pre, post, gate, scale, 0.0)
+    kind, shape, device = described[1], x.shape, x.device
+    c = shape[1]
+    _same(x, shape, dr, dh)
+    if stats.dtype is not torch.float32 or stats.shape != (2, shape[0]) or not stats.is_contiguous() or stats.get_device() != x.get_device():
         _refuse("stats is not what the forward call gave")
-    dx, dy = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(2))
-    a.stats, a.dr, a.dh, a.dx, a.dy = stats.data_ptr(), _rows(dr), _rows(dh), _rows(dx), _rows(dy)
-    dpre, dpost, dgate = into if into is not None else (None, None, None)
-    c = x.shape[1]
+    dx, dy = torch.empty(shape, dtype=x.dtype, device=device), torch.empty(shape, dtype=x.dtype, device=device)
     if into is None:
-        dpre = torch.empty(c, dtype=torch.float32, device=x.device)
-        dpost = torch.empty_like(dpre) if post is not None else None
-        dgate = torch.empty_like(dpre) if a.gate_kind == GATE_CHANNEL else None
-    a.accumulate = 0 if into is None else 1
-    a.dpre = _vector(dpre, c, x)
+        dpre, dpost, dgate = torch.empty((3, c), dtype=torch.float32, device=device).unbind(0)
+        dpost = dpost if post is not None else None
+        dgate = dgate if kind == GATE_CHANNEL else None
+    else:
+        dpre, dpost, dgate = into
+    to = [_vector(dpre, c, x), None, None]
     if post is not None:
-        a.dpost = _vector(dpost, c, x)
-    if a.gate_kind == GATE_CHANNEL:
-        a.dgate_channel = _vector(dgate, c, x)
-    elif a.gate_kind == GATE_TOKEN:
-        dgate = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        a.dgate = _rows(dgate)
+        to[1] = _vector(dpost, c, x)
+    at = (None, 0)
+    if kind == GATE_CHANNEL:
+        to[2] = _vector(dgate, c, x)
+    elif kind == GATE_TOKEN:
+        dgate = torch.empty(shape, dtype=x.dtype, device=device)
+        at = (dgate.data_ptr(), c)
+    a = _FlatNorm(*described, stats.data_ptr(), None, 0, None, 0, *_rows(dr), *_rows(dh), dx.data_ptr(), c, dy.data_ptr(), c, *at, *to,
+                  0 if into is None else 1)
     n = C.c_size_t()
     binding._check(lib.tessel_residual_norm_backward_workspace_bytes(C.byref(a), C.byref(n)))
     ws = _workspace(n.value, x)
@@ -274,23 +300,20 @@ class Checkpoint:
     def __init__(self, tokens, channels, dtype, device):
         import torch
         groups = -(-channels // GROUP)
-        self.tokens, self.channels, self.dtype, self.device = tokens, channels, dtype, torch.device(device)
-        self.values = torch.empty(tokens, groups * GROUP, dtype=torch.int8, device=device)
-        self.exponents = torch.empty(tokens, groups, dtype=torch.uint8, device=device)
+        self.tokens, self.channels, self.dtype = tokens, channels, dtype
+        self.values = torch.empty((tokens, groups * GROUP), dtype=torch.int8, device=device)
+        self.exponents = torch.empty((tokens, groups), dtype=torch.uint8, device=device)
+        self.device = self.values.device
+        self._words = (self.values.data_ptr(), self.exponents.data_ptr(), groups * GROUP, groups, tokens, channels, _TYPES[dtype])
+        self._desc = CheckpointDesc(*self._words)
 
     @property
     def nbytes(self):
         return self.values.numel() + self.exponents.numel()
 
-    def _desc(self):
-        import torch
-        return CheckpointDesc(self.values.data_ptr(), self.exponents.data_ptr(), self.values.shape[1], self.exponents.shape[1], self.tokens,
-                              self.channels, _type(torch.empty(0, dtype=self.dtype)))
-
-    def _like(self, *tensors):
-        for t in tensors:
-            if not t.is_cuda or t.device != self.values.device or t.dtype != self.dtype or tuple(t.shape) != (self.tokens, self.channels):
-                _refuse("expected %s [%d, %d] on %s, got %s %s" % (self.dtype, self.tokens, self.channels, self.values.device, t.dtype, tuple(t.shape)))
+    def _like(self, t):
+        if not t.is_cuda or t.dtype is not self.dtype or t.shape != (self.tokens, self.channels) or t.get_device() != self.values.get_device():
+            _refuse("expected %s [%d, %d] on %s, got %s %s" % (self.dtype, self.tokens, self.channels, self.device, t.dtype, tuple(t.shape)))
 
 
 def _new_checkpoint(x):
@@ -303,15 +326,17 @@ def _new_checkpoint(x):
 def checkpoint(x):
     """tessel_checkpoint_store: x [tokens, channels] in 8 bits"""
     c = _new_checkpoint(x)
-    binding._check(_library().tessel_checkpoint_store(C.byref(c._desc()), C.byref(_rows(x)), _stream(x)))
+    rows = Rows(*_rows(x))
+    binding._check(_library().tessel_checkpoint_store(C.byref(c._desc), C.byref(rows), _stream(x)))
     return c
 
 
 def restore(c):
     """tessel_checkpoint_restore: what a checkpoint stands for, in the type of what was stored"""
     import torch
-    x = torch.empty(c.tokens, c.channels, dtype=c.dtype, device=c.values.device)
-    binding._check(_library().tessel_checkpoint_restore(C.byref(c._desc()), C.byref(_rows(x)), _stream(x)))
+    x = torch.empty((c.tokens, c.channels), dtype=c.dtype, device=c.device)
+    rows = Rows(x.data_ptr(), c.channels)
+    binding._check(_library().tessel_checkpoint_restore(C.byref(c._desc), C.byref(rows), _stream(x)))
     return x
 
 
@@ -325,11 +350,13 @@ def gated(g, u, act="silu"):
     """tessel_gated_forward: (a, checkpoint of g, checkpoint of u) with a = act(g) u"""
     import torch
     kind = _act(act)
-    kg, ku = _new_checkpoint(g), _new_checkpoint(u)
+    kg = _new_checkpoint(g)
     kg._like(u)
+    ku = _new_checkpoint(u)
     a = torch.empty(g.shape, dtype=g.dtype, device=g.device)
-    binding._check(_library().tessel_gated_forward(kind, C.byref(_rows(g)), C.byref(_rows(u)), C.byref(_rows(a)), C.byref(kg._desc()),
-                                                   C.byref(ku._desc()), _stream(g)))
+    rows = Rows(*_rows(g)), Rows(*_rows(u)), Rows(a.data_ptr(), kg.channels)
+    binding._check(_library().tessel_gated_forward(kind, C.byref(rows[0]), C.byref(rows[1]), C.byref(rows[2]), C.byref(kg._desc),
+                                                   C.byref(ku._desc), _stream(g)))
     return a, kg, ku
 
 
@@ -338,11 +365,12 @@ def gated_backward(da, kg, ku, act="silu", with_output=False):
     import torch
     kind = _act(act)
     kg._like(da)
-    dg, du = (torch.empty(da.shape, dtype=da.dtype, device=da.device) for _ in range(2))
-    a = torch.empty(da.shape, dtype=da.dtype, device=da.device) if with_output else None
-    binding._check(_library().tessel_gated_backward(kind, C.byref(_rows(da)), C.byref(kg._desc()), C.byref(ku._desc()), C.byref(_rows(dg)),
-                                                    C.byref(_rows(du)), C.byref(_rows(a)) if with_output else None, _stream(da)))
-    return (dg, du, a) if with_output else (dg, du)
+    outs = [torch.empty(da.shape, dtype=da.dtype, device=da.device) for _ in range(3 if with_output else 2)]
+    rows = [Rows(t.data_ptr(), kg.channels) for t in outs]
+    d = Rows(*_rows(da))
+    binding._check(_library().tessel_gated_backward(kind, C.byref(d), C.byref(kg._desc), C.byref(ku._desc), C.byref(rows[0]), C.byref(rows[1]),
+                                                    C.byref(rows[2]) if with_output else None, _stream(da)))
+    return tuple(outs)
 
 
 def weight_gradient(dy, x, into=None):
@@ -350,16 +378,19 @@ def weight_gradient(dy, x, into=None):
     to `into` (and that returned) if it is given"""
     import torch
     lib = _library()
-    if dy.dim() != 2 or not dy.is_cuda or dy.device != x.values.device or dy.dtype != x.dtype or dy.shape[0] != x.tokens:
+    if dy.dim() != 2 or not dy.is_cuda or dy.get_device() != x.values.get_device() or dy.dtype is not x.dtype or dy.shape[0] != x.tokens:
         _refuse("dy %s %s does not go with a checkpoint of %s [%d, %d]" % (dy.dtype, tuple(dy.shape), x.dtype, x.tokens, x.channels))
     shape = (dy.shape[1], x.channels)
-    if into is not None and (into.dtype != torch.float32 or tuple(into.shape) != shape or into.device != dy.device or (shape[1] > 1 and into.stride(1) != 1)):
-        _refuse("the sum has to be 32-bit %s on %s" % (shape, dy.device))
-    dw = torch.empty(shape, dtype=torch.float32, device=dy.device) if into is None else into
-    a = WeightGrad(x=x._desc(), dy=_rows(dy), outputs=shape[0], accumulate=0 if into is None else 1, dw=dw.data_ptr(),
-                   dw_stride=dw.stride(0) if shape[0] > 1 else shape[1])
+    if into is None:
+        dw = torch.empty(shape, dtype=torch.float32, device=dy.device)
+    else:
+        dw = into
+        if dw.dtype is not torch.float32 or dw.shape != shape or dw.get_device() != dy.get_device() or (shape[1] > 1 and dw.stride(1) != 1):
+            _refuse("the sum has to be 32-bit %s on %s" % (shape, dy.device))
+    a = _FlatWeight(*x._words, *_rows(dy), shape[0], 0 if into is None else 1, dw.data_ptr(), dw.stride(0) if shape[0] > 1 else shape[1])
     n = C.c_size_t()
     binding._check(lib.tessel_weight_gradient_workspace_bytes(C.byref(a), C.byref(n)))
-    ws = _workspace(n.value, dy)
-    binding._check(lib.tessel_weight_gradient(C.byref(a), ws.data_ptr(), ws.numel(), _stream(dy)))
+    need = n.value
+    ws = _workspace(need, dy) if need else None
+    binding._check(lib.tessel_weight_gradient(C.byref(a), ws.data_ptr() if need else None, need, _stream(dy)))
     return dw

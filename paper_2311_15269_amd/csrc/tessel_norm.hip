@@ -1,9 +1,9 @@
 // The norms around a block with its gate and residual scale, forward and backward (formulas: include/tessel_block_ops.h).
 //
-// A row stays in the registers of its lanes from its one read to its one write: LANES lanes hold it, CHUNKS chunks of eight channels each.
-// Rows of up to 1024 channels take a wave (four rows a workgroup and no barrier), longer ones a workgroup.  Workgroups go over many
-// rows, so the parameters are read once a workgroup and their gradients are summed in registers, then over the workgroups
-// in the order of their numbers by a second kernel.
+// A row stays in the registers of its lanes from its one read to its one write: LANES lanes hold it, CHUNKS times eight channels each.
+// Rows of up to 128 channels take 16 lanes, up to 512 a wave, longer ones up to 1024 lanes.  Workgroups go over many
+// rows, so the parameters are read once a workgroup and their gradients are summed in registers, then over the rows a workgroup
+// works on at once (LDS), then over the workgroups in the order of their numbers by a second kernel.
 #include "tessel_rows.h"
 
 namespace tessel {
@@ -14,14 +14,16 @@ struct NormLaunch {
     int    num_parts;
 };
 
+// sum over a row's lanes; scratch: a word for each wave of the workgroup
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float *scratch)
 {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    for (int d = LANES < 64 ? LANES / 2 : 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
     if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
         __syncthreads();
+        scratch += threadIdx.x / LANES * (LANES / 64);
         v = 0;
 #pragma unroll
         for (int w = 0; w < LANES / 64; w++) v += scratch[w];
@@ -32,31 +34,104 @@ __device__ __forceinline__ float row_sum(float v, float *scratch)
 template <typename T>
 __device__ __forceinline__ T *row_of(const tessel_rows &r, int64_t row) { return (T *)r.data + row * r.stride; }
 
-template <int LANES> constexpr int threads_of() { return LANES > 64 ? LANES : 256; }
+template <int LANES> constexpr int threads_of() { return LANES > 256 ? LANES : 256; }
 
-template <typename T, int LANES, int CHUNKS>
+// The parameters of a lane's channels, ones for those that a call does not have (multiplying by them changes nothing, and one path through
+// the kernels keeps their registers low).  They are kept in registers, in LDS (backward, two chunks: 48 registers less, of which there
+// are then enough: 80 instead of 128 us for 8192 rows of 4096), or read again for each row (backward, more than 8192 channels, which LDS does not hold).
+enum { kInRegisters, kInLds, kInMemory };
+template <int LANES, int CHUNKS, int WHERE>
+struct Parameters {
+    static constexpr int kLds = WHERE == kInLds ? 3 * CHUNKS * 2 * LANES : 1;
+    float kept[WHERE == kInRegisters ? 3 * CHUNKS : 1][8];
+    const float *from[3];
+    float4v *lds;
+    __device__ __forceinline__ void read(float *v, int w, int k, int channels) const
+    {
+        if (from[w]) {
+            load8<float>(v, from[w], 8 * ((int)threadIdx.x % LANES + k * LANES), channels);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[j] = 1.0f;
+        }
+    }
+    __device__ __forceinline__ Parameters(const tessel_residual_norm &a, float4v *shared) : lds(shared + threadIdx.x % LANES)
+    {
+        from[0] = a.pre;
+        from[1] = a.post;
+        from[2] = a.gate_kind == TESSEL_GATE_CHANNEL ? (const float *)a.gate.data : nullptr;
+        if constexpr (WHERE == kInRegisters) {
+#pragma unroll
+            for (int w = 0; w < 3; w++)
+#pragma unroll
+                for (int k = 0; k < CHUNKS; k++) read(kept[w * CHUNKS + k], w, k, a.channels);
+        } else if constexpr (WHERE == kInLds) {
+#pragma unroll
+            for (int w = 0; w < 3; w++)
+#pragma unroll
+                for (int k = 0; k < CHUNKS; k++) {
+                    float v[8];
+                    read(v, w, k, a.channels);
+                    lds[((w * CHUNKS + k) * 2) * LANES] = float4v{v[0], v[1], v[2], v[3]};
+                    lds[((w * CHUNKS + k) * 2 + 1) * LANES] = float4v{v[4], v[5], v[6], v[7]};
+                }
+        }                                                        // (each lane reads back what it wrote itself)
+    }
+    __device__ __forceinline__ void get(float *v, int w, int k, int channels) const
+    {
+        if constexpr (WHERE == kInRegisters) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[j] = kept[w * CHUNKS + k][j];
+        } else if constexpr (WHERE == kInLds) {
+            const float4v x = lds[((w * CHUNKS + k) * 2) * LANES], y = lds[((w * CHUNKS + k) * 2 + 1) * LANES];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                v[j] = x[j];
+                v[4 + j] = y[j];
+            }
+        } else {
+            read(v, w, k, channels);
+        }
+    }
+};
+
+// The rows of a workgroup: neighbours, so that a line of memory that two rows share is written through one cache (rows of 1000 channels,
+// forward and backward: 163 us, with a workgroup's rows spread over the batch 180; rows of whole lines the same).
+struct Range {
+    int64_t begin, end;
+    __device__ __forceinline__ Range(int64_t tokens, int rows)
+    {
+        const int64_t steps = (tokens + rows - 1) / rows, per = steps / gridDim.x, more = steps % gridDim.x, b = blockIdx.x;
+        begin = (b * per + min(b, more)) * rows;
+        end = min(begin + (per + (b < more ? 1 : 0)) * rows, tokens);
+    }
+};
+
+// TOKEN: a gate for each token and channel
+template <typename T, int LANES, int CHUNKS, bool TOKEN>
 __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
 {
+    typedef Parameters<LANES, CHUNKS, kInRegisters> P;
     constexpr int kRows = threads_of<LANES>() / LANES;
-    __shared__ float scratch[2][LANES > 64 ? LANES / 64 : 1];
+    __shared__ float scratch[2][threads_of<LANES>() / 64];
+    __shared__ float4v shared[P::kLds];
     const tessel_residual_norm &a = l.a;
-    const int lane = threadIdx.x % LANES, C = a.channels;
-    float pre[CHUNKS][8], post[CHUNKS][8], gate[CHUNKS][8];
-#pragma unroll
-    for (int k = 0; k < CHUNKS; k++) {
-        const int col = 8 * (lane + k * LANES);
-        load8<float>(pre[k], a.pre, col, C);
-        if (a.post) load8<float>(post[k], a.post, col, C);
-        if (a.gate_kind == TESSEL_GATE_CHANNEL) load8<float>(gate[k], (const float *)a.gate.data, col, C);
-    }
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < a.tokens; row += (int64_t)gridDim.x * kRows) {
+    const int lane = threadIdx.x % LANES;
+    const P p(a, shared);
+    const Range range(a.tokens, kRows);
+    for (int64_t first = range.begin; first < range.end; first += kRows) {
+        // (a workgroup's rows go through the barriers together; behind the last row, the last one once more without a write)
+        const bool there = first + threadIdx.x / LANES < range.end;
+        const int64_t row = there ? first + threadIdx.x / LANES : range.end - 1;
+        const int C = there ? a.channels : 0;
         float x[CHUNKS][8], y[CHUNKS][8], sum = 0;
+        typename Eight<T>::type rg[CHUNKS];
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
             const int col = 8 * (lane + k * LANES);
             load8<T>(x[k], row_of<T>(a.x, row), col, C);
             load8<T>(y[k], row_of<T>(a.y, row), col, C);
-            if (a.gate_kind == TESSEL_GATE_TOKEN) load8<T>(gate[k], row_of<T>(a.gate, row), col, C);
+            if (TOKEN) rg[k] = raw8<T>(row_of<T>(a.gate, row), col, C);
         }
         float over_y = 1.0f;
         if (a.post) {
@@ -64,29 +139,32 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
             for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
                 for (int j = 0; j < 8; j++) sum += y[k][j] * y[k][j];
-            over_y = 1.0f / sqrtf(row_sum<LANES>(sum, scratch[0]) / C + a.eps);
+            over_y = 1.0f / sqrtf(row_sum<LANES>(sum, scratch[0]) / a.channels + a.eps);
         }
         sum = 0;
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
+            float post[8], gate[8];
+            p.get(post, 1, k, C);
+            if (!TOKEN) p.get(gate, 2, k, C);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                float u = y[k][j];
-                if (a.post) u = u * over_y * post[k][j];
-                if (a.gate_kind != TESSEL_GATE_NONE) u *= gate[k][j];
-                x[k][j] = a.scale * x[k][j] + u;
+                const float u = y[k][j] * over_y * post[j];
+                x[k][j] = a.scale * x[k][j] + (TOKEN ? (float)rg[k][j] : gate[j]) * u;
                 sum += x[k][j] * x[k][j];
             }
             store8<T>(row_of<T>(a.r, row), x[k], 8 * (lane + k * LANES), C);
         }
-        const float over_r = 1.0f / sqrtf(row_sum<LANES>(sum, scratch[1]) / C + a.eps);
+        const float over_r = 1.0f / sqrtf(row_sum<LANES>(sum, scratch[1]) / a.channels + a.eps);
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
+            float pre[8];
+            p.get(pre, 0, k, C);
 #pragma unroll
-            for (int j = 0; j < 8; j++) x[k][j] *= over_r * pre[k][j];
+            for (int j = 0; j < 8; j++) x[k][j] *= over_r * pre[j];
             store8<T>(row_of<T>(a.h, row), x[k], 8 * (lane + k * LANES), C);
         }
-        if (lane == 0) {
+        if (lane == 0 && there) {
             a.stats[row] = over_y;
             a.stats[a.tokens + row] = over_r;
         }
@@ -94,87 +172,113 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
     }
 }
 
-template <typename T, int LANES, int CHUNKS>
-__global__ __launch_bounds__(threads_of<LANES>()) void norm_backward_kernel(NormLaunch l)
+template <typename T, int LANES, int CHUNKS, bool TOKEN>
+__global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 ? 4 : CHUNKS == 2 ? 2 : 3) void norm_backward_kernel(NormLaunch l)
 {
+    typedef Parameters<LANES, CHUNKS, CHUNKS == 1 ? kInRegisters : LANES <= 512 ? kInLds : kInMemory> P;
+    __shared__ float4v shared[P::kLds];
     constexpr int kRows = threads_of<LANES>() / LANES;
-    __shared__ float scratch[2][LANES > 64 ? LANES / 64 : 1];
+    __shared__ float scratch[2][threads_of<LANES>() / 64];
     const tessel_residual_norm &a = l.a;
     const int lane = threadIdx.x % LANES, C = a.channels;
-    float pre[CHUNKS][8], post[CHUNKS][8], gate[CHUNKS][8], dpre[CHUNKS][8] = {}, dpost[CHUNKS][8] = {}, dgate[CHUNKS][8] = {};
-#pragma unroll
-    for (int k = 0; k < CHUNKS; k++) {
-        const int col = 8 * (lane + k * LANES);
-        load8<float>(pre[k], a.pre, col, C);
-        if (a.post) load8<float>(post[k], a.post, col, C);
-        if (a.gate_kind == TESSEL_GATE_CHANNEL) load8<float>(gate[k], (const float *)a.gate.data, col, C);
-    }
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < a.tokens; row += (int64_t)gridDim.x * kRows) {
-        float x[CHUNKS][8], y[CHUNKS][8], dr[CHUNKS][8], dh[CHUNKS][8], sum = 0;
+    const P p(a, shared);
+    float dpre[CHUNKS][8] = {}, dpost[CHUNKS][8] = {}, dgate[CHUNKS][8] = {};
+    const Range range(a.tokens, kRows);
+    for (int64_t first = range.begin; first < range.end; first += kRows) {
+        const bool there = first + threadIdx.x / LANES < range.end;           // (as in norm_kernel)
+        const int64_t row = there ? first + threadIdx.x / LANES : range.end - 1;
+        const int C = there ? a.channels : 0;
+        typename Eight<T>::type rx[CHUNKS], ry[CHUNKS], rr[CHUNKS], rh[CHUNKS], rg[CHUNKS];
+        float x[CHUNKS][8], y[CHUNKS][8], dn[CHUNKS][8], sum = 0;
         const float over_y = a.stats[row], over_r = a.stats[a.tokens + row];
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
             const int col = 8 * (lane + k * LANES);
-            load8<T>(x[k], row_of<T>(a.x, row), col, C);
-            load8<T>(y[k], row_of<T>(a.y, row), col, C);
-            load8<T>(dr[k], row_of<T>(a.dr, row), col, C);
-            load8<T>(dh[k], row_of<T>(a.dh, row), col, C);
-            if (a.gate_kind == TESSEL_GATE_TOKEN) load8<T>(gate[k], row_of<T>(a.gate, row), col, C);
+            rx[k] = raw8<T>(row_of<T>(a.x, row), col, C);
+            ry[k] = raw8<T>(row_of<T>(a.y, row), col, C);
+            rr[k] = raw8<T>(row_of<T>(a.dr, row), col, C);
+            rh[k] = raw8<T>(row_of<T>(a.dh, row), col, C);
+            if (TOKEN) rg[k] = raw8<T>(row_of<T>(a.gate, row), col, C);
         }
 #pragma unroll
-        for (int k = 0; k < CHUNKS; k++)
+        for (int k = 0; k < CHUNKS; k++) {
+            float pre[8], post[8], gate[8];
+            p.get(pre, 0, k, C);
+            p.get(post, 1, k, C);
+            if (!TOKEN) p.get(gate, 2, k, C);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                if (a.post) y[k][j] *= over_y;
-                float u = a.post ? y[k][j] * post[k][j] : y[k][j];
-                if (a.gate_kind != TESSEL_GATE_NONE) u *= gate[k][j];
-                x[k][j] = (a.scale * x[k][j] + u) * over_r;      // r by its root mean square
-                dpre[k][j] += dh[k][j] * x[k][j];
-                dh[k][j] *= pre[k][j];
-                sum += dh[k][j] * x[k][j];
+                y[k][j] = (float)ry[k][j] * over_y;
+                const float u = y[k][j] * post[j];
+                x[k][j] = (a.scale * (float)rx[k][j] + (TOKEN ? (float)rg[k][j] : gate[j]) * u) * over_r;      // r by its root mean square
+                dn[k][j] = (float)rh[k][j];
+                dpre[k][j] += dn[k][j] * x[k][j];
+                dn[k][j] *= pre[j];
+                sum += dn[k][j] * x[k][j];
             }
-        const float mean_r = row_sum<LANES>(sum, scratch[0]) / C;
+        }
+        const float mean_r = row_sum<LANES>(sum, scratch[0]) / a.channels;
         sum = 0;
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
             const int col = 8 * (lane + k * LANES);
+            float v[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                dr[k][j] += over_r * (dh[k][j] - x[k][j] * mean_r);
-                x[k][j] = a.scale * dr[k][j];
+                dn[k][j] = (float)rr[k][j] + over_r * (dn[k][j] - x[k][j] * mean_r);      // the gradient of r
+                v[j] = a.scale * dn[k][j];
             }
-            store8<T>(row_of<T>(a.dx, row), x[k], col, C);
-            if (a.gate_kind != TESSEL_GATE_NONE) {
+            store8<T>(row_of<T>(a.dx, row), v, col, C);
+            float post[8], gate[8];
+            p.get(post, 1, k, C);
+            if (!TOKEN) p.get(gate, 2, k, C);
 #pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    const float u = a.post ? y[k][j] * post[k][j] : y[k][j];
-                    x[k][j] = dr[k][j] * u;
-                    dgate[k][j] += x[k][j];
-                    dr[k][j] *= gate[k][j];
-                }
-                if (a.gate_kind == TESSEL_GATE_TOKEN) store8<T>(row_of<T>(a.dgate, row), x[k], col, C);
+            for (int j = 0; j < 8; j++) {
+                v[j] = dn[k][j] * (y[k][j] * post[j]);
+                if (!TOKEN) dgate[k][j] += v[j];
+                dn[k][j] *= TOKEN ? (float)rg[k][j] : gate[j];
+                dpost[k][j] += dn[k][j] * y[k][j];
+                dn[k][j] *= post[j];
+                sum += dn[k][j] * y[k][j];
             }
-            if (a.post) {
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    dpost[k][j] += dr[k][j] * y[k][j];
-                    dr[k][j] *= post[k][j];
-                    sum += dr[k][j] * y[k][j];
-                }
-            }
+            if (TOKEN) store8<T>(row_of<T>(a.dgate, row), v, col, C);
         }
-        if (a.post) {
-            const float mean_y = row_sum<LANES>(sum, scratch[1]) / C;
+        const float mean_y = a.post ? row_sum<LANES>(sum, scratch[1]) / a.channels : 0.0f;
 #pragma unroll
-            for (int k = 0; k < CHUNKS; k++)
+        for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
-                for (int j = 0; j < 8; j++) dr[k][j] = over_y * (dr[k][j] - y[k][j] * mean_y);
-        }
+            for (int j = 0; j < 8; j++) dn[k][j] = over_y * (dn[k][j] - y[k][j] * mean_y);
 #pragma unroll
-        for (int k = 0; k < CHUNKS; k++) store8<T>(row_of<T>(a.dy, row), dr[k], 8 * (lane + k * LANES), C);
+        for (int k = 0; k < CHUNKS; k++) store8<T>(row_of<T>(a.dy, row), dn[k], 8 * (lane + k * LANES), C);
         if constexpr (LANES > 64) __syncthreads();
     }
-    float *out = l.parts + (int64_t)(blockIdx.x * kRows + threadIdx.x / LANES) * 3 * C;
+    // the rows of a workgroup add up in order
+    if constexpr (kRows > 1) {
+        __shared__ float sums[(kRows - 1) * LANES * 8 * 3];
+        static_assert(CHUNKS == 1, "one chunk a lane");
+        const int group = threadIdx.x / LANES;
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            float *at = sums + ((group - 1) * 24 + j) * LANES + lane;
+            if (group > 0) {
+                at[0] = dpre[0][j];
+                at[8 * LANES] = dpost[0][j];
+                at[16 * LANES] = dgate[0][j];
+            }
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll 1
+        for (int g = 0; g < kRows - 1; g++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                const float *at = sums + (g * 24 + j) * LANES + lane;
+                dpre[0][j] += at[0];
+                dpost[0][j] += at[8 * LANES];
+                dgate[0][j] += at[16 * LANES];
+            }
+    }
+    float *out = l.parts + (int64_t)blockIdx.x * 3 * C;
 #pragma unroll
     for (int k = 0; k < CHUNKS; k++) {
         const int col = 8 * (lane + k * LANES);
@@ -184,24 +288,25 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_backward_kernel(Norm
     }
 }
 
-// sums of the workgroups' parts: 32 columns a workgroup, eight lanes a column over every eighth part
-__global__ __launch_bounds__(256) void norm_sum_kernel(NormLaunch l)
+// sums of the workgroups' parts: 64 columns a workgroup, sixteen waves over every sixteenth part each
+__global__ __launch_bounds__(1024) void norm_sum_kernel(NormLaunch l)
 {
-    __shared__ float sums[8][32];
+    __shared__ float sums[16][64];
     const tessel_residual_norm &a = l.a;
-    const int which = blockIdx.y, col = blockIdx.x * 32 + (threadIdx.x & 31), group = threadIdx.x >> 5;
+    const int which = blockIdx.y, lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane, group = threadIdx.x >> 6;
     float *out = which == 0 ? a.dpre : which == 1 ? a.dpost : a.dgate_channel;
     if (which == 1 && !a.post) return;
     if (which == 2 && a.gate_kind != TESSEL_GATE_CHANNEL) return;
     float sum = 0;
     if (col < a.channels)
-        for (int p = group; p < l.num_parts; p += 8) sum += l.parts[((int64_t)p * 3 + which) * a.channels + col];
-    sums[group][threadIdx.x & 31] = sum;
+#pragma unroll 8
+        for (int p = group; p < l.num_parts; p += 16) sum += l.parts[((int64_t)p * 3 + which) * a.channels + col];
+    sums[group][lane] = sum;
     __syncthreads();
     if (group == 0 && col < a.channels) {
         sum = a.accumulate ? out[col] : 0.0f;
 #pragma unroll
-        for (int g = 0; g < 8; g++) sum += sums[g][threadIdx.x];
+        for (int g = 0; g < 16; g++) sum += sums[g][lane];
         out[col] = sum;
     }
 }
@@ -211,13 +316,13 @@ struct NormShape {
 };
 static NormShape shape_of(int channels)
 {
-    const int lanes = channels <= 1024 ? 64 : channels <= 4096 ? 256 : 1024;
-    const int chunks = channels <= lanes * 8 ? 1 : 2;
-    const int threads = lanes > 64 ? lanes : 256;
-    return {lanes, chunks, threads, threads / lanes};
+    // (4096 channels: 256 lanes with two chunks; 512 with one meet at barriers of eight waves, 61 instead of 50 us forward for 8192 rows)
+    const int lanes = channels <= 128 ? 16 : channels <= 512 ? 64 : channels <= 1024 ? 128 : channels <= 4096 ? 256 : channels <= 8192 ? 512 : 1024;
+    const int threads = lanes > 256 ? lanes : 256;
+    return {lanes, channels > lanes * 8 ? 2 : 1, threads, threads / lanes};
 }
 
-// workgroups: as many as are resident at once, at most one for each row (or four)
+// workgroups: at most one for each row that they work on at once
 static int64_t groups_of(const tessel_residual_norm &a, int64_t most)
 {
     const NormShape s = shape_of(a.channels);
@@ -225,30 +330,38 @@ static int64_t groups_of(const tessel_residual_norm &a, int64_t most)
     return need < most ? need : most;
 }
 
+// backward: as many workgroups as are resident at once, each leaves a part
 int norm_parts(const tessel_residual_norm &a)
 {
     const NormShape s = shape_of(a.channels);
-    return (int)(groups_of(a, s.threads == 1024 ? 256 : 512) * s.rows);
+    return (int)groups_of(a, s.threads > 256 ? 256 : s.chunks == 2 ? 512 : 768);
 }
 
-template <typename T>
+template <typename T, bool TOKEN>
 static const void *norm_of(const NormShape &s, bool back)
 {
-#define PICK(L, K) if (s.lanes == L && s.chunks == K) return back ? (const void *)norm_backward_kernel<T, L, K> : (const void *)norm_kernel<T, L, K>;
+#define PICK(L, K) if (s.lanes == L && s.chunks == K) return back ? (const void *)norm_backward_kernel<T, L, K, TOKEN> : (const void *)norm_kernel<T, L, K, TOKEN>;
+    PICK(16, 1)
     PICK(64, 1)
-    PICK(64, 2)
+    PICK(128, 1)
     PICK(256, 1)
     PICK(256, 2)
-    PICK(1024, 1)
+    PICK(512, 2)
     PICK(1024, 2)
 #undef PICK
     return nullptr;
 }
 
+template <bool TOKEN>
 static const void *norm_of(const tessel_residual_norm &a, bool back)
 {
     const NormShape s = shape_of(a.channels);
-    return a.type == TESSEL_BF16 ? norm_of<bf16>(s, back) : a.type == TESSEL_F16 ? norm_of<f16>(s, back) : norm_of<float>(s, back);
+    return a.type == TESSEL_BF16 ? norm_of<bf16, TOKEN>(s, back) : a.type == TESSEL_F16 ? norm_of<f16, TOKEN>(s, back) : norm_of<float, TOKEN>(s, back);
+}
+
+static const void *norm_of(const tessel_residual_norm &a, bool back)
+{
+    return a.gate_kind == TESSEL_GATE_TOKEN ? norm_of<true>(a, back) : norm_of<false>(a, back);
 }
 
 int launch_norm(const tessel_residual_norm &a, void *stream)
@@ -256,7 +369,7 @@ int launch_norm(const tessel_residual_norm &a, void *stream)
     NormLaunch l = {a, nullptr, 0};
     void *args[] = {&l};
     const NormShape s = shape_of(a.channels);
-    const int64_t groups = groups_of(a, s.threads == 1024 ? 512 : 2048);
+    const int64_t groups = groups_of(a, s.threads > 256 ? 512 : 2048);
     if (groups == 0) return 0;
     return launched(hipLaunchKernel(norm_of(a, false), dim3((unsigned)groups), dim3(s.threads), args, 0, (hipStream_t)stream));
 }
@@ -268,9 +381,9 @@ int launch_norm_backward(const tessel_residual_norm &a, float *parts, void *stre
     const NormShape s = shape_of(a.channels);
     int e = 0;
     if (l.num_parts > 0)
-        e = launched(hipLaunchKernel(norm_of(a, true), dim3((unsigned)(l.num_parts / s.rows)), dim3(s.threads), args, 0, (hipStream_t)stream));
+        e = launched(hipLaunchKernel(norm_of(a, true), dim3((unsigned)l.num_parts), dim3(s.threads), args, 0, (hipStream_t)stream));
     if (e == 0)
-        e = launched(hipLaunchKernel((const void *)norm_sum_kernel, dim3((unsigned)((a.channels + 31) / 32), 3), dim3(256), args, 0, (hipStream_t)stream));
+        e = launched(hipLaunchKernel((const void *)norm_sum_kernel, dim3((unsigned)((a.channels + 63) / 64), 3), dim3(1024), args, 0, (hipStream_t)stream));
     return e;
 }
 

@@ -13,33 +13,59 @@ template <typename T> struct Eight {
     typedef T type __attribute__((ext_vector_type(8), aligned(sizeof(T))));
 };
 
-// values col .. col + 7 of a row of `channels`, zeros behind its end
+// values col .. col + 7 of a row of `channels`, zeros behind its end, as they are.  The end of a row in pieces of four, two and one.
+template <typename T>
+__device__ __forceinline__ typename Eight<T>::type raw8(const T *row, int col, int channels)
+{
+    typedef T V4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    typedef T V2 __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+    if (col + 8 <= channels) return *(const typename Eight<T>::type *)(row + col);
+    typename Eight<T>::type v = {};
+    const int n = channels - col;
+    if (n <= 0) return v;
+    V4 x = {};
+    V2 y = {};
+    T z = (T)0.0f;
+    if (n & 4) x = *(const V4 *)(row + col);
+    if (n & 2) y = *(const V2 *)(row + col + (n & 4));
+    if (n & 1) z = row[col + (n & 6)];
+    const V2 last = (n & 2) ? y : V2{z, (T)0.0f}, after = (n & 2) ? V2{z, (T)0.0f} : V2{(T)0.0f, (T)0.0f};
+    if (n & 4) {
+        v[0] = x[0], v[1] = x[1], v[2] = x[2], v[3] = x[3];
+        v[4] = last[0], v[5] = last[1], v[6] = after[0];
+    } else {
+        v[0] = last[0], v[1] = last[1], v[2] = after[0];
+    }
+    return v;
+}
+
+// the same in 32 bits
 template <typename T>
 __device__ __forceinline__ void load8(float *v, const T *row, int col, int channels)
 {
-    if (col + 8 <= channels) {
-        const typename Eight<T>::type w = *(const typename Eight<T>::type *)(row + col);
+    const typename Eight<T>::type w = raw8<T>(row, col, channels);
 #pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = (float)w[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = col + j < channels ? (float)row[col + j] : 0.0f;
-    }
+    for (int j = 0; j < 8; j++) v[j] = (float)w[j];
 }
 
 template <typename T>
 __device__ __forceinline__ void store8(T *row, const float *v, int col, int channels)
 {
+    typedef T V4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    typedef T V2 __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+    typename Eight<T>::type w;
+#pragma unroll
+    for (int j = 0; j < 8; j++) w[j] = (T)v[j];
     if (col + 8 <= channels) {
-        typename Eight<T>::type w;
-#pragma unroll
-        for (int j = 0; j < 8; j++) w[j] = (T)v[j];
         *(typename Eight<T>::type *)(row + col) = w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j++)
-            if (col + j < channels) row[col + j] = (T)v[j];
+        return;
     }
+    const int n = channels - col;
+    if (n <= 0) return;
+    if (n & 4) *(V4 *)(row + col) = V4{w[0], w[1], w[2], w[3]};
+    const V2 pair = (n & 4) ? V2{w[4], w[5]} : V2{w[0], w[1]}, next = (n & 4) ? V2{w[6], w[7]} : V2{w[2], w[3]};
+    if (n & 2) *(V2 *)(row + col + (n & 4)) = pair;
+    if (n & 1) row[col + (n & 6)] = (n & 2) ? next[0] : pair[0];
 }
 
 // exponents of a checkpoint as they are held, e + 127: the least of a type, and the one at which 64 2^e leaves its range
