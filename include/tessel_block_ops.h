@@ -152,7 +152,7 @@ int  tessel_gated_backward(int act, const tessel_rows *da, const tessel_checkpoi
  * dw in 32 bits, products of the checkpoint's type (bf16 or f16) summed in 32 bits. */
 typedef struct {
     tessel_checkpoint x;
-    tessel_rows dy;            /* [tokens][outputs], the checkpoint's type                                 */
+    tessel_rows dy;            /* [tokens][outputs], the checkpoint's type; strides here at most 2^24     */
     int32_t  outputs;
     int32_t  accumulate;
     float   *dw;               /* [outputs][channels]                                                      */

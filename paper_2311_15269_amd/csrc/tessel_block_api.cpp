@@ -30,6 +30,8 @@ int hip_result(int e)
 constexpr int64_t kMostBlocks = INT32_MAX;
 constexpr int64_t kMostStride = (int64_t)1 << 40;    // (elements; a product with a token's number stays far inside 64 bits)
 
+constexpr int64_t kMostNear = (int64_t)1 << 24;      // (where a kernel takes 32-bit offsets over 64 rows)
+
 int size_of(int type) { return type == TESSEL_F32 ? 4 : 2; }
 bool is_type(int type) { return type == TESSEL_BF16 || type == TESSEL_F16 || type == TESSEL_F32; }
 bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -109,6 +111,7 @@ int weight_ok(const tessel_weight_grad *a)
     if (e) return e;
     if (a->x.type == TESSEL_F32) return TESSEL_E_UNSUPPORTED;
     if ((int64_t)((a->outputs + 127) / 128) * ((a->x.channels + 127) / 128) > kMostBlocks) return TESSEL_E_TOOBIG;
+    if (a->dy.stride > kMostNear || a->x.value_stride > kMostNear || a->x.exponent_stride > kMostNear) return TESSEL_E_TOOBIG;
     if (!a->dw || !aligned(a->dw, 4) || a->dw_stride < a->x.channels || a->dw_stride > kMostStride) return TESSEL_E_INVALID_ARG;
     return rows_ok(a->dy, a->x.type, a->x.tokens, a->outputs, false) ? TESSEL_OK : TESSEL_E_INVALID_ARG;
 }

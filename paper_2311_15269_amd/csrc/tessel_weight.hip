@@ -1,14 +1,18 @@
 // Gradient of a product's weights from an input kept in 8 bits: dw[n][c] = sum_t dy[t][n] x[t][c] (include/tessel_block_ops.h).
 //
-// A workgroup of four waves takes 128 x 128 of dw, 64 x 64 a wave, and goes over the tokens 64 at a time.  The summed index runs along
-// the rows of both inputs, so both operands come out of LDS by transposing reads.  The checkpoint is turned into numbers
-// of the matrix instruction's type on its way to LDS, which is exact.  Few tiles: the tokens are split over several workgroups,
-// whose sums a second kernel adds in the order of their numbers.
+// A workgroup takes a tile of dw and goes over the tokens 64 at a time; each wave has 64 columns (c) of it and 32 MB rows (n).  The summed
+// index runs along the rows of both inputs, so both operands come out of LDS by transposing reads.  The checkpoint is turned into
+// numbers of the matrix instruction's type on its way to LDS, which is exact.  Few tiles: the tokens are split over several
+// workgroups, whose sums a second kernel adds in the order of their numbers.
+#include <type_traits>
+
 #include "tessel_rows.h"
 
 namespace tessel {
 
-constexpr int kThreads = 256, kTile = 128, kSteps = 64;
+constexpr int kSteps = 64;       // tokens at a time
+constexpr int kPanel = 128;      // columns of a panel in LDS
+constexpr int kPanelSize = kSteps * kPanel / 8;
 
 struct WeightLaunch {
     tessel_weight_grad a;
@@ -18,132 +22,264 @@ struct WeightLaunch {
     int     tiles_c;
 };
 
-template <typename T>
+// What dy looks like decides how it comes to LDS.
+//   kStraight  rows of whole chunks of 16 bytes: from memory to LDS without passing registers, three buffers, two tiles ahead
+//   kAny       through registers, one tile ahead
+enum { kStraight, kAny };
+
+// 64 tokens x COLUMNS of dy through registers
+template <typename T, int COLUMNS, int THREADS>
 struct DyStage {
-    uint4v v[4];
+    static constexpr int kChunks = COLUMNS / 8, kPer = kSteps * kChunks / THREADS, kRows = THREADS / kChunks;
+    typename Eight<T>::type v[kPer];
     __device__ __forceinline__ void fetch(const tessel_weight_grad &a, int64_t t0, int64_t end, int n0)
     {
+        const int r = threadIdx.x / kChunks, col = n0 + 8 * (threadIdx.x % kChunks);
+        const T *p = (const T *)a.dy.data + (t0 + r) * a.dy.stride;
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int k = threadIdx.x + i * kThreads, col = n0 + 8 * (k % 16);
-            const int64_t t = t0 + k / 16;
-            typename Eight<T>::type w = {};
-            if (t < end) {
-                const T *row = (const T *)a.dy.data + t * a.dy.stride;
-                if (col + 8 <= a.outputs) {
-                    w = *(const typename Eight<T>::type *)(row + col);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; j++)
-                        if (col + j < a.outputs) w[j] = row[col + j];
-                }
-            }
-            v[i] = __builtin_bit_cast(uint4v, w);
+        for (int i = 0; i < kPer; i++) {
+            v[i] = typename Eight<T>::type{};
+            if (t0 + r + i * kRows < end) v[i] = raw8<T>(p + i * kRows * a.dy.stride, col, a.outputs);
         }
     }
     __device__ __forceinline__ void put(uint4v *tile) const
     {
+        const int r = threadIdx.x / kChunks, c = threadIdx.x % kChunks;
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int k = threadIdx.x + i * kThreads;
-            tile[chunk_at<128>(k / 16, k % 16)] = v[i];
-        }
+        for (int i = 0; i < kPer; i++) tile[c / 16 * kPanelSize + chunk_at<kPanel>(r + i * kRows, c % 16)] = __builtin_bit_cast(uint4v, v[i]);
     }
 };
 
-template <typename T>
-struct HeldStage {
-    uint2    v[4];
-    uint32_t e[4];
-    __device__ __forceinline__ void fetch(const tessel_weight_grad &a, int64_t t0, int64_t end, int c0)
+// The same from memory straight to LDS.  Columns behind the outputs and rows behind the tokens repeat the last ones; the rows are
+// overwritten with zeros (clear), the columns' sums are not stored.
+template <typename T, int COLUMNS, int THREADS>
+struct DyCopy {
+    static constexpr int kChunks = COLUMNS / 8, kPer = kSteps * kChunks / THREADS;
+    static constexpr int kRows = THREADS / 16, kEach = kSteps / kRows;         // a panel at a time: rows an instruction, instructions
+    static_assert(kRows % 16 == 0 && kEach * (COLUMNS / kPanel) == kPer, "the order of chunks repeats after 16 rows");
+    __device__ __forceinline__ static void start(uint4v *tile, const tessel_weight_grad &a, int64_t t0, int64_t end, int n0)
     {
+        const int r = threadIdx.x / 16, c = (threadIdx.x % 16) ^ (chunk_at<kPanel>(r, 0) % 16);
+        const T *p = (const T *)a.dy.data + t0 * a.dy.stride;
+        const uint32_t stride = (uint32_t)a.dy.stride, last = (uint32_t)min((int64_t)kSteps, end - t0) - 1;
+        lds_uint4v *to = (lds_uint4v *)(tile + __builtin_amdgcn_readfirstlane(threadIdx.x & ~63));
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int k = threadIdx.x + i * kThreads, col = c0 + 8 * (k % 16);
-            const int64_t t = t0 + k / 16;
-            v[i] = make_uint2(0, 0);
-            e[i] = 1;
-            if (t < end && col < a.x.channels) {
-                v[i] = *(const uint2 *)(a.x.values + t * a.x.value_stride + col);
-                e[i] = a.x.exponents[t * a.x.exponent_stride + col / kGroup];
-            }
+        for (int b = 0; b < COLUMNS / kPanel; b++) {
+            const uint32_t col = min(n0 + b * kPanel + 8 * c, a.outputs - 8);
+#pragma unroll
+            for (int i = 0; i < kEach; i++)
+                __builtin_amdgcn_global_load_lds((global_uint4v *)(p + (min((uint32_t)(r + i * kRows), last) * stride + col)), to + b * kPanelSize + i * THREADS, 16, 0, 0);
         }
     }
-    __device__ __forceinline__ void put(uint4v *tile) const
+    __device__ __forceinline__ static void clear(uint4v *tile, int rows)
     {
+        for (int k = threadIdx.x; k < (kSteps - rows) * kChunks; k += THREADS)
+            tile[k / (16 * (kSteps - rows)) * kPanelSize + (rows + k / 16 % (kSteps - rows)) * 16 + k % 16] = uint4v{0, 0, 0, 0};
+    }
+};
+
+// 64 tokens x COLUMNS of a checkpoint through registers, sixteen values a lane.  Columns behind the channels repeat others.
+template <typename T, int COLUMNS, int THREADS>
+struct HeldStage {
+    static constexpr int kChunks = COLUMNS / 16, kPer = kSteps * kChunks / THREADS, kRows = THREADS / kChunks;
+    uint4v   v[kPer];
+    uint32_t e[kPer];
+    __device__ __forceinline__ void fetch(const tessel_weight_grad &a, int64_t t0, int64_t end, int c0)
+    {
+        const int r = threadIdx.x / kChunks;
+        const uint32_t col = min(c0 + 16 * ((int)threadIdx.x % kChunks), (a.x.channels - 1) & ~15);   // (behind the channels, values to the end of the group)
+        const int8_t *p = a.x.values + t0 * a.x.value_stride;
+        const uint8_t *q = a.x.exponents + t0 * a.x.exponent_stride;
+        const uint32_t last = (uint32_t)min((int64_t)kSteps, end - t0) - 1;
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int k = threadIdx.x + i * kThreads;
+        for (int i = 0; i < kPer; i++) {
+            const uint32_t row = min((uint32_t)(r + i * kRows), last);
+            v[i] = *(const uint4v *)(p + (row * (uint32_t)a.x.value_stride + col));
+            e[i] = q[row * (uint32_t)a.x.exponent_stride + col / kGroup];
+        }
+    }
+    // rows: of which tokens there are
+    __device__ __forceinline__ void put(uint4v *tile, int rows, int i) const
+    {
+        const int r = threadIdx.x / kChunks + i * kRows, c = 2 * (threadIdx.x % kChunks);
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
             float f[8];
-            held8(f, v[i], e[i]);
+            held8(f, make_uint2(v[i][2 * h], v[i][2 * h + 1]), e[i]);
             uint4v w;
 #pragma unroll
             for (int j = 0; j < 4; j++) w[j] = pack2<T>(f[2 * j], f[2 * j + 1]);
-            tile[chunk_at<128>(k / 16, k % 16)] = w;
+            if (r >= rows) w = uint4v{0, 0, 0, 0};
+            tile[c / 16 * kPanelSize + chunk_at<kPanel>(r, (c + h) % 16)] = w;
         }
     }
 };
 
-template <typename T>
-__global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightLaunch l)
+// The operands of one step of sixteen tokens, MB of rows and two of columns, by transposing reads from LDS in one piece that ends when all
+// have arrived.  (The compiler, where it places such a read itself, first waits for every copy to LDS that is on its way.)
+__device__ __forceinline__ uint4v join(uint64_t lo, uint64_t hi)
 {
-    __shared__ __attribute__((aligned(256))) uint4v rows[kSteps * kTile / 8], columns[kSteps * kTile / 8];
+    typedef uint64_t V __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint4v, V{lo, hi});
+}
+template <int S>
+__device__ __forceinline__ void read_step(uint4v (&f)[4], uint4v (&g)[2], const uint32_t (&x)[8], const uint32_t (&y)[4])
+{
+    uint64_t r[12];
+    asm volatile("ds_read_b64_tr_b16 %0, %12 offset:%24\n\tds_read_b64_tr_b16 %1, %13 offset:%25\n\t"
+                 "ds_read_b64_tr_b16 %8, %20 offset:%24\n\tds_read_b64_tr_b16 %9, %21 offset:%25\n\t"
+                 "ds_read_b64_tr_b16 %2, %14 offset:%24\n\tds_read_b64_tr_b16 %3, %15 offset:%25\n\t"
+                 "ds_read_b64_tr_b16 %10, %22 offset:%24\n\tds_read_b64_tr_b16 %11, %23 offset:%25\n\t"
+                 "ds_read_b64_tr_b16 %4, %16 offset:%24\n\tds_read_b64_tr_b16 %5, %17 offset:%25\n\t"
+                 "ds_read_b64_tr_b16 %6, %18 offset:%24\n\tds_read_b64_tr_b16 %7, %19 offset:%25\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]), "=&v"(r[8]), "=&v"(r[9]),
+                   "=&v"(r[10]), "=&v"(r[11])
+                 : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(x[4]), "v"(x[5]), "v"(x[6]), "v"(x[7]), "v"(y[0]), "v"(y[1]), "v"(y[2]), "v"(y[3]),
+                   "n"(S * 16 * 2 * kPanel), "n"(S * 16 * 2 * kPanel + 8 * 2 * kPanel)
+                 : "memory");
+#pragma unroll
+    for (int b = 0; b < 4; b++) f[b] = join(r[2 * b], r[2 * b + 1]);
+#pragma unroll
+    for (int b = 0; b < 2; b++) g[b] = join(r[8 + 2 * b], r[9 + 2 * b]);
+}
+template <int S>
+__device__ __forceinline__ void read_step(uint4v (&f)[2], uint4v (&g)[2], const uint32_t (&x)[4], const uint32_t (&y)[4])
+{
+    uint64_t r[8];
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %2, %10 offset:%16\n\tds_read_b64_tr_b16 %3, %11 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%17\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+                 : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(y[0]), "v"(y[1]), "v"(y[2]), "v"(y[3]),
+                   "n"(S * 16 * 2 * kPanel), "n"(S * 16 * 2 * kPanel + 8 * 2 * kPanel)
+                 : "memory");
+#pragma unroll
+    for (int b = 0; b < 2; b++) f[b] = join(r[2 * b], r[2 * b + 1]);
+#pragma unroll
+    for (int b = 0; b < 2; b++) g[b] = join(r[4 + 2 * b], r[5 + 2 * b]);
+}
+
+// WN x WC waves, 32 MB x 64 of dw each
+template <typename T, int WN, int WC, int MB, int HOW>
+__global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
+{
+    constexpr int kThreads = 64 * WN * WC, kRows = WN * MB * 32, kColumns = WC * 64, kBuffers = HOW == kStraight ? 3 : 2;
+    static_assert(kRows % kPanel == 0 && kColumns % kPanel == 0, "whole panels");
+    typedef DyCopy<T, kRows, kThreads> Copy;
+    __shared__ __attribute__((aligned(256))) uint4v rows[kBuffers][kSteps * kRows / 8], columns[2][kSteps * kColumns / 8];
     const tessel_weight_grad &a = l.a;
-    const int n0 = blockIdx.x / l.tiles_c * kTile, c0 = blockIdx.x % l.tiles_c * kTile;
+    // workgroups go to the eight L2 caches in turn: each cache gets neighbouring tiles, which share their inputs
+    const int all = gridDim.x, per = all / 8, more = all % 8, x = blockIdx.x % 8;
+    const int place = x * per + min(x, more) + blockIdx.x / 8;
+    const int n0 = place / l.tiles_c * kRows, c0 = place % l.tiles_c * kColumns;
     const int64_t begin = blockIdx.y * l.per, end = min(begin + l.per, a.x.tokens);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-    const int wn = wave >> 1, wc = wave & 1;
-    const Reader<128> at;
-    float16v acc[2][2] = {};
-    DyStage<T> ds;
-    HeldStage<T> hs;
-    ds.fetch(a, begin, end, n0);
-    hs.fetch(a, begin, end, c0);
-    for (int64_t t = begin; t < end; t += kSteps) {
-        __syncthreads();
-        ds.put(rows);
-        hs.put(columns);
-        __syncthreads();
-        ds.fetch(a, t + kSteps, end, n0);
-        hs.fetch(a, t + kSteps, end, c0);
+    const int wn = wave / WC * MB, wc = wave % WC * 2;           // in blocks of 32
+    float16v acc[MB][2] = {};
+    if (begin < end) {
+        const Reader<kPanel> at;
+        uint32_t fx[2 * MB], gy[4];                              // operands' addresses: blocks of 32, both halves of their eight tokens
 #pragma unroll
-        for (int s = 0; s < kSteps / 16; s++) {
-            uint4v x[2], y[2];
+        for (int b = 0; b < MB; b++)
 #pragma unroll
-            for (int b = 0; b < 2; b++) {
-                x[b] = at.columns((const lds_tile *)rows, 16 * s, 2 * wn + b);
-                y[b] = at.columns((const lds_tile *)columns, 16 * s, 2 * wc + b);
+            for (int h = 0; h < 2; h++) fx[2 * b + h] = (uint32_t)(uintptr_t)(lds_tile *)rows[0] + (wn + b) / 4 * kPanelSize * 16 + (at.c ^ (64 * ((wn + b) % 4) + 32 * h));
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) gy[2 * b + h] = (uint32_t)(uintptr_t)(lds_tile *)columns[0] + wc / 4 * kPanelSize * 16 + (at.c ^ (64 * (wc % 4 + b) + 32 * h));
+        HeldStage<T, kColumns, kThreads> hs;
+        DyStage<T, HOW == kAny ? kRows : 8, HOW == kAny ? kThreads : 8> ds;
+        const int64_t tiles = (end - begin + kSteps - 1) / kSteps;
+        auto left = [&](int64_t n) { return (int)min((int64_t)kSteps, end - begin - n * kSteps); };
+        hs.fetch(a, begin, end, c0);
+        if constexpr (HOW == kStraight) Copy::start(rows[0], a, begin, end, n0);
+        else ds.fetch(a, begin, end, n0);
+#pragma unroll
+        for (int i = 0; i < hs.kPer; i++) hs.put(columns[0], left(0), i);
+        if constexpr (HOW == kAny) ds.put(rows[0]);
+        if (tiles > 1) {
+            hs.fetch(a, begin + kSteps, end, c0);
+            if constexpr (HOW == kStraight) Copy::start(rows[1], a, begin + kSteps, end, n0);
+        }
+        int buffer = 0;
+        for (int64_t n = 0; n < tiles; n++) {
+            const int turn = n & 1;
+            // Waits for this tile's copies.  Those of the next one, which were started behind them, and its values of the checkpoint may
+            // still be on their way: as many loads as stand between two calls of sched_barrier below.
+            if constexpr (HOW == kStraight) {
+                if (n + 1 < tiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copy::kPer + 2 * hs.kPer) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                if (left(n) < kSteps) {
+                    __syncthreads();                             // (all waves' copies, before zeros go over them)
+                    Copy::clear(rows[buffer], left(n));
+                }
             }
+            __syncthreads();                                     // (this tile is there, and all are done with the one before)
+            if constexpr (HOW == kAny) {
+                if (n + 1 < tiles) ds.fetch(a, begin + (n + 1) * kSteps, end, n0);
+            }
+            uint32_t fa[2 * MB], ga[4];
 #pragma unroll
-            for (int i = 0; i < 2; i++)
+            for (int b = 0; b < 2 * MB; b++) fa[b] = fx[b] + buffer * (kSteps * kRows * 2);
 #pragma unroll
-                for (int j = 0; j < 2; j++) acc[i][j] = mma<T>(x[i], y[j], acc[i][j]);
+            for (int b = 0; b < 4; b++) ga[b] = gy[b] + turn * (kSteps * kColumns * 2);
+            auto step = [&](auto s) {
+                uint4v f[MB], g[2];
+                read_step<s>(f, g, fa, ga);
+#pragma unroll
+                for (int i = 0; i < MB; i++)
+#pragma unroll
+                    for (int j = 0; j < 2; j++) acc[i][j] = mma<T>(f[i], g[j], acc[i][j]);
+            };
+            step(std::integral_constant<int, 0>{});
+            step(std::integral_constant<int, 1>{});
+            if (n + 1 < tiles) {
+#pragma unroll
+                for (int i = 0; i < hs.kPer; i++) hs.put(columns[turn ^ 1], left(n + 1), i);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (HOW == kStraight) {
+                    if (n + 2 < tiles) Copy::start(rows[buffer >= 1 ? buffer - 1 : 2], a, begin + (n + 2) * kSteps, end, n0);
+                }
+                if (n + 2 < tiles) hs.fetch(a, begin + (n + 2) * kSteps, end, c0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            step(std::integral_constant<int, 2>{});
+            step(std::integral_constant<int, 3>{});
+            if constexpr (HOW == kAny) {
+                if (n + 1 < tiles) ds.put(rows[turn ^ 1]);
+                buffer ^= 1;
+            } else {
+                buffer = buffer == 2 ? 0 : buffer + 1;
+            }
         }
     }
     float *out = l.parts ? l.parts + (int64_t)blockIdx.y * a.outputs * a.x.channels : a.dw;
     const int64_t stride = l.parts ? a.x.channels : a.dw_stride;
     const bool add = !l.parts && a.accumulate;
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+    for (int j = 0; j < 2; j++) {
+        const int c = c0 + 32 * (wc + j) + (lane & 31);
+        if (c >= a.x.channels) continue;
 #pragma unroll
-        for (int j = 0; j < 2; j++) {
-            const int c = c0 + 64 * wc + 32 * j + (lane & 31);
-            if (c >= a.x.channels) continue;
+        for (int i = 0; i < MB; i++)
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                const int n = n0 + 64 * wn + 32 * i + 8 * (r / 4) + 4 * half + r % 4;
+                const int n = n0 + 32 * (wn + i) + 8 * (r / 4) + 4 * half + r % 4;
                 if (n >= a.outputs) continue;
                 float *p = out + n * stride + c;
                 *p = add ? *p + acc[i][j][r] : acc[i][j][r];
             }
-        }
+    }
 }
 
-__global__ __launch_bounds__(kThreads) void weight_sum_kernel(WeightLaunch l)
+__global__ __launch_bounds__(256) void weight_sum_kernel(WeightLaunch l)
 {
     const tessel_weight_grad &a = l.a;
     const int64_t size = (int64_t)a.outputs * a.x.channels;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < size; i += (int64_t)gridDim.x * kThreads) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
         float *p = a.dw + i / a.x.channels * a.dw_stride + i % a.x.channels;
         float sum = a.accumulate ? *p : 0.0f;
         for (int s = 0; s < l.splits; s++) sum += l.parts[s * size + i];
@@ -151,29 +287,39 @@ __global__ __launch_bounds__(kThreads) void weight_sum_kernel(WeightLaunch l)
     }
 }
 
-static int64_t tiles_of(const tessel_weight_grad &a)
+struct WeightShape {
+    int     tile;                // rows and columns of dw a workgroup takes
+    int64_t tiles;
+    int     splits;
+};
+static WeightShape shape_of(const tessel_weight_grad &a)
 {
-    return (int64_t)((a.outputs + kTile - 1) / kTile) * ((a.x.channels + kTile - 1) / kTile);
+    auto tiles_of = [&](int64_t n) { return ((a.outputs + n - 1) / n) * ((a.x.channels + n - 1) / n); };
+    WeightShape s = {256, tiles_of(256), 1};
+    if (s.tiles < 128) s = {128, tiles_of(128), 1};
+    // splits of the tokens: until 512 workgroups are there (256 of the large tiles), none shorter than 256 tokens
+    const int64_t most = (a.x.tokens + 255) / 256, want = (s.tile == 256 ? 256 : 512) / s.tiles, n = want < most ? want : most;
+    s.splits = n < 1 ? 1 : (int)n;
+    return s;
 }
 
-// splits of the tokens: until 512 workgroups are there (two a compute unit), none shorter than 256 tokens
-int weight_parts(const tessel_weight_grad &a)
-{
-    const int64_t tiles = tiles_of(a), most = (a.x.tokens + 255) / 256, want = tiles > 0 ? 512 / tiles : 1;
-    const int64_t s = want < most ? want : most;
-    return s < 1 ? 1 : (int)s;
-}
+int weight_parts(const tessel_weight_grad &a) { return shape_of(a).splits; }
 
 int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stream)
 {
-    WeightLaunch l = {a, nullptr, weight_parts(a), 0, (a.x.channels + kTile - 1) / kTile};
+    const WeightShape s = shape_of(a);
+    WeightLaunch l = {a, nullptr, s.splits, 0, (a.x.channels + s.tile - 1) / s.tile};
     l.per = ((a.x.tokens + l.splits - 1) / l.splits + kSteps - 1) / kSteps * kSteps;
     if (l.splits > 1) l.parts = parts;
     void *args[] = {&l};
-    const void *kernel = a.x.type == TESSEL_BF16 ? (const void *)weight_kernel<bf16> : (const void *)weight_kernel<f16>;
-    int e = launched(hipLaunchKernel(kernel, dim3((unsigned)tiles_of(a), (unsigned)l.splits), dim3(kThreads), args, 0, (hipStream_t)stream));
+    const bool large = s.tile == 256, straight = a.outputs % 8 == 0 && a.dy.stride % 8 == 0 && (uintptr_t)a.dy.data % 16 == 0;
+#define KERNEL(T) (large ? (straight ? (const void *)weight_kernel<T, 2, 4, 4, kStraight> : (const void *)weight_kernel<T, 2, 4, 4, kAny>) \
+                         : (straight ? (const void *)weight_kernel<T, 2, 2, 2, kStraight> : (const void *)weight_kernel<T, 2, 2, 2, kAny>))
+    const void *kernel = a.x.type == TESSEL_BF16 ? KERNEL(bf16) : KERNEL(f16);
+#undef KERNEL
+    int e = launched(hipLaunchKernel(kernel, dim3((unsigned)s.tiles, (unsigned)l.splits), dim3(large ? 512 : 256), args, 0, (hipStream_t)stream));
     if (e == 0 && l.parts)
-        e = launched(hipLaunchKernel((const void *)weight_sum_kernel, dim3(1024), dim3(kThreads), args, 0, (hipStream_t)stream));
+        e = launched(hipLaunchKernel((const void *)weight_sum_kernel, dim3(1024), dim3(256), args, 0, (hipStream_t)stream));
     return e;
 }
 
