@@ -275,15 +275,28 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
     }
 }
 
+// four values a lane
 __global__ __launch_bounds__(256) void weight_sum_kernel(WeightLaunch l)
 {
+    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
     const tessel_weight_grad &a = l.a;
-    const int64_t size = (int64_t)a.outputs * a.x.channels;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
-        float *p = a.dw + i / a.x.channels * a.dw_stride + i % a.x.channels;
-        float sum = a.accumulate ? *p : 0.0f;
-        for (int s = 0; s < l.splits; s++) sum += l.parts[s * size + i];
-        *p = sum;
+    const int64_t size = (int64_t)a.outputs * a.x.channels, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= size) return;
+    const int64_t row = i / a.x.channels, col = i - row * a.x.channels;
+    float *p = a.dw + row * a.dw_stride + col;
+    if (col + 4 <= a.x.channels) {
+        V sum = {};
+        if (a.accumulate) sum = *(const V *)p;
+#pragma unroll 4
+        for (int s = 0; s < l.splits; s++) sum += *(const V *)(l.parts + s * size + i);
+        *(V *)p = sum;
+    } else {
+        for (int64_t k = i; k < min(i + 4, size); k++) {
+            p = a.dw + k / a.x.channels * a.dw_stride + k % a.x.channels;
+            float sum = a.accumulate ? *p : 0.0f;
+            for (int s = 0; s < l.splits; s++) sum += l.parts[s * size + k];
+            *p = sum;
+        }
     }
 }
 
@@ -295,8 +308,10 @@ struct WeightShape {
 static WeightShape shape_of(const tessel_weight_grad &a)
 {
     auto tiles_of = [&](int64_t n) { return ((a.outputs + n - 1) / n) * ((a.x.channels + n - 1) / n); };
+    // Large tiles read LDS less for each product, small ones fill the compute units with less splitting.  Large where there are 128 of them, or
+    // where the splits that fill the units keep 2048 tokens (8192 tokens, 2048 x 2048: 111 us, small 131; 2048 tokens: 52, small 46).
     WeightShape s = {256, tiles_of(256), 1};
-    if (s.tiles < 128) s = {128, tiles_of(128), 1};
+    if (s.tiles < 128 && a.x.tokens * s.tiles < 2048 * 256) s = {128, tiles_of(128), 1};
     // splits of the tokens: until 512 workgroups are there (256 of the large tiles), none shorter than 256 tokens
     const int64_t most = (a.x.tokens + 255) / 256, want = (s.tile == 256 ? 256 : 512) / s.tiles, n = want < most ? want : most;
     s.splits = n < 1 ? 1 : (int)n;
@@ -319,7 +334,7 @@ int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stre
 #undef KERNEL
     int e = launched(hipLaunchKernel(kernel, dim3((unsigned)s.tiles, (unsigned)l.splits), dim3(large ? 512 : 256), args, 0, (hipStream_t)stream));
     if (e == 0 && l.parts)
-        e = launched(hipLaunchKernel((const void *)weight_sum_kernel, dim3(1024), dim3(256), args, 0, (hipStream_t)stream));
+        e = launched(hipLaunchKernel((const void *)weight_sum_kernel, dim3((unsigned)(((int64_t)a.outputs * a.x.channels + 1023) / 1024)), dim3(256), args, 0, (hipStream_t)stream));
     return e;
 }
 
