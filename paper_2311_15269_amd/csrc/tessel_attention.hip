@@ -156,12 +156,16 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
                 s[b][i] = __builtin_amdgcn_exp2f(s[b][i] * by - off);
                 sum += s[b][i];
             }
-#pragma unroll
-        for (int n = 0; n < 4; n++) {
+        uint32_t va[W / 16];
+        column_addresses<W>(va, values, at);
+        unrolled<4>([&](auto c) {
+            constexpr int n = decltype(c)::value;
             const uint4v p = operand<T>(s[n / 2], n % 2);
+            uint4v f[W / 32];
+            read_columns<32 * n * W>(f, va);
 #pragma unroll
-            for (int b = 0; b < W / 32; b++) o[b] = mma<T>(at.columns(values, 16 * n, b), p, o[b]);
-        }
+            for (int b = 0; b < W / 32; b++) o[b] = mma<T>(f[b], p, o[b]);
+        });
     }
     sum += other_half(sum);
     if (!valid) return;
@@ -172,97 +176,22 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
     if (half == 0) l.a.lse[head * l.tokens + token] = m * l.a.scale + logf(sum);
 }
 
-// delta_i = sum_d do_i o_i, and in half precision the largest |do| of the launch (by workgroup): the gradients of the scores are scaled by a
-// power of two near it before they are rounded, which keeps them in the middle of the type's short range.
-//
-// The first 128 queries of a sequence take delta_i = sum_j p_ij (do_i . v_j) instead, the same sum from the inputs: o is rounded,
-// and where a query sees few keys that error is as large as the one of rounding the gradients of the scores (dq and dk of sequences of 1 to 40 tokens were
-// 2.1 times as far from the 64-bit values as the rounding of the results alone puts them, and are 1.4 times now).
-template <typename T, int W>
-__global__ __launch_bounds__(kThreads) void attend_delta_kernel(AttendLaunch l)
-{
-    typedef typename Vec8<T>::type V;
-    __shared__ float tops[kThreads / 64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-    const int part = threadIdx.x & 15, dim = l.a.dim;
-    float top = 0;
-    for (int64_t w = blockIdx.x; w < (int64_t)l.num_tiles * l.a.heads; w += gridDim.x) {
-        const AttendTile tile = l.tiles[w / l.a.heads];
-        const int head = w % l.a.heads;
-        if (tile.length < 0) continue;
-        if (tile.tile == 0) {
-            const int kv = head / (l.a.heads / l.a.kv_heads), query = 32 * wave + (lane & 31);
-            const int64_t token = tile.begin + query;
-            const bool valid = query < tile.length;
-            uint4v q[W / 16], g[W / 16], k[W / 16], v[W / 16];
-            fetch_rows<T, W>(q, row_of<T>(l.a.q, token, head), valid, dim);
-            fetch_rows<T, W>(g, row_of<T>(l.a.d_o, token, head), valid, dim);
-            const float by = l.a.scale * kLog2e, lse = valid ? l.a.lse[head * l.tokens + token] * kLog2e : 0.0f;
-            float sum = 0;
-            for (int k0 = 0; k0 <= 32 * wave && k0 < tile.length; k0 += 32) {
-                const int key = k0 + (lane & 31);
-                fetch_rows<T, W>(k, row_of<T>(l.a.k, tile.begin + key, kv), key < tile.length, dim);
-                fetch_rows<T, W>(v, row_of<T>(l.a.v, tile.begin + key, kv), key < tile.length, dim);
-                float16v s = {}, d = {};
-#pragma unroll
-                for (int n = 0; n < W / 16; n++) {
-                    s = mma<T>(k[n], q[n], s);
-                    d = mma<T>(v[n], g[n], d);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; i++)
-                    if (k0 + 8 * (i / 4) + 4 * half + i % 4 <= query) sum += __builtin_amdgcn_exp2f(s[i] * by - lse) * d[i];
-            }
-            sum += other_half(sum);
-            if (valid && half == 0) l.delta[head * l.tokens + token] = sum;
-            if constexpr (__is_same(T, f16)) {
-#pragma unroll
-                for (int n = 0; n < W / 16; n++)
-#pragma unroll
-                    for (int j = 0; j < 8; j++) top = fmaxf(top, fabsf((float)__builtin_bit_cast(V, g[n])[j]));
-            }
-            continue;
-        }
-        const int first = tile.tile * kAttendRows, rows = min(kAttendRows, tile.length - first);
-        for (int r = threadIdx.x >> 4; r < rows; r += kThreads / 16) {
-            const int64_t token = tile.begin + first + r;
-            float sum = 0;
-            if (8 * part < dim) {
-                const V x = __builtin_bit_cast(V, load16(row_of<T>(l.a.o, token, head) + 8 * part));
-                const V y = __builtin_bit_cast(V, load16(row_of<T>(l.a.d_o, token, head) + 8 * part));
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    sum += (float)x[j] * (float)y[j];
-                    top = fmaxf(top, fabsf((float)y[j]));
-                }
-            }
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-            if (part == 0) l.delta[head * l.tokens + token] = sum;
-        }
-    }
-    if constexpr (__is_same(T, f16)) {
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        if (lane == 0) tops[wave] = top;
-        __syncthreads();
-        if (threadIdx.x == 0) l.largest[blockIdx.x] = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    }
-}
-
-// the power of two that brings the largest |do| into 1..2 (f16); 1 for bf16, whose range is that of 32 bits
+// The power of two that brings `top`, the largest |do| of a row or a launch, into 1..2: in half precision the gradients of the scores are scaled by
+// it before they are rounded, which keeps them in the middle of the type's short range.  1 for bf16, whose range is that of 32 bits.
 template <typename T>
-__device__ __forceinline__ float gradient_scale(const AttendLaunch &l)
+__device__ __forceinline__ float gradient_scale(float top)
 {
-    if constexpr (__is_same(T, bf16)) return 1.0f;
-    float top = 0;
-    for (int i = threadIdx.x & 63; i < kAmaxParts; i += 64) top = fmaxf(top, l.largest[i]);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (!(top > 0.0f && top < INFINITY)) return 1.0f;
+    if (__is_same(T, bf16) || !(top > 0.0f && top < INFINITY)) return 1.0f;
     return __uint_as_float((254u << 23) - (__float_as_uint(top) & 0x7F800000u));
 }
 
+__global__ void attend_clear_kernel(uint32_t *word) { *word = 0; }
+
+// The gradient of q, and for the kernel behind it delta_i = sum_d do_i o_i and in half precision the largest |do|.
+//
+// The first 128 queries of a sequence take delta_i = sum_j p_ij (do_i . v_j) instead, the same sum from the inputs: o is rounded,
+// and where a query sees few keys that error is as large as the one of rounding the gradients of the scores.  (dq and dk of sequences of 1, 17
+// and 40 tokens in half precision are 2.9e-4 off the 64-bit values with it, 3.3e-4 without; rounding the results alone: 2.1e-4.)
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 {
@@ -281,14 +210,53 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     const int kv = head / (l.a.heads / l.a.kv_heads);
     const int64_t token = tile.begin + query;
     const bool valid = query < tile.length;
-    const float grow = gradient_scale<T>(l);
 
+    typedef typename Vec8<T>::type V;
     uint4v q[W / 16], g[W / 16];
     fetch_rows<T, W>(q, row_of<T>(l.a.q, token, head), valid, dim);
     fetch_rows<T, W>(g, row_of<T>(l.a.d_o, token, head), valid, dim);
     const float by = l.a.scale * kLog2e;
     const float lse = valid ? l.a.lse[head * l.tokens + token] * kLog2e : 0.0f;
-    const float delta = valid ? l.delta[head * l.tokens + token] : 0.0f;
+    float grow = 1.0f;
+    if constexpr (__is_same(T, f16)) {
+        float top = 0;
+#pragma unroll
+        for (int n = 0; n < W / 16; n++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) top = fmaxf(top, fabsf((float)__builtin_bit_cast(V, g[n])[j]));
+        top = fmaxf(top, other_half(top));
+        grow = gradient_scale<T>(top);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        if (lane == 0) atomicMax(l.largest, __float_as_uint(top));             // (not below nought: ordered as whole numbers are; in any order the same)
+    }
+    float delta = 0;
+    if (tile.tile == 0) {
+        uint4v k[W / 16], v[W / 16];
+        for (int k0 = 0; k0 <= 32 * wave && k0 < tile.length; k0 += 32) {
+            const int key = k0 + (lane & 31);
+            fetch_rows<T, W>(k, row_of<T>(l.a.k, tile.begin + key, kv), key < tile.length, dim);
+            fetch_rows<T, W>(v, row_of<T>(l.a.v, tile.begin + key, kv), key < tile.length, dim);
+            float16v s = {}, d = {};
+#pragma unroll
+            for (int n = 0; n < W / 16; n++) {
+                s = mma<T>(k[n], q[n], s);
+                d = mma<T>(v[n], g[n], d);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                if (k0 + 8 * (i / 4) + 4 * half + i % 4 <= query) delta += __builtin_amdgcn_exp2f(s[i] * by - lse) * d[i];
+        }
+    } else {
+        uint4v o[W / 16];
+        fetch_rows<T, W>(o, row_of<T>(l.a.o, token, head), valid, dim);
+#pragma unroll
+        for (int n = 0; n < W / 16; n++)
+#pragma unroll
+            for (int j = 0; j < 8; j++) delta += (float)__builtin_bit_cast(V, o[n])[j] * (float)__builtin_bit_cast(V, g[n])[j];
+    }
+    delta += other_half(delta);
+    if (valid && half == 0) l.delta[head * l.tokens + token] = delta;
     float16v dq[W / 32] = {};
 
     const T *kp = row_of<T>(l.a.k, tile.begin, kv), *vp = row_of<T>(l.a.v, tile.begin, kv);
@@ -303,9 +271,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
             Copy<T, W, kThreads>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
             Copy<T, W, kThreads>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
         }
-#pragma unroll
-        for (int b = 0; b < 2; b++) {
-            if (k0 + 32 * b > wfirst + 31) continue;
+        uint32_t ka[W / 16];
+        column_addresses<W>(ka, keys, at);
+        unrolled<2>([&](auto block) {
+            constexpr int b = decltype(block)::value;
+            if (k0 + 32 * b > wfirst + 31) return;
             float16v s = {}, d = {};
 #pragma unroll
             for (int n = 0; n < W / 16; n++) {
@@ -316,16 +286,18 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 const float p = __builtin_amdgcn_exp2f(s[i] * by - lse);
-                s[i] = p * (d[i] - delta) * grow;
+                s[i] = __is_same(T, f16) ? p * (d[i] - delta) * grow : p * (d[i] - delta);
                 if (edge && k0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4 > query) s[i] = 0.0f;
             }
-#pragma unroll
-            for (int n = 0; n < 2; n++) {
+            unrolled<2>([&](auto h) {
+                constexpr int n = decltype(h)::value;
                 const uint4v p = operand<T>(s, n);
+                uint4v f[W / 32];
+                read_columns<32 * (2 * b + n) * W>(f, ka);
 #pragma unroll
-                for (int c = 0; c < W / 32; c++) dq[c] = mma<T>(at.columns(keys, 32 * b + 16 * n, c), p, dq[c]);
-            }
-        }
+                for (int c = 0; c < W / 32; c++) dq[c] = mma<T>(f[c], p, dq[c]);
+            });
+        });
     }
     if (!valid) return;
     T *out = (T *)row_of<T>(l.a.dq, token, head);
@@ -334,27 +306,22 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     for (int b = 0; b < W / 32; b++) put_rows<T>(out, dq[b], b, back, dim);
 }
 
-// What a wave of the kernel below does with a block of 32 queries and its 32 keys.  LDS is read one step ahead of the products.
-template <typename T, int W, bool EDGE>
+// What a wave of the kernel below does with a block of 32 queries and its 32 keys.  LDS is read one step ahead of the products.  `copy` starts
+// the copies of the next tile: behind the first products, as the compiler lets no read of LDS that it places itself pass a copy.
+template <typename T, int W, bool EDGE, typename F>
 __device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_tile *grads, int row, Reader<W> at, const float4v *lses, const float4v *deltas, const uint4v *k,
-                                          const uint4v *values, float16v *dk, float16v *dv, float by, float grow, int before)
+                                          const uint4v *values, float16v *dk, float16v *dv, float by, float grow, int before, F &&copy)
 {
     constexpr int S = W / 16;                                    // steps a phase, two products each
     const int half = threadIdx.x >> 5 & 1;
     at.hold();
-    uint4v f[2 * S][2], v[S];
+    uint4v f[S][2], v[S];
     float16v s, d;
     uint4v p[2], e[2];
     auto read = [&](int t) {
-        if (t < S) {
-            f[t][0] = at.rows(queries, row, t);
-            f[t][1] = at.rows(grads, row, t);
-            v[t] = values[64 * t];
-        } else if (t < 2 * S) {
-            const int n = t - S, h = n / (W / 32), c = n % (W / 32);
-            f[t][0] = at.columns(queries, row + 16 * h, c);
-            f[t][1] = at.columns(grads, row + 16 * h, c);
-        }
+        f[t][0] = at.rows(queries, row, t);
+        f[t][1] = at.rows(grads, row, t);
+        v[t] = values[64 * t];
     };
     read(0);
     // the sums of the first products start from what is taken off them
@@ -376,9 +343,7 @@ __device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_til
         d = mma<T>(f[t][1], v[t], d);
         __builtin_amdgcn_sched_barrier(0);
     }
-    read(S);
-    read(S + 1);
-    __builtin_amdgcn_sched_barrier(0);
+    copy();
 #pragma unroll
     for (int i = 0; i < 16; i++) {
         float x = __builtin_amdgcn_exp2f(s[i] * by);
@@ -392,14 +357,19 @@ __device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_til
         e[h] = operand<T>(d, h);
     }
     __builtin_amdgcn_sched_barrier(0);
+    unrolled<2>([&](auto c) {
+        constexpr int h = decltype(c)::value;
+        uint32_t qa[W / 16];
+        uint4v x[W / 32];
+        column_addresses<W>(qa, grads + row * W / 8, at);
+        read_columns<32 * h * W>(x, qa);
 #pragma unroll
-    for (int t = S; t < 2 * S; t++) {
-        const int n = t - S, h = n / (W / 32), c = n % (W / 32);
-        read(t + 2);
-        dk[c] = mma<T>(f[t][0], e[h], dk[c]);
-        dv[c] = mma<T>(f[t][1], p[h], dv[c]);
-        __builtin_amdgcn_sched_barrier(0);
-    }
+        for (int b = 0; b < W / 32; b++) dv[b] = mma<T>(x[b], p[h], dv[b]);
+        column_addresses<W>(qa, queries + row * W / 8, at);
+        read_columns<32 * h * W>(x, qa);
+#pragma unroll
+        for (int b = 0; b < W / 32; b++) dk[b] = mma<T>(x[b], e[h], dk[b]);
+    });
 }
 
 constexpr int kDkvThreads = 512;
@@ -426,7 +396,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     const int64_t token = tile.begin + key;
     const bool valid = key < tile.length;
     const int shared = l.a.heads / l.a.kv_heads;
-    const float grow = gradient_scale<T>(l);
+    const float grow = __is_same(T, f16) ? gradient_scale<T>(__uint_as_float(*l.largest)) : 1.0f;
 
     uint4v k[W / 16], v[W / 16];
     fetch_rows<T, W>(k, row_of<T>(l.a.k, token, kv), valid, dim);
@@ -459,13 +429,15 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     for (int n = 0; n < all; n++) {
         if (threadIdx.x < 128) ((float *)numbers[n & 1])[threadIdx.x] = number;
         copies_arrive();                                         // (tile n has arrived, and all are done with the one before)
-        if (n + 1 < all) fetch(n + 1);
+        auto copy = [&]() {
+            if (n + 1 < all) fetch(n + 1);
+        };
         const lds_tile *queries = (const lds_tile *)buffers[2 * (n & 1)], *grads = (const lds_tile *)buffers[2 * (n & 1) + 1];
         const float4v *lses = numbers[n & 1][0], *deltas = numbers[n & 1][1];
         const int before = 32 * wave - n % tiles * 64 - row;     // (this block's queries of which the wave's first key is ahead)
-        if (before > 31) continue;
-        if (before > -32) dkv_block<T, W, true>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, before + (lane & 31) - 4 * half);
-        else dkv_block<T, W, false>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, 0);
+        if (before > 31) copy();
+        else if (before > -32) dkv_block<T, W, true>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, before + (lane & 31) - 4 * half, copy);
+        else dkv_block<T, W, false>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, 0, copy);
     }
     float4v *sums = (float4v *)buffers + wave * (W / 32 * 4 * 64) + lane;
     const float back = l.a.scale / grow;
@@ -512,9 +484,15 @@ int launch_attend(const AttendLaunch &l, void *stream)
 
 int launch_attend_backward(const AttendLaunch &l, void *stream)
 {
-    int e = launch(ATTEND_KERNEL(attend_delta_kernel), kAmaxParts, l, stream);
-    if (e == 0) e = launch(ATTEND_KERNEL(attend_dkv_kernel), (int64_t)l.num_tiles * l.a.kv_heads, l, stream, kDkvThreads);
+    int e = 0;
+    if (l.a.type == TESSEL_F16) {
+        AttendLaunch copy = l;
+        void *args[] = {&copy.largest};
+        e = (int)hipLaunchKernel((const void *)attend_clear_kernel, dim3(1), dim3(1), args, 0, (hipStream_t)stream);
+        if (e) (void)hipGetLastError();
+    }
     if (e == 0) e = launch(ATTEND_KERNEL(attend_dq_kernel), (int64_t)l.num_tiles * l.a.heads, l, stream);
+    if (e == 0) e = launch(ATTEND_KERNEL(attend_dkv_kernel), (int64_t)l.num_tiles * l.a.kv_heads, l, stream, kDkvThreads);
     return e;
 }
 

@@ -20,9 +20,8 @@ struct AttendLaunch {
     int32_t  num_tiles;
     int64_t  tokens;
     float   *delta;              // [heads][tokens]
-    float   *largest;            // [kAmaxParts] (f16)
+    uint32_t *largest;           // the bits of the largest |do| (f16)
 };
-constexpr int kAmaxParts = 512;
 
 int launch_attend(const AttendLaunch &l, void *stream);
 int launch_attend_backward(const AttendLaunch &l, void *stream);

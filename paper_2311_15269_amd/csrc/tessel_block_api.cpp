@@ -65,7 +65,7 @@ AttendLaunch attend_launch(const tessel_packing *p, const tessel_attention *a)
 
 size_t attend_workspace(const tessel_packing *p, const tessel_attention *a)
 {
-    return ((size_t)p->tokens * a->heads + kAmaxParts) * sizeof(float);
+    return ((size_t)p->tokens * a->heads + 1) * sizeof(float);
 }
 
 // ---- rows
@@ -225,7 +225,7 @@ int tessel_attention_backward(const tessel_packing *p, const tessel_attention *a
     if (!p->table || !workspace_ok(workspace_dev, workspace_bytes, attend_workspace(p, a))) return TESSEL_E_WORKSPACE;
     AttendLaunch l = attend_launch(p, a);
     l.delta = (float *)workspace_dev;
-    l.largest = l.delta + p->tokens * a->heads;
+    l.largest = (uint32_t *)(l.delta + p->tokens * a->heads);
     return hip_result(launch_attend_backward(l, hip_stream));
 }
 

@@ -93,6 +93,62 @@ struct Reader {
     }
 };
 
+// Column operands of one step of sixteen rows for all W / 32 blocks, by reads in one piece that ends when all have arrived.  (Where the
+// compiler places a transposing read itself, it first waits for every copy to LDS that is on its way.)  `at`: the addresses of the
+// blocks' two halves in the tile, `OFFSET`: the step's distance from its start.
+__device__ __forceinline__ uint4v join(uint64_t lo, uint64_t hi)
+{
+    typedef uint64_t V __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint4v, V{lo, hi});
+}
+template <int W>
+__device__ __forceinline__ void column_addresses(uint32_t *at, const lds_tile *tile, const Reader<W> &r)
+{
+#pragma unroll
+    for (int b = 0; b < W / 16; b++) at[b] = (uint32_t)(uintptr_t)tile + (r.c ^ (32 * b));
+}
+template <int OFFSET>
+__device__ __forceinline__ void read_columns(uint4v (&f)[4], const uint32_t (&at)[8])
+{
+    uint64_t r[8];
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %9 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %2, %10 offset:%16\n\tds_read_b64_tr_b16 %3, %11 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %4, %12 offset:%16\n\tds_read_b64_tr_b16 %5, %13 offset:%17\n\t"
+                 "ds_read_b64_tr_b16 %6, %14 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%17\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7]), "n"(OFFSET), "n"(OFFSET + 8 * 256)
+                 : "memory");
+#pragma unroll
+    for (int b = 0; b < 4; b++) f[b] = join(r[2 * b], r[2 * b + 1]);
+}
+template <int OFFSET>
+__device__ __forceinline__ void read_columns(uint4v (&f)[2], const uint32_t (&at)[4])
+{
+    uint64_t r[4];
+    asm volatile("ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %5 offset:%9\n\t"
+                 "ds_read_b64_tr_b16 %2, %6 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%9\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(OFFSET), "n"(OFFSET + 8 * 128)
+                 : "memory");
+#pragma unroll
+    for (int b = 0; b < 2; b++) f[b] = join(r[2 * b], r[2 * b + 1]);
+}
+
+// a loop whose counter is a constant in each turn: body(constant<0>) .. body(constant<N - 1>)
+template <int I> struct constant {
+    static constexpr int value = I;
+};
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unrolled(F &&body)
+{
+    if constexpr (I < N) {
+        body(constant<I>{});
+        unrolled<N, I + 1>(body);
+    }
+}
+
 typedef __attribute__((address_space(1))) const uint4v global_uint4v;
 
 // A tile of 64 rows x W on its way from memory straight to LDS by all threads of a workgroup, without passing registers: a wave's

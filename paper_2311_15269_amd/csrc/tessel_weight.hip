@@ -4,8 +4,6 @@
 // index runs along the rows of both inputs, so both operands come out of LDS by transposing reads.  The checkpoint is turned into
 // numbers of the matrix instruction's type on its way to LDS, which is exact.  Few tiles: the tokens are split over several
 // workgroups, whose sums a second kernel adds in the order of their numbers.
-#include <type_traits>
-
 #include "tessel_rows.h"
 
 namespace tessel {
@@ -117,11 +115,6 @@ struct HeldStage {
 
 // The operands of one step of sixteen tokens, MB of rows and two of columns, by transposing reads from LDS in one piece that ends when all
 // have arrived.  (The compiler, where it places such a read itself, first waits for every copy to LDS that is on its way.)
-__device__ __forceinline__ uint4v join(uint64_t lo, uint64_t hi)
-{
-    typedef uint64_t V __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint4v, V{lo, hi});
-}
 template <int S>
 __device__ __forceinline__ void read_step(uint4v (&f)[4], uint4v (&g)[2], const uint32_t (&x)[8], const uint32_t (&y)[4])
 {
@@ -228,14 +221,14 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
             for (int b = 0; b < 4; b++) ga[b] = gy[b] + turn * (kSteps * kColumns * 2);
             auto step = [&](auto s) {
                 uint4v f[MB], g[2];
-                read_step<s>(f, g, fa, ga);
+                read_step<decltype(s)::value>(f, g, fa, ga);
 #pragma unroll
                 for (int i = 0; i < MB; i++)
 #pragma unroll
                     for (int j = 0; j < 2; j++) acc[i][j] = mma<T>(f[i], g[j], acc[i][j]);
             };
-            step(std::integral_constant<int, 0>{});
-            step(std::integral_constant<int, 1>{});
+            step(constant<0>{});
+            step(constant<1>{});
             if (n + 1 < tiles) {
 #pragma unroll
                 for (int i = 0; i < hs.kPer; i++) hs.put(columns[turn ^ 1], left(n + 1), i);
@@ -246,8 +239,8 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
                 if (n + 2 < tiles) hs.fetch(a, begin + (n + 2) * kSteps, end, c0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            step(std::integral_constant<int, 2>{});
-            step(std::integral_constant<int, 3>{});
+            step(constant<2>{});
+            step(constant<3>{});
             if constexpr (HOW == kAny) {
                 if (n + 1 < tiles) ds.put(rows[turn ^ 1]);
                 buffer ^= 1;
