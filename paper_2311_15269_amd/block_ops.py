@@ -149,15 +149,20 @@ def _rows(t):
 
 
 def _vector(t, channels, like):
-    import torch
-    if t.dtype is not torch.float32 or t.shape != (channels,) or (channels > 1 and t.stride(0) != 1) or t.get_device() != like.get_device():
+    if _type(t) != 2 or t.shape != (channels,) or not t.is_contiguous() or t.get_device() != like.get_device():
         _refuse("expected %d contiguous 32-bit numbers on %s, got %s %s" % (channels, like.device, t.dtype, tuple(t.shape)))
     return t.data_ptr()
 
 
+def _like(t):
+    """a contiguous tensor of the same shape, type and place (half the time of torch.empty with all of them)"""
+    import torch
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _workspace(n, like):
     import torch
-    return torch.empty(max(16, n), dtype=torch.uint8, device=like.device)
+    return like.new_empty((max(16, n),), dtype=torch.uint8)
 
 
 class Packing:
@@ -206,8 +211,8 @@ class Packing:
         import torch
         stream = _stream(q)
         described = self._describe(q, k, v, scale, stream)
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((q.shape[1], self.tokens), dtype=torch.float32, device=q.device)
+        o = _like(q)
+        lse = q.new_empty((q.shape[1], self.tokens), dtype=torch.float32)
         a = _FlatAttention(*described, *_heads(o), lse.data_ptr())
         binding._check(_library().tessel_attention_forward(self._h, C.byref(a), stream))
         return o, lse
@@ -220,7 +225,7 @@ class Packing:
         _same(q, q.shape, d_o, o)
         if lse.dtype is not torch.float32 or lse.shape != (q.shape[1], self.tokens) or not lse.is_contiguous() or lse.get_device() != q.get_device():
             _refuse("lse is not what the forward call gave")
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dq, dk, dv = _like(q), _like(k), _like(v)
         a = _FlatAttention(*described, *_heads(o), lse.data_ptr(), *_heads(d_o), *_heads(dq), *_heads(dk), *_heads(dv))
         n = C.c_size_t()
         binding._check(lib.tessel_attention_backward_workspace_bytes(self._h, C.byref(a), C.byref(n)))
@@ -249,10 +254,9 @@ def residual_norm(x, y, pre, post=None, gate=None, scale=1.0, eps=1e-6):
     None, [channels] in 32 bits or [tokens, channels] like x."""
     import torch
     described = _describe_norm(x, y, pre, post, gate, scale, eps)
-    shape, dtype, device = x.shape, x.dtype, x.device
-    r, h = torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)
-    stats = torch.empty((2, shape[0]), dtype=torch.float32, device=device)
-    a = _FlatNorm(*described, stats.data_ptr(), r.data_ptr(), shape[1], h.data_ptr(), shape[1])
+    n, c = described[2], described[3]
+    r, h, stats = _like(x), _like(x), x.new_empty((2, n), dtype=torch.float32)
+    a = _FlatNorm(*described, stats.data_ptr(), r.data_ptr(), c, h.data_ptr(), c)
     binding._check(_library().tessel_residual_norm_forward(C.byref(a), _stream(x)))
     return r, h, stats
 
@@ -263,14 +267,13 @@ def residual_norm_backward(dr, dh, x, y, stats, pre, post=None, gate=None, scale
     import torch
     lib = _library()
     described = _describe_norm(x, y, pre, post, gate, scale, 0.0)
-    kind, shape, device = described[1], x.shape, x.device
-    c = shape[1]
+    kind, shape, c = described[1], x.shape, described[3]
     _same(x, shape, dr, dh)
     if stats.dtype is not torch.float32 or stats.shape != (2, shape[0]) or not stats.is_contiguous() or stats.get_device() != x.get_device():
         _refuse("stats is not what the forward call gave")
-    dx, dy = torch.empty(shape, dtype=x.dtype, device=device), torch.empty(shape, dtype=x.dtype, device=device)
+    dx, dy = _like(x), _like(x)
     if into is None:
-        dpre, dpost, dgate = torch.empty((3, c), dtype=torch.float32, device=device).unbind(0)
+        dpre, dpost, dgate = x.new_empty((3, c), dtype=torch.float32).unbind(0)
         dpost = dpost if post is not None else None
         dgate = dgate if kind == GATE_CHANNEL else None
     else:
@@ -282,7 +285,7 @@ def residual_norm_backward(dr, dh, x, y, stats, pre, post=None, gate=None, scale
     if kind == GATE_CHANNEL:
         to[2] = _vector(dgate, c, x)
     elif kind == GATE_TOKEN:
-        dgate = torch.empty(shape, dtype=x.dtype, device=device)
+        dgate = _like(x)
         at = (dgate.data_ptr(), c)
     a = _FlatNorm(*described, stats.data_ptr(), None, 0, None, 0, *_rows(dr), *_rows(dh), dx.data_ptr(), c, dy.data_ptr(), c, *at, *to,
                   0 if into is None else 1)
@@ -297,14 +300,15 @@ class Checkpoint:
     """An activation [tokens, channels] in 8 bits: `values` [tokens, channels up to the next multiple of 64] and `exponents`
     [tokens, groups of 64 channels], of a tensor of type `dtype`."""
 
-    def __init__(self, tokens, channels, dtype, device):
+    def __init__(self, like):
+        """room for a tensor like this one"""
         import torch
+        tokens, channels = like.shape
         groups = -(-channels // GROUP)
-        self.tokens, self.channels, self.dtype = tokens, channels, dtype
-        self.values = torch.empty((tokens, groups * GROUP), dtype=torch.int8, device=device)
-        self.exponents = torch.empty((tokens, groups), dtype=torch.uint8, device=device)
-        self.device = self.values.device
-        self._words = (self.values.data_ptr(), self.exponents.data_ptr(), groups * GROUP, groups, tokens, channels, _TYPES[dtype])
+        self.tokens, self.channels, self.dtype, self.device = tokens, channels, like.dtype, like.device
+        self.values = like.new_empty((tokens, groups * GROUP), dtype=torch.int8)
+        self.exponents = like.new_empty((tokens, groups), dtype=torch.uint8)
+        self._words = (self.values.data_ptr(), self.exponents.data_ptr(), groups * GROUP, groups, tokens, channels, _type(like))
         self._desc = CheckpointDesc(*self._words)
 
     @property
@@ -319,8 +323,7 @@ class Checkpoint:
 def _new_checkpoint(x):
     if x.dim() != 2 or not x.is_cuda:
         _refuse("expected [tokens, channels] on the GPU")
-    _type(x)
-    return Checkpoint(x.shape[0], x.shape[1], x.dtype, x.device)
+    return Checkpoint(x)
 
 
 def checkpoint(x):
@@ -333,8 +336,7 @@ def checkpoint(x):
 
 def restore(c):
     """tessel_checkpoint_restore: what a checkpoint stands for, in the type of what was stored"""
-    import torch
-    x = torch.empty((c.tokens, c.channels), dtype=c.dtype, device=c.device)
+    x = c.values.new_empty((c.tokens, c.channels), dtype=c.dtype)
     rows = Rows(x.data_ptr(), c.channels)
     binding._check(_library().tessel_checkpoint_restore(C.byref(c._desc), C.byref(rows), _stream(x)))
     return x
@@ -348,12 +350,11 @@ def _act(act):
 
 def gated(g, u, act="silu"):
     """tessel_gated_forward: (a, checkpoint of g, checkpoint of u) with a = act(g) u"""
-    import torch
     kind = _act(act)
     kg = _new_checkpoint(g)
     kg._like(u)
     ku = _new_checkpoint(u)
-    a = torch.empty(g.shape, dtype=g.dtype, device=g.device)
+    a = _like(g)
     rows = Rows(*_rows(g)), Rows(*_rows(u)), Rows(a.data_ptr(), kg.channels)
     binding._check(_library().tessel_gated_forward(kind, C.byref(rows[0]), C.byref(rows[1]), C.byref(rows[2]), C.byref(kg._desc),
                                                    C.byref(ku._desc), _stream(g)))
@@ -362,10 +363,9 @@ def gated(g, u, act="silu"):
 
 def gated_backward(da, kg, ku, act="silu", with_output=False):
     """tessel_gated_backward: (dg, du), or (dg, du, a) with the checkpoints' own act(g) u"""
-    import torch
     kind = _act(act)
     kg._like(da)
-    outs = [torch.empty(da.shape, dtype=da.dtype, device=da.device) for _ in range(3 if with_output else 2)]
+    outs = [_like(da) for _ in range(3 if with_output else 2)]
     rows = [Rows(t.data_ptr(), kg.channels) for t in outs]
     d = Rows(*_rows(da))
     binding._check(_library().tessel_gated_backward(kind, C.byref(d), C.byref(kg._desc), C.byref(ku._desc), C.byref(rows[0]), C.byref(rows[1]),
@@ -382,7 +382,7 @@ def weight_gradient(dy, x, into=None):
         _refuse("dy %s %s does not go with a checkpoint of %s [%d, %d]" % (dy.dtype, tuple(dy.shape), x.dtype, x.tokens, x.channels))
     shape = (dy.shape[1], x.channels)
     if into is None:
-        dw = torch.empty(shape, dtype=torch.float32, device=dy.device)
+        dw = dy.new_empty(shape, dtype=torch.float32)
     else:
         dw = into
         if dw.dtype is not torch.float32 or dw.shape != shape or dw.get_device() != dy.get_device() or (shape[1] > 1 and dw.stride(1) != 1):
