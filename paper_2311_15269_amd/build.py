@@ -105,9 +105,60 @@ def misaligned_scalar_loads(asm):
     return bad
 
 
+def _registers(text):
+    """the vector and accumulation registers that an instruction's text names"""
+    found = set()
+    for m in re.finditer(r"\b([av])(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
+        first, last = (m.group(2), m.group(3)) if m.group(2) else (m.group(4), m.group(4))
+        found |= {(m.group(1), r) for r in range(int(first), int(last) + 1)}
+    return found
+
+
+# wait states between a matrix instruction of 8 passes and one of another kind that touches its result
+_MFMA_WAIT = 11
+
+
+def early_reads_of_products(asm):
+    """Instructions of the device code that touch the result of a matrix instruction before it is written, along any path.  Nothing
+    in the hardware holds them back; the compiler fills the time with other instructions and s_nop.  (Seen where accumulators were
+    moved to other registers at the top of a loop that ended with the product: the way back was not counted, and the last registers
+    of the result were read too early.)  Returns the offending lines."""
+    code, label = [], {}
+    for n, line in enumerate(asm.split("\n")):
+        m = re.match(r"([^\s;]+):", line)
+        if m:
+            label[m.group(1)] = len(code)
+            continue
+        text = line.split(";")[0].strip()
+        if text and not text.startswith("."):
+            code.append((n + 1, text))
+    bad = {}
+    for i, (_, text) in enumerate(code):
+        if not text.startswith("v_mfma"):
+            continue
+        result = _registers(text.split(",")[0])
+        paths, seen = [(i + 1, 0)], {}
+        while paths:
+            j, waited = paths.pop()
+            while j < len(code) and waited < _MFMA_WAIT and seen.get(j, _MFMA_WAIT) > waited:
+                seen[j] = waited
+                n, t = code[j]
+                op = t.split()[0]
+                if not op.startswith(("s_", "v_mfma")) and _registers(t) & result:
+                    bad[n] = "%d: %s" % (n, t)
+                waited += int(t.split()[1], 0) + 1 if op == "s_nop" else 8 if op.startswith("v_mfma") else 1
+                if op.startswith("s_cbranch") and t.split()[1] in label:
+                    paths.append((label[t.split()[1]], waited))
+                if op in ("s_endpgm", "s_setpc_b64"):
+                    break
+                j = label.get(t.split()[1], len(code)) if op == "s_branch" else j + 1
+    return [bad[n] for n in sorted(bad)]
+
+
 def build_library(force=True, verbose=False, check=True):
     """hipcc --offload-arch=gfx950 ... -> paper_2311_15269_amd/libtessel_hip.so.  With `check` the device assembly
-    the compiler leaves behind is scanned for scalar loads at addresses that may not be word aligned."""
+    the compiler leaves behind is scanned for scalar loads at addresses that may not be word aligned and for results of matrix
+    instructions that are touched too early."""
     if not force and not is_stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -136,9 +187,11 @@ def build_library(force=True, verbose=False, check=True):
             if not listings:
                 raise RuntimeError("no device assembly found to check")
             for path in listings:
-                bad = misaligned_scalar_loads(open(path).read())
-                if bad:
-                    raise RuntimeError("scalar loads at possibly unaligned addresses in %s:\n%s" % (os.path.basename(path), "\n".join(bad[:10])))
+                asm = open(path).read()
+                for what, bad in (("scalar loads at possibly unaligned addresses", misaligned_scalar_loads(asm)),
+                                  ("results of matrix instructions touched too early", early_reads_of_products(asm))):
+                    if bad:
+                        raise RuntimeError("%s in %s:\n%s" % (what, os.path.basename(path), "\n".join(bad[:10])))
         shutil.move(out, LIB)
     finally:
         shutil.rmtree(tmp, ignore_errors=True)
