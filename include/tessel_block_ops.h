@@ -49,7 +49,8 @@ int  tessel_block_last_hip_error(void);
  * The tokens of sequence i are lengths[0] + .. + lengths[i-1] and the lengths[i] (0 or more) that follow; tokens behind the
  * last sequence belong to none.  For head h, which reads key-value head h / (heads / kv_heads), and token i of a sequence
  *     lse_i = log sum_{j <= i} exp(scale q_i . k_j),    o_i = sum_{j <= i} exp(scale q_i . k_j - lse_i) v_j.
- * A token of no sequence gets o = 0 and lse = -infinity, is read by nobody, and has gradients of 0.
+ * A token of no sequence gets o = 0 and lse = -infinity, is read by nobody, and has gradients of 0.  Infinities and NaN reach the
+ * tokens that see them by the formula and no others; in the backward pass, any token of the same sequence.
  * Products are taken in the inputs' type and summed in 32 bits; the probabilities (and, going back, the gradients of the
  * scores) are rounded to the inputs' type before the second product. */
 typedef struct tessel_packing tessel_packing;   /* opaque, host memory only: the tiles of a set of lengths */

@@ -82,6 +82,47 @@ __device__ __forceinline__ void clear_tiles(uint4v (*tiles)[64 * W / 8], int row
     __syncthreads();
 }
 
+// the sign bits of those halves of a word that hold an infinity or NaN
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x)
+{
+    return __is_same(T, bf16) ? ((x & 0x7F807F80u) + 0x00800080u) & 0x80008000u : ((x & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+}
+
+// A query's probability of a key behind it is nought, but nought times infinity or NaN is not.  Where sixteen rows of values `f`, from row
+// `row` of the tile on, hold any: they are taken out of the product, and added for those queries that see them.
+template <typename T, int W>
+__device__ __forceinline__ void part_with_later(uint4v (&f)[W / 32], float16v *o, const lds_tile *values, int row, int seen)
+{
+    uint32_t any = 0;
+#pragma unroll
+    for (int b = 0; b < W / 32; b++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) any |= not_finite<T>(f[b][j]);
+    if (!__any(any != 0u)) return;
+#pragma unroll
+    for (int b = 0; b < W / 32; b++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) f[b][j] &= ~((not_finite<T>(f[b][j]) >> 15) * 0xFFFFu);
+    const int half = threadIdx.x >> 5 & 1;
+#pragma unroll 1
+    for (int r = row; r < row + 16 && r <= seen; r++) {
+#pragma unroll
+        for (int b = 0; b < W / 32; b++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                typedef T V __attribute__((ext_vector_type(8)));
+                const V v = __builtin_bit_cast(V, (uint4v)values[chunk_at<W>(r, 4 * b + i)]);
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float x = half ? (float)v[4 + j] : (float)v[j];
+                    o[b][4 * i + j] += fabsf(x) < INFINITY ? 0.0f : x;
+                }
+                __builtin_amdgcn_sched_barrier(0);               // (one value after the other: this is rare, and its registers count for all)
+            }
+    }
+}
+
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
 {
@@ -126,7 +167,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int n = 0; n < W / 16; n++) s[b] = mma<T>(at.rows(keys, 32 * b, n), q[n], s[b]);
-        if (k0 + 63 > wfirst) {
+        const bool edge = k0 + 63 > wfirst;
+        if (edge) {
 #pragma unroll
             for (int b = 0; b < 2; b++)
 #pragma unroll
@@ -163,6 +205,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
             const uint4v p = operand<T>(s[n / 2], n % 2);
             uint4v f[W / 32];
             read_columns<32 * n * W>(f, va);
+            if (edge) part_with_later<T, W>(f, o, values, 16 * n, query - k0);
 #pragma unroll
             for (int b = 0; b < W / 32; b++) o[b] = mma<T>(f[b], p, o[b]);
         });

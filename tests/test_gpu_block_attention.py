@@ -150,6 +150,29 @@ def test_sequences_do_not_see_each_other(ops):
         assert torch.equal(lse[:, :100], lse2[:, :100]) and torch.equal(lse[:, 150:], lse2[:, 150:])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_queries_do_not_see_later_tokens(ops, dtype, dim):
+    """infinities and NaN in a sequence's keys and values leave the tokens before them alone, and reach those behind"""
+    n = 300
+    q, k, v, _ = (t.cuda() for t in inputs(n, 2, 1, dim, dtype, 16, 0.5))
+    packing = ops.Packing([n])
+    o, lse = packing.attention(q, k, v)
+    for at in (3, 70, 127, 150, 191, 260):
+        bad_k, bad_v = k.clone(), v.clone()
+        bad_v[at, 0, 5] = math.inf
+        bad_v[at + 10:at + 12, 0, 7] = math.nan
+        bad_v[at + 20, 0, 5] = -math.inf
+        bad_k[at + 30] = math.nan
+        o2, lse2 = packing.attention(q, bad_k, bad_v)
+        assert torch.equal(o[:at], o2[:at]) and torch.equal(lse[:, :at + 30], lse2[:, :at + 30])
+        rest = [c for c in range(dim) if c not in (5, 7)]
+        assert bool((o2[at:at + 20, :, 5] == math.inf).all()) and bool(o2[at + 20:at + 30, :, 5].isnan().all())
+        assert torch.equal(o[at:at + 10, :, 7], o2[at:at + 10, :, 7]) and bool(o2[at + 10:at + 30, :, 7].isnan().all())
+        assert torch.equal(o[at:at + 30][:, :, rest], o2[at:at + 30][:, :, rest])
+        assert bool(o2[at + 30:].isnan().all()) and bool(lse2[:, at + 30:].isnan().all())
+
+
 def test_repeats_are_equal(ops):
     q, k, v, d = (t.cuda() for t in inputs(900, 8, 2, 128, BF16, 12))
     packing = ops.Packing([500, 3, 397])
