@@ -219,7 +219,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
     if (half == 0) l.a.lse[head * l.tokens + token] = m * l.a.scale + logf(sum);
 }
 
-// The power of two that brings `top`, the largest |do| of a row or a launch, into 1..2: in half precision the gradients of the scores are scaled by
+// The power of two that brings `top`, the largest |do| of a row or a sequence's head, into 1..2: in half precision the gradients of the scores are scaled by
 // it before they are rounded, which keeps them in the middle of the type's short range.  1 for bf16, whose range is that of 32 bits.
 template <typename T>
 __device__ __forceinline__ float gradient_scale(float top)
@@ -228,7 +228,14 @@ __device__ __forceinline__ float gradient_scale(float top)
     return __uint_as_float((254u << 23) - (__float_as_uint(top) & 0x7F800000u));
 }
 
-__global__ void attend_clear_kernel(uint32_t *word) { *word = 0; }
+// l.largest[head][first token of a sequence]: the bits of the largest |do| there (f16)
+__global__ __launch_bounds__(kThreads) void attend_clear_kernel(AttendLaunch l)
+{
+    const int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (n >= (int64_t)l.num_tiles * l.a.heads) return;
+    const AttendTile tile = l.tiles[n / l.a.heads];
+    if (tile.length > 0 && tile.tile == 0) l.largest[n % l.a.heads * l.tokens + tile.begin] = 0;
+}
 
 // The gradient of q, and for the kernel behind it delta_i = sum_d do_i o_i and in half precision the largest |do|.
 //
@@ -271,7 +278,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
         grow = gradient_scale<T>(top);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        if (lane == 0) atomicMax(l.largest, __float_as_uint(top));             // (not below nought: ordered as whole numbers are; in any order the same)
+        // (not below nought: ordered as whole numbers are, and the same in any order)
+        if (lane == 0) atomicMax(l.largest + head * l.tokens + tile.begin, __float_as_uint(top));
     }
     float delta = 0;
     if (tile.tile == 0) {
@@ -439,7 +447,12 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     const int64_t token = tile.begin + key;
     const bool valid = key < tile.length;
     const int shared = l.a.heads / l.a.kv_heads;
-    const float grow = __is_same(T, f16) ? gradient_scale<T>(__uint_as_float(*l.largest)) : 1.0f;
+    float grow = 1.0f;
+    if constexpr (__is_same(T, f16)) {
+        uint32_t top = 0;
+        for (int head = kv * shared; head < (kv + 1) * shared; head++) top = max(top, l.largest[head * l.tokens + tile.begin]);
+        grow = gradient_scale<T>(__uint_as_float(top));
+    }
 
     uint4v k[W / 16], v[W / 16];
     fetch_rows<T, W>(k, row_of<T>(l.a.k, token, kv), valid, dim);
@@ -528,12 +541,7 @@ int launch_attend(const AttendLaunch &l, void *stream)
 int launch_attend_backward(const AttendLaunch &l, void *stream)
 {
     int e = 0;
-    if (l.a.type == TESSEL_F16) {
-        AttendLaunch copy = l;
-        void *args[] = {&copy.largest};
-        e = (int)hipLaunchKernel((const void *)attend_clear_kernel, dim3(1), dim3(1), args, 0, (hipStream_t)stream);
-        if (e) (void)hipGetLastError();
-    }
+    if (l.a.type == TESSEL_F16) e = launch((const void *)attend_clear_kernel, ((int64_t)l.num_tiles * l.a.heads + kThreads - 1) / kThreads, l, stream);
     if (e == 0) e = launch(ATTEND_KERNEL(attend_dq_kernel), (int64_t)l.num_tiles * l.a.heads, l, stream);
     if (e == 0) e = launch(ATTEND_KERNEL(attend_dkv_kernel), (int64_t)l.num_tiles * l.a.kv_heads, l, stream, kDkvThreads);
     return e;

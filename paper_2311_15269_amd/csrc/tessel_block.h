@@ -20,7 +20,7 @@ struct AttendLaunch {
     int32_t  num_tiles;
     int64_t  tokens;
     float   *delta;              // [heads][tokens]
-    uint32_t *largest;           // the bits of the largest |do| (f16)
+    uint32_t *largest;           // [heads][tokens] (f16): at a sequence's first token the bits of its largest |do|
 };
 
 int launch_attend(const AttendLaunch &l, void *stream);

@@ -65,7 +65,7 @@ AttendLaunch attend_launch(const tessel_packing *p, const tessel_attention *a)
 
 size_t attend_workspace(const tessel_packing *p, const tessel_attention *a)
 {
-    return ((size_t)p->tokens * a->heads + 1) * sizeof(float);
+    return (size_t)p->tokens * a->heads * sizeof(float) * (a->type == TESSEL_F16 ? 2 : 1);
 }
 
 // ---- rows

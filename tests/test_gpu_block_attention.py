@@ -100,6 +100,20 @@ def test_small_gradients_in_half_precision(ops):
         assert bool(((a - b).abs() <= 2.0 ** -11 * a.abs() + 2.0 ** -24).all())
 
 
+def test_sequences_and_heads_keep_their_own_scale(ops):
+    """in half precision the gradients of one sequence, and of the heads on one key, do not depend on the sizes of others'"""
+    q, k, v, d = (t.cuda() for t in inputs(260, 4, 2, 64, F16, 6))
+    packing = ops.Packing([100, 160])
+    o, lse = packing.attention(q, k, v)
+    want = packing.attention_backward(d, q, k, v, o, lse)
+    far = d.clone()
+    far[:100] *= 500.0
+    far[:, 2:] = math.inf
+    got = packing.attention_backward(far, q, k, v, o, lse)
+    for a, b, heads in zip(want, got, (2, 1, 1)):
+        assert torch.equal(a[100:, :heads], b[100:, :heads])
+
+
 def test_strided_views(ops):
     """one tensor of all projections, heads before tokens, keys shared through a stride of nought"""
     lengths, n = [90, 41], 131
