@@ -79,10 +79,13 @@ typedef struct {
     tessel_heads dq, dk, dv;/* backward: written                                                           */
 } tessel_attention;
 
-/* Errors: INVALID_ARG, UNSUPPORTED (type, dim), TOOBIG (more workgroups than one launch holds), WORKSPACE (`p` is not bound), HIP. */
-int  tessel_attention_forward(const tessel_packing *p, const tessel_attention *a, void *hip_stream);
+/* Workspaces: 16-byte aligned, contents need not be kept between calls (the forward pass needs none, and 0 bytes are asked for, unless a few
+ * heads go over long sequences: their work is then split over the keys).
+ * Errors: INVALID_ARG, UNSUPPORTED (type, dim), TOOBIG (more workgroups than one launch holds), WORKSPACE (also: `p` is not bound), HIP. */
+int  tessel_attention_forward_workspace_bytes(const tessel_packing *p, const tessel_attention *a, size_t *bytes);
+int  tessel_attention_forward(const tessel_packing *p, const tessel_attention *a, void *workspace_dev, size_t workspace_bytes,
+                              void *hip_stream);
 int  tessel_attention_backward_workspace_bytes(const tessel_packing *p, const tessel_attention *a, size_t *bytes);
-/* workspace: 16-byte aligned, contents need not be kept between calls. */
 int  tessel_attention_backward(const tessel_packing *p, const tessel_attention *a, void *workspace_dev, size_t workspace_bytes,
                                void *hip_stream);
 

@@ -13,7 +13,7 @@ from . import binding
 
 EXPORTS = (
     "tessel_block_last_hip_error", "tessel_packing_create", "tessel_packing_destroy", "tessel_packing_table_bytes", "tessel_packing_bind",
-    "tessel_attention_forward", "tessel_attention_backward_workspace_bytes", "tessel_attention_backward",
+    "tessel_attention_forward_workspace_bytes", "tessel_attention_forward", "tessel_attention_backward_workspace_bytes", "tessel_attention_backward",
     "tessel_residual_norm_forward", "tessel_residual_norm_backward_workspace_bytes", "tessel_residual_norm_backward",
     "tessel_checkpoint_store", "tessel_checkpoint_restore", "tessel_gated_forward", "tessel_gated_backward",
     "tessel_weight_gradient_workspace_bytes", "tessel_weight_gradient",
@@ -83,7 +83,8 @@ def _library():
         lib.tessel_packing_table_bytes.argtypes = [ptr, size]
         lib.tessel_packing_bind.argtypes = [ptr, ptr, C.c_size_t, ptr]
         # (structures by address: the nested ones above and their flat twins alike)
-        lib.tessel_attention_forward.argtypes = [ptr, ptr, ptr]
+        lib.tessel_attention_forward_workspace_bytes.argtypes = [ptr, ptr, size]
+        lib.tessel_attention_forward.argtypes = [ptr, ptr, ptr, C.c_size_t, ptr]
         lib.tessel_attention_backward_workspace_bytes.argtypes = [ptr, ptr, size]
         lib.tessel_attention_backward.argtypes = [ptr, ptr, ptr, C.c_size_t, ptr]
         lib.tessel_residual_norm_forward.argtypes = [ptr, ptr]
@@ -209,12 +210,15 @@ class Packing:
     def attention(self, q, k, v, scale=None):
         """tessel_attention_forward: q [tokens, heads, dim], k and v [tokens, kv_heads, dim] -> (o like q, lse [heads, tokens])"""
         import torch
-        stream = _stream(q)
+        lib, stream = _library(), _stream(q)
         described = self._describe(q, k, v, scale, stream)
         o = _like(q)
         lse = q.new_empty((q.shape[1], self.tokens), dtype=torch.float32)
         a = _FlatAttention(*described, *_heads(o), lse.data_ptr())
-        binding._check(_library().tessel_attention_forward(self._h, C.byref(a), stream))
+        n = C.c_size_t()
+        binding._check(lib.tessel_attention_forward_workspace_bytes(self._h, C.byref(a), C.byref(n)))
+        ws = _workspace(n.value, q) if n.value else None
+        binding._check(lib.tessel_attention_forward(self._h, C.byref(a), None if ws is None else ws.data_ptr(), n.value, stream))
         return o, lse
 
     def attention_backward(self, d_o, q, k, v, o, lse, scale=None):

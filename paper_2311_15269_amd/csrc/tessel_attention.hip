@@ -4,6 +4,8 @@
 // products are 32 x 32 x 16 matrix instructions, arranged so that a lane of the score tile holds ONE query (key) and its registers the other
 // axis: the softmax's maximum and sum are then sums over registers and one exchange between half-waves, and the probabilities
 // go into the second product from the registers in which the first left them (tessel_tile.h: operand, column_operand).
+#include <algorithm>
+
 #include "tessel_block.h"
 #include "tessel_tile.h"
 
@@ -13,18 +15,30 @@ constexpr int kThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // The work of a workgroup.  Tiles are in order of falling work, so that the last ones to start are short.  Workgroups go to the eight
-// L2 caches in turn: with heads in eights, each cache sees an eighth of the heads, and those that share keys and values together.
-__device__ __forceinline__ void work_of(int heads, int &tile, int &head)
+// L2 caches in turn: with heads (times splits) in eights, each cache sees an eighth of the heads, and those that share keys and values together.
+__device__ __forceinline__ void work_of(int heads, int splits, int &tile, int &head, int &split)
 {
-    const int b = blockIdx.x;
-    if (heads % 8 == 0) {
-        const int per = heads / 8, slot = b >> 3;
+    const int b = blockIdx.x, all = heads * splits;
+    int which;
+    if (all % 8 == 0) {
+        const int per = all / 8, slot = b >> 3;
         tile = slot / per;
-        head = (b & 7) * per + slot % per;
+        which = (b & 7) * per + slot % per;
     } else {
-        tile = b / heads;
-        head = b % heads;
+        tile = b / all;
+        which = b % all;
     }
+    head = which / splits;
+    split = which % splits;
+}
+
+// The steps of split `split` of a tile with `all` of them, first .. end - 1: shares as even as whole steps allow.  (With fewer steps than splits the
+// first splits have one each, the others none.)
+__device__ __forceinline__ void share_of(int all, int splits, int split, int &first, int &end)
+{
+    const int sharing = min(all, splits);
+    first = split < sharing ? (int)((int64_t)all * split / sharing) : all;
+    end = split < sharing ? (int)((int64_t)all * (split + 1) / sharing) : all;
 }
 
 template <typename T>
@@ -61,6 +75,17 @@ __device__ __forceinline__ void put_rows(T *row, const float16v &c, int b, float
             w.y = pack2<T>(c[4 * i + 2] * by, c[4 * i + 3] * by);
             *(uint2 *)(row + d) = w;
         }
+    }
+}
+
+// the same in 32 bits, into a split's part
+__device__ __forceinline__ void put_part(float *row, const float16v &c, int b, float by, int dim)
+{
+    const int half = threadIdx.x >> 5 & 1;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int d = 32 * b + 8 * i + 4 * half;
+        if (d < dim) *(float4v *)(row + d) = float4v{c[4 * i] * by, c[4 * i + 1] * by, c[4 * i + 2] * by, c[4 * i + 3] * by};
     }
 }
 
@@ -127,11 +152,12 @@ template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
 {
     __shared__ __attribute__((aligned(256))) uint4v buffers[4][64 * W / 8];
-    int t, head;
-    work_of(l.a.heads, t, head);
+    int t, head, split;
+    work_of(l.a.heads, l.splits, t, head, split);
     const AttendTile tile = l.tiles[t];
     const int dim = l.a.dim;
     if (tile.length < 0) {
+        if (split) return;
         clear_rows<T>(l.a.o, tile.begin, -tile.length, head, dim);
         for (int n = threadIdx.x; n < -tile.length; n += kThreads) l.a.lse[head * l.tokens + tile.begin + n] = -INFINITY;
         return;
@@ -139,6 +165,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
     const int first = tile.tile * kAttendRows, wfirst = first + 32 * wave, query = wfirst + (lane & 31);
     const int last = min(first + kAttendRows, tile.length);
+    int from, to;
+    share_of((last + 63) / 64, l.splits, split, from, to);
+    if (from == to) return;
+    from *= 64;
+    to = min(64 * to, last);
     const int kv = head / (l.a.heads / l.a.kv_heads);
     const int64_t token = tile.begin + query;
     const bool valid = query < tile.length;
@@ -151,15 +182,15 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
 
     const T *kp = row_of<T>(l.a.k, tile.begin, kv), *vp = row_of<T>(l.a.v, tile.begin, kv);
     Reader<W> at;
-    clear_tiles<4, W>(buffers, last, dim);
-    Copy<T, W, kThreads>::start(buffers[0], kp, l.a.k.token_stride, last, dim);
-    Copy<T, W, kThreads>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
-    for (int k0 = 0, turn = 0; k0 < last; k0 += 64, turn ^= 2) {
+    clear_tiles<4, W>(buffers, to - from, dim);
+    Copy<T, W, kThreads>::start(buffers[0], kp + from * l.a.k.token_stride, l.a.k.token_stride, to - from, dim);
+    Copy<T, W, kThreads>::start(buffers[1], vp + from * l.a.v.token_stride, l.a.v.token_stride, to - from, dim);
+    for (int k0 = from, turn = 0; k0 < to; k0 += 64, turn ^= 2) {
         const lds_tile *keys = (const lds_tile *)buffers[turn], *values = (const lds_tile *)buffers[turn + 1];
         copies_arrive();                                         // (this tile has arrived, and all are done with the one before)
-        if (k0 + 64 < last) {
-            Copy<T, W, kThreads>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
-            Copy<T, W, kThreads>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
+        if (k0 + 64 < to) {
+            Copy<T, W, kThreads>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, to - k0 - 64, dim);
+            Copy<T, W, kThreads>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, to - k0 - 64, dim);
         }
         if (k0 > wfirst + 31) continue;
         float16v s[2] = {};
@@ -212,11 +243,63 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
     }
     sum += other_half(sum);
     if (!valid) return;
+    if (l.splits > 1) {
+        const int64_t row = ((int64_t)split * l.a.heads + head) * l.tokens + token;
+#pragma unroll
+        for (int b = 0; b < W / 32; b++) put_part(l.parts + row * dim, o[b], b, 1.0f, dim);
+        if (half == 0) {
+            l.tops[2 * row] = m;
+            l.tops[2 * row + 1] = sum;
+        }
+        return;
+    }
     T *out = (T *)row_of<T>(l.a.o, token, head);
     const float inv = 1.0f / sum;
 #pragma unroll
     for (int b = 0; b < W / 32; b++) put_rows<T>(out, o[b], b, inv, dim);
     if (half == 0) l.a.lse[head * l.tokens + token] = m * l.a.scale + logf(sum);
+}
+
+// Joins the parts of the forward pass (FORWARD: sums of exponentials that each go by their own largest score) or adds up those of gradients,
+// in the order of the splits.  Eight rows a workgroup, 32 lanes of four columns each.  blockIdx.y: of the two arrays that a part of dk and
+// dv holds one behind the other; steps_by: heads on a key, `turned`: tiles of keys (see attend_dkv_kernel).
+constexpr int kJoinRows = 8;
+template <typename T, bool FORWARD>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendLaunch l, tessel_heads first_out, tessel_heads second_out, int heads, int steps_by, bool turned)
+{
+    constexpr int kGroups = kAttendRows / kJoinRows;
+    const int group = blockIdx.x % kGroups, head = blockIdx.x / kGroups % heads;
+    const AttendTile tile = l.tiles[blockIdx.x / kGroups / heads];
+    if (tile.length < 0) return;
+    const int col = 4 * (threadIdx.x & 31), dim = l.a.dim;
+    const int first = (turned ? tile.tiles - 1 - tile.tile : tile.tile) * kAttendRows, r = first + group * kJoinRows + (threadIdx.x >> 5);
+    if (r >= tile.length) return;
+    const int steps = turned ? (tile.length - first + 63) / 64 * steps_by : (min(first + kAttendRows, tile.length) + 63) / 64;
+    const int parts = min(steps, l.splits);
+    const int64_t token = tile.begin + r, row = ((int64_t)blockIdx.y * heads + head) * l.tokens + token, next = (int64_t)gridDim.y * heads * l.tokens;
+    float top = -INFINITY, total = 0;
+    if constexpr (FORWARD)
+#pragma unroll 4
+        for (int s = 0; s < parts; s++) top = fmaxf(top, l.tops[2 * (row + s * next)]);
+    float4v sum = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int s = 0; s < parts; s++) {
+        float by = 1.0f;
+        if constexpr (FORWARD) {
+            const float2 t = *(const float2 *)(l.tops + 2 * (row + s * next));
+            by = t.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((t.x - top) * (l.a.scale * kLog2e));
+            total += by * t.y;
+        }
+        if (col < dim) sum += *(const float4v *)(l.parts + (row + s * next) * dim + col) * by;
+    }
+    if (col < dim) {
+        const float by = FORWARD ? 1.0f / total : 1.0f;
+        uint2 w;
+        w.x = pack2<T>(sum[0] * by, sum[1] * by);
+        w.y = pack2<T>(sum[2] * by, sum[3] * by);
+        *(uint2 *)((T *)row_of<T>(blockIdx.y ? second_out : first_out, token, head) + col) = w;
+    }
+    if (FORWARD && col == 0) l.a.lse[head * l.tokens + token] = top * l.a.scale + logf(total);
 }
 
 // The power of two that brings `top`, the largest |do| of a row or a sequence's head, into 1..2: in half precision the gradients of the scores are scaled by
@@ -246,17 +329,23 @@ template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 {
     __shared__ __attribute__((aligned(256))) uint4v buffers[4][64 * W / 8];
-    int t, head;
-    work_of(l.a.heads, t, head);
+    int t, head, split;
+    work_of(l.a.heads, l.splits, t, head, split);
     const AttendTile tile = l.tiles[t];
     const int dim = l.a.dim;
     if (tile.length < 0) {
+        if (split) return;
         clear_rows<T>(l.a.dq, tile.begin, -tile.length, head, dim);
         return;
     }
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
     const int first = tile.tile * kAttendRows, wfirst = first + 32 * wave, query = wfirst + (lane & 31);
     const int last = min(first + kAttendRows, tile.length);
+    int from, to;
+    share_of((last + 63) / 64, l.splits, split, from, to);
+    if (from == to) return;
+    from *= 64;
+    to = min(64 * to, last);
     const int kv = head / (l.a.heads / l.a.kv_heads);
     const int64_t token = tile.begin + query;
     const bool valid = query < tile.length;
@@ -279,7 +368,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
         // (not below nought: ordered as whole numbers are, and the same in any order)
-        if (lane == 0) atomicMax(l.largest + head * l.tokens + tile.begin, __float_as_uint(top));
+        if (lane == 0 && to == last) atomicMax(l.largest + head * l.tokens + tile.begin, __float_as_uint(top));
     }
     float delta = 0;
     if (tile.tile == 0) {
@@ -307,20 +396,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
             for (int j = 0; j < 8; j++) delta += (float)__builtin_bit_cast(V, o[n])[j] * (float)__builtin_bit_cast(V, g[n])[j];
     }
     delta += other_half(delta);
-    if (valid && half == 0) l.delta[head * l.tokens + token] = delta;
+    if (valid && half == 0 && to == last) l.delta[head * l.tokens + token] = delta;
     float16v dq[W / 32] = {};
 
     const T *kp = row_of<T>(l.a.k, tile.begin, kv), *vp = row_of<T>(l.a.v, tile.begin, kv);
     Reader<W> at;
-    clear_tiles<4, W>(buffers, last, dim);
-    Copy<T, W, kThreads>::start(buffers[0], kp, l.a.k.token_stride, last, dim);
-    Copy<T, W, kThreads>::start(buffers[1], vp, l.a.v.token_stride, last, dim);
-    for (int k0 = 0, turn = 0; k0 < last; k0 += 64, turn ^= 2) {
+    clear_tiles<4, W>(buffers, to - from, dim);
+    Copy<T, W, kThreads>::start(buffers[0], kp + from * l.a.k.token_stride, l.a.k.token_stride, to - from, dim);
+    Copy<T, W, kThreads>::start(buffers[1], vp + from * l.a.v.token_stride, l.a.v.token_stride, to - from, dim);
+    for (int k0 = from, turn = 0; k0 < to; k0 += 64, turn ^= 2) {
         const lds_tile *keys = (const lds_tile *)buffers[turn], *values = (const lds_tile *)buffers[turn + 1];
         copies_arrive();
-        if (k0 + 64 < last) {
-            Copy<T, W, kThreads>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, last - k0 - 64, dim);
-            Copy<T, W, kThreads>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, last - k0 - 64, dim);
+        if (k0 + 64 < to) {
+            Copy<T, W, kThreads>::start(buffers[turn ^ 2], kp + (k0 + 64) * l.a.k.token_stride, l.a.k.token_stride, to - k0 - 64, dim);
+            Copy<T, W, kThreads>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, to - k0 - 64, dim);
         }
         uint32_t ka[W / 16];
         column_addresses<W>(ka, keys, at);
@@ -353,6 +442,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     if (!valid) return;
     T *out = (T *)row_of<T>(l.a.dq, token, head);
     const float back = l.a.scale / grow;
+    if (l.splits > 1) {
+        float *part = l.parts + (((int64_t)split * l.a.heads + head) * l.tokens + token) * dim;
+#pragma unroll
+        for (int b = 0; b < W / 32; b++) put_part(part, dq[b], b, back, dim);
+        return;
+    }
 #pragma unroll
     for (int b = 0; b < W / 32; b++) put_rows<T>(out, dq[b], b, back, dim);
 }
@@ -432,11 +527,12 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
 {
     __shared__ __attribute__((aligned(256))) uint4v buffers[4][64 * W / 8], values[128 * W / 8];
     __shared__ float4v numbers[2][2][16];                        // - log-sum / scale and - delta of a tile's queries
-    int t, kv;
-    work_of(l.a.kv_heads, t, kv);
+    int t, kv, split;
+    work_of(l.a.kv_heads, l.splits, t, kv, split);
     const AttendTile tile = l.tiles[t];
     const int dim = l.a.dim;
     if (tile.length < 0) {
+        if (split) return;
         clear_rows<T>(l.a.dk, tile.begin, -tile.length, kv, dim);
         clear_rows<T>(l.a.dv, tile.begin, -tile.length, kv, dim);
         return;
@@ -447,6 +543,11 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     const int64_t token = tile.begin + key;
     const bool valid = key < tile.length;
     const int shared = l.a.heads / l.a.kv_heads;
+    // the tiles of all heads that share these keys, one behind the other, and of those this split's share
+    const int tiles = (tile.length - first + 63) / 64;
+    int from, to;
+    share_of(tiles * shared, l.splits, split, from, to);
+    if (from == to) return;
     float grow = 1.0f;
     if constexpr (__is_same(T, f16)) {
         uint32_t top = 0;
@@ -463,8 +564,6 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     const float by = l.a.scale * kLog2e;
     float16v dk[W / 32] = {}, dv[W / 32] = {};
 
-    // the tiles of all heads that share these keys, one behind the other
-    const int tiles = (tile.length - first + 63) / 64, all = tiles * shared;
     float number = 0;                                            // (on its way to LDS, one tile ahead)
     auto fetch = [&](int n) {
         const int head = kv * shared + n / tiles, q0 = first + n % tiles * 64, rows = tile.length - q0;
@@ -480,13 +579,14 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
         }
     };
     const Reader<W> at;
-    clear_tiles<4, W, kDkvThreads>(buffers, tile.length - first, dim);
-    fetch(0);
-    for (int n = 0; n < all; n++) {
+    // (a head's last tile may be short: where it comes first or second, nothing has filled the rows behind it yet)
+    clear_tiles<4, W, kDkvThreads>(buffers, from % tiles + 2 >= tiles ? 0 : 128, dim);
+    fetch(from);
+    for (int n = from; n < to; n++) {
         if (threadIdx.x < 128) ((float *)numbers[n & 1])[threadIdx.x] = number;
         copies_arrive();                                         // (tile n has arrived, and all are done with the one before)
         auto copy = [&]() {
-            if (n + 1 < all) fetch(n + 1);
+            if (n + 1 < to) fetch(n + 1);
         };
         const lds_tile *queries = (const lds_tile *)buffers[2 * (n & 1)], *grads = (const lds_tile *)buffers[2 * (n & 1) + 1];
         const float4v *lses = numbers[n & 1][0], *deltas = numbers[n & 1][1];
@@ -509,12 +609,14 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
         }
         __syncthreads();
         if (row == 0 && valid) {
-            T *to = (T *)row_of<T>(x == 0 ? l.a.dk : l.a.dv, token, kv);
+            T *out = (T *)row_of<T>(x == 0 ? l.a.dk : l.a.dv, token, kv);
+            float *part = l.parts + ((((int64_t)split * 2 + x) * l.a.kv_heads + kv) * l.tokens + token) * dim;
 #pragma unroll
             for (int b = 0; b < W / 32; b++) {
 #pragma unroll
                 for (int i = 0; i < 16; i++) c[b][i] += sums[(4 * b + i / 4) * 64][i % 4];
-                put_rows<T>(to, c[b], b, x == 0 ? back : 1.0f, dim);
+                if (l.splits > 1) put_part(part, c[b], b, x == 0 ? back : 1.0f, dim);
+                else put_rows<T>(out, c[b], b, x == 0 ? back : 1.0f, dim);
             }
         }
     }
@@ -533,17 +635,58 @@ static int launch(const void *kernel, int64_t blocks, const AttendLaunch &l, voi
 #define ATTEND_KERNEL(name) (l.a.type == TESSEL_BF16 ? (l.a.dim <= 64 ? (const void *)name<bf16, 64> : (const void *)name<bf16, 128>) \
                                                      : (l.a.dim <= 64 ? (const void *)name<f16, 64> : (const void *)name<f16, 128>))
 
-int launch_attend(const AttendLaunch &l, void *stream)
+// Splits of a launch's tiles.  The longest tile alone takes `longest` steps of some `step` us, all together `total`, `resident` of them at once; each
+// split leaves `bytes`, which are written and read again at some 4.5 GB/ms, and the join is a launch more.  The number with the least
+// of the sum, none of fewer than four steps.  (2 heads of 128 over 4096 tokens: forward 107 -> 39 us, and with the backward pass 373 -> 133; 8
+// heads over 8192: 220 -> 187 and 801 -> 734; with 32 nothing is split.)
+int attend_splits(int64_t longest, int64_t total, int resident, double step, double bytes)
 {
-    return launch(ATTEND_KERNEL(attend_kernel), (int64_t)l.num_tiles * l.a.heads, l, stream);
+    int best = 1;
+    double least = 1e30;
+    for (int64_t s = 1; s <= std::max<int64_t>(1, longest / 4) && s <= 64; s++) {
+        const double us = step * std::max((double)((longest + s - 1) / s), (double)total / resident) + (s > 1 ? 4.0 + s * bytes * 2 / 4.5e6 : 0.0);
+        if (us < least) {
+            least = us;
+            best = (int)s;
+        }
+    }
+    return best;
 }
 
-int launch_attend_backward(const AttendLaunch &l, void *stream)
+static int join(const AttendLaunch &l, bool forward, const tessel_heads &first, const tessel_heads *second, int heads, int steps_by, void *stream)
+{
+    AttendLaunch copy = l;
+    tessel_heads x = first, y = second ? *second : first;
+    bool turned = second != nullptr;
+    void *args[] = {&copy, &x, &y, &heads, &steps_by, &turned};
+    const void *kernel = l.a.type == TESSEL_BF16 ? (forward ? (const void *)attend_join_kernel<bf16, true> : (const void *)attend_join_kernel<bf16, false>)
+                                                 : (forward ? (const void *)attend_join_kernel<f16, true> : (const void *)attend_join_kernel<f16, false>);
+    const dim3 grid((unsigned)(l.num_tiles * heads * (kAttendRows / kJoinRows)), second ? 2 : 1);
+    const hipError_t e = hipLaunchKernel(kernel, grid, dim3(kThreads), args, 0, (hipStream_t)stream);
+    if (e != hipSuccess) (void)hipGetLastError();
+    return (int)e;
+}
+
+int launch_attend(const AttendLaunch &l, void *stream)
+{
+    int e = launch(ATTEND_KERNEL(attend_kernel), (int64_t)l.num_tiles * l.a.heads * l.splits, l, stream);
+    if (e == 0 && l.splits > 1) e = join(l, true, l.a.o, nullptr, l.a.heads, 1, stream);
+    return e;
+}
+
+int launch_attend_dq(const AttendLaunch &l, void *stream)
 {
     int e = 0;
     if (l.a.type == TESSEL_F16) e = launch((const void *)attend_clear_kernel, ((int64_t)l.num_tiles * l.a.heads + kThreads - 1) / kThreads, l, stream);
-    if (e == 0) e = launch(ATTEND_KERNEL(attend_dq_kernel), (int64_t)l.num_tiles * l.a.heads, l, stream);
-    if (e == 0) e = launch(ATTEND_KERNEL(attend_dkv_kernel), (int64_t)l.num_tiles * l.a.kv_heads, l, stream, kDkvThreads);
+    if (e == 0) e = launch(ATTEND_KERNEL(attend_dq_kernel), (int64_t)l.num_tiles * l.a.heads * l.splits, l, stream);
+    if (e == 0 && l.splits > 1) e = join(l, false, l.a.dq, nullptr, l.a.heads, 1, stream);
+    return e;
+}
+
+int launch_attend_dkv(const AttendLaunch &l, void *stream)
+{
+    int e = launch(ATTEND_KERNEL(attend_dkv_kernel), (int64_t)l.num_tiles * l.a.kv_heads * l.splits, l, stream, kDkvThreads);
+    if (e == 0 && l.splits > 1) e = join(l, false, l.a.dk, &l.a.dv, l.a.kv_heads, l.a.heads / l.a.kv_heads, stream);
     return e;
 }
 

@@ -18,13 +18,18 @@ struct AttendLaunch {
     tessel_attention a;
     const AttendTile *tiles;
     int32_t  num_tiles;
+    int32_t  splits;             // workgroups that share a tile's keys (forward, dq) or queries (dk, dv) among them
     int64_t  tokens;
+    float   *parts;              // their sums, where there are several: [splits][2 dk, dv][heads][tokens][dim] in 32 bits (one for o, dq)
+    float   *tops;               // forward: [splits][heads][tokens][2], a query's largest score and its sum of exponentials
     float   *delta;              // [heads][tokens]
     uint32_t *largest;           // [heads][tokens] (f16): at a sequence's first token the bits of its largest |do|
 };
 
+int attend_splits(int64_t longest, int64_t total, int resident, double step, double bytes);
 int launch_attend(const AttendLaunch &l, void *stream);
-int launch_attend_backward(const AttendLaunch &l, void *stream);
+int launch_attend_dq(const AttendLaunch &l, void *stream);
+int launch_attend_dkv(const AttendLaunch &l, void *stream);
 
 int launch_norm(const tessel_residual_norm &a, void *stream);
 int norm_parts(const tessel_residual_norm &a);

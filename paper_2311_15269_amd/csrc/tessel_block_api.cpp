@@ -12,6 +12,7 @@ using namespace tessel;
 
 struct tessel_packing {
     int64_t tokens = 0;
+    int64_t longest = 0, steps = 0;         // steps of 64 keys of the longest sequence's last tile, and of all tiles
     std::vector<AttendTile> tiles;
     const AttendTile *table = nullptr;      // device copy
 };
@@ -49,7 +50,7 @@ int attention_ok(const tessel_packing *p, const tessel_attention *a)
     if (!p || !a || a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->dim < 1) return TESSEL_E_INVALID_ARG;
     if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return TESSEL_E_INVALID_ARG;
     if ((a->type != TESSEL_BF16 && a->type != TESSEL_F16) || a->dim % 8 || a->dim > 128) return TESSEL_E_UNSUPPORTED;
-    if ((int64_t)p->tiles.size() * a->heads > kMostBlocks) return TESSEL_E_TOOBIG;
+    if ((int64_t)p->tiles.size() * a->heads > kMostBlocks) return TESSEL_E_TOOBIG;           // (splits: of small launches only)
     return TESSEL_OK;
 }
 
@@ -63,10 +64,36 @@ AttendLaunch attend_launch(const tessel_packing *p, const tessel_attention *a)
     return l;
 }
 
-size_t attend_workspace(const tessel_packing *p, const tessel_attention *a)
+// How the forward pass and dq (of which two workgroups are resident on a compute unit) and dk, dv (one) are split: over the 64-key steps of a
+// tile, and the 64-query steps of a tile for all heads on its keys (of which there are as many in all).
+int query_splits(const tessel_packing *p, const tessel_attention *a)
 {
-    return (size_t)p->tokens * a->heads * sizeof(float) * (a->type == TESSEL_F16 ? 2 : 1);
+    return attend_splits(p->longest, p->steps * a->heads, 512, 1.6, 4.0 * p->tokens * a->heads * a->dim);
 }
+int key_splits(const tessel_packing *p, const tessel_attention *a)
+{
+    return attend_splits(p->longest * (a->heads / a->kv_heads), p->steps * a->heads, 256, 2.6, 8.0 * p->tokens * a->kv_heads * a->dim);
+}
+
+size_t forward_workspace(const tessel_packing *p, const tessel_attention *a)
+{
+    const int s = query_splits(p, a);
+    return s > 1 ? (size_t)s * p->tokens * a->heads * (a->dim + 2) * sizeof(float) : 0;
+}
+
+// delta (and the largest gradients, f16), then the parts of dq and after them those of dk and dv
+size_t gradient_words(const tessel_packing *p, const tessel_attention *a)
+{
+    return ((size_t)p->tokens * a->heads * (a->type == TESSEL_F16 ? 2 : 1) + 3) / 4 * 4;
+}
+size_t backward_workspace(const tessel_packing *p, const tessel_attention *a)
+{
+    const size_t q = query_splits(p, a), k = key_splits(p, a), row = (size_t)p->tokens * a->dim;
+    const size_t parts = std::max(q > 1 ? q * row * a->heads : 0, k > 1 ? k * 2 * row * a->kv_heads : 0);
+    return (gradient_words(p, a) + parts) * sizeof(float);
+}
+
+bool workspace_ok(const void *p, size_t have, size_t need) { return need == 0 || (p && aligned(p, 16) && have >= need); }
 
 // ---- rows
 bool rows_ok(const tessel_rows &r, int type, int64_t tokens, int channels, bool written)
@@ -122,8 +149,6 @@ size_t weight_workspace(const tessel_weight_grad *a)
     return parts > 1 ? (size_t)parts * a->outputs * a->x.channels * sizeof(float) : 0;
 }
 
-bool workspace_ok(const void *p, size_t have, size_t need) { return need == 0 || (p && aligned(p, 16) && have >= need); }
-
 }  // namespace
 
 extern "C" {
@@ -149,7 +174,12 @@ int tessel_packing_create(const int32_t *lengths, int32_t num_sequences, int64_t
             int32_t begin = 0;
             for (int32_t i = 0; i < num_sequences; i++) {
                 const int32_t tiles = (int32_t)(((int64_t)lengths[i] + kAttendRows - 1) / kAttendRows);
-                for (int32_t t = 0; t < tiles; t++) p->tiles.push_back({begin, lengths[i], t, tiles});
+                for (int32_t t = 0; t < tiles; t++) {
+                    const int64_t steps = (std::min<int64_t>((int64_t)(t + 1) * kAttendRows, lengths[i]) + 63) / 64;
+                    p->tiles.push_back({begin, lengths[i], t, tiles});
+                    p->steps += steps;
+                    p->longest = std::max(p->longest, steps);
+                }
                 begin += lengths[i];
             }
             // a tile's work is the number of tiles up to it
@@ -193,15 +223,28 @@ int tessel_packing_bind(tessel_packing *p, void *table_dev, size_t table_bytes, 
     return TESSEL_OK;
 }
 
-int tessel_attention_forward(const tessel_packing *p, const tessel_attention *a, void *hip_stream)
+int tessel_attention_forward_workspace_bytes(const tessel_packing *p, const tessel_attention *a, size_t *bytes)
+{
+    if (!bytes) return TESSEL_E_INVALID_ARG;
+    const int e = attention_ok(p, a);
+    if (e) return e;
+    *bytes = forward_workspace(p, a);
+    return TESSEL_OK;
+}
+
+int tessel_attention_forward(const tessel_packing *p, const tessel_attention *a, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
 {
     int e = attention_ok(p, a);
     if (e) return e;
     if (p->tokens == 0) return TESSEL_OK;
     if (!heads_ok(a->q, false, a->heads, a->dim) || !heads_ok(a->k, false, a->kv_heads, a->dim) || !heads_ok(a->v, false, a->kv_heads, a->dim) ||
         !heads_ok(a->o, true, a->heads, a->dim) || !a->lse || !aligned(a->lse, 4)) return TESSEL_E_INVALID_ARG;
-    if (!p->table) return TESSEL_E_WORKSPACE;
-    return hip_result(launch_attend(attend_launch(p, a), hip_stream));
+    if (!p->table || !workspace_ok(workspace_dev, workspace_bytes, forward_workspace(p, a))) return TESSEL_E_WORKSPACE;
+    AttendLaunch l = attend_launch(p, a);
+    l.splits = query_splits(p, a);
+    l.parts = (float *)workspace_dev;
+    if (l.splits > 1) l.tops = l.parts + (size_t)l.splits * p->tokens * a->heads * a->dim;
+    return hip_result(launch_attend(l, hip_stream));
 }
 
 int tessel_attention_backward_workspace_bytes(const tessel_packing *p, const tessel_attention *a, size_t *bytes)
@@ -209,7 +252,7 @@ int tessel_attention_backward_workspace_bytes(const tessel_packing *p, const tes
     if (!bytes) return TESSEL_E_INVALID_ARG;
     const int e = attention_ok(p, a);
     if (e) return e;
-    *bytes = attend_workspace(p, a);
+    *bytes = backward_workspace(p, a);
     return TESSEL_OK;
 }
 
@@ -222,11 +265,16 @@ int tessel_attention_backward(const tessel_packing *p, const tessel_attention *a
         !heads_ok(a->o, false, a->heads, a->dim) || !heads_ok(a->d_o, false, a->heads, a->dim) || !heads_ok(a->dq, true, a->heads, a->dim) ||
         !heads_ok(a->dk, true, a->kv_heads, a->dim) || !heads_ok(a->dv, true, a->kv_heads, a->dim) || !a->lse || !aligned(a->lse, 4))
         return TESSEL_E_INVALID_ARG;
-    if (!p->table || !workspace_ok(workspace_dev, workspace_bytes, attend_workspace(p, a))) return TESSEL_E_WORKSPACE;
+    if (!p->table || !workspace_ok(workspace_dev, workspace_bytes, backward_workspace(p, a))) return TESSEL_E_WORKSPACE;
     AttendLaunch l = attend_launch(p, a);
     l.delta = (float *)workspace_dev;
     l.largest = (uint32_t *)(l.delta + p->tokens * a->heads);
-    return hip_result(launch_attend_backward(l, hip_stream));
+    l.parts = l.delta + gradient_words(p, a);
+    l.splits = query_splits(p, a);
+    e = launch_attend_dq(l, hip_stream);
+    l.splits = key_splits(p, a);
+    if (e == 0) e = launch_attend_dkv(l, hip_stream);
+    return hip_result(e);
 }
 
 int tessel_residual_norm_forward(const tessel_residual_norm *a, void *hip_stream)

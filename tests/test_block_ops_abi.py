@@ -79,7 +79,7 @@ def test_attention_forward_refuses(change, code):
     rc, h = packing([5, 300])
     lib = B._library()
     a = attention(**change)
-    assert lib.tessel_attention_forward(h, C.byref(a), None) == code
+    assert lib.tessel_attention_forward(h, C.byref(a), AT, 1 << 40, None) == code
     lib.tessel_packing_destroy(h)
 
 
@@ -99,13 +99,26 @@ def test_attention_backward_refuses(change, code):
     lib.tessel_packing_destroy(h)
 
 
+def test_attention_forward_asks_for_room_where_it_splits():
+    """one head over a long sequence is split over its keys, many heads are not"""
+    lib, n = B._library(), C.c_size_t()
+    rc, h = packing([8192])
+    for heads, splits in ((1, True), (32, False)):
+        a = attention(heads=heads, kv_heads=1)
+        assert lib.tessel_attention_forward_workspace_bytes(h, C.byref(a), C.byref(n)) == OK and (n.value > 0) == splits
+        if splits:
+            assert lib.tessel_attention_forward(h, C.byref(a), None, 0, None) == WORKSPACE
+    assert lib.tessel_attention_forward_workspace_bytes(h, C.byref(a), None) == INVALID
+    lib.tessel_packing_destroy(h)
+
+
 def test_attention_over_no_tokens_does_nothing():
     rc, h = packing([0, 0])
     a = attention(q=B.Heads(None, 0, 0))
-    assert B._library().tessel_attention_forward(h, C.byref(a), None) == OK
+    assert B._library().tessel_attention_forward(h, C.byref(a), AT, 1 << 40, None) == OK
     assert B._library().tessel_attention_backward(h, C.byref(a), None, 0, None) == OK
-    assert B._library().tessel_attention_forward(None, C.byref(a), None) == INVALID
-    assert B._library().tessel_attention_forward(h, None, None) == INVALID
+    assert B._library().tessel_attention_forward(None, C.byref(a), None, 0, None) == INVALID
+    assert B._library().tessel_attention_forward(h, None, None, 0, None) == INVALID
     B._library().tessel_packing_destroy(h)
 
 

@@ -76,6 +76,13 @@ def test_several_tiles_of_wide_heads(ops, dtype):
     check(ops, [700, 1, 385], 4, 2, 128, dtype)
 
 
+@pytest.mark.parametrize("lengths, heads, kv_heads, dim, dtype", [([1500], 1, 1, 64, BF16), ([1500], 2, 1, 128, F16), ([1030, 5, 200], 2, 2, 128, BF16),
+                                                                  ([1025, 0, 640], 4, 1, 40, F16), ([600, 600], 3, 1, 96, BF16), ([64 * 17 + 1], 2, 1, 128, BF16)])
+def test_few_heads_over_long_sequences(ops, lengths, heads, kv_heads, dim, dtype):
+    """work split over keys and queries, and joined: tiles with fewer steps than splits, heads that share keys, tokens of none"""
+    check(ops, lengths, heads, kv_heads, dim, dtype, padding=9)
+
+
 @pytest.mark.parametrize("dtype, by", [(BF16, 0.01), (BF16, 3.0), (F16, 0.01), (F16, 3.0)])
 def test_sizes_of_values(ops, dtype, by):
     """scores all alike, and scores that leave one key a row"""
