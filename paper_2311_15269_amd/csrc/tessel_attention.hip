@@ -12,6 +12,7 @@
 namespace tessel {
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 4;        // operands that are read from LDS ahead of their products
 constexpr float kLog2e = 1.4426950408889634f;
 
 // The work of a workgroup.  Tiles are in order of falling work, so that the last ones to start are short.  Workgroups go to the eight
@@ -40,6 +41,9 @@ __device__ __forceinline__ void share_of(int all, int splits, int split, int &fi
     first = split < sharing ? (int)((int64_t)all * split / sharing) : all;
     end = split < sharing ? (int)((int64_t)all * (split + 1) / sharing) : all;
 }
+
+// this wave's number in its workgroup, in a scalar register: what is compared with it is one branch for the wave
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 template <typename T>
 __device__ __forceinline__ const T *row_of(const tessel_heads &h, int64_t token, int head)
@@ -162,7 +166,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
         for (int n = threadIdx.x; n < -tile.length; n += kThreads) l.a.lse[head * l.tokens + tile.begin + n] = -INFINITY;
         return;
     }
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+    const int wave = wave_number(), lane = threadIdx.x & 63, half = lane >> 5;
     const int first = tile.tile * kAttendRows, wfirst = first + 32 * wave, query = wfirst + (lane & 31);
     const int last = min(first + kAttendRows, tile.length);
     int from, to;
@@ -193,25 +197,33 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
             Copy<T, W, kThreads>::start(buffers[turn ^ 2 | 1], vp + (k0 + 64) * l.a.v.token_stride, l.a.v.token_stride, to - k0 - 64, dim);
         }
         if (k0 > wfirst + 31) continue;
+        // (LDS is read a few products ahead: the compiler would wait for each operand right behind its read)
         float16v s[2] = {};
+        uint4v f[W / 8];
 #pragma unroll
-        for (int b = 0; b < 2; b++)
+        for (int t = 0; t < kAhead; t++) f[t] = at.rows(keys, 32 * (t % 2), t / 2);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int n = 0; n < W / 16; n++) s[b] = mma<T>(at.rows(keys, 32 * b, n), q[n], s[b]);
+        for (int t = 0; t < W / 8; t++) {
+            if (t + kAhead < W / 8) f[t + kAhead] = at.rows(keys, 32 * (t % 2), (t + kAhead) / 2);
+            s[t % 2] = mma<T>(f[t], q[t / 2], s[t % 2]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         const bool edge = k0 + 63 > wfirst;
         if (edge) {
+            const int seen = query - k0 - 4 * half;
 #pragma unroll
             for (int b = 0; b < 2; b++)
 #pragma unroll
                 for (int i = 0; i < 16; i++)
-                    if (k0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4 > query) s[b][i] = -INFINITY;
+                    if (32 * b + 8 * (i / 4) + i % 4 > seen) s[b][i] = -INFINITY;
         }
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int i = 0; i < 16; i++) top = fmaxf(top, s[b][i]);
-        top = fmaxf(top, other_half(top));
+        top = max_of_halves(top);
         // The maximum moves only where it grows by more than a factor of 2^8: until then the probabilities stay below that, which 32 bits and
         // both types hold, and the sums need no scaling.
         if (__any(top > m + slack)) {
@@ -241,7 +253,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
             for (int b = 0; b < W / 32; b++) o[b] = mma<T>(f[b], p, o[b]);
         });
     }
-    sum += other_half(sum);
+    sum = sum_of_halves(sum);
     if (!valid) return;
     if (l.splits > 1) {
         const int64_t row = ((int64_t)split * l.a.heads + head) * l.tokens + token;
@@ -338,7 +350,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
         clear_rows<T>(l.a.dq, tile.begin, -tile.length, head, dim);
         return;
     }
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+    const int wave = wave_number(), lane = threadIdx.x & 63, half = lane >> 5;
     const int first = tile.tile * kAttendRows, wfirst = first + 32 * wave, query = wfirst + (lane & 31);
     const int last = min(first + kAttendRows, tile.length);
     int from, to;
@@ -363,7 +375,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
         for (int n = 0; n < W / 16; n++)
 #pragma unroll
             for (int j = 0; j < 8; j++) top = fmaxf(top, fabsf((float)__builtin_bit_cast(V, g[n])[j]));
-        top = fmaxf(top, other_half(top));
+        top = max_of_halves(top);
         grow = gradient_scale<T>(top);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -395,7 +407,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 #pragma unroll
             for (int j = 0; j < 8; j++) delta += (float)__builtin_bit_cast(V, o[n])[j] * (float)__builtin_bit_cast(V, g[n])[j];
     }
-    delta += other_half(delta);
+    delta = sum_of_halves(delta);
     if (valid && half == 0 && to == last) l.delta[head * l.tokens + token] = delta;
     float16v dq[W / 32] = {};
 
@@ -417,17 +429,33 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
             constexpr int b = decltype(block)::value;
             if (k0 + 32 * b > wfirst + 31) return;
             float16v s = {}, d = {};
+            uint4v x[W / 16], y[W / 16];
+#pragma unroll
+            for (int n = 0; n < kAhead / 2; n++) {
+                x[n] = at.rows(keys, 32 * b, n);
+                y[n] = at.rows(values, 32 * b, n);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int n = 0; n < W / 16; n++) {
-                s = mma<T>(at.rows(keys, 32 * b, n), q[n], s);
-                d = mma<T>(at.rows(values, 32 * b, n), g[n], d);
+                if (n + kAhead / 2 < W / 16) {
+                    x[n + kAhead / 2] = at.rows(keys, 32 * b, n + kAhead / 2);
+                    y[n + kAhead / 2] = at.rows(values, 32 * b, n + kAhead / 2);
+                }
+                s = mma<T>(x[n], q[n], s);
+                d = mma<T>(y[n], g[n], d);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            const bool edge = k0 + 32 * b + 31 > wfirst;
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 const float p = __builtin_amdgcn_exp2f(s[i] * by - lse);
                 s[i] = __is_same(T, f16) ? p * (d[i] - delta) * grow : p * (d[i] - delta);
-                if (edge && k0 + 32 * b + 8 * (i / 4) + 4 * half + i % 4 > query) s[i] = 0.0f;
+            }
+            if (k0 + 32 * b + 31 > wfirst) {
+                const int seen = query - k0 - 4 * half;
+#pragma unroll
+                for (int i = 0; i < 16; i++)
+                    if (32 * b + 8 * (i / 4) + i % 4 > seen) s[i] = 0.0f;
             }
             unrolled<2>([&](auto h) {
                 constexpr int n = decltype(h)::value;

@@ -183,10 +183,16 @@ __device__ __forceinline__ void copies_arrive()
     __syncthreads();
 }
 
-// the other half-wave's value of the same column
-__device__ __forceinline__ float other_half(float x)
+// sum and maximum of a value and that of the same column in the other half-wave
+__device__ __forceinline__ float sum_of_halves(float x)
 {
-    return __shfl_xor(x, 32);
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max_of_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 }  // namespace tessel
