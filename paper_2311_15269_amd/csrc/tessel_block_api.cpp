@@ -129,7 +129,7 @@ int norm_ok(const tessel_residual_norm *a)
     return TESSEL_OK;
 }
 
-size_t norm_workspace(const tessel_residual_norm *a) { return (size_t)norm_parts(*a) * 3 * a->channels * sizeof(float); }
+size_t norm_workspace(const tessel_residual_norm *a) { return (size_t)norm_parts(*a) * 2 * a->channels * sizeof(float); }
 
 int weight_ok(const tessel_weight_grad *a)
 {

@@ -10,7 +10,7 @@ namespace tessel {
 
 struct NormLaunch {
     tessel_residual_norm a;
-    float *parts;                // [parts][3][channels]: gradients of pre, post and the channels' gate, by workgroup
+    float *parts;                // [parts][2][channels]: what the gradients of pre, and of post and the channels' gate, are made of, by workgroup
     int    num_parts;
 };
 
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
 }
 
 template <typename T, int LANES, int CHUNKS, bool TOKEN>
-__global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 ? 4 : CHUNKS == 2 ? 2 : 3) void norm_backward_kernel(NormLaunch l)
+__global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 || CHUNKS == 1 ? 4 : LANES > 256 || sizeof(T) == 4 ? 2 : 3) void norm_backward_kernel(NormLaunch l)
 {
     typedef Parameters<LANES, CHUNKS, CHUNKS == 1 ? kInRegisters : LANES <= 512 ? kInLds : kInMemory> P;
     __shared__ float4v shared[P::kLds];
@@ -182,7 +182,9 @@ __global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 ? 4 : CHUNKS == 2 
     const tessel_residual_norm &a = l.a;
     const int lane = threadIdx.x % LANES, C = a.channels;
     const P p(a, shared);
-    float dpre[CHUNKS][8] = {}, dpost[CHUNKS][8] = {}, dgate[CHUNKS][8] = {};
+    // by: sum of r's gradient times y over its root mean square (of which the gradients of post and the channels' gate are multiples);
+    // with TOKEN, times the gate, and so post's
+    float dpre[CHUNKS][8] = {}, by[CHUNKS][8] = {};
     const Range range(a.tokens, kRows);
     for (int64_t first = range.begin; first < range.end; first += kRows) {
         const bool there = first + threadIdx.x / LANES < range.end;           // (as in norm_kernel)
@@ -234,11 +236,12 @@ __global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 ? 4 : CHUNKS == 2 
             if (!TOKEN) p.get(gate, 2, k, C);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                v[j] = dn[k][j] * (y[k][j] * post[j]);
-                if (!TOKEN) dgate[k][j] += v[j];
-                dn[k][j] *= TOKEN ? (float)rg[k][j] : gate[j];
-                dpost[k][j] += dn[k][j] * y[k][j];
-                dn[k][j] *= post[j];
+                if (TOKEN) {
+                    v[j] = dn[k][j] * (y[k][j] * post[j]);
+                    dn[k][j] *= (float)rg[k][j];
+                }
+                by[k][j] += dn[k][j] * y[k][j];
+                dn[k][j] *= TOKEN ? post[j] : gate[j] * post[j];
                 sum += dn[k][j] * y[k][j];
             }
             if (TOKEN) store8<T>(row_of<T>(a.dgate, row), v, col, C);
@@ -254,16 +257,15 @@ __global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 ? 4 : CHUNKS == 2 
     }
     // the rows of a workgroup add up in order
     if constexpr (kRows > 1) {
-        __shared__ float sums[(kRows - 1) * LANES * 8 * 3];
+        __shared__ float sums[(kRows - 1) * LANES * 8 * 2];
         static_assert(CHUNKS == 1, "one chunk a lane");
         const int group = threadIdx.x / LANES;
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            float *at = sums + ((group - 1) * 24 + j) * LANES + lane;
+            float *at = sums + ((group - 1) * 16 + j) * LANES + lane;
             if (group > 0) {
                 at[0] = dpre[0][j];
-                at[8 * LANES] = dpost[0][j];
-                at[16 * LANES] = dgate[0][j];
+                at[8 * LANES] = by[0][j];
             }
         }
         __syncthreads();
@@ -272,19 +274,17 @@ __global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 ? 4 : CHUNKS == 2 
         for (int g = 0; g < kRows - 1; g++)
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                const float *at = sums + (g * 24 + j) * LANES + lane;
+                const float *at = sums + (g * 16 + j) * LANES + lane;
                 dpre[0][j] += at[0];
-                dpost[0][j] += at[8 * LANES];
-                dgate[0][j] += at[16 * LANES];
+                by[0][j] += at[8 * LANES];
             }
     }
-    float *out = l.parts + (int64_t)blockIdx.x * 3 * C;
+    float *out = l.parts + (int64_t)blockIdx.x * 2 * C;
 #pragma unroll
     for (int k = 0; k < CHUNKS; k++) {
         const int col = 8 * (lane + k * LANES);
         store8<float>(out, dpre[k], col, C);
-        if (a.post) store8<float>(out + C, dpost[k], col, C);
-        if (a.gate_kind == TESSEL_GATE_CHANNEL) store8<float>(out + 2 * C, dgate[k], col, C);
+        store8<float>(out + C, by[k], col, C);
     }
 }
 
@@ -294,20 +294,24 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(NormLaunch l)
     __shared__ float sums[16][64];
     const tessel_residual_norm &a = l.a;
     const int which = blockIdx.y, lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane, group = threadIdx.x >> 6;
-    float *out = which == 0 ? a.dpre : which == 1 ? a.dpost : a.dgate_channel;
-    if (which == 1 && !a.post) return;
-    if (which == 2 && a.gate_kind != TESSEL_GATE_CHANNEL) return;
+    const bool gated = a.gate_kind == TESSEL_GATE_CHANNEL;
+    if (which == 1 && !a.post && !gated) return;
     float sum = 0;
     if (col < a.channels)
 #pragma unroll 8
-        for (int p = group; p < l.num_parts; p += 16) sum += l.parts[((int64_t)p * 3 + which) * a.channels + col];
+        for (int p = group; p < l.num_parts; p += 16) sum += l.parts[((int64_t)p * 2 + which) * a.channels + col];
     sums[group][lane] = sum;
     __syncthreads();
-    if (group == 0 && col < a.channels) {
-        sum = a.accumulate ? out[col] : 0.0f;
+    if (group != 0 || col >= a.channels) return;
+    sum = 0;
 #pragma unroll
-        for (int g = 0; g < 16; g++) sum += sums[g][lane];
-        out[col] = sum;
+    for (int g = 0; g < 16; g++) sum += sums[g][lane];
+    const auto put = [&](float *out, float v) { out[col] = a.accumulate ? out[col] + v : v; };
+    if (which == 0) {
+        put(a.dpre, sum);
+    } else {
+        if (a.post) put(a.dpost, gated ? sum * ((const float *)a.gate.data)[col] : sum);
+        if (gated) put(a.dgate_channel, a.post ? sum * a.post[col] : sum);
     }
 }
 
@@ -330,11 +334,14 @@ static int64_t groups_of(const tessel_residual_norm &a, int64_t most)
     return need < most ? need : most;
 }
 
-// backward: as many workgroups as are resident at once, each leaves a part
+// backward: as many workgroups as are resident at once, each leaves a part.  More of them where their loads are many small ones (rows of 4095
+// bf16: 193 instead of 216 us forward and backward, of 500: 238 instead of 264), fewer where a few waves keep memory busy (32 bits, a gate
+// for each token, 1000 channels: 376 instead of 380 us; 4096 channels of bf16 138 instead of 142).
 int norm_parts(const tessel_residual_norm &a)
 {
     const NormShape s = shape_of(a.channels);
-    return (int)groups_of(a, s.threads > 256 ? 256 : s.chunks == 2 ? 512 : 768);
+    const bool half = a.type != TESSEL_F32;
+    return (int)groups_of(a, s.threads > 256 ? 256 : s.chunks == 1 ? (half ? 1024 : 768) : half && a.channels % 8 ? 768 : 512);
 }
 
 template <typename T, bool TOKEN>
@@ -383,7 +390,7 @@ int launch_norm_backward(const tessel_residual_norm &a, float *parts, void *stre
     if (l.num_parts > 0)
         e = launched(hipLaunchKernel(norm_of(a, true), dim3((unsigned)l.num_parts), dim3(s.threads), args, 0, (hipStream_t)stream));
     if (e == 0)
-        e = launched(hipLaunchKernel((const void *)norm_sum_kernel, dim3((unsigned)((a.channels + 63) / 64), 3), dim3(1024), args, 0, (hipStream_t)stream));
+        e = launched(hipLaunchKernel((const void *)norm_sum_kernel, dim3((unsigned)((a.channels + 63) / 64), 2), dim3(1024), args, 0, (hipStream_t)stream));
     return e;
 }
 
