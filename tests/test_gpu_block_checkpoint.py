@@ -113,6 +113,19 @@ def test_gated_of_large_values(ops):
         assert float((dg.cpu() - torch.tensor([[0.0, 0.0, 1.0, 1.0, 0.5]])).abs().max()) <= 1e-4 and bool(du.isfinite().all())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gated_where_powers_of_the_argument_leave_32_bits(ops, dtype):
+    for act in ("silu", "gelu"):
+        g = torch.tensor([1e12, 1e13, 1.8e19, 2e19, 1e25, 1e38], device="cuda")[:, None]
+        g = torch.cat([g, -g]).to(dtype)
+        u = torch.ones_like(g)
+        a, kg, ku = ops.gated(g, u, act)
+        dg, du, again = ops.gated_backward(u, kg, ku, act, with_output=True)
+        kept = ops.restore(kg)
+        assert torch.equal(a, g.clamp(min=0)) and torch.equal(again, kept.clamp(min=0)) and torch.equal(du, again)
+        assert torch.equal(dg, (g > 0).to(dtype))
+
+
 def check_weight(ops, n, m, c, dtype, seed=1, into=None):
     dy, x = rows(n, m, dtype, seed), rows(n, c, dtype, seed + 1)
     k = ops.checkpoint(x.cuda())
