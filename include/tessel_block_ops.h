@@ -71,7 +71,7 @@ typedef struct {
     int32_t  heads;         /* a multiple of kv_heads                                                      */
     int32_t  kv_heads;
     int32_t  dim;           /* a multiple of 8, at most 128                                                */
-    float    scale;         /* positive                                                                    */
+    float    scale;         /* 2^-100 .. 2^100                                                             */
     tessel_heads q, k, v;   /* data and strides: multiples of 16 bytes, strides not negative               */
     tessel_heads o;         /* forward: written; backward: read                                            */
     float   *lse;           /* [heads][total_tokens]; forward: written; backward: read                     */

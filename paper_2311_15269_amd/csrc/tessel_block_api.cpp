@@ -48,7 +48,7 @@ bool heads_ok(const tessel_heads &h, bool written, int heads, int dim)
 int attention_ok(const tessel_packing *p, const tessel_attention *a)
 {
     if (!p || !a || a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->dim < 1) return TESSEL_E_INVALID_ARG;
-    if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return TESSEL_E_INVALID_ARG;
+    if (!(a->scale >= 0x1p-100f && a->scale <= 0x1p100f)) return TESSEL_E_INVALID_ARG;        // (the kernels divide by it)
     if ((a->type != TESSEL_BF16 && a->type != TESSEL_F16) || a->dim % 8 || a->dim > 128) return TESSEL_E_UNSUPPORTED;
     if ((int64_t)p->tiles.size() * a->heads > kMostBlocks) return TESSEL_E_TOOBIG;           // (splits: of small launches only)
     return TESSEL_OK;

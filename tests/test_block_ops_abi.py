@@ -83,6 +83,16 @@ def test_attention_forward_refuses(change, code):
     lib.tessel_packing_destroy(h)
 
 
+@pytest.mark.parametrize("scale, code", [(2.0 ** -100, WORKSPACE), (2.0 ** 100, WORKSPACE), (2.0 ** -101, INVALID), (2.0 ** 101, INVALID), (1e-44, INVALID)])
+def test_attention_takes_scales_that_it_can_divide_by(scale, code):
+    rc, h = packing([5, 300])
+    lib = B._library()
+    a = attention(scale=scale)
+    assert lib.tessel_attention_forward(h, C.byref(a), AT, 1 << 40, None) == code
+    assert lib.tessel_attention_backward(h, C.byref(a), AT, 1 << 40, None) == code
+    lib.tessel_packing_destroy(h)
+
+
 @pytest.mark.parametrize("change, code", [
     ({}, WORKSPACE), ({"type": 2}, UNSUPPORTED), ({"d_o": B.Heads(AT + 2, 256, 64)}, INVALID), ({"dq": B.Heads(AT, 8, 64)}, INVALID),
     ({"dk": B.Heads(None, 128, 64)}, INVALID), ({"dv": B.Heads(AT, 128, 8)}, INVALID), ({"d_o": B.Heads(AT, 0, 0)}, WORKSPACE), ({"lse": 0}, INVALID),
