@@ -138,7 +138,7 @@ int weight_ok(const tessel_weight_grad *a)
     if (e) return e;
     if (a->x.type == TESSEL_F32) return TESSEL_E_UNSUPPORTED;
     if ((int64_t)((a->outputs + 127) / 128) * ((a->x.channels + 127) / 128) > kMostBlocks) return TESSEL_E_TOOBIG;
-    if (a->dy.stride > kMostNear || a->x.value_stride > kMostNear || a->x.exponent_stride > kMostNear) return TESSEL_E_TOOBIG;
+    if (a->outputs > kMostNear || a->dy.stride > kMostNear || a->x.value_stride > kMostNear || a->x.exponent_stride > kMostNear) return TESSEL_E_TOOBIG;
     if (!a->dw || !aligned(a->dw, 4) || a->dw_stride < a->x.channels || a->dw_stride > kMostStride) return TESSEL_E_INVALID_ARG;
     return rows_ok(a->dy, a->x.type, a->x.tokens, a->outputs, false) ? TESSEL_OK : TESSEL_E_INVALID_ARG;
 }

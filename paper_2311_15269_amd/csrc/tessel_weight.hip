@@ -22,29 +22,45 @@ struct WeightLaunch {
 
 // What dy looks like decides how it comes to LDS.
 //   kStraight  rows of whole chunks of 16 bytes: from memory to LDS without passing registers, three buffers, two tiles ahead
-//   kAny       through registers, one tile ahead
-enum { kStraight, kAny };
+//   kUneven    other rows of eight outputs or more, through registers: a chunk that would pass the row's end starts eight before it
+//   kNarrow    fewer outputs, value by value
+// (No load stands in a branch: the compiler would wait for it where the branch ends.)
+enum { kStraight, kUneven, kNarrow };
 
-// 64 tokens x COLUMNS of dy through registers
-template <typename T, int COLUMNS, int THREADS>
+// the output that a lane's chunk at output n starts with
+template <int HOW>
+__device__ __forceinline__ int chunk_start(int n, int outputs) { return HOW == kNarrow ? n : min(n, outputs - 8); }
+
+// 64 tokens x COLUMNS of dy through registers.  Rows behind the tokens repeat the last one and are put as zeros.
+template <typename T, int COLUMNS, int THREADS, int HOW>
 struct DyStage {
     static constexpr int kChunks = COLUMNS / 8, kPer = kSteps * kChunks / THREADS, kRows = THREADS / kChunks;
     typename Eight<T>::type v[kPer];
     __device__ __forceinline__ void fetch(const tessel_weight_grad &a, int64_t t0, int64_t end, int n0)
     {
-        const int r = threadIdx.x / kChunks, col = n0 + 8 * (threadIdx.x % kChunks);
-        const T *p = (const T *)a.dy.data + (t0 + r) * a.dy.stride;
+        const int r = threadIdx.x / kChunks, col = chunk_start<HOW>(n0 + 8 * (threadIdx.x % kChunks), a.outputs);
+        const T *p = (const T *)a.dy.data + t0 * a.dy.stride;
+        const uint32_t stride = (uint32_t)a.dy.stride, last = (uint32_t)min((int64_t)kSteps, end - t0) - 1;
 #pragma unroll
         for (int i = 0; i < kPer; i++) {
-            v[i] = typename Eight<T>::type{};
-            if (t0 + r + i * kRows < end) v[i] = raw8<T>(p + i * kRows * a.dy.stride, col, a.outputs);
+            const uint32_t row = min((uint32_t)(r + i * kRows), last) * stride;
+            if constexpr (HOW == kNarrow) {
+#pragma unroll
+                for (int j = 0; j < 8; j++) v[i][j] = p[row + (uint32_t)min(col + j, a.outputs - 1)];
+            } else {
+                v[i] = *(const typename Eight<T>::type *)(p + (row + (uint32_t)col));
+            }
         }
     }
-    __device__ __forceinline__ void put(uint4v *tile) const
+    __device__ __forceinline__ void put(uint4v *tile, int rows) const
     {
         const int r = threadIdx.x / kChunks, c = threadIdx.x % kChunks;
 #pragma unroll
-        for (int i = 0; i < kPer; i++) tile[c / 16 * kPanelSize + chunk_at<kPanel>(r + i * kRows, c % 16)] = __builtin_bit_cast(uint4v, v[i]);
+        for (int i = 0; i < kPer; i++) {
+            uint4v w = __builtin_bit_cast(uint4v, v[i]);
+            if (r + i * kRows >= rows) w = uint4v{0, 0, 0, 0};
+            tile[c / 16 * kPanelSize + chunk_at<kPanel>(r + i * kRows, c % 16)] = w;
+        }
     }
 };
 
@@ -184,7 +200,7 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
 #pragma unroll
             for (int h = 0; h < 2; h++) gy[2 * b + h] = (uint32_t)(uintptr_t)(lds_tile *)columns[0] + wc / 4 * kPanelSize * 16 + (at.c ^ (64 * (wc % 4 + b) + 32 * h));
         HeldStage<T, kColumns, kThreads> hs;
-        DyStage<T, HOW == kAny ? kRows : 8, HOW == kAny ? kThreads : 8> ds;
+        DyStage<T, HOW == kStraight ? 8 : kRows, HOW == kStraight ? 8 : kThreads, HOW> ds;
         const int64_t tiles = (end - begin + kSteps - 1) / kSteps;
         auto left = [&](int64_t n) { return (int)min((int64_t)kSteps, end - begin - n * kSteps); };
         hs.fetch(a, begin, end, c0);
@@ -192,10 +208,11 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
         else ds.fetch(a, begin, end, n0);
 #pragma unroll
         for (int i = 0; i < hs.kPer; i++) hs.put(columns[0], left(0), i);
-        if constexpr (HOW == kAny) ds.put(rows[0]);
+        if constexpr (HOW != kStraight) ds.put(rows[0], left(0));
         if (tiles > 1) {
             hs.fetch(a, begin + kSteps, end, c0);
             if constexpr (HOW == kStraight) Copy::start(rows[1], a, begin + kSteps, end, n0);
+            else ds.fetch(a, begin + kSteps, end, n0);
         }
         int buffer = 0;
         for (int64_t n = 0; n < tiles; n++) {
@@ -211,9 +228,6 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
                 }
             }
             __syncthreads();                                     // (this tile is there, and all are done with the one before)
-            if constexpr (HOW == kAny) {
-                if (n + 1 < tiles) ds.fetch(a, begin + (n + 1) * kSteps, end, n0);
-            }
             uint32_t fa[2 * MB], ga[4];
 #pragma unroll
             for (int b = 0; b < 2 * MB; b++) fa[b] = fx[b] + buffer * (kSteps * kRows * 2);
@@ -232,21 +246,20 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
             if (n + 1 < tiles) {
 #pragma unroll
                 for (int i = 0; i < hs.kPer; i++) hs.put(columns[turn ^ 1], left(n + 1), i);
+                if constexpr (HOW != kStraight) ds.put(rows[turn ^ 1], left(n + 1));
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (HOW == kStraight) {
                     if (n + 2 < tiles) Copy::start(rows[buffer >= 1 ? buffer - 1 : 2], a, begin + (n + 2) * kSteps, end, n0);
                 }
-                if (n + 2 < tiles) hs.fetch(a, begin + (n + 2) * kSteps, end, c0);
+                if (n + 2 < tiles) {
+                    hs.fetch(a, begin + (n + 2) * kSteps, end, c0);
+                    if constexpr (HOW != kStraight) ds.fetch(a, begin + (n + 2) * kSteps, end, n0);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             step(constant<2>{});
             step(constant<3>{});
-            if constexpr (HOW == kAny) {
-                if (n + 1 < tiles) ds.put(rows[turn ^ 1]);
-                buffer ^= 1;
-            } else {
-                buffer = buffer == 2 ? 0 : buffer + 1;
-            }
+            buffer = buffer == kBuffers - 1 ? 0 : buffer + 1;
         }
     }
     float *out = l.parts ? l.parts + (int64_t)blockIdx.y * a.outputs * a.x.channels : a.dw;
@@ -260,8 +273,8 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
         for (int i = 0; i < MB; i++)
 #pragma unroll
             for (int r = 0; r < 16; r++) {
-                const int n = n0 + 32 * (wn + i) + 8 * (r / 4) + 4 * half + r % 4;
-                if (n >= a.outputs) continue;
+                const int chunk = n0 + 32 * (wn + i) + 8 * (r / 4), n = chunk_start<HOW>(chunk, a.outputs) + 4 * half + r % 4;
+                if (n >= a.outputs || n < chunk) continue;       // (what a shifted chunk holds of the one before is stored there)
                 float *p = out + n * stride + c;
                 *p = add ? *p + acc[i][j][r] : acc[i][j][r];
             }
@@ -304,7 +317,7 @@ static WeightShape shape_of(const tessel_weight_grad &a)
     // Large tiles read LDS less for each product, small ones fill the compute units with less splitting.  Large where there are 128 of them, or
     // where the splits that fill the units keep 2048 tokens (8192 tokens, 2048 x 2048: 111 us, small 131; 2048 tokens: 52, small 46).
     WeightShape s = {256, tiles_of(256), 1};
-    if (s.tiles < 128 && a.x.tokens * s.tiles < 2048 * 256) s = {128, tiles_of(128), 1};
+    if (a.outputs < 8 || (s.tiles < 128 && a.x.tokens * s.tiles < 2048 * 256)) s = {128, tiles_of(128), 1};
     // splits of the tokens: until 512 workgroups are there (256 of the large tiles), none shorter than 256 tokens
     const int64_t most = (a.x.tokens + 255) / 256, want = (s.tile == 256 ? 256 : 512) / s.tiles, n = want < most ? want : most;
     s.splits = n < 1 ? 1 : (int)n;
@@ -321,8 +334,9 @@ int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stre
     if (l.splits > 1) l.parts = parts;
     void *args[] = {&l};
     const bool large = s.tile == 256, straight = a.outputs % 8 == 0 && a.dy.stride % 8 == 0 && (uintptr_t)a.dy.data % 16 == 0;
-#define KERNEL(T) (large ? (straight ? (const void *)weight_kernel<T, 2, 4, 4, kStraight> : (const void *)weight_kernel<T, 2, 4, 4, kAny>) \
-                         : (straight ? (const void *)weight_kernel<T, 2, 2, 2, kStraight> : (const void *)weight_kernel<T, 2, 2, 2, kAny>))
+#define KERNEL(T) (a.outputs < 8 ? (const void *)weight_kernel<T, 2, 2, 2, kNarrow> \
+                   : large ? (straight ? (const void *)weight_kernel<T, 2, 4, 4, kStraight> : (const void *)weight_kernel<T, 2, 4, 4, kUneven>) \
+                           : (straight ? (const void *)weight_kernel<T, 2, 2, 2, kStraight> : (const void *)weight_kernel<T, 2, 2, 2, kUneven>))
     const void *kernel = a.x.type == TESSEL_BF16 ? KERNEL(bf16) : KERNEL(f16);
 #undef KERNEL
     int e = launched(hipLaunchKernel(kernel, dim3((unsigned)s.tiles, (unsigned)l.splits), dim3(large ? 512 : 256), args, 0, (hipStream_t)stream));
