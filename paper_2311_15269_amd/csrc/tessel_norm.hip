@@ -107,6 +107,23 @@ struct Range {
     }
 };
 
+// Eight values of a row, in their places behind settled().  Rows of up to 8192 channels are read without branches (32 Mi values of bf16, forward and
+// backward: rows of 4095 157 us, in pieces behind a branch 192; of 1500 163 and 229; of 4096 138 both); longer ones have no registers
+// left for it (10000 channels of 32 bits: 779 and 652).
+template <typename T, int LANES>
+__device__ __forceinline__ typename Eight<T>::type chunk8(const T *row, int col, int channels)
+{
+    if constexpr (LANES > 512) return raw8<T>(row, col, channels);
+    else return take8<T, LANES == 16>(row, col, channels);
+}
+template <typename T, int LANES, bool TOKEN, typename... V>
+__device__ __forceinline__ void settled(int col, int channels, typename Eight<T>::type &gate, V &...v)
+{
+    if constexpr (LANES > 512) return;
+    else if constexpr (TOKEN) settle8<T, LANES == 16>(col, channels, v..., gate);
+    else settle8<T, LANES == 16>(col, channels, v...);
+}
+
 // TOKEN: a gate for each token and channel
 template <typename T, int LANES, int CHUNKS, bool TOKEN>
 __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
@@ -116,22 +133,29 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
     __shared__ float scratch[2][threads_of<LANES>() / 64];
     __shared__ float4v shared[P::kLds];
     const tessel_residual_norm &a = l.a;
-    const int lane = threadIdx.x % LANES;
+    const int lane = threadIdx.x % LANES, C = a.channels;
     const P p(a, shared);
     const Range range(a.tokens, kRows);
     for (int64_t first = range.begin; first < range.end; first += kRows) {
         // (a workgroup's rows go through the barriers together; behind the last row, the last one once more without a write)
         const bool there = first + threadIdx.x / LANES < range.end;
         const int64_t row = there ? first + threadIdx.x / LANES : range.end - 1;
-        const int C = there ? a.channels : 0;
+        const int begin = there ? 8 * lane : C;
         float x[CHUNKS][8], y[CHUNKS][8], sum = 0;
-        typename Eight<T>::type rg[CHUNKS];
+        typename Eight<T>::type rx[CHUNKS], ry[CHUNKS], rg[CHUNKS];
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            const int col = 8 * (lane + k * LANES);
-            load8<T>(x[k], row_of<T>(a.x, row), col, C);
-            load8<T>(y[k], row_of<T>(a.y, row), col, C);
-            if (TOKEN) rg[k] = raw8<T>(row_of<T>(a.gate, row), col, C);
+            const int col = begin + 8 * k * LANES;
+            rx[k] = chunk8<T, LANES>(row_of<T>(a.x, row), col, C);
+            ry[k] = chunk8<T, LANES>(row_of<T>(a.y, row), col, C);
+            if (TOKEN) rg[k] = chunk8<T, LANES>(row_of<T>(a.gate, row), col, C);
+        }
+#pragma unroll
+        for (int k = 0; k < CHUNKS; k++) {
+            const int col = begin + 8 * k * LANES;
+            settled<T, LANES, TOKEN>(col, C, rg[k], rx[k], ry[k]);
+            widen8<T>(x[k], rx[k]);
+            widen8<T>(y[k], ry[k]);
         }
         float over_y = 1.0f;
         if (a.post) {
@@ -153,7 +177,7 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
                 x[k][j] = a.scale * x[k][j] + (TOKEN ? (float)rg[k][j] : gate[j]) * u;
                 sum += x[k][j] * x[k][j];
             }
-            store8<T>(row_of<T>(a.r, row), x[k], 8 * (lane + k * LANES), C);
+            store8<T>(row_of<T>(a.r, row), x[k], begin + 8 * k * LANES, C);
         }
         const float over_r = 1.0f / sqrtf(row_sum<LANES>(sum, scratch[1]) / a.channels + a.eps);
 #pragma unroll
@@ -162,7 +186,7 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
             p.get(pre, 0, k, C);
 #pragma unroll
             for (int j = 0; j < 8; j++) x[k][j] *= over_r * pre[j];
-            store8<T>(row_of<T>(a.h, row), x[k], 8 * (lane + k * LANES), C);
+            store8<T>(row_of<T>(a.h, row), x[k], begin + 8 * k * LANES, C);
         }
         if (lane == 0 && there) {
             a.stats[row] = over_y;
@@ -173,7 +197,7 @@ __global__ __launch_bounds__(threads_of<LANES>()) void norm_kernel(NormLaunch l)
 }
 
 template <typename T, int LANES, int CHUNKS, bool TOKEN>
-__global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 || CHUNKS == 1 ? 4 : LANES > 256 || sizeof(T) == 4 ? 2 : 3) void norm_backward_kernel(NormLaunch l)
+__global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 || (LANES < 128 && sizeof(T) == 2) ? 4 : CHUNKS == 1 ? 3 : LANES > 256 || sizeof(T) == 4 ? 2 : 3) void norm_backward_kernel(NormLaunch l)
 {
     typedef Parameters<LANES, CHUNKS, CHUNKS == 1 ? kInRegisters : LANES <= 512 ? kInLds : kInMemory> P;
     __shared__ float4v shared[P::kLds];
@@ -189,18 +213,23 @@ __global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 || CHUNKS == 1 ? 4
     for (int64_t first = range.begin; first < range.end; first += kRows) {
         const bool there = first + threadIdx.x / LANES < range.end;           // (as in norm_kernel)
         const int64_t row = there ? first + threadIdx.x / LANES : range.end - 1;
-        const int C = there ? a.channels : 0;
+        const int begin = there ? 8 * lane : C;
         typename Eight<T>::type rx[CHUNKS], ry[CHUNKS], rr[CHUNKS], rh[CHUNKS], rg[CHUNKS];
         float x[CHUNKS][8], y[CHUNKS][8], dn[CHUNKS][8], sum = 0;
         const float over_y = a.stats[row], over_r = a.stats[a.tokens + row];
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            const int col = 8 * (lane + k * LANES);
-            rx[k] = raw8<T>(row_of<T>(a.x, row), col, C);
-            ry[k] = raw8<T>(row_of<T>(a.y, row), col, C);
-            rr[k] = raw8<T>(row_of<T>(a.dr, row), col, C);
-            rh[k] = raw8<T>(row_of<T>(a.dh, row), col, C);
-            if (TOKEN) rg[k] = raw8<T>(row_of<T>(a.gate, row), col, C);
+            const int col = begin + 8 * k * LANES;
+            rx[k] = chunk8<T, LANES>(row_of<T>(a.x, row), col, C);
+            ry[k] = chunk8<T, LANES>(row_of<T>(a.y, row), col, C);
+            rr[k] = chunk8<T, LANES>(row_of<T>(a.dr, row), col, C);
+            rh[k] = chunk8<T, LANES>(row_of<T>(a.dh, row), col, C);
+            if (TOKEN) rg[k] = chunk8<T, LANES>(row_of<T>(a.gate, row), col, C);
+        }
+#pragma unroll
+        for (int k = 0; k < CHUNKS; k++) {
+            const int col = begin + 8 * k * LANES;
+            settled<T, LANES, TOKEN>(col, C, rg[k], rx[k], ry[k], rr[k], rh[k]);
         }
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
@@ -223,7 +252,7 @@ __global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 || CHUNKS == 1 ? 4
         sum = 0;
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            const int col = 8 * (lane + k * LANES);
+            const int col = begin + 8 * k * LANES;
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) {
@@ -252,7 +281,7 @@ __global__ __launch_bounds__(threads_of<LANES>(), LANES > 512 || CHUNKS == 1 ? 4
 #pragma unroll
             for (int j = 0; j < 8; j++) dn[k][j] = over_y * (dn[k][j] - y[k][j] * mean_y);
 #pragma unroll
-        for (int k = 0; k < CHUNKS; k++) store8<T>(row_of<T>(a.dy, row), dn[k], 8 * (lane + k * LANES), C);
+        for (int k = 0; k < CHUNKS; k++) store8<T>(row_of<T>(a.dy, row), dn[k], begin + 8 * k * LANES, C);
         if constexpr (LANES > 64) __syncthreads();
     }
     // the rows of a workgroup add up in order
@@ -334,14 +363,14 @@ static int64_t groups_of(const tessel_residual_norm &a, int64_t most)
     return need < most ? need : most;
 }
 
-// backward: as many workgroups as are resident at once, each leaves a part.  More of them where their loads are many small ones (rows of 4095
-// bf16: 193 instead of 216 us forward and backward, of 500: 238 instead of 264), fewer where a few waves keep memory busy (32 bits, a gate
-// for each token, 1000 channels: 376 instead of 380 us; 4096 channels of bf16 138 instead of 142).
+// backward: as many workgroups as are resident at once, each leaves a part.  More of them where reads of 16 bits are many small ones (rows of
+// 4095 bf16: 193 instead of 216 us forward and backward, of 500: 238 instead of 264), fewer where a few waves keep memory busy (4096
+// channels of bf16: 138 instead of 142).
 int norm_parts(const tessel_residual_norm &a)
 {
     const NormShape s = shape_of(a.channels);
     const bool half = a.type != TESSEL_F32;
-    return (int)groups_of(a, s.threads > 256 ? 256 : s.chunks == 1 ? (half ? 1024 : 768) : half && a.channels % 8 ? 768 : 512);
+    return (int)groups_of(a, s.threads > 256 ? 256 : s.chunks == 1 ? (half && s.lanes < 128 ? 1024 : 768) : half && a.channels % 8 ? 768 : 512);
 }
 
 template <typename T, bool TOKEN>

@@ -48,6 +48,64 @@ __device__ __forceinline__ void load8(float *v, const T *row, int col, int chann
     for (int j = 0; j < 8; j++) v[j] = (float)w[j];
 }
 
+// The same without a branch around a read, where the compiler would wait for it: take8 reads, settle8 puts the values in their places, several
+// chunks of the same columns at once and behind all reads.  What would pass the row's end is read from eight values before it and moved
+// up.  Rows of fewer than eight, where the caller may have such (NARROW): value by value.
+template <typename T, bool NARROW>
+__device__ __forceinline__ typename Eight<T>::type take8(const T *row, int col, int channels)
+{
+    if (NARROW && channels < 8) {
+        typename Eight<T>::type v;
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = row[min(j, channels - 1)];
+        return v;
+    }
+    return *(const typename Eight<T>::type *)(row + min(col, channels - 8));
+}
+template <typename T, bool NARROW, typename... V>
+__device__ __forceinline__ void settle8(int col, int channels, V &...v)
+{
+    typedef uint32_t Words __attribute__((ext_vector_type(2 * sizeof(T))));
+    constexpr int N = 2 * sizeof(T), kWord = 4 / sizeof(T);
+    if (channels & 7) {
+        const int by = NARROW && channels < 8 ? (col < channels ? 0 : 8) : col - min(col, channels - 8);
+        const auto move = [by](typename Eight<T>::type &x) {
+            Words w = __builtin_bit_cast(Words, x);
+#pragma unroll
+            for (int step = 4; step >= kWord; step /= 2)
+#pragma unroll
+                for (int j = 0; j < N; j++) w[j] = (by & step) ? (j + step / kWord < N ? w[j + step / kWord] : 0u) : w[j];
+            if constexpr (kWord == 2) {
+#pragma unroll
+                for (int j = 0; j < N; j++) w[j] = (by & 1) ? __builtin_amdgcn_alignbit(j + 1 < N ? w[j + 1] : 0u, w[j], 16) : w[j];
+            }
+            x = __builtin_bit_cast(typename Eight<T>::type, w);
+        };
+        (move(v), ...);
+    }
+    // (a branch where waves have whole chunks; in 32 bits, where its copies cost registers that there are not, without it)
+    if (sizeof(T) == 4 || __any(col >= channels || (NARROW && channels < 8))) {
+        const auto end = [&](typename Eight<T>::type &x) {
+            if (NARROW && channels < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; j++) x[j] = j < channels ? x[j] : (T)0.0f;
+            }
+            Words w = __builtin_bit_cast(Words, x);
+#pragma unroll
+            for (int j = 0; j < N; j++) w[j] = col < channels ? w[j] : 0u;
+            x = __builtin_bit_cast(typename Eight<T>::type, w);
+        };
+        (end(v), ...);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void widen8(float *v, const typename Eight<T>::type &w)
+{
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = (float)w[j];
+}
+
 template <typename T>
 __device__ __forceinline__ void store8(T *row, const float *v, int col, int channels)
 {
