@@ -7,12 +7,9 @@ namespace tessel {
 
 typedef __bf16   bf16;
 typedef _Float16 f16;
-typedef short    short4v __attribute__((ext_vector_type(4)));
-typedef short    short8v __attribute__((ext_vector_type(8)));
 typedef float    float4v __attribute__((ext_vector_type(4)));
 typedef float    float16v __attribute__((ext_vector_type(16)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) short4v lds_short4v;
 
 // Eight values of a type, as one operand of a matrix instruction.
 template <typename T> struct Vec8;
@@ -82,20 +79,12 @@ struct Reader {
     {
         return *(const lds_tile *)((uint32_t)(uintptr_t)tile + (r ^ (32 * s)) + row * 2 * W);
     }
-    // a operand whose rows are the tile's columns 32 b .. 32 b + 31 and whose summed index are the tile's rows row .. row + 15 (row: a
-    // multiple of 16) in the order of operand(): two transposing reads, of which each group of 16 lanes takes 4 rows x 16 columns.
-    __device__ __forceinline__ uint4v columns(const lds_tile *tile, int row, int b) const
-    {
-        const uint32_t at = (uint32_t)(uintptr_t)tile + row * 2 * W;
-        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(at + (c ^ (64 * b))));
-        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(at + 8 * 2 * W + (c ^ (64 * b + 32))));
-        return __builtin_bit_cast(uint4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
 };
 
-// Column operands of one step of sixteen rows for all W / 32 blocks, by reads in one piece that ends when all have arrived.  (Where the
-// compiler places a transposing read itself, it first waits for every copy to LDS that is on its way.)  `at`: the addresses of the
-// blocks' two halves in the tile, `OFFSET`: the step's distance from its start.
+// Column operands of one step of sixteen rows for all W / 32 blocks: a operands whose rows are 32 columns of the tile and whose summed index are
+// its rows, in the order of operand().  Each is two transposing reads, of which a group of 16 lanes takes 4 rows x 16 columns, all in one piece
+// that ends when they have arrived.  (Where the compiler places a transposing read itself, it first waits for every copy to LDS that is on its
+// way.)  `at`: the addresses of the blocks' two halves in the tile, `OFFSET`: the step's distance from its start.
 __device__ __forceinline__ uint4v join(uint64_t lo, uint64_t hi)
 {
     typedef uint64_t V __attribute__((ext_vector_type(2)));

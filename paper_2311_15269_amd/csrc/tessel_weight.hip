@@ -4,6 +4,11 @@
 // index runs along the rows of both inputs, so both operands come out of LDS by transposing reads.  The checkpoint is turned into
 // numbers of the matrix instruction's type on its way to LDS, which is exact.  Few tiles: the tokens are split over several
 // workgroups, whose sums a second kernel adds in the order of their numbers.
+//
+// Bound by the matrix instructions, and with them by the clock that they leave: 4096 x 4096 from 8192 tokens of bf16 in 269 us, 1020 TF/s (a
+// library product of 16-bit inputs of that shape takes 230 to 285 us, the input first written out in 16 bits not counted).  A wave's
+// 128 x 64 reads six operands from LDS for eight products, so that LDS is not the bound.  Small ones are bound by the time from a tile's
+// reads to its use and by the parts' traffic: 1001 x 715 from 1999 tokens in 25 us.
 #include "tessel_rows.h"
 
 namespace tessel {
