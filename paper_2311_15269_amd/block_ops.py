@@ -100,14 +100,17 @@ def _library():
     return _lib
 
 
-def _stream(t):
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return torch.cuda.current_stream(t.device).cuda_stream if raw is None else raw(t.get_device())
-
-
 def _refuse(text):
     raise binding.TesselError(E_INVALID_ARG, text)
+
+
+def _stream(t):
+    """the current stream, which is one of the current GPU, so that a tensor of another one is refused"""
+    import torch
+    if t.is_cuda and t.get_device() != torch.cuda.current_device():
+        _refuse("a tensor on %s, but the current GPU is number %d" % (t.device, torch.cuda.current_device()))
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream(t.device).cuda_stream if raw is None else raw(t.get_device())
 
 
 _TYPES = {}
@@ -277,18 +280,19 @@ def residual_norm_backward(dr, dh, x, y, stats, pre, post=None, gate=None, scale
         _refuse("stats is not what the forward call gave")
     dx, dy = _like(x), _like(x)
     if into is None:
-        dpre, dpost, dgate = x.new_empty((3, c), dtype=torch.float32).unbind(0)
-        dpost = dpost if post is not None else None
-        dgate = dgate if kind == GATE_CHANNEL else None
+        new = x.new_empty((3, c), dtype=torch.float32)
+        dpre, dpost, dgate = new.unbind(0)
+        first = new.data_ptr()
+        to = [first, first + 4 * c, first + 8 * c]
     else:
         dpre, dpost, dgate = into
-    to = [_vector(dpre, c, x), None, None]
-    if post is not None:
-        to[1] = _vector(dpost, c, x)
+        to = [_vector(dpre, c, x), None if post is None else _vector(dpost, c, x), _vector(dgate, c, x) if kind == GATE_CHANNEL else None]
+    if post is None:
+        dpost = to[1] = None
     at = (None, 0)
-    if kind == GATE_CHANNEL:
-        to[2] = _vector(dgate, c, x)
-    elif kind == GATE_TOKEN:
+    if kind != GATE_CHANNEL:
+        dgate = to[2] = None
+    if kind == GATE_TOKEN:
         dgate = _like(x)
         at = (dgate.data_ptr(), c)
     a = _FlatNorm(*described, stats.data_ptr(), None, 0, None, 0, *_rows(dr), *_rows(dh), dx.data_ptr(), c, dy.data_ptr(), c, *at, *to,

@@ -241,3 +241,22 @@ def test_binding_refuses_what_it_can_see():
     with pytest.raises(binding.TesselError) as e:
         B._type(torch.zeros(1, dtype=torch.float64))
     assert e.value.code == UNSUPPORTED
+
+
+def test_tensors_of_another_gpu_are_refused(monkeypatch):
+    """the stream is one of the current GPU: a tensor of another one must not reach a kernel there"""
+    import torch
+
+    class There:
+        is_cuda, device = True, "cuda:1"
+
+        @staticmethod
+        def get_device():
+            return 1
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 77, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(binding.TesselError) as error:
+        B._stream(There())
+    assert error.value.code == INVALID and "cuda:1" in str(error.value)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    assert B._stream(There()) == 77
