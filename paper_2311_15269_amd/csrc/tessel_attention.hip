@@ -332,18 +332,10 @@ __device__ __forceinline__ float gradient_scale(float top)
     return __uint_as_float((254u << 23) - (__float_as_uint(top) & 0x7F800000u));
 }
 
-// l.largest[head][first token of a sequence]: the bits of the largest |do| there (f16)
-__global__ __launch_bounds__(kThreads) void attend_clear_kernel(AttendLaunch l)
-{
-    const int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (n >= (int64_t)l.num_tiles * l.a.heads) return;
-    const AttendTile tile = l.tiles[n / l.a.heads];
-    if (tile.length > 0 && tile.tile == 0) l.largest[n % l.a.heads * l.tokens + tile.begin] = 0;
-}
-
 // The gradient of q: three products (scores, do v, and their gradients times k), one operand from LDS for each.  The documents above: 247 us, 830
 // TF/s.  (It and the kernel of dk and dv both compute the scores, seven products instead of five: one kernel for all three gradients would add
-// to dq from many workgroups, in no fixed order.)  Also, for the kernel behind it delta_i = sum_d do_i o_i and in half precision the largest |do|.
+// to dq from many workgroups, in no fixed order.)  Also, for the kernel behind it delta_i = sum_d do_i o_i and in half precision the largest |do| of
+// every 32 queries.
 //
 // The first 128 queries of a sequence take delta_i = sum_j p_ij (do_i . v_j) instead, the same sum from the inputs: o is rounded,
 // and where a query sees few keys that error is as large as the one of rounding the gradients of the scores.  (dq and dk of sequences of 1, 17
@@ -390,8 +382,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
         grow = gradient_scale<T>(top);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        // (not below nought: ordered as whole numbers are, and the same in any order)
-        if (lane == 0 && to == last) atomicMax(l.largest + head * l.tokens + tile.begin, __float_as_uint(top));
+        if (lane == 0 && to == last && wfirst < tile.length) l.largest[head * l.tokens + tile.begin + wfirst] = top;
     }
     float delta = 0;
     if (tile.tile == 0) {
@@ -593,9 +584,12 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     if (from == to) return;
     float grow = 1.0f;
     if constexpr (__is_same(T, f16)) {
-        uint32_t top = 0;
-        for (int head = kv * shared; head < (kv + 1) * shared; head++) top = max(top, l.largest[head * l.tokens + tile.begin]);
-        grow = gradient_scale<T>(__uint_as_float(top));
+        float top = 0;
+        for (int head = kv * shared; head < (kv + 1) * shared; head++)
+            for (int i = 32 * lane; i < tile.length; i += 32 * 64) top = fmaxf(top, l.largest[head * l.tokens + tile.begin + i]);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        grow = gradient_scale<T>(top);
     }
 
     uint4v k[W / 16], v[W / 16];
@@ -719,9 +713,7 @@ int launch_attend(const AttendLaunch &l, void *stream)
 
 int launch_attend_dq(const AttendLaunch &l, void *stream)
 {
-    int e = 0;
-    if (l.a.type == TESSEL_F16) e = launch((const void *)attend_clear_kernel, ((int64_t)l.num_tiles * l.a.heads + kThreads - 1) / kThreads, l, stream);
-    if (e == 0) e = launch(ATTEND_KERNEL(attend_dq_kernel), (int64_t)l.num_tiles * l.a.heads * l.splits, l, stream);
+    int e = launch(ATTEND_KERNEL(attend_dq_kernel), (int64_t)l.num_tiles * l.a.heads * l.splits, l, stream);
     if (e == 0 && l.splits > 1) e = join(l, false, l.a.dq, nullptr, l.a.heads, 1, stream);
     return e;
 }

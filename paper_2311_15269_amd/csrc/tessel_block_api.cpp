@@ -268,7 +268,7 @@ int tessel_attention_backward(const tessel_packing *p, const tessel_attention *a
     if (!p->table || !workspace_ok(workspace_dev, workspace_bytes, backward_workspace(p, a))) return TESSEL_E_WORKSPACE;
     AttendLaunch l = attend_launch(p, a);
     l.delta = (float *)workspace_dev;
-    l.largest = (uint32_t *)(l.delta + p->tokens * a->heads);
+    l.largest = l.delta + p->tokens * a->heads;
     l.parts = l.delta + gradient_words(p, a);
     l.splits = query_splits(p, a);
     e = launch_attend_dq(l, hip_stream);
