@@ -41,9 +41,9 @@ template <typename T, int COLUMNS, int THREADS, int HOW>
 struct DyStage {
     static constexpr int kChunks = COLUMNS / 8, kPer = kSteps * kChunks / THREADS, kRows = THREADS / kChunks;
     typename Eight<T>::type v[kPer];
-    __device__ __forceinline__ void fetch(const tessel_weight_grad &a, int64_t t0, int64_t end, int n0)
+    __device__ __forceinline__ void fetch(const tessel_weight_grad &a, int64_t t0, int64_t end, int n0, int thread)
     {
-        const int r = threadIdx.x / kChunks, col = chunk_start<HOW>(n0 + 8 * (threadIdx.x % kChunks), a.outputs);
+        const int r = thread / kChunks, col = chunk_start<HOW>(n0 + 8 * (thread % kChunks), a.outputs);
         const T *p = (const T *)a.dy.data + t0 * a.dy.stride;
         const uint32_t stride = (uint32_t)a.dy.stride, last = (uint32_t)min((int64_t)kSteps, end - t0) - 1;
 #pragma unroll
@@ -57,9 +57,9 @@ struct DyStage {
             }
         }
     }
-    __device__ __forceinline__ void put(uint4v *tile, int rows) const
+    __device__ __forceinline__ void put(uint4v *tile, int rows, int thread) const
     {
-        const int r = threadIdx.x / kChunks, c = threadIdx.x % kChunks;
+        const int r = thread / kChunks, c = thread % kChunks;
 #pragma unroll
         for (int i = 0; i < kPer; i++) {
             uint4v w = __builtin_bit_cast(uint4v, v[i]);
@@ -76,12 +76,12 @@ struct DyCopy {
     static constexpr int kChunks = COLUMNS / 8, kPer = kSteps * kChunks / THREADS;
     static constexpr int kRows = THREADS / 16, kEach = kSteps / kRows;         // a panel at a time: rows an instruction, instructions
     static_assert(kRows % 16 == 0 && kEach * (COLUMNS / kPanel) == kPer, "the order of chunks repeats after 16 rows");
-    __device__ __forceinline__ static void start(uint4v *tile, const tessel_weight_grad &a, int64_t t0, int64_t end, int n0)
+    __device__ __forceinline__ static void start(uint4v *tile, const tessel_weight_grad &a, int64_t t0, int64_t end, int n0, int thread)
     {
-        const int r = threadIdx.x / 16, c = (threadIdx.x % 16) ^ (chunk_at<kPanel>(r, 0) % 16);
+        const int r = thread / 16, c = (thread % 16) ^ (chunk_at<kPanel>(r, 0) % 16);
         const T *p = (const T *)a.dy.data + t0 * a.dy.stride;
         const uint32_t stride = (uint32_t)a.dy.stride, last = (uint32_t)min((int64_t)kSteps, end - t0) - 1;
-        lds_uint4v *to = (lds_uint4v *)(tile + __builtin_amdgcn_readfirstlane(threadIdx.x & ~63));
+        lds_uint4v *to = (lds_uint4v *)(tile + __builtin_amdgcn_readfirstlane(thread & ~63));
 #pragma unroll
         for (int b = 0; b < COLUMNS / kPanel; b++) {
             const uint32_t col = min(n0 + b * kPanel + 8 * c, a.outputs - 8);
@@ -90,9 +90,9 @@ struct DyCopy {
                 __builtin_amdgcn_global_load_lds((global_uint4v *)(p + (min((uint32_t)(r + i * kRows), last) * stride + col)), to + b * kPanelSize + i * THREADS, 16, 0, 0);
         }
     }
-    __device__ __forceinline__ static void clear(uint4v *tile, int rows)
+    __device__ __forceinline__ static void clear(uint4v *tile, int rows, int thread)
     {
-        for (int k = threadIdx.x; k < (kSteps - rows) * kChunks; k += THREADS)
+        for (int k = thread; k < (kSteps - rows) * kChunks; k += THREADS)
             tile[k / (16 * (kSteps - rows)) * kPanelSize + (rows + k / 16 % (kSteps - rows)) * 16 + k % 16] = uint4v{0, 0, 0, 0};
     }
 };
@@ -103,10 +103,10 @@ struct HeldStage {
     static constexpr int kChunks = COLUMNS / 16, kPer = kSteps * kChunks / THREADS, kRows = THREADS / kChunks;
     uint4v   v[kPer];
     uint32_t e[kPer];
-    __device__ __forceinline__ void fetch(const tessel_weight_grad &a, int64_t t0, int64_t end, int c0)
+    __device__ __forceinline__ void fetch(const tessel_weight_grad &a, int64_t t0, int64_t end, int c0, int thread)
     {
-        const int r = threadIdx.x / kChunks;
-        const uint32_t col = min(c0 + 16 * ((int)threadIdx.x % kChunks), (a.x.channels - 1) & ~15);   // (behind the channels, values to the end of the group)
+        const int r = thread / kChunks;
+        const uint32_t col = min(c0 + 16 * (thread % kChunks), (a.x.channels - 1) & ~15);   // (behind the channels, values to the end of the group)
         const int8_t *p = a.x.values + t0 * a.x.value_stride;
         const uint8_t *q = a.x.exponents + t0 * a.x.exponent_stride;
         const uint32_t last = (uint32_t)min((int64_t)kSteps, end - t0) - 1;
@@ -118,9 +118,9 @@ struct HeldStage {
         }
     }
     // rows: of which tokens there are
-    __device__ __forceinline__ void put(uint4v *tile, int rows, int i) const
+    __device__ __forceinline__ void put(uint4v *tile, int rows, int i, int thread) const
     {
-        const int r = threadIdx.x / kChunks + i * kRows, c = 2 * (threadIdx.x % kChunks);
+        const int r = thread / kChunks + i * kRows, c = 2 * (thread % kChunks);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             float f[8];
@@ -176,24 +176,29 @@ __device__ __forceinline__ void read_step(uint4v (&f)[2], uint4v (&g)[2], const 
     for (int b = 0; b < 2; b++) g[b] = join(r[4 + 2 * b], r[5 + 2 * b]);
 }
 
-// WN x WC waves, 32 MB x 64 of dw each
-template <typename T, int WN, int WC, int MB, int HOW>
-__global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
+// WN x WC waves, 32 MB x 64 of dw each, GROUPS times, each group for its share of the workgroup's tokens (two, where tiles are small: with half as many
+// parts in memory as two workgroups would leave)
+template <typename T, int WN, int WC, int MB, int HOW, int GROUPS>
+__global__ __launch_bounds__(64 * WN * WC * GROUPS, 2) void weight_kernel(WeightLaunch l)
 {
     constexpr int kThreads = 64 * WN * WC, kRows = WN * MB * 32, kColumns = WC * 64, kBuffers = HOW == kStraight ? 3 : 2;
     static_assert(kRows % kPanel == 0 && kColumns % kPanel == 0, "whole panels");
     typedef DyCopy<T, kRows, kThreads> Copy;
-    __shared__ __attribute__((aligned(256))) uint4v rows[kBuffers][kSteps * kRows / 8], columns[2][kSteps * kColumns / 8];
+    __shared__ __attribute__((aligned(256))) uint4v all_rows[GROUPS][kBuffers][kSteps * kRows / 8], all_columns[GROUPS][2][kSteps * kColumns / 8];
+    const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads), thread = threadIdx.x % kThreads;
+    uint4v (*const rows)[kSteps * kRows / 8] = all_rows[group], (*const columns)[kSteps * kColumns / 8] = all_columns[group];
     const tessel_weight_grad &a = l.a;
     // workgroups go to the eight L2 caches in turn: each cache gets neighbouring tiles, which share their inputs
     const int all = gridDim.x, per = all / 8, more = all % 8, x = blockIdx.x % 8;
     const int place = x * per + min(x, more) + blockIdx.x / 8;
     const int n0 = place / l.tiles_c * kRows, c0 = place % l.tiles_c * kColumns;
-    const int64_t begin = blockIdx.y * l.per, end = min(begin + l.per, a.x.tokens);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+    // the first group's share has as many steps as any other's: all go through its barriers
+    const int64_t from = blockIdx.y * l.per, to = min(from + l.per, a.x.tokens), share = ((to - from + kSteps - 1) / kSteps + GROUPS - 1) / GROUPS;
+    const int64_t begin = min(from + group * share * kSteps, to), end = min(begin + share * kSteps, to);
+    const int wave = thread >> 6, lane = threadIdx.x & 63, half = lane >> 5;
     const int wn = wave / WC * MB, wc = wave % WC * 2;           // in blocks of 32
     float16v acc[MB][2] = {};
-    if (begin < end) {
+    if (from < to) {
         const Reader<kPanel> at;
         uint32_t fx[2 * MB], gy[4];                              // operands' addresses: blocks of 32, both halves of their eight tokens
 #pragma unroll
@@ -208,31 +213,35 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
         DyStage<T, HOW == kStraight ? 8 : kRows, HOW == kStraight ? 8 : kThreads, HOW> ds;
         const int64_t tiles = (end - begin + kSteps - 1) / kSteps;
         auto left = [&](int64_t n) { return (int)min((int64_t)kSteps, end - begin - n * kSteps); };
-        hs.fetch(a, begin, end, c0);
-        if constexpr (HOW == kStraight) Copy::start(rows[0], a, begin, end, n0);
-        else ds.fetch(a, begin, end, n0);
+        if (tiles > 0) {
+            hs.fetch(a, begin, end, c0, thread);
+            if constexpr (HOW == kStraight) Copy::start(rows[0], a, begin, end, n0, thread);
+            else ds.fetch(a, begin, end, n0, thread);
 #pragma unroll
-        for (int i = 0; i < hs.kPer; i++) hs.put(columns[0], left(0), i);
-        if constexpr (HOW != kStraight) ds.put(rows[0], left(0));
-        if (tiles > 1) {
-            hs.fetch(a, begin + kSteps, end, c0);
-            if constexpr (HOW == kStraight) Copy::start(rows[1], a, begin + kSteps, end, n0);
-            else ds.fetch(a, begin + kSteps, end, n0);
+            for (int i = 0; i < hs.kPer; i++) hs.put(columns[0], left(0), i, thread);
+            if constexpr (HOW != kStraight) ds.put(rows[0], left(0), thread);
         }
+        if (tiles > 1) {
+            hs.fetch(a, begin + kSteps, end, c0, thread);
+            if constexpr (HOW == kStraight) Copy::start(rows[1], a, begin + kSteps, end, n0, thread);
+            else ds.fetch(a, begin + kSteps, end, n0, thread);
+        }
+        const int64_t short_one = (to - from) % kSteps ? ((to - from) / kSteps) % share : -1;       // the step of the tile that is not whole
         int buffer = 0;
-        for (int64_t n = 0; n < tiles; n++) {
+        for (int64_t n = 0; n < share; n++) {
             const int turn = n & 1;
             // Waits for this tile's copies.  Those of the next one, which were started behind them, and its values of the checkpoint may
             // still be on their way: as many loads as stand between two calls of sched_barrier below.
             if constexpr (HOW == kStraight) {
                 if (n + 1 < tiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copy::kPer + 2 * hs.kPer) : "memory");
                 else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                if (left(n) < kSteps) {
+                if (n == short_one) {
                     __syncthreads();                             // (all waves' copies, before zeros go over them)
-                    Copy::clear(rows[buffer], left(n));
+                    if (n < tiles) Copy::clear(rows[buffer], left(n), thread);
                 }
             }
             __syncthreads();                                     // (this tile is there, and all are done with the one before)
+            if (GROUPS > 1 && n >= tiles) continue;
             uint32_t fa[2 * MB], ga[4];
 #pragma unroll
             for (int b = 0; b < 2 * MB; b++) fa[b] = fx[b] + buffer * (kSteps * kRows * 2);
@@ -250,15 +259,15 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
             step(constant<1>{});
             if (n + 1 < tiles) {
 #pragma unroll
-                for (int i = 0; i < hs.kPer; i++) hs.put(columns[turn ^ 1], left(n + 1), i);
-                if constexpr (HOW != kStraight) ds.put(rows[turn ^ 1], left(n + 1));
+                for (int i = 0; i < hs.kPer; i++) hs.put(columns[turn ^ 1], left(n + 1), i, thread);
+                if constexpr (HOW != kStraight) ds.put(rows[turn ^ 1], left(n + 1), thread);
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (HOW == kStraight) {
-                    if (n + 2 < tiles) Copy::start(rows[buffer >= 1 ? buffer - 1 : 2], a, begin + (n + 2) * kSteps, end, n0);
+                    if (n + 2 < tiles) Copy::start(rows[buffer >= 1 ? buffer - 1 : 2], a, begin + (n + 2) * kSteps, end, n0, thread);
                 }
                 if (n + 2 < tiles) {
-                    hs.fetch(a, begin + (n + 2) * kSteps, end, c0);
-                    if constexpr (HOW != kStraight) ds.fetch(a, begin + (n + 2) * kSteps, end, n0);
+                    hs.fetch(a, begin + (n + 2) * kSteps, end, c0, thread);
+                    if constexpr (HOW != kStraight) ds.fetch(a, begin + (n + 2) * kSteps, end, n0, thread);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -266,6 +275,24 @@ __global__ __launch_bounds__(64 * WN * WC, 2) void weight_kernel(WeightLaunch l)
             step(constant<3>{});
             buffer = buffer == kBuffers - 1 ? 0 : buffer + 1;
         }
+    }
+    if constexpr (GROUPS > 1) {
+        static_assert(GROUPS == 2 && sizeof(all_rows) >= sizeof(acc) * kThreads, "one group's sums");
+        float4v *sums = (float4v *)all_rows + thread;
+        __syncthreads();
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < MB * 8; i++) {
+                const float16v &c = acc[i / 8][i / 4 % 2];
+                sums[i * kThreads] = float4v{c[4 * (i % 4)], c[4 * (i % 4) + 1], c[4 * (i % 4) + 2], c[4 * (i % 4) + 3]};
+            }
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int i = 0; i < MB * 8; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[i / 8][i / 4 % 2][4 * (i % 4) + j] += sums[i * kThreads][j];
     }
     float *out = l.parts ? l.parts + (int64_t)blockIdx.y * a.outputs * a.x.channels : a.dw;
     const int64_t stride = l.parts ? a.x.channels : a.dw_stride;
@@ -323,8 +350,8 @@ static WeightShape shape_of(const tessel_weight_grad &a)
     // where the splits that fill the units keep 2048 tokens (8192 tokens, 2048 x 2048: 111 us, small 131; 2048 tokens: 52, small 46).
     WeightShape s = {256, tiles_of(256), 1};
     if (a.outputs < 8 || (s.tiles < 128 && a.x.tokens * s.tiles < 2048 * 256)) s = {128, tiles_of(128), 1};
-    // splits of the tokens: until 512 workgroups are there (256 of the large tiles), none shorter than 256 tokens
-    const int64_t most = (a.x.tokens + 255) / 256, want = (s.tile == 256 ? 256 : 512) / s.tiles, n = want < most ? want : most;
+    // splits of the tokens: until 256 workgroups are there, none shorter than 256 tokens a group
+    const int64_t least = s.tile == 256 ? 256 : 512, most = (a.x.tokens + least - 1) / least, want = 256 / s.tiles, n = want < most ? want : most;
     s.splits = n < 1 ? 1 : (int)n;
     return s;
 }
@@ -339,12 +366,12 @@ int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stre
     if (l.splits > 1) l.parts = parts;
     void *args[] = {&l};
     const bool large = s.tile == 256, straight = a.outputs % 8 == 0 && a.dy.stride % 8 == 0 && (uintptr_t)a.dy.data % 16 == 0;
-#define KERNEL(T) (a.outputs < 8 ? (const void *)weight_kernel<T, 2, 2, 2, kNarrow> \
-                   : large ? (straight ? (const void *)weight_kernel<T, 2, 4, 4, kStraight> : (const void *)weight_kernel<T, 2, 4, 4, kUneven>) \
-                           : (straight ? (const void *)weight_kernel<T, 2, 2, 2, kStraight> : (const void *)weight_kernel<T, 2, 2, 2, kUneven>))
+#define KERNEL(T) (a.outputs < 8 ? (const void *)weight_kernel<T, 2, 2, 2, kNarrow, 2> \
+                   : large ? (straight ? (const void *)weight_kernel<T, 2, 4, 4, kStraight, 1> : (const void *)weight_kernel<T, 2, 4, 4, kUneven, 1>) \
+                           : (straight ? (const void *)weight_kernel<T, 2, 2, 2, kStraight, 2> : (const void *)weight_kernel<T, 2, 2, 2, kUneven, 2>))
     const void *kernel = a.x.type == TESSEL_BF16 ? KERNEL(bf16) : KERNEL(f16);
 #undef KERNEL
-    int e = launched(hipLaunchKernel(kernel, dim3((unsigned)s.tiles, (unsigned)l.splits), dim3(large ? 512 : 256), args, 0, (hipStream_t)stream));
+    int e = launched(hipLaunchKernel(kernel, dim3((unsigned)s.tiles, (unsigned)l.splits), dim3(512), args, 0, (hipStream_t)stream));
     if (e == 0 && l.parts)
         e = launched(hipLaunchKernel((const void *)weight_sum_kernel, dim3((unsigned)(((int64_t)a.outputs * a.x.channels + 1023) / 1024)), dim3(256), args, 0, (hipStream_t)stream));
     return e;
