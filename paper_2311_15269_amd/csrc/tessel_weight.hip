@@ -121,10 +121,13 @@ struct HeldStage {
     __device__ __forceinline__ void put(uint4v *tile, int rows, int i, int thread) const
     {
         const int r = thread / kChunks + i * kRows, c = 2 * (thread % kChunks);
+        uint4v bytes = v[i];
+        uint32_t exponent = e[i];
+        asm volatile("" : "+v"(bytes), "+v"(exponent));          // (or the compiler takes the bytes apart where it reads them, and waits for them there)
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             float f[8];
-            held8(f, make_uint2(v[i][2 * h], v[i][2 * h + 1]), e[i]);
+            held8(f, make_uint2(bytes[2 * h], bytes[2 * h + 1]), exponent);
             uint4v w;
 #pragma unroll
             for (int j = 0; j < 4; j++) w[j] = pack2<T>(f[2 * j], f[2 * j + 1]);
@@ -176,9 +179,24 @@ __device__ __forceinline__ void read_step(uint4v (&f)[2], uint4v (&g)[2], const 
     for (int b = 0; b < 2; b++) g[b] = join(r[4 + 2 * b], r[5 + 2 * b]);
 }
 
+// A barrier behind this wave's LDS writes.  (The library's waits for all loads from memory too, also those that belong to later tiles.)
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// nothing is moved across, by any pass of the compiler
+__device__ __forceinline__ void in_order()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // WN x WC waves, 32 MB x 64 of dw each, GROUPS times, each group for its share of the workgroup's tokens (two, where tiles are small: with half as many
-// parts in memory as two workgroups would leave)
-template <typename T, int WN, int WC, int MB, int HOW, int GROUPS>
+// parts in memory as two workgroups would leave).  DEPTH: tiles on their way in registers
+template <typename T, int WN, int WC, int MB, int HOW, int GROUPS, int DEPTH>
 __global__ __launch_bounds__(64 * WN * WC * GROUPS, 2) void weight_kernel(WeightLaunch l)
 {
     constexpr int kThreads = 64 * WN * WC, kRows = WN * MB * 32, kColumns = WC * 64, kBuffers = HOW == kStraight ? 3 : 2;
@@ -209,44 +227,63 @@ __global__ __launch_bounds__(64 * WN * WC * GROUPS, 2) void weight_kernel(Weight
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int h = 0; h < 2; h++) gy[2 * b + h] = (uint32_t)(uintptr_t)(lds_tile *)columns[0] + wc / 4 * kPanelSize * 16 + (at.c ^ (64 * (wc % 4 + b) + 32 * h));
-        HeldStage<T, kColumns, kThreads> hs;
-        DyStage<T, HOW == kStraight ? 8 : kRows, HOW == kStraight ? 8 : kThreads, HOW> ds;
+        HeldStage<T, kColumns, kThreads> hs[DEPTH];
+        DyStage<T, HOW == kStraight ? 8 : kRows, HOW == kStraight ? 8 : kThreads, HOW> ds[DEPTH];
+        constexpr int kHeld = hs[0].kPer;
         const int64_t tiles = (end - begin + kSteps - 1) / kSteps;
         auto left = [&](int64_t n) { return (int)min((int64_t)kSteps, end - begin - n * kSteps); };
-        if (tiles > 0) {
-            hs.fetch(a, begin, end, c0, thread);
-            if constexpr (HOW == kStraight) Copy::start(rows[0], a, begin, end, n0, thread);
-            else ds.fetch(a, begin, end, n0, thread);
+        // tile n to stage `stage` of the registers, the rest of it from memory to LDS, and from the registers to LDS
+        auto fetch = [&](int stage, int64_t n) {
+            hs[stage].fetch(a, begin + n * kSteps, end, c0, thread);
+            if constexpr (HOW != kStraight) ds[stage].fetch(a, begin + n * kSteps, end, n0, thread);
+        };
+        auto copy = [&](int64_t n, int to) {
+            if constexpr (HOW == kStraight) Copy::start(rows[to], a, begin + n * kSteps, end, n0, thread);
+        };
+        auto put = [&](int stage, int64_t n) {
 #pragma unroll
-            for (int i = 0; i < hs.kPer; i++) hs.put(columns[0], left(0), i, thread);
-            if constexpr (HOW != kStraight) ds.put(rows[0], left(0), thread);
-        }
-        if (tiles > 1) {
-            hs.fetch(a, begin + kSteps, end, c0, thread);
-            if constexpr (HOW == kStraight) Copy::start(rows[1], a, begin + kSteps, end, n0, thread);
-            else ds.fetch(a, begin + kSteps, end, n0, thread);
-        }
+            for (int i = 0; i < kHeld; i++) hs[stage].put(columns[n & 1], left(n), i, thread);
+            if constexpr (HOW != kStraight) ds[stage].put(rows[n & 1], left(n), thread);
+        };
+        // the first tiles, in this order, on which the waits below count: behind a tile's copies come one tile of the checkpoint and the next
+        // tile's copies
+        auto start = [&](auto more) {
+            constexpr bool MORE = decltype(more)::value != 0;
+            fetch(0, 0);
+            if (DEPTH == 2 && (MORE || tiles > 1)) fetch(1, 1);
+            in_order();
+            copy(0, 0);
+            in_order();
+            put(0, 0);
+            in_order();
+            if (MORE || tiles > DEPTH) fetch(0, DEPTH);
+            in_order();
+            if (MORE || tiles > 1) copy(1, 1);
+            in_order();
+        };
         const int64_t short_one = (to - from) % kSteps ? ((to - from) / kSteps) % share : -1;       // the step of the tile that is not whole
         int buffer = 0;
-        for (int64_t n = 0; n < share; n++) {
-            const int turn = n & 1;
-            // Waits for this tile's copies.  Those of the next one, which were started behind them, and its values of the checkpoint may
-            // still be on their way: as many loads as stand between two calls of sched_barrier below.
+        // One tile.  MORE: all that is to be read behind it is there, so that no read stands in a branch (behind which the compiler would wait for more than
+        // it has to)
+        auto tile = [&](auto stage, auto more, int64_t n) {
+            constexpr int kNext = (decltype(stage)::value + 1) % DEPTH;
+            constexpr bool MORE = decltype(more)::value != 0;
             if constexpr (HOW == kStraight) {
-                if (n + 1 < tiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copy::kPer + 2 * hs.kPer) : "memory");
+                if (MORE || n + DEPTH < tiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copy::kPer + 2 * kHeld) : "memory");
+                else if (DEPTH == 2 && n + 1 < tiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copy::kPer) : "memory");
                 else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                if (n == short_one) {
-                    __syncthreads();                             // (all waves' copies, before zeros go over them)
+                if (!MORE && n == short_one) {
+                    lds_barrier();                               // (all waves' copies, before zeros go over them)
                     if (n < tiles) Copy::clear(rows[buffer], left(n), thread);
                 }
             }
-            __syncthreads();                                     // (this tile is there, and all are done with the one before)
-            if (GROUPS > 1 && n >= tiles) continue;
+            lds_barrier();                                       // (this tile is there, and all are done with the one before)
+            if (!MORE && GROUPS > 1 && n >= tiles) return;
             uint32_t fa[2 * MB], ga[4];
 #pragma unroll
             for (int b = 0; b < 2 * MB; b++) fa[b] = fx[b] + buffer * (kSteps * kRows * 2);
 #pragma unroll
-            for (int b = 0; b < 4; b++) ga[b] = gy[b] + turn * (kSteps * kColumns * 2);
+            for (int b = 0; b < 4; b++) ga[b] = gy[b] + (uint32_t)(n & 1) * (kSteps * kColumns * 2);
             auto step = [&](auto s) {
                 uint4v f[MB], g[2];
                 read_step<decltype(s)::value>(f, g, fa, ga);
@@ -257,24 +294,28 @@ __global__ __launch_bounds__(64 * WN * WC * GROUPS, 2) void weight_kernel(Weight
             };
             step(constant<0>{});
             step(constant<1>{});
-            if (n + 1 < tiles) {
-#pragma unroll
-                for (int i = 0; i < hs.kPer; i++) hs.put(columns[turn ^ 1], left(n + 1), i, thread);
-                if constexpr (HOW != kStraight) ds.put(rows[turn ^ 1], left(n + 1), thread);
-                __builtin_amdgcn_sched_barrier(0);
-                if constexpr (HOW == kStraight) {
-                    if (n + 2 < tiles) Copy::start(rows[buffer >= 1 ? buffer - 1 : 2], a, begin + (n + 2) * kSteps, end, n0, thread);
-                }
-                if (n + 2 < tiles) {
-                    hs.fetch(a, begin + (n + 2) * kSteps, end, c0, thread);
-                    if constexpr (HOW != kStraight) ds.fetch(a, begin + (n + 2) * kSteps, end, n0, thread);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            if (MORE || n + 1 < tiles) put(kNext, n + 1);
+            in_order();
+            if (MORE || n + 1 + DEPTH < tiles) fetch(kNext, n + 1 + DEPTH);
+            in_order();
+            if (MORE || n + 2 < tiles) copy(n + 2, buffer >= 1 ? buffer - 1 : 2);
+            in_order();
             step(constant<2>{});
             step(constant<3>{});
             buffer = buffer == kBuffers - 1 ? 0 : buffer + 1;
+        };
+        int64_t n = 0;
+        if (tiles > 2 * DEPTH) {
+            start(constant<1>{});
+            // (whole tiles alone: the short one is the last of all)
+            for (; n + 2 * DEPTH < tiles; n += DEPTH) unrolled<DEPTH>([&](auto c) { tile(c, constant<1>{}, n + decltype(c)::value); });
+        } else if (tiles > 0) {
+            start(constant<0>{});
         }
+        for (; n < share; n += DEPTH)
+            unrolled<DEPTH>([&](auto c) {
+                if (n + decltype(c)::value < share) tile(c, constant<0>{}, n + decltype(c)::value);
+            });
     }
     if constexpr (GROUPS > 1) {
         static_assert(GROUPS == 2 && sizeof(all_rows) >= sizeof(acc) * kThreads, "one group's sums");
@@ -302,14 +343,26 @@ __global__ __launch_bounds__(64 * WN * WC * GROUPS, 2) void weight_kernel(Weight
         const int c = c0 + 32 * (wc + j) + (lane & 31);
         if (c >= a.x.channels) continue;
 #pragma unroll
-        for (int i = 0; i < MB; i++)
+        for (int i = 0; i < MB; i++) {
+            float *p[16];
+            bool there[16];
 #pragma unroll
             for (int r = 0; r < 16; r++) {
                 const int chunk = n0 + 32 * (wn + i) + 8 * (r / 4), n = chunk_start<HOW>(chunk, a.outputs) + 4 * half + r % 4;
-                if (n >= a.outputs || n < chunk) continue;       // (what a shifted chunk holds of the one before is stored there)
-                float *p = out + n * stride + c;
-                *p = add ? *p + acc[i][j][r] : acc[i][j][r];
+                there[r] = n < a.outputs && n >= chunk;          // (what a shifted chunk holds of the one before is stored there)
+                p[r] = out + (there[r] ? n * stride : 0) + c;
             }
+            if (add) {
+                float v[16];
+#pragma unroll
+                for (int r = 0; r < 16; r++) v[r] = *p[r];       // (all sixteen on their way at once; the first row's where there is none)
+#pragma unroll
+                for (int r = 0; r < 16; r++) acc[i][j][r] += v[r];
+            }
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                if (there[r]) *p[r] = acc[i][j][r];
+        }
     }
 }
 
@@ -366,9 +419,9 @@ int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stre
     if (l.splits > 1) l.parts = parts;
     void *args[] = {&l};
     const bool large = s.tile == 256, straight = a.outputs % 8 == 0 && a.dy.stride % 8 == 0 && (uintptr_t)a.dy.data % 16 == 0;
-#define KERNEL(T) (a.outputs < 8 ? (const void *)weight_kernel<T, 2, 2, 2, kNarrow, 2> \
-                   : large ? (straight ? (const void *)weight_kernel<T, 2, 4, 4, kStraight, 1> : (const void *)weight_kernel<T, 2, 4, 4, kUneven, 1>) \
-                           : (straight ? (const void *)weight_kernel<T, 2, 2, 2, kStraight, 2> : (const void *)weight_kernel<T, 2, 2, 2, kUneven, 2>))
+#define KERNEL(T) (a.outputs < 8 ? (const void *)weight_kernel<T, 2, 2, 2, kNarrow, 2, 1> \
+                   : large ? (straight ? (const void *)weight_kernel<T, 2, 4, 4, kStraight, 1, 1> : (const void *)weight_kernel<T, 2, 4, 4, kUneven, 1, 1>) \
+                           : (straight ? (const void *)weight_kernel<T, 2, 2, 2, kStraight, 2, 2> : (const void *)weight_kernel<T, 2, 2, 2, kUneven, 2, 2>))
     const void *kernel = a.x.type == TESSEL_BF16 ? KERNEL(bf16) : KERNEL(f16);
 #undef KERNEL
     int e = launched(hipLaunchKernel(kernel, dim3((unsigned)s.tiles, (unsigned)l.splits), dim3(512), args, 0, (hipStream_t)stream));
