@@ -323,7 +323,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendLaunch l, t
     if (FORWARD && col == 0) l.a.lse[head * l.tokens + token] = top * l.a.scale + logf(total);
 }
 
-// The power of two that brings `top`, the largest |do| of a row or a sequence's head, into 1..2: in half precision the gradients of the scores are scaled by
+// The power of two that brings `top`, the largest |do| of a row or of 32 queries, into 1..2: in half precision the gradients of the scores are scaled by
 // it before they are rounded, which keeps them in the middle of the type's short range.  1 for bf16, whose range is that of 32 bits.
 template <typename T>
 __device__ __forceinline__ float gradient_scale(float top)
@@ -561,6 +561,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
 {
     __shared__ __attribute__((aligned(256))) uint4v buffers[4][64 * W / 8], values[128 * W / 8];
     __shared__ float4v numbers[2][2][16];                        // - log-sum / scale and - delta of a tile's queries
+    __shared__ float tops[2][2];                                 // (f16) the largest |do| of its two blocks of 32
     int t, kv, split;
     work_of(l.a.kv_heads, l.splits, t, kv, split);
     const AttendTile tile = l.tiles[t];
@@ -582,15 +583,6 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     int from, to;
     share_of(tiles * shared, l.splits, split, from, to);
     if (from == to) return;
-    float grow = 1.0f;
-    if constexpr (__is_same(T, f16)) {
-        float top = 0;
-        for (int head = kv * shared; head < (kv + 1) * shared; head++)
-            for (int i = 32 * lane; i < tile.length; i += 32 * 64) top = fmaxf(top, l.largest[head * l.tokens + tile.begin + i]);
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        grow = gradient_scale<T>(top);
-    }
 
     uint4v k[W / 16], v[W / 16];
     fetch_rows<T, W>(k, row_of<T>(l.a.k, token, kv), valid, dim);
@@ -613,6 +605,22 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
             // (queries behind the sequence's end: a probability of nought)
             if (threadIdx.x < 64) number = r < rows ? -l.a.lse[at] / l.a.scale : -INFINITY;
             else number = r < rows ? -l.delta[at] : 0.0f;
+        } else if (__is_same(T, f16) && threadIdx.x < 130) {
+            const int r = (threadIdx.x & 1) * 32;
+            number = r < rows ? l.largest[head * l.tokens + tile.begin + q0 + r] : 0.0f;
+        }
+    };
+    // In half precision dk is summed in units of 1 / grow, which goes with the blocks of queries: lower where a block has larger gradients,
+    // higher where they are below a quarter of what it is for.  (One scale a sequence loses the others where one query's gradient is 2^14 times theirs.)
+    float grow = 1.0f;
+    auto scale_for = [&](float top) {
+        if (!(top > 0.0f && top < INFINITY)) return;             // (nothing to scale, or nothing that scaling would help)
+        const float next = gradient_scale<T>(top);
+        if (__any(next < grow || next > 4.0f * grow)) {
+            const float by = next / grow;
+#pragma unroll
+            for (int b = 0; b < W / 32; b++) dk[b] *= by;
+            grow = next;
         }
     };
     const Reader<W> at;
@@ -621,6 +629,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     fetch(from);
     for (int n = from; n < to; n++) {
         if (threadIdx.x < 128) ((float *)numbers[n & 1])[threadIdx.x] = number;
+        else if (__is_same(T, f16) && threadIdx.x < 130) tops[n & 1][threadIdx.x & 1] = number;
         copies_arrive();                                         // (tile n has arrived, and all are done with the one before)
         auto copy = [&]() {
             if (n + 1 < to) fetch(n + 1);
@@ -628,12 +637,19 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
         const lds_tile *queries = (const lds_tile *)buffers[2 * (n & 1)], *grads = (const lds_tile *)buffers[2 * (n & 1) + 1];
         const float4v *lses = numbers[n & 1][0], *deltas = numbers[n & 1][1];
         const int before = 32 * wave - n % tiles * 64 - row;     // (this block's queries of which the wave's first key is ahead)
+        if constexpr (__is_same(T, f16)) {
+            if (before <= 31) scale_for(tops[n & 1][row >> 5]);
+        }
         if (before > 31) copy();
         else if (before > -32) dkv_block<T, W, true>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, before + (lane & 31) - 4 * half, copy);
         else dkv_block<T, W, false>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, 0, copy);
     }
     float4v *sums = (float4v *)buffers + wave * (W / 32 * 4 * 64) + lane;
-    const float back = l.a.scale / grow;
+    const float back = l.a.scale;
+    if constexpr (__is_same(T, f16)) {
+#pragma unroll
+        for (int b = 0; b < W / 32; b++) dk[b] *= 1.0f / grow;   // (each wave's own)
+    }
 #pragma unroll
     for (int x = 0; x < 2; x++) {
         float16v *c = x == 0 ? dk : dv;

@@ -121,6 +121,23 @@ def test_sequences_and_heads_keep_their_own_scale(ops):
         assert torch.equal(a[100:, :heads], b[100:, :heads])
 
 
+@pytest.mark.parametrize("token", [0, 31, 127, 128, 2047, 2048, 2499])
+def test_the_largest_gradient_may_be_anywhere(ops, token):
+    """in half precision: one query's gradient 2^14 times the others', which those of the scores must not leave the type's range for.  Rounding
+    probabilities, gradients of the scores and results: 2^-11 each of the largest, six of them at most"""
+    q, k, v, d = inputs(2500, 2, 1, 64, F16, 7)
+    d = d * 2.0 ** -4
+    d[token] *= 2.0 ** 14
+    want, _ = R.attention(q, k, v, [2500], 0.125, d)
+    packing = ops.Packing([2500])
+    gq, gk, gv, gd = (t.cuda() for t in (q, k, v, d))
+    o, lse = packing.attention(gq, gk, gv)
+    for name, got in zip(("dq", "dk", "dv"), packing.attention_backward(gd, gq, gk, gv, o, lse)):
+        got = got.double().cpu()
+        assert bool(got.isfinite().all()), name
+        assert float((got - want[name]).norm()) <= 6 * 2.0 ** -11 * float(want[name].norm()), name
+
+
 def test_strided_views(ops):
     """one tensor of all projections, heads before tokens, keys shared through a stride of nought"""
     lengths, n = [90, 41], 131

@@ -150,6 +150,37 @@ def test_weight_gradient(ops, n, m, c, dtype):
     check_weight(ops, n, m, c, dtype, into=1.5)
 
 
+@pytest.mark.parametrize("m", [5, 7, 8, 9, 104, 131])
+@pytest.mark.parametrize("n", [2, 64, 127, 128, 129, 191, 193, 256, 257, 513, 640, 1025])
+def test_weight_gradient_where_tiles_of_tokens_end(ops, n, m):
+    """outputs of less than a chunk, of whole chunks and of others; tokens that leave the second group of waves nothing, less or as much"""
+    check_weight(ops, n, m, 70, torch.bfloat16)
+    check_weight(ops, n, m, 70, torch.float16, into=-0.5)
+
+
+@pytest.mark.parametrize("n, m, c", [(1, 4096, 2048), (130, 4096, 2050), (130, 4095, 2048), (64, 2051, 4001)])
+def test_weight_gradient_by_large_tiles(ops, n, m, c):
+    check_weight(ops, n, m, c, torch.bfloat16)
+    check_weight(ops, n, m, c, torch.bfloat16, into=0.25)
+
+
+@pytest.mark.parametrize("m", [6, 64, 77])
+@pytest.mark.parametrize("token", [0, 63, 99])
+def test_weight_gradient_of_gradients_that_are_not_finite(ops, m, token):
+    """an output's infinity or NaN reaches its own row and no other"""
+    dy, x = rows(100, m, torch.bfloat16, 1), rows(100, 200, torch.bfloat16, 2)
+    k = ops.checkpoint(x.cuda())
+    want = ops.weight_gradient(dy.cuda(), k)
+    dy[token, m - 1], dy[token, 2] = math.inf, math.nan
+    got = ops.weight_gradient(dy.cuda(), k)
+    held = ops.restore(k)[token].float()
+    assert bool(got[2].isnan().all())
+    signs = torch.where(held == 0, torch.nan, held.sign() * math.inf)
+    assert torch.equal(got[m - 1].nan_to_num(7.0, 8.0, 9.0), signs.nan_to_num(7.0, 8.0, 9.0))
+    others = [i for i in range(m) if i not in (2, m - 1)]
+    assert torch.equal(got[others], want[others])
+
+
 def test_weight_gradient_of_no_tokens(ops):
     k = ops.checkpoint(torch.empty(0, 100, dtype=torch.bfloat16, device="cuda"))
     dy = torch.empty(0, 30, dtype=torch.bfloat16, device="cuda")
