@@ -5,10 +5,10 @@
 // numbers of the matrix instruction's type on its way to LDS, which is exact.  Few tiles: the tokens are split over several
 // workgroups, whose sums a second kernel adds in the order of their numbers.
 //
-// Bound by the matrix instructions, and with them by the clock that they leave: 4096 x 4096 from 8192 tokens of bf16 in 269 us, 1020 TF/s (a
+// Bound by the matrix instructions, and with them by the clock that they leave: 4096 x 4096 from 8192 tokens of bf16 in 248 us, 1110 TF/s (a
 // library product of 16-bit inputs of that shape takes 230 to 285 us, the input first written out in 16 bits not counted).  A wave's
 // 128 x 64 reads six operands from LDS for eight products, so that LDS is not the bound.  Small ones are bound by the time from a tile's
-// reads to its use and by the parts' traffic: 1001 x 715 from 1999 tokens in 25 us.
+// reads to its use and by the parts' traffic: 1001 x 715 from 1999 tokens in 23.5 us, 5 of them the second kernel.
 #include "tessel_rows.h"
 
 namespace tessel {
@@ -399,10 +399,11 @@ struct WeightShape {
 static WeightShape shape_of(const tessel_weight_grad &a)
 {
     auto tiles_of = [&](int64_t n) { return ((a.outputs + n - 1) / n) * ((a.x.channels + n - 1) / n); };
-    // Large tiles read LDS less for each product, small ones fill the compute units with less splitting.  Large where there are 128 of them, or
-    // where the splits that fill the units keep 2048 tokens (8192 tokens, 2048 x 2048: 111 us, small 131; 2048 tokens: 52, small 46).
+    // Large tiles read LDS less for each product, small ones fill the compute units with less splitting.  Large where more than 128 of them fill the units
+    // as they are (1024 tokens, 4096 x 2400: 42 us, small 52), or where the splits that do keep some 1300 tokens (8192 tokens, 2048 x 2048: 104, small 108; 4096
+    // tokens, 3500 x 1500: 78, small 93; but 1024 tokens, 4096 x 2048: 45, small 36; 2048 tokens, 2048 x 2048: 45, small 30).
     WeightShape s = {256, tiles_of(256), 1};
-    if (a.outputs < 8 || (s.tiles < 128 && a.x.tokens * s.tiles < 2048 * 256)) s = {128, tiles_of(128), 1};
+    if (a.outputs < 8 || (s.tiles <= 128 && a.x.tokens * s.tiles < 1280 * 256)) s = {128, tiles_of(128), 1};
     // splits of the tokens: until 256 workgroups are there, none shorter than 256 tokens a group
     const int64_t least = s.tile == 256 ? 256 : 512, most = (a.x.tokens + least - 1) / least, want = 256 / s.tiles, n = want < most ? want : most;
     s.splits = n < 1 ? 1 : (int)n;

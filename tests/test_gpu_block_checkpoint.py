@@ -164,6 +164,11 @@ def test_weight_gradient_by_large_tiles(ops, n, m, c):
     check_weight(ops, n, m, c, torch.bfloat16, into=0.25)
 
 
+@pytest.mark.parametrize("m", [2048, 2050])
+def test_weight_gradient_by_large_tiles_in_splits(ops, m):
+    check_weight(ops, 5300, m, 2048, torch.float16, into=1.0)
+
+
 @pytest.mark.parametrize("m", [6, 64, 77])
 @pytest.mark.parametrize("token", [0, 63, 99])
 def test_weight_gradient_of_gradients_that_are_not_finite(ops, m, token):
