@@ -314,17 +314,28 @@ class Checkpoint:
         tokens, channels = like.shape
         groups = -(-channels // GROUP)
         self.tokens, self.channels, self.dtype, self.device = tokens, channels, like.dtype, like.device
-        self.values = like.new_empty((tokens, groups * GROUP), dtype=torch.int8)
-        self.exponents = like.new_empty((tokens, groups), dtype=torch.uint8)
-        self._words = (self.values.data_ptr(), self.exponents.data_ptr(), groups * GROUP, groups, tokens, channels, _type(like))
+        # (one tensor for both: half the time of two)
+        self._room = like.new_empty((tokens * groups * (GROUP + 1),), dtype=torch.uint8)
+        self._groups, self._at = groups, like.get_device()
+        first = self._room.data_ptr()
+        self._words = (first, first + tokens * groups * GROUP, groups * GROUP, groups, tokens, channels, _type(like))
         self._desc = CheckpointDesc(*self._words)
 
     @property
+    def values(self):
+        import torch
+        return self._room[:self.tokens * self._groups * GROUP].view(torch.int8).view(self.tokens, self._groups * GROUP)
+
+    @property
+    def exponents(self):
+        return self._room[self.tokens * self._groups * GROUP:].view(self.tokens, self._groups)
+
+    @property
     def nbytes(self):
-        return self.values.numel() + self.exponents.numel()
+        return self._room.numel()
 
     def _like(self, t):
-        if not t.is_cuda or t.dtype is not self.dtype or t.shape != (self.tokens, self.channels) or t.get_device() != self.values.get_device():
+        if not t.is_cuda or t.dtype is not self.dtype or t.shape != (self.tokens, self.channels) or t.get_device() != self._at:
             _refuse("expected %s [%d, %d] on %s, got %s %s" % (self.dtype, self.tokens, self.channels, self.device, t.dtype, tuple(t.shape)))
 
 
@@ -344,7 +355,7 @@ def checkpoint(x):
 
 def restore(c):
     """tessel_checkpoint_restore: what a checkpoint stands for, in the type of what was stored"""
-    x = c.values.new_empty((c.tokens, c.channels), dtype=c.dtype)
+    x = c._room.new_empty((c.tokens, c.channels), dtype=c.dtype)
     rows = Rows(x.data_ptr(), c.channels)
     binding._check(_library().tessel_checkpoint_restore(C.byref(c._desc), C.byref(rows), _stream(x)))
     return x
@@ -386,7 +397,7 @@ def weight_gradient(dy, x, into=None):
     to `into` (and that returned) if it is given"""
     import torch
     lib = _library()
-    if dy.dim() != 2 or not dy.is_cuda or dy.get_device() != x.values.get_device() or dy.dtype is not x.dtype or dy.shape[0] != x.tokens:
+    if dy.dim() != 2 or not dy.is_cuda or dy.get_device() != x._at or dy.dtype is not x.dtype or dy.shape[0] != x.tokens:
         _refuse("dy %s %s does not go with a checkpoint of %s [%d, %d]" % (dy.dtype, tuple(dy.shape), x.dtype, x.tokens, x.channels))
     shape = (dy.shape[1], x.channels)
     if into is None:
