@@ -323,19 +323,27 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendLaunch l, t
     if (FORWARD && col == 0) l.a.lse[head * l.tokens + token] = top * l.a.scale + logf(total);
 }
 
-// The power of two that brings `top`, the largest |do| of a row or of 32 queries, into 1..2: in half precision the gradients of the scores are scaled by
-// it before they are rounded, which keeps them in the middle of the type's short range.  1 for bf16, whose range is that of 32 bits.
-template <typename T>
-__device__ __forceinline__ float gradient_scale(float top)
+// In half precision the gradients of the scores are rounded in units of their own, 1 / grow, and what is summed from them with it: a lane of either kernel
+// below has the scores of one query (key), so it keeps the unit that its largest gradient so far needs.  `top`: the largest of a block of 32 scores.
+// Where it would pass 2^15, the unit goes to where it is 2^8: what is 2^-22 of the largest still has all of the type's bits.  The first
+// block sets it, as grow starts where nothing fits.  (The sizes of do and v together say nothing of do . v - delta, let alone of one key's.)
+template <int N>
+__device__ __forceinline__ void fit(float top, float &grow, float16v *sums)
 {
-    if (__is_same(T, bf16) || !(top > 0.0f && top < INFINITY)) return 1.0f;
-    return __uint_as_float((254u << 23) - (__float_as_uint(top) & 0x7F800000u));
+    top = max_of_halves(top);
+    const bool over = top * grow > 0x1p15f && top < INFINITY;
+    if (!__any(over)) return;
+    const float next = over ? __uint_as_float((262u << 23) - (__float_as_uint(top) & 0x7F800000u)) : grow, by = next / grow;
+    grow = next;
+#pragma unroll
+    for (int b = 0; b < N; b++) sums[b] *= by;
 }
+template <typename T>
+__device__ __forceinline__ constexpr float first_grow() { return __is_same(T, f16) ? 0x1p126f : 1.0f; }
 
 // The gradient of q: three products (scores, do v, and their gradients times k), one operand from LDS for each.  The documents above: 247 us, 830
 // TF/s.  (It and the kernel of dk and dv both compute the scores, seven products instead of five: one kernel for all three gradients would add
-// to dq from many workgroups, in no fixed order.)  Also, for the kernel behind it delta_i = sum_d do_i o_i and in half precision the largest |do| of
-// every 32 queries.
+// to dq from many workgroups, in no fixed order.)  Also, for the kernel behind it, delta_i = sum_d do_i o_i.
 //
 // The first 128 queries of a sequence take delta_i = sum_j p_ij (do_i . v_j) instead, the same sum from the inputs: o is rounded,
 // and where a query sees few keys that error is as large as the one of rounding the gradients of the scores.  (dq and dk of sequences of 1, 17
@@ -371,19 +379,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     fetch_rows<T, W>(g, row_of<T>(l.a.d_o, token, head), valid, dim);
     const float by = l.a.scale * kLog2e;
     const float lse = valid ? l.a.lse[head * l.tokens + token] * kLog2e : 0.0f;
-    float grow = 1.0f;
-    if constexpr (__is_same(T, f16)) {
-        float top = 0;
-#pragma unroll
-        for (int n = 0; n < W / 16; n++)
-#pragma unroll
-            for (int j = 0; j < 8; j++) top = fmaxf(top, fabsf((float)__builtin_bit_cast(V, g[n])[j]));
-        top = max_of_halves(top);
-        grow = gradient_scale<T>(top);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        if (lane == 0 && to == last && wfirst < tile.length) l.largest[head * l.tokens + tile.begin + wfirst] = top;
-    }
     float delta = 0;
     if (tile.tile == 0) {
         uint4v k[W / 16], v[W / 16];
@@ -412,6 +407,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     delta = sum_of_halves(delta);
     if (valid && half == 0 && to == last) l.delta[head * l.tokens + token] = delta;
     float16v dq[W / 32] = {};
+    float grow = first_grow<T>();
 
     const T *kp = row_of<T>(l.a.k, tile.begin, kv), *vp = row_of<T>(l.a.v, tile.begin, kv);
     Reader<W> at;
@@ -451,13 +447,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 #pragma unroll
             for (int i = 0; i < 16; i++) {
                 const float p = __builtin_amdgcn_exp2f(s[i] * by - lse);
-                s[i] = __is_same(T, f16) ? p * (d[i] - delta) * grow : p * (d[i] - delta);
+                s[i] = p * (d[i] - delta);
             }
             if (k0 + 32 * b + 31 > wfirst) {
                 const int seen = query - k0 - 4 * half;
 #pragma unroll
                 for (int i = 0; i < 16; i++)
                     if (32 * b + 8 * (i / 4) + i % 4 > seen) s[i] = 0.0f;
+            }
+            if constexpr (__is_same(T, f16)) {
+                float top = 0;
+#pragma unroll
+                for (int i = 0; i < 16; i++) top = fmaxf(top, fabsf(s[i]));
+                fit<W / 32>(top, grow, dq);
+                s *= grow;
             }
             unrolled<2>([&](auto h) {
                 constexpr int n = decltype(h)::value;
@@ -486,7 +489,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 // the copies of the next tile: behind the first products, as the compiler lets no read of LDS that it places itself pass a copy.
 template <typename T, int W, bool EDGE, typename F>
 __device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_tile *grads, int row, Reader<W> at, const float4v *lses, const float4v *deltas, const uint4v *k,
-                                          const uint4v *values, float16v *dk, float16v *dv, float by, float grow, int before, F &&copy)
+                                          const uint4v *values, float16v *dk, float16v *dv, float by, float &grow, int before, F &&copy)
 {
     constexpr int S = W / 16;                                    // steps a phase, two products each
     const int half = threadIdx.x >> 5 & 1;
@@ -524,8 +527,15 @@ __device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_til
     for (int i = 0; i < 16; i++) {
         float x = __builtin_amdgcn_exp2f(s[i] * by);
         if (EDGE && 8 * (i / 4) + i % 4 < before) x = 0.0f;
-        d[i] *= __is_same(T, f16) ? x * grow : x;
+        d[i] *= x;
         s[i] = x;
+    }
+    if constexpr (__is_same(T, f16)) {
+        float top = 0;
+#pragma unroll
+        for (int i = 0; i < 16; i++) top = fmaxf(top, fabsf(d[i]));
+        fit<W / 32>(top, grow, dk);
+        d *= grow;
     }
 #pragma unroll
     for (int h = 0; h < 2; h++) {
@@ -561,7 +571,6 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
 {
     __shared__ __attribute__((aligned(256))) uint4v buffers[4][64 * W / 8], values[128 * W / 8];
     __shared__ float4v numbers[2][2][16];                        // - log-sum / scale and - delta of a tile's queries
-    __shared__ float tops[2][2];                                 // (f16) the largest |do| of its two blocks of 32
     int t, kv, split;
     work_of(l.a.kv_heads, l.splits, t, kv, split);
     const AttendTile tile = l.tiles[t];
@@ -605,31 +614,15 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
             // (queries behind the sequence's end: a probability of nought)
             if (threadIdx.x < 64) number = r < rows ? -l.a.lse[at] / l.a.scale : -INFINITY;
             else number = r < rows ? -l.delta[at] : 0.0f;
-        } else if (__is_same(T, f16) && threadIdx.x < 130) {
-            const int r = (threadIdx.x & 1) * 32;
-            number = r < rows ? l.largest[head * l.tokens + tile.begin + q0 + r] : 0.0f;
         }
     };
-    // In half precision dk is summed in units of 1 / grow, which goes with the blocks of queries: lower where a block has larger gradients,
-    // higher where they are below a quarter of what it is for.  (One scale a sequence loses the others where one query's gradient is 2^14 times theirs.)
-    float grow = 1.0f;
-    auto scale_for = [&](float top) {
-        if (!(top > 0.0f && top < INFINITY)) return;             // (nothing to scale, or nothing that scaling would help)
-        const float next = gradient_scale<T>(top);
-        if (__any(next < grow || next > 4.0f * grow)) {
-            const float by = next / grow;
-#pragma unroll
-            for (int b = 0; b < W / 32; b++) dk[b] *= by;
-            grow = next;
-        }
-    };
+    float grow = first_grow<T>();
     const Reader<W> at;
     // (a head's last tile may be short: where it comes first or second, nothing has filled the rows behind it yet)
     clear_tiles<4, W, kDkvThreads>(buffers, from % tiles + 2 >= tiles ? 0 : 128, dim);
     fetch(from);
     for (int n = from; n < to; n++) {
         if (threadIdx.x < 128) ((float *)numbers[n & 1])[threadIdx.x] = number;
-        else if (__is_same(T, f16) && threadIdx.x < 130) tops[n & 1][threadIdx.x & 1] = number;
         copies_arrive();                                         // (tile n has arrived, and all are done with the one before)
         auto copy = [&]() {
             if (n + 1 < to) fetch(n + 1);
@@ -637,9 +630,6 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
         const lds_tile *queries = (const lds_tile *)buffers[2 * (n & 1)], *grads = (const lds_tile *)buffers[2 * (n & 1) + 1];
         const float4v *lses = numbers[n & 1][0], *deltas = numbers[n & 1][1];
         const int before = 32 * wave - n % tiles * 64 - row;     // (this block's queries of which the wave's first key is ahead)
-        if constexpr (__is_same(T, f16)) {
-            if (before <= 31) scale_for(tops[n & 1][row >> 5]);
-        }
         if (before > 31) copy();
         else if (before > -32) dkv_block<T, W, true>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, before + (lane & 31) - 4 * half, copy);
         else dkv_block<T, W, false>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, 0, copy);
@@ -648,7 +638,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
     const float back = l.a.scale;
     if constexpr (__is_same(T, f16)) {
 #pragma unroll
-        for (int b = 0; b < W / 32; b++) dk[b] *= 1.0f / grow;   // (each wave's own)
+        for (int b = 0; b < W / 32; b++) dk[b] *= 1.0f / grow;   // (each lane's own)
     }
 #pragma unroll
     for (int x = 0; x < 2; x++) {

@@ -23,7 +23,6 @@ struct AttendLaunch {
     float   *parts;              // their sums, where there are several: [splits][2 dk, dv][heads][tokens][dim] in 32 bits (one for o, dq)
     float   *tops;               // forward: [splits][heads][tokens][2], a query's largest score and its sum of exponentials
     float   *delta;              // [heads][tokens]
-    float   *largest;            // [heads][tokens] (f16): at every 32nd token of a sequence the largest |do| of 32
 };
 
 int attend_splits(int64_t longest, int64_t total, int resident, double step, double bytes);

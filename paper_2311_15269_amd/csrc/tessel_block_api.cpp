@@ -81,11 +81,8 @@ size_t forward_workspace(const tessel_packing *p, const tessel_attention *a)
     return s > 1 ? (size_t)s * p->tokens * a->heads * (a->dim + 2) * sizeof(float) : 0;
 }
 
-// delta (and the largest gradients, f16), then the parts of dq and after them those of dk and dv
-size_t gradient_words(const tessel_packing *p, const tessel_attention *a)
-{
-    return ((size_t)p->tokens * a->heads * (a->type == TESSEL_F16 ? 2 : 1) + 3) / 4 * 4;
-}
+// delta, then the parts of dq and after them those of dk and dv
+size_t gradient_words(const tessel_packing *p, const tessel_attention *a) { return ((size_t)p->tokens * a->heads + 3) / 4 * 4; }
 size_t backward_workspace(const tessel_packing *p, const tessel_attention *a)
 {
     const size_t q = query_splits(p, a), k = key_splits(p, a), row = (size_t)p->tokens * a->dim;
@@ -268,7 +265,6 @@ int tessel_attention_backward(const tessel_packing *p, const tessel_attention *a
     if (!p->table || !workspace_ok(workspace_dev, workspace_bytes, backward_workspace(p, a))) return TESSEL_E_WORKSPACE;
     AttendLaunch l = attend_launch(p, a);
     l.delta = (float *)workspace_dev;
-    l.largest = l.delta + p->tokens * a->heads;
     l.parts = l.delta + gradient_words(p, a);
     l.splits = query_splits(p, a);
     e = launch_attend_dq(l, hip_stream);
