@@ -485,6 +485,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
     for (int b = 0; b < W / 32; b++) put_rows<T>(out, dq[b], b, back, dim);
 }
 
+// In half precision the probabilities for dv are held 2^12 times as large: the type's normal numbers end at 2^-14, and a query that sees 2^16 keys alike
+// gives each 2^-16 (rounded as it is, dv of the last of 200000 tokens is off by 3.5e-3 of its norm).  A probability is 1 at most.
+constexpr float kRaise = 12.0f, kLower = 0x1p-12f;
+
 // What a wave of the kernel below does with a block of 32 queries and its 32 keys.  LDS is read one step ahead of the products.  `copy` starts
 // the copies of the next tile: behind the first products, as the compiler lets no read of LDS that it places itself pass a copy.
 template <typename T, int W, bool EDGE, typename F>
@@ -525,7 +529,7 @@ __device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_til
     copy();
 #pragma unroll
     for (int i = 0; i < 16; i++) {
-        float x = __builtin_amdgcn_exp2f(s[i] * by);
+        float x = __builtin_amdgcn_exp2f(__is_same(T, f16) ? s[i] * by + kRaise : s[i] * by);
         if (EDGE && 8 * (i / 4) + i % 4 < before) x = 0.0f;
         d[i] *= x;
         s[i] = x;
@@ -635,7 +639,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
         else dkv_block<T, W, false>(queries, grads, row, at, lses, deltas, k, mine, dk, dv, by, grow, 0, copy);
     }
     float4v *sums = (float4v *)buffers + wave * (W / 32 * 4 * 64) + lane;
-    const float back = l.a.scale;
+    constexpr float lower = __is_same(T, f16) ? kLower : 1.0f;
     if constexpr (__is_same(T, f16)) {
 #pragma unroll
         for (int b = 0; b < W / 32; b++) dk[b] *= 1.0f / grow;   // (each lane's own)
@@ -658,8 +662,8 @@ __global__ __launch_bounds__(kDkvThreads, 2) void attend_dkv_kernel(AttendLaunch
             for (int b = 0; b < W / 32; b++) {
 #pragma unroll
                 for (int i = 0; i < 16; i++) c[b][i] += sums[(4 * b + i / 4) * 64][i % 4];
-                if (l.splits > 1) put_part(part, c[b], b, x == 0 ? back : 1.0f, dim);
-                else put_rows<T>(out, c[b], b, x == 0 ? back : 1.0f, dim);
+                if (l.splits > 1) put_part(part, c[b], b, x == 0 ? l.a.scale * lower : lower, dim);
+                else put_rows<T>(out, c[b], b, x == 0 ? l.a.scale * lower : lower, dim);
             }
         }
     }

@@ -127,3 +127,16 @@ def test_gradients_that_are_not_finite_stay_in_their_sequence(ops):
     assert torch.equal(dq[:130], want[0][:130]) and torch.equal(dq[131:], want[0][131:]) and bool(dq[130, :2].isnan().all())
     for a, b in ((dk, want[1]), (dv, want[2])):
         assert torch.equal(a[:, 1], b[:, 1]) and bool(a[100:131, 0].isnan().all())
+
+
+def test_probabilities_of_very_many_keys(ops):
+    """queries that see 2^17 keys alike: probabilities of 2^-17 are rounded to as many bits as larger ones.  q = 0, so p = 1 / (i + 1); of dv, which
+    is rounded twice, the last keys"""
+    n, first = 200000, 1 << 17
+    gen = torch.Generator().manual_seed(26)
+    k, v = normal(gen, n, 1, 8).to(F16), normal(gen, n, 1, 8).to(F16)
+    d = (2.0 ** 10 * normal(gen, n, 1, 8)).to(F16)
+    got = gradients(ops, torch.zeros(n, 1, 8, dtype=F16), k, v, d, [n])["dv"]
+    terms = d.double() / torch.arange(1, n + 1, dtype=torch.float64)[:, None, None]
+    want = terms.flip(0).cumsum(0).flip(0)
+    near({"dv": got[first:]}, {"dv": want[first:]}, ("dv",), 2 * 2.0 ** -11 + 2.0 ** -16)
