@@ -41,11 +41,12 @@ class Stage:
 
     # -- one product and the two of its backward pass
     def _add(self, name, dy, x):
-        """the gradient of weight `name` from dy and its input, as it was kept"""
+        """the gradient of weight `name` from dy and its input, as it was kept: products of 16 bits, summed and left in 32"""
+        import torch
         if isinstance(x, block_ops.Checkpoint):
             block_ops.weight_gradient(dy, x, into=self.gradients[name])
         else:
-            self.gradients[name] += (dy.t() @ x).float()
+            self.gradients[name] += torch.mm(dy.t(), x, out_dtype=torch.float32)
 
     def _keep(self, x):
         return block_ops.checkpoint(x) if self.small else x
