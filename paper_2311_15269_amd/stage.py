@@ -2,18 +2,30 @@
 
 `Stage` is one layer -- attention over packed sequences and a gated block inside, each between the norms around it -- whose
 forward and backward passes are made of block_ops and plain matrix products.  It keeps its inputs to the products in 8 bits
-(or, for comparison, everything in 16), which is the activation memory m of its blocks.  `plan` measures t and m of its blocks,
+(or, for comparison, everything in 16, with the gated activation by torch's own operations), which is the activation memory m of its blocks.  `plan` measures t and m of its blocks,
 searches the best window under a memory cap and completes it; `run` executes the blocks of that schedule on one GPU, every
 simulated device holding a stage of its own, and sums the weights' gradients over the micro-batches.
 
     python -m paper_2311_15269_amd.stage            (needs an MI355X)
 """
 import argparse
+import math
 import time
 
 from . import block_ops
 from .binding import search
 from .workloads import linear_placement, pipeline_problem
+
+
+def _activation(kind, z):
+    """an activation of 32-bit numbers and its derivative (formulas: include/tessel_block_ops.h)"""
+    import torch
+    if kind == "silu":
+        s = torch.sigmoid(z)
+        return z * s, s * (1 + z * (1 - s))
+    root, cube = (2 / math.pi) ** 0.5, 0.044715
+    t = torch.tanh(root * (z + cube * z * z * z))
+    return 0.5 * z * (1 + t), 0.5 * (1 + t) + 0.5 * (1 - t * t) * z * root * (1 + 3 * cube * (z * z).clamp(max=1e6))
 
 
 class Stage:
@@ -51,6 +63,20 @@ class Stage:
     def _keep(self, x):
         return block_ops.checkpoint(x) if self.small else x
 
+    def _gated(self, g, u):
+        """act(g) u, and g and u as they are kept"""
+        if self.small:
+            return block_ops.gated(g, u, self.act)
+        return (_activation(self.act, g.float())[0] * u.float()).to(g.dtype), g, u
+
+    def _gated_backward(self, da, g, u):
+        """gradients of g and u from those of act(g) u, and that once more"""
+        if self.small:
+            return block_ops.gated_backward(da, g, u, self.act, with_output=True)
+        f, slope = _activation(self.act, g.float())
+        d, w = da.float(), u.float()
+        return tuple(t.to(da.dtype) for t in (d * w * slope, d * f, f * w))
+
     def _norm(self, i, x, y):
         n = self.norms[i]
         return block_ops.residual_norm(x, y, n["pre"], n["post"], n["gate"], self.scale)
@@ -68,11 +94,7 @@ class Stage:
         o, lse = packing.attention(q, k, v)
         y = o.view(n, -1) @ w["out"].t()
         r, hr, stats = self._norm(0, x, y)
-        g, u = hr @ w["gate"].t(), hr @ w["up"].t()
-        if self.small:
-            a, g, u = block_ops.gated(g, u, self.act)           # (g and u from here on: their checkpoints)
-        else:
-            a = block_ops.gated(g, u, self.act)[0]
+        a, g, u = self._gated(hr @ w["gate"].t(), hr @ w["up"].t())
         z = a @ w["down"].t()
         r2, h2, stats2 = self._norm(1, r, z)
         self.kept[number] = (packing, x, self._keep(h), qkv, o, lse, y, stats, r, self._keep(hr), g, u, z, stats2)
@@ -84,9 +106,7 @@ class Stage:
         w, n = self.weights, x.shape[0]
         dr, dz = self._norm_backward(1, dr, dh, r, z, stats2)
         da = dz @ w["down"]
-        if not self.small:
-            g, u = block_ops.checkpoint(g), block_ops.checkpoint(u)
-        dg, du, a = block_ops.gated_backward(da, g, u, self.act, with_output=True)
+        dg, du, a = self._gated_backward(da, g, u)
         self._add("down", dz, a)
         self._add("gate", dg, hr)
         self._add("up", du, hr)

@@ -1,4 +1,4 @@
-"""What a transformer stage promises of itself: gradients of all weights summed in 32 bits."""
+"""What a transformer stage promises of itself: gradients of all weights summed in 32 bits, no 8 bits where it keeps 16."""
 import pytest
 import torch
 
@@ -39,3 +39,34 @@ def test_all_gradients_of_weights_are_sums_in_32_bits(stage, small):
     for name, g in s.gradients.items():
         off = (g.double().cpu() - want[name]).abs() - (n + 16) * 2.0 ** -24 * size[name]
         assert g.dtype == torch.float32 and float(off.max()) <= 0.0, (name, float(off.max()))
+
+
+def test_a_stage_of_16_bits_holds_nothing_in_8(stage, monkeypatch):
+    from paper_2311_15269_amd import block_ops
+    (s,), (packing,), (x,), (h,) = stage.make(1, 1, LENGTHS, 128, 4, 2, 256, False, seed=5)
+
+    def refuse(*args, **more):
+        raise AssertionError("8 bits")
+    for name in ("checkpoint", "gated", "gated_backward", "weight_gradient"):
+        monkeypatch.setattr(block_ops, name, refuse)
+    r, hr = s.forward(0, packing, x, h)
+    assert not any(isinstance(t, block_ops.Checkpoint) for t in s.kept[0])
+    s.backward(0, r, hr)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_the_gated_part_of_a_stage_of_16_bits(stage, act):
+    """the activation and its gradients from g and u as they are, rounded once each: 2^-8 of the value, and 1e-5 of the factors' sizes for 32 bits"""
+    (s,), (packing,), (x,), (h,) = stage.make(1, 1, LENGTHS, 128, 4, 2, 256, False, seed=6)
+    s.act = act
+    gen = torch.Generator().manual_seed(7)
+    g, u, da = (torch.randn(50, 256, generator=gen).bfloat16() for _ in range(3))
+    x, y = g.double().requires_grad_(), u.double().requires_grad_()
+    f = torch.nn.functional.silu(x) if act == "silu" else torch.nn.functional.gelu(x, approximate="tanh")
+    a = f * y
+    wg, wu = torch.autograd.grad(a, [x, y], da.double())
+    got = (s._gated(g.cuda(), u.cuda())[0], *s._gated_backward(da.cuda(), g.cuda(), u.cuda())[:2])
+    for p, q in zip(got, (a.detach(), wg, wu)):
+        assert p.dtype == torch.bfloat16
+        off = (p.double().cpu() - q).abs() - 2.0 ** -8 * q.abs() - 1e-5 * (1 + g.double().abs()) ** 2 * (1 + u.double().abs()) * (1 + da.double().abs())
+        assert float(off.max()) <= 0.0
