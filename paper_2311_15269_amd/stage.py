@@ -120,9 +120,9 @@ class Stage:
         return dx, dqkv @ w["qkv"]
 
     def kept_bytes(self, number):
-        """what a forward pass keeps beyond its arguments: m of its block"""
-        x = self.kept[number][1]
-        return sum(t.nbytes for t in self.kept[number] if hasattr(t, "nbytes") and t is not x)
+        """what a forward pass keeps until its backward pass: m of its block.  (The residual stream that it was given too: the stage that made it does not
+        keep it.)"""
+        return sum(t.nbytes for t in self.kept[number] if hasattr(t, "nbytes"))
 
 
 def measure(stage, packing, x, h):

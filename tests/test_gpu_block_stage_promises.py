@@ -1,4 +1,5 @@
-"""What a transformer stage promises of itself: gradients of all weights summed in 32 bits, no 8 bits where it keeps 16."""
+"""What a transformer stage promises of itself: gradients of all weights summed in 32 bits, no 8 bits where it keeps 16, and the bytes that it
+holds between forward and backward."""
 import pytest
 import torch
 
@@ -70,3 +71,20 @@ def test_the_gated_part_of_a_stage_of_16_bits(stage, act):
         assert p.dtype == torch.bfloat16
         off = (p.double().cpu() - q).abs() - 2.0 ** -8 * q.abs() - 1e-5 * (1 + g.double().abs()) ** 2 * (1 + u.double().abs()) * (1 + da.double().abs())
         assert float(off.max()) <= 0.0
+
+
+@pytest.mark.parametrize("small", [True, False])
+def test_kept_bytes_are_what_the_stage_holds(stage, small):
+    """all that stays on the GPU from a forward pass to its backward pass, its input of the residual stream among it (the stage before does not
+    keep that): against what the allocator has given away, which rounds each of some twenty tensors up to 512 bytes"""
+    (s,), (packing,), (x,), (h,) = stage.make(1, 1, LENGTHS, 128, 4, 2, 256, small, seed=8)
+    s.backward(0, *s.forward(0, packing, x, h))                 # (what libraries keep for themselves is there now)
+    torch.cuda.synchronize()
+    empty = torch.cuda.memory_allocated()
+    x2, h2 = x.clone(), h.clone()
+    out = s.forward(1, packing, x2, h2)
+    del x2, h2, out
+    torch.cuda.synchronize()
+    held = torch.cuda.memory_allocated() - empty
+    assert held - 20 * 512 <= s.kept_bytes(1) <= held
+    s.backward(1, x, h)
