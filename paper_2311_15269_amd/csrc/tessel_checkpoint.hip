@@ -79,8 +79,8 @@ __device__ __forceinline__ float activation(float z, float &slope)
         const float root = 0.7978845608028654f, cube = 0.044715f;
         // tanh(w) = 1 - 2 / (1 + exp(2 w)); half of 1 + tanh is s = 1 / (1 + exp(-2 w))
         const float s = logistic<T>(2.0f * root * (z + cube * z * z * z));
-        // (s (1 - s) is nought long before the square leaves 32 bits)
-        slope = s + 2.0f * z * s * (1.0f - s) * root * (1.0f + 3.0f * cube * fminf(z * z, 1e6f));
+        // (s (1 - s) is nought long before the square leaves 32 bits, and z s is z at most, where 2 z may be infinite)
+        slope = s + z * s * (1.0f - s) * (2.0f * root) * (1.0f + 3.0f * cube * fminf(z * z, 1e6f));
         return z * s;
     }
 }
