@@ -4,7 +4,8 @@ the backward pass.
 
 Tensors are torch's, on the GPU; every call runs on torch's current stream and allocates its outputs and workspace there
 (a tensor that another stream wrote is the caller's to wait for, as with torch's own operators).  There is no CPU fallback.
-Nothing here records torch's automatic differentiation: forward and backward are two calls.
+Nothing here records torch's automatic differentiation: forward and backward are two calls, and a tensor that requires a gradient is
+refused while torch records (under torch.no_grad(), and in the passes of a torch.autograd.Function, it is taken as it is).
 """
 import ctypes as C
 import math
@@ -113,6 +114,12 @@ def _stream(t):
     return torch.cuda.current_stream(t.device).cuda_stream if raw is None else raw(t.get_device())
 
 
+def _refuse_gradient(t):
+    import torch
+    if torch.is_grad_enabled():
+        _refuse("a tensor of shape %s requires a gradient, which no operator here records: detach it or call under torch.no_grad()" % (tuple(t.shape),))
+
+
 _TYPES = {}
 
 
@@ -132,6 +139,8 @@ def _same(like, shape, *tensors):
     for t in tensors:
         if not t.is_cuda or t.dtype is not dtype or t.shape != shape or t.get_device() != at:
             _refuse("expected a %s tensor of shape %s on %s, got %s %s on %s" % (like.dtype, tuple(shape), like.device, t.dtype, tuple(t.shape), t.device))
+        if t.requires_grad:
+            _refuse_gradient(t)
 
 
 def _heads(t):
@@ -155,6 +164,8 @@ def _rows(t):
 def _vector(t, channels, like):
     if _type(t) != 2 or t.shape != (channels,) or not t.is_contiguous() or t.get_device() != like.get_device():
         _refuse("expected %d contiguous 32-bit numbers on %s, got %s %s" % (channels, like.device, t.dtype, tuple(t.shape)))
+    if t.requires_grad:
+        _refuse_gradient(t)
     return t.data_ptr()
 
 
@@ -337,11 +348,15 @@ class Checkpoint:
     def _like(self, t):
         if not t.is_cuda or t.dtype is not self.dtype or t.shape != (self.tokens, self.channels) or t.get_device() != self._at:
             _refuse("expected %s [%d, %d] on %s, got %s %s" % (self.dtype, self.tokens, self.channels, self.device, t.dtype, tuple(t.shape)))
+        if t.requires_grad:
+            _refuse_gradient(t)
 
 
 def _new_checkpoint(x):
     if x.dim() != 2 or not x.is_cuda:
         _refuse("expected [tokens, channels] on the GPU")
+    if x.requires_grad:
+        _refuse_gradient(x)
     return Checkpoint(x)
 
 
@@ -399,6 +414,8 @@ def weight_gradient(dy, x, into=None):
     lib = _library()
     if dy.dim() != 2 or not dy.is_cuda or dy.get_device() != x._at or dy.dtype is not x.dtype or dy.shape[0] != x.tokens:
         _refuse("dy %s %s does not go with a checkpoint of %s [%d, %d]" % (dy.dtype, tuple(dy.shape), x.dtype, x.tokens, x.channels))
+    if dy.requires_grad:
+        _refuse_gradient(dy)
     shape = (dy.shape[1], x.channels)
     if into is None:
         dw = dy.new_empty(shape, dtype=torch.float32)
@@ -406,6 +423,8 @@ def weight_gradient(dy, x, into=None):
         dw = into
         if dw.dtype is not torch.float32 or dw.shape != shape or dw.get_device() != dy.get_device() or (shape[1] > 1 and dw.stride(1) != 1):
             _refuse("the sum has to be 32-bit %s on %s" % (shape, dy.device))
+        if dw.requires_grad:
+            _refuse_gradient(dw)
     a = _FlatWeight(*x._words, *_rows(dy), shape[0], 0 if into is None else 1, dw.data_ptr(), dw.stride(0) if shape[0] > 1 else shape[1])
     n = C.c_size_t()
     binding._check(lib.tessel_weight_gradient_workspace_bytes(C.byref(a), C.byref(n)))
