@@ -399,6 +399,8 @@ def gated_backward(da, kg, ku, act="silu", with_output=False):
     """tessel_gated_backward: (dg, du), or (dg, du, a) with the checkpoints' own act(g) u"""
     kind = _act(act)
     kg._like(da)
+    if ku._at != kg._at:
+        _refuse("checkpoints on %s and %s" % (kg.device, ku.device))
     outs = [_like(da) for _ in range(3 if with_output else 2)]
     rows = [Rows(t.data_ptr(), kg.channels) for t in outs]
     d = Rows(*_rows(da))
