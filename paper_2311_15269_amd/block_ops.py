@@ -21,6 +21,7 @@ EXPORTS = (
 )
 
 E_INVALID_ARG = -1
+E_TOOBIG = -4
 E_UNSUPPORTED = -9
 GROUP = 64
 ACT = {"silu": 0, "gelu": 1}
@@ -103,6 +104,12 @@ def _library():
 
 def _refuse(text):
     raise binding.TesselError(E_INVALID_ARG, text)
+
+
+def _fits(*sizes):
+    """the structures' 32-bit fields take a number's low bits without a word"""
+    if max(sizes) > 0x7FFFFFFF:
+        raise binding.TesselError(E_TOOBIG, "%d does not fit 32 bits" % max(sizes))
 
 
 def _stream(t):
@@ -189,6 +196,9 @@ class Packing:
         lib = _library()
         self.lengths = [int(n) for n in lengths]
         self.tokens = sum(self.lengths) if total_tokens is None else int(total_tokens)
+        if min(self.lengths, default=0) < 0:
+            _refuse("a length of %d" % min(self.lengths))
+        _fits(0, *self.lengths)
         array = (C.c_int32 * max(1, len(self.lengths)))(*self.lengths)
         h = C.c_void_p()
         binding._check(lib.tessel_packing_create(array, len(self.lengths), self.tokens, C.byref(h)))
@@ -215,6 +225,7 @@ class Packing:
         if q.dim() != 3 or k.dim() != 3 or q.device != self._table.device:
             _refuse("expected [tokens, heads, dim] on %s" % self._table.device)
         heads, kv_heads, dim = q.shape[1], k.shape[1], q.shape[2]
+        _fits(heads, kv_heads, dim)
         _same(q, (self.tokens, heads, dim), q)
         _same(q, (self.tokens, kv_heads, dim), k, v)
         if stream != self._made_on:                         # (the table must not be given away while that stream still reads it)
@@ -255,8 +266,9 @@ class Packing:
 def _describe_norm(x, y, pre, post, gate, scale, eps):
     if x.dim() != 2:
         _refuse("expected [tokens, channels]")
-    _same(x, x.shape, x, y)
     n, c = x.shape
+    _fits(c)
+    _same(x, x.shape, x, y)
     if gate is None:
         kind, at = GATE_NONE, (None, 0)
     elif gate.dim() == 1:
@@ -323,6 +335,7 @@ class Checkpoint:
         """room for a tensor like this one"""
         import torch
         tokens, channels = like.shape
+        _fits(channels)
         groups = -(-channels // GROUP)
         self.tokens, self.channels, self.dtype, self.device = tokens, channels, like.dtype, like.device
         # (one tensor for both: half the time of two)
@@ -419,6 +432,7 @@ def weight_gradient(dy, x, into=None):
     if dy.requires_grad:
         _refuse_gradient(dy)
     shape = (dy.shape[1], x.channels)
+    _fits(*shape)
     if into is None:
         dw = dy.new_empty(shape, dtype=torch.float32)
     else:
