@@ -17,7 +17,7 @@
 
 namespace tessel {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kAttendThreads;
 constexpr int kAhead = 4;        // operands that are read from LDS ahead of their products
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -284,7 +284,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
 // Joins the parts of the forward pass (FORWARD: sums of exponentials that each go by their own largest score) or adds up those of gradients,
 // in the order of the splits.  Eight rows a workgroup, 32 lanes of four columns each.  blockIdx.y: of the two arrays that a part of dk and
 // dv holds one behind the other; steps_by: heads on a key, `turned`: tiles of keys (see attend_dkv_kernel).
-constexpr int kJoinRows = 8;
 template <typename T, bool FORWARD>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendLaunch l, tessel_heads first_out, tessel_heads second_out, int heads, int steps_by, bool turned)
 {
@@ -561,8 +560,6 @@ __device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_til
         for (int b = 0; b < W / 32; b++) dk[b] = mma<T>(x[b], e[h], dk[b]);
     });
 }
-
-constexpr int kDkvThreads = 512;
 
 // The gradients of k and v: four products, and five operands from LDS for them, as registers hold the sums of both (128), the keys' operands (32) and
 // the scores' (32), but not the values'.  LDS bounds it: the documents above take 399 us, 690 TF/s.  (One wave on a SIMD with twice the registers:

@@ -13,6 +13,8 @@ struct AttendTile {
     int32_t begin, length, tile, tiles;
 };
 constexpr int kAttendRows = 128;
+constexpr int kAttendThreads = 256, kDkvThreads = 512;   // of a workgroup over queries, over keys
+constexpr int kJoinRows = 8;                             // that a workgroup joins of its splits
 
 struct AttendLaunch {
     tessel_attention a;
@@ -41,6 +43,8 @@ int launch_gated(int act, const tessel_rows &g, const tessel_rows &u, const tess
 int launch_gated_backward(int act, const tessel_rows &da, const tessel_checkpoint &kg, const tessel_checkpoint &ku,
                           const tessel_rows &dg, const tessel_rows &du, const tessel_rows &a, void *stream);
 
+constexpr int kWeightThreads = 512;
+int64_t weight_tiles(const tessel_weight_grad &a);
 int weight_parts(const tessel_weight_grad &a);
 int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stream);
 

@@ -28,7 +28,7 @@ int hip_result(int e)
     return TESSEL_E_HIP;
 }
 
-constexpr int64_t kMostBlocks = INT32_MAX;
+constexpr int64_t kMostThreads = UINT32_MAX;         // of a launch
 constexpr int64_t kMostStride = (int64_t)1 << 40;    // (elements; a product with a token's number stays far inside 64 bits)
 
 constexpr int64_t kMostNear = (int64_t)1 << 24;      // (where a kernel takes 32-bit offsets over 64 rows)
@@ -50,7 +50,7 @@ int attention_ok(const tessel_packing *p, const tessel_attention *a)
     if (!p || !a || a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->dim < 1) return TESSEL_E_INVALID_ARG;
     if (!(a->scale >= 0x1p-100f && a->scale <= 0x1p100f)) return TESSEL_E_INVALID_ARG;        // (the kernels divide by it)
     if ((a->type != TESSEL_BF16 && a->type != TESSEL_F16) || a->dim % 8 || a->dim > 128) return TESSEL_E_UNSUPPORTED;
-    if ((int64_t)p->tiles.size() * a->heads > kMostBlocks) return TESSEL_E_TOOBIG;           // (splits: of small launches only)
+    if ((int64_t)p->tiles.size() > kMostThreads / kAttendThreads / a->heads) return TESSEL_E_TOOBIG;
     return TESSEL_OK;
 }
 
@@ -73,6 +73,23 @@ int query_splits(const tessel_packing *p, const tessel_attention *a)
 int key_splits(const tessel_packing *p, const tessel_attention *a)
 {
     return attend_splits(p->longest * (a->heads / a->kv_heads), p->steps * a->heads, 256, 2.6, 8.0 * p->tokens * a->kv_heads * a->dim);
+}
+
+// whether launches over all tiles for `heads` heads in so many splits hold their threads, that which joins the splits among them
+bool launchable(const tessel_packing *p, int heads, int splits, int threads)
+{
+    const int64_t blocks = (int64_t)p->tiles.size() * heads;      // (2^24 at most: attention_ok)
+    return blocks * splits <= kMostThreads / threads && (splits == 1 || blocks * (kAttendRows / kJoinRows) <= kMostThreads / kAttendThreads);
+}
+int forward_ok(const tessel_packing *p, const tessel_attention *a)
+{
+    const int e = attention_ok(p, a);
+    return e == TESSEL_OK && !launchable(p, a->heads, query_splits(p, a), kAttendThreads) ? TESSEL_E_TOOBIG : e;
+}
+int backward_ok(const tessel_packing *p, const tessel_attention *a)
+{
+    const int e = forward_ok(p, a);
+    return e == TESSEL_OK && !launchable(p, a->kv_heads, key_splits(p, a), kDkvThreads) ? TESSEL_E_TOOBIG : e;
 }
 
 size_t forward_workspace(const tessel_packing *p, const tessel_attention *a)
@@ -134,7 +151,7 @@ int weight_ok(const tessel_weight_grad *a)
     const int e = checkpoint_ok(&a->x);
     if (e) return e;
     if (a->x.type == TESSEL_F32) return TESSEL_E_UNSUPPORTED;
-    if ((int64_t)((a->outputs + 127) / 128) * ((a->x.channels + 127) / 128) > kMostBlocks) return TESSEL_E_TOOBIG;
+    if (weight_tiles(*a) > kMostThreads / kWeightThreads / weight_parts(*a)) return TESSEL_E_TOOBIG;
     if (a->outputs > kMostNear || a->dy.stride > kMostNear || a->x.value_stride > kMostNear || a->x.exponent_stride > kMostNear) return TESSEL_E_TOOBIG;
     if (!a->dw || !aligned(a->dw, 4) || a->dw_stride < a->x.channels || a->dw_stride > kMostStride) return TESSEL_E_INVALID_ARG;
     return rows_ok(a->dy, a->x.type, a->x.tokens, a->outputs, false) ? TESSEL_OK : TESSEL_E_INVALID_ARG;
@@ -223,7 +240,7 @@ int tessel_packing_bind(tessel_packing *p, void *table_dev, size_t table_bytes, 
 int tessel_attention_forward_workspace_bytes(const tessel_packing *p, const tessel_attention *a, size_t *bytes)
 {
     if (!bytes) return TESSEL_E_INVALID_ARG;
-    const int e = attention_ok(p, a);
+    const int e = forward_ok(p, a);
     if (e) return e;
     *bytes = forward_workspace(p, a);
     return TESSEL_OK;
@@ -231,7 +248,7 @@ int tessel_attention_forward_workspace_bytes(const tessel_packing *p, const tess
 
 int tessel_attention_forward(const tessel_packing *p, const tessel_attention *a, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
 {
-    int e = attention_ok(p, a);
+    int e = forward_ok(p, a);
     if (e) return e;
     if (p->tokens == 0) return TESSEL_OK;
     if (!heads_ok(a->q, false, a->heads, a->dim) || !heads_ok(a->k, false, a->kv_heads, a->dim) || !heads_ok(a->v, false, a->kv_heads, a->dim) ||
@@ -247,7 +264,7 @@ int tessel_attention_forward(const tessel_packing *p, const tessel_attention *a,
 int tessel_attention_backward_workspace_bytes(const tessel_packing *p, const tessel_attention *a, size_t *bytes)
 {
     if (!bytes) return TESSEL_E_INVALID_ARG;
-    const int e = attention_ok(p, a);
+    const int e = backward_ok(p, a);
     if (e) return e;
     *bytes = backward_workspace(p, a);
     return TESSEL_OK;
@@ -255,7 +272,7 @@ int tessel_attention_backward_workspace_bytes(const tessel_packing *p, const tes
 
 int tessel_attention_backward(const tessel_packing *p, const tessel_attention *a, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
 {
-    int e = attention_ok(p, a);
+    int e = backward_ok(p, a);
     if (e) return e;
     if (p->tokens == 0) return TESSEL_OK;
     if (!heads_ok(a->q, false, a->heads, a->dim) || !heads_ok(a->k, false, a->kv_heads, a->dim) || !heads_ok(a->v, false, a->kv_heads, a->dim) ||
@@ -354,6 +371,7 @@ int tessel_gated_backward(int act, const tessel_rows *da, const tessel_checkpoin
 int tessel_weight_gradient_workspace_bytes(const tessel_weight_grad *a, size_t *bytes)
 {
     if (!bytes || !a || a->outputs < 1 || a->x.channels < 1 || a->x.tokens < 0) return TESSEL_E_INVALID_ARG;
+    if (a->x.tokens > INT32_MAX) return TESSEL_E_TOOBIG;
     *bytes = weight_workspace(a);
     return TESSEL_OK;
 }

@@ -410,12 +410,13 @@ static WeightShape shape_of(const tessel_weight_grad &a)
     return s;
 }
 
+int64_t weight_tiles(const tessel_weight_grad &a) { return shape_of(a).tiles; }
 int weight_parts(const tessel_weight_grad &a) { return shape_of(a).splits; }
 
 int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stream)
 {
     const WeightShape s = shape_of(a);
-    WeightLaunch l = {a, nullptr, s.splits, 0, (a.x.channels + s.tile - 1) / s.tile};
+    WeightLaunch l = {a, nullptr, s.splits, 0, (int)(((int64_t)a.x.channels + s.tile - 1) / s.tile)};
     l.per = ((a.x.tokens + l.splits - 1) / l.splits + kSteps - 1) / kSteps * kSteps;
     if (l.splits > 1) l.parts = parts;
     void *args[] = {&l};
@@ -425,7 +426,7 @@ int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stre
                            : (straight ? (const void *)weight_kernel<T, 2, 2, 2, kStraight, 2, 2> : (const void *)weight_kernel<T, 2, 2, 2, kUneven, 2, 2>))
     const void *kernel = a.x.type == TESSEL_BF16 ? KERNEL(bf16) : KERNEL(f16);
 #undef KERNEL
-    int e = launched(hipLaunchKernel(kernel, dim3((unsigned)s.tiles, (unsigned)l.splits), dim3(512), args, 0, (hipStream_t)stream));
+    int e = launched(hipLaunchKernel(kernel, dim3((unsigned)s.tiles, (unsigned)l.splits), dim3(kWeightThreads), args, 0, (hipStream_t)stream));
     if (e == 0 && l.parts)
         e = launched(hipLaunchKernel((const void *)weight_sum_kernel, dim3((unsigned)(((int64_t)a.outputs * a.x.channels + 1023) / 1024)), dim3(256), args, 0, (hipStream_t)stream));
     return e;
