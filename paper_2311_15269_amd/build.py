@@ -155,10 +155,45 @@ def early_reads_of_products(asm):
     return [bad[n] for n in sorted(bad)]
 
 
+def miscounted_reads(asm):
+    """Places of the device code where a wait counts on more reads from memory than there are.  A kernel that waits for all but the last N
+    of its reads (`s_waitcnt vmcnt(N) ; counted`) marks the stretches in which it starts them, `; counted reads begin` and `; counted reads
+    end N`: each has to hold N of them, in one piece without labels or branches.  Fewer (merged, left out, moved away), and the wait ends
+    while a read that it is for is still under way.  Returns the offending lines."""
+    bad, begun, reads, stretches, waits = [], None, 0, 0, []
+    for n, line in enumerate(asm.split("\n"), 1):
+        mark = re.search(r"; counted reads (begin|end (\d+))", line)
+        text = line.split(";")[0].strip()
+        if mark and mark.group(2) is None:
+            if begun:
+                bad.append("%d: begins again inside the stretch of line %d" % (n, begun))
+            begun, reads = n, 0
+        elif mark:
+            if not begun:
+                bad.append("%d: ends without a beginning" % n)
+            elif reads != int(mark.group(2)):
+                bad.append("%d: %d reads since line %d, not %s" % (n, reads, begun, mark.group(2)))
+            begun, stretches = None, stretches + 1
+        elif begun and (re.match(r"[^\s;.]*\.?L?\w+:", line) or text.startswith(("s_cbranch", "s_branch", "s_endpgm", "s_setpc"))):
+            bad.append("%d: %s in the stretch of line %d" % (n, text, begun))
+            begun = None
+        elif begun and text.startswith(("global_load", "buffer_load", "flat_load")):
+            reads += 1
+        if re.search(r"s_waitcnt vmcnt\(\d+\) ; counted", line):
+            waits.append(n)
+        if line.startswith(".Lfunc_end"):
+            if begun:
+                bad.append("%d: the stretch of line %d has no end" % (n, begun))
+            if waits and not stretches:
+                bad.append("%d: a counted wait, but no reads are marked" % waits[0])
+            begun, stretches, waits = None, 0, []
+    return bad
+
+
 def build_library(force=True, verbose=False, check=True):
     """hipcc --offload-arch=gfx950 ... -> paper_2311_15269_amd/libtessel_hip.so.  With `check` the device assembly
-    the compiler leaves behind is scanned for scalar loads at addresses that may not be word aligned and for results of matrix
-    instructions that are touched too early."""
+    the compiler leaves behind is scanned for scalar loads at addresses that may not be word aligned, for results of matrix
+    instructions that are touched too early and for reads that a wait counts on but that are not there."""
     if not force and not is_stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -189,7 +224,8 @@ def build_library(force=True, verbose=False, check=True):
             for path in listings:
                 asm = open(path).read()
                 for what, bad in (("scalar loads at possibly unaligned addresses", misaligned_scalar_loads(asm)),
-                                  ("results of matrix instructions touched too early", early_reads_of_products(asm))):
+                                  ("results of matrix instructions touched too early", early_reads_of_products(asm)),
+                                  ("reads from memory that a wait counts on", miscounted_reads(asm))):
                     if bad:
                         raise RuntimeError("%s in %s:\n%s" % (what, os.path.basename(path), "\n".join(bad[:10])))
         shutil.move(out, LIB)

@@ -194,6 +194,25 @@ __device__ __forceinline__ void in_order()
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// Reads from memory that a wait further on counts on: it lets the last so many be under way, so one that the compiler merged with another, left out
+// or moved behind the end would let one of the copies before them be, too.  The build counts them in the listing, between these two marks.
+__device__ __forceinline__ void counted_reads()
+{
+    in_order();
+    asm volatile("; counted reads begin" ::: "memory");
+}
+template <int READS>
+__device__ __forceinline__ void counted_reads_end()
+{
+    asm volatile("; counted reads end %0" ::"n"(READS) : "memory");
+    in_order();
+}
+template <int READS>
+__device__ __forceinline__ void wait_for_all_but()
+{
+    asm volatile("s_waitcnt vmcnt(%0) ; counted" ::"n"(READS) : "memory");
+}
+
 // WN x WC waves, 32 MB x 64 of dw each, GROUPS times, each group for its share of the workgroup's tokens (two, where tiles are small: with half as many
 // parts in memory as two workgroups would leave).  DEPTH: tiles on their way in registers
 template <typename T, int WN, int WC, int MB, int HOW, int GROUPS, int DEPTH>
@@ -234,11 +253,17 @@ __global__ __launch_bounds__(64 * WN * WC * GROUPS, 2) void weight_kernel(Weight
         auto left = [&](int64_t n) { return (int)min((int64_t)kSteps, end - begin - n * kSteps); };
         // tile n to stage `stage` of the registers, the rest of it from memory to LDS, and from the registers to LDS
         auto fetch = [&](int stage, int64_t n) {
+            if constexpr (HOW == kStraight) counted_reads();
             hs[stage].fetch(a, begin + n * kSteps, end, c0, thread);
-            if constexpr (HOW != kStraight) ds[stage].fetch(a, begin + n * kSteps, end, n0, thread);
+            if constexpr (HOW == kStraight) counted_reads_end<2 * kHeld>();
+            else ds[stage].fetch(a, begin + n * kSteps, end, n0, thread);
         };
         auto copy = [&](int64_t n, int to) {
-            if constexpr (HOW == kStraight) Copy::start(rows[to], a, begin + n * kSteps, end, n0, thread);
+            if constexpr (HOW == kStraight) {
+                counted_reads();
+                Copy::start(rows[to], a, begin + n * kSteps, end, n0, thread);
+                counted_reads_end<Copy::kPer>();
+            }
         };
         auto put = [&](int stage, int64_t n) {
 #pragma unroll
@@ -269,9 +294,9 @@ __global__ __launch_bounds__(64 * WN * WC * GROUPS, 2) void weight_kernel(Weight
             constexpr int kNext = (decltype(stage)::value + 1) % DEPTH;
             constexpr bool MORE = decltype(more)::value != 0;
             if constexpr (HOW == kStraight) {
-                if (MORE || n + DEPTH < tiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copy::kPer + 2 * kHeld) : "memory");
-                else if (DEPTH == 2 && n + 1 < tiles) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copy::kPer) : "memory");
-                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                if (MORE || n + DEPTH < tiles) wait_for_all_but<Copy::kPer + 2 * kHeld>();
+                else if (DEPTH == 2 && n + 1 < tiles) wait_for_all_but<Copy::kPer>();
+                else wait_for_all_but<0>();
                 if (!MORE && n == short_one) {
                     lds_barrier();                               // (all waves' copies, before zeros go over them)
                     if (n < tiles) Copy::clear(rows[buffer], left(n), thread);
