@@ -106,10 +106,11 @@ def _refuse(text):
     raise binding.TesselError(E_INVALID_ARG, text)
 
 
-def _fits(*sizes):
-    """the structures' 32-bit fields take a number's low bits without a word"""
-    if max(sizes) > 0x7FFFFFFF:
-        raise binding.TesselError(E_TOOBIG, "%d does not fit 32 bits" % max(sizes))
+MOST = 0x7FFFFFFF       # that the structures' 32-bit fields hold: of more they take the low bits without a word
+
+
+def _too_big(size):
+    raise binding.TesselError(E_TOOBIG, "%d does not fit 32 bits" % size)
 
 
 def _stream(t):
@@ -198,7 +199,8 @@ class Packing:
         self.tokens = sum(self.lengths) if total_tokens is None else int(total_tokens)
         if min(self.lengths, default=0) < 0:
             _refuse("a length of %d" % min(self.lengths))
-        _fits(0, *self.lengths)
+        if max(self.lengths, default=0) > MOST:
+            _too_big(max(self.lengths))
         array = (C.c_int32 * max(1, len(self.lengths)))(*self.lengths)
         h = C.c_void_p()
         binding._check(lib.tessel_packing_create(array, len(self.lengths), self.tokens, C.byref(h)))
@@ -225,7 +227,8 @@ class Packing:
         if q.dim() != 3 or k.dim() != 3 or q.device != self._table.device:
             _refuse("expected [tokens, heads, dim] on %s" % self._table.device)
         heads, kv_heads, dim = q.shape[1], k.shape[1], q.shape[2]
-        _fits(heads, kv_heads, dim)
+        if heads > MOST or kv_heads > MOST or dim > MOST:
+            _too_big(max(heads, kv_heads, dim))
         _same(q, (self.tokens, heads, dim), q)
         _same(q, (self.tokens, kv_heads, dim), k, v)
         if stream != self._made_on:                         # (the table must not be given away while that stream still reads it)
@@ -267,7 +270,8 @@ def _describe_norm(x, y, pre, post, gate, scale, eps):
     if x.dim() != 2:
         _refuse("expected [tokens, channels]")
     n, c = x.shape
-    _fits(c)
+    if c > MOST:
+        _too_big(c)
     _same(x, x.shape, x, y)
     if gate is None:
         kind, at = GATE_NONE, (None, 0)
@@ -335,7 +339,8 @@ class Checkpoint:
         """room for a tensor like this one"""
         import torch
         tokens, channels = like.shape
-        _fits(channels)
+        if channels > MOST:
+            _too_big(channels)
         groups = -(-channels // GROUP)
         self.tokens, self.channels, self.dtype, self.device = tokens, channels, like.dtype, like.device
         # (one tensor for both: half the time of two)
@@ -432,7 +437,8 @@ def weight_gradient(dy, x, into=None):
     if dy.requires_grad:
         _refuse_gradient(dy)
     shape = (dy.shape[1], x.channels)
-    _fits(*shape)
+    if shape[0] > MOST:
+        _too_big(shape[0])
     if into is None:
         dw = dy.new_empty(shape, dtype=torch.float32)
     else:
