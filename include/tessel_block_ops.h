@@ -129,7 +129,7 @@ int  tessel_residual_norm_backward(const tessel_residual_norm *a, void *workspac
  * so a matrix product takes it as it is.  A group with an infinity or NaN reads back as NaN. */
 #define TESSEL_CHECKPOINT_GROUP 64
 typedef struct {
-    int8_t  *values;           /* [tokens][channels]                                                       */
+    int8_t  *values;           /* [tokens][channels up to the next multiple of 64], all of it written and read */
     uint8_t *exponents;        /* [tokens][ceil(channels / 64)]: e + 127; 0 marks a group that is not finite */
     int64_t  value_stride;     /* a multiple of 64, at least channels; data 16-byte aligned                */
     int64_t  exponent_stride;  /* at least ceil(channels / 64)                                             */

@@ -159,8 +159,9 @@ __device__ __forceinline__ void part_with_later(uint4v (&f)[W / 32], float16v *o
 }
 
 // Keys and values once over, with the largest score and the sum of a query's exponentials kept as it goes.  One prompt of 16384 tokens, 32
-// heads of 128 on 8 of keys: 2.13 ms, 1030 TF/s; documents of 1 to 3001 tokens, 8192 in all, 32 heads: 181 us, 760 TF/s (half of the
-// tiles on the diagonal of short ones are masked); 58 tokens in three sequences: 5.6 us.
+// heads of 128 on 8 of keys: 2.13 ms, 1030 TF/s; documents of 1 to 3001 tokens, 8192 in all, 32 heads: 179 us, 760 TF/s (a workgroup has 17 steps of 64
+// keys on average where the prompt's has 129, so that its first reads, one behind the other, and its end weigh more, and a tenth of its scores
+// is masked); 58 tokens in three sequences: 5.6 us.
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendLaunch l)
 {
@@ -340,13 +341,13 @@ __device__ __forceinline__ void fit(float top, float &grow, float16v *sums)
 template <typename T>
 __device__ __forceinline__ constexpr float first_grow() { return __is_same(T, f16) ? 0x1p126f : 1.0f; }
 
-// The gradient of q: three products (scores, do v, and their gradients times k), one operand from LDS for each.  The documents above: 247 us, 830
+// The gradient of q: three products (scores, do v, and their gradients times k), one operand from LDS for each.  The documents above: 246 us, 830
 // TF/s.  (It and the kernel of dk and dv both compute the scores, seven products instead of five: one kernel for all three gradients would add
 // to dq from many workgroups, in no fixed order.)  Also, for the kernel behind it, delta_i = sum_d do_i o_i.
 //
 // The first 128 queries of a sequence take delta_i = sum_j p_ij (do_i . v_j) instead, the same sum from the inputs: o is rounded,
 // and where a query sees few keys that error is as large as the one of rounding the gradients of the scores.  (dq and dk of sequences of 1, 17
-// and 40 tokens in half precision are 2.9e-4 off the 64-bit values with it, 3.3e-4 without; rounding the results alone: 2.1e-4.)
+// and 40 tokens in half precision are 2.9e-4 off the 64-bit values with it, 3.4e-4 without; rounding the results alone: 2.1e-4.)
 template <typename T, int W>
 __global__ __launch_bounds__(kThreads, 2) void attend_dq_kernel(AttendLaunch l)
 {
@@ -562,8 +563,10 @@ __device__ __forceinline__ void dkv_block(const lds_tile *queries, const lds_til
 }
 
 // The gradients of k and v: four products, and five operands from LDS for them, as registers hold the sums of both (128), the keys' operands (32) and
-// the scores' (32), but not the values'.  LDS bounds it: the documents above take 399 us, 690 TF/s.  (One wave on a SIMD with twice the registers:
-// 440 us; queries in tiles of 32 for two workgroups on a compute unit: the same.)
+// the scores' (32), but not the values'.  The documents above take 389 us, 710 TF/s.  LDS, 2,560 clocks for 2,048 of products, leaves 1000 TF/s of the
+// 1260; what is lost beside that is a wait in every tile: its log-sums and deltas are read behind the copies of the same tile and used at
+// once, and as reads come back in order, two of the eight waves stand there until all of those copies have arrived.  (One wave on a SIMD with twice the
+// registers: 440 us; queries in tiles of 32 for two workgroups on a compute unit: the same.)
 //
 // Eight waves: the first four take the tile's first 32 queries, the others the last 32, each 32 of the workgroup's 128 keys; two
 // waves on a SIMD, so that one's exponentials run beside the other's products.  At the end the second four hand their sums to the first.
@@ -681,7 +684,8 @@ static int launch(const void *kernel, int64_t blocks, const AttendLaunch &l, voi
 
 // Splits of a launch's tiles.  The longest tile alone takes `longest` steps of some `step` us, all together `total`, `resident` of them at once; each
 // split leaves `bytes`, which are written and read again at some 4.5 GB/ms, and the join is a launch more.  The number with the least
-// of the sum, none of fewer than four steps.  (2 heads of 128 over 4096 tokens: forward 107 -> 39 us, and with the backward pass 373 -> 133; 8
+// of the sum, none of fewer than four steps.  (The times of a step and the numbers of resident workgroups are those of heads of 128; narrower ones go by
+// them too.  2 heads of 128 over 4096 tokens: forward 107 -> 39 us, and with the backward pass 373 -> 133; 8
 // heads over 8192: 220 -> 187 and 801 -> 734; with 32 nothing is split.)
 int attend_splits(int64_t longest, int64_t total, int resident, double step, double bytes)
 {

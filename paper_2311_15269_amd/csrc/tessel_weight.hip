@@ -26,7 +26,9 @@ struct WeightLaunch {
 };
 
 // What dy looks like decides how it comes to LDS.
-//   kStraight  rows of whole chunks of 16 bytes: from memory to LDS without passing registers, three buffers, two tiles ahead
+//   kStraight  rows of whole chunks of 16 bytes: from memory to LDS without passing registers, three buffers.  Copies start two tiles ahead; the
+//              checkpoint's bytes pass registers, and the compiler's wait before it writes them to LDS is for all reads, so that it ends the
+//              next tile's copies too: in the large tiles every time, in the small ones every other time
 //   kUneven    other rows of eight outputs or more, through registers: a chunk that would pass the row's end starts eight before it
 //   kNarrow    fewer outputs, value by value
 // (No load stands in a branch: the compiler would wait for it where the branch ends.)
@@ -429,7 +431,8 @@ static WeightShape shape_of(const tessel_weight_grad &a)
     // tokens, 3500 x 1500: 78, small 93; but 1024 tokens, 4096 x 2048: 45, small 36; 2048 tokens, 2048 x 2048: 45, small 30).
     WeightShape s = {256, tiles_of(256), 1};
     if (a.outputs < 8 || (s.tiles <= 128 && a.x.tokens * s.tiles < 1280 * 256)) s = {128, tiles_of(128), 1};
-    // splits of the tokens: until 256 workgroups are there, none shorter than 256 tokens a group
+    // splits of the tokens: until 256 workgroups are there, as many as leave a group more than 128 tokens on average (their last ones, in whole
+    // steps, may be shorter: 513 tokens by small tiles are 320 and 193, those of two groups 128 and 65)
     const int64_t least = s.tile == 256 ? 256 : 512, most = (a.x.tokens + least - 1) / least, want = 256 / s.tiles, n = want < most ? want : most;
     s.splits = n < 1 ? 1 : (int)n;
     return s;
