@@ -7,6 +7,10 @@
  *   the norms around a block with its gate and residual scale                    tessel_residual_norm_*
  *   activation checkpoints in 8 bits and their use in the backward pass          tessel_checkpoint_*, tessel_gated_*,
  *                                                                                tessel_weight_gradient
+ *   between the tokens and the attention: the embedding of a shard of the
+ *   vocabulary, the norms of queries and keys with the rotation by position,
+ *   dropout whose mask is never stored                                           tessel_embedding_*, tessel_rotation_*,
+ *                                                                                tessel_dropout_apply
  * Conventions are those of tessel.h: every function returns TESSEL_OK or a negative TESSEL_E_* code and nothing aborts or
  * throws; the caller owns all device memory and the stream; calls are asynchronous on `hip_stream` (NULL = default stream)
  * unless stated otherwise and may be captured into a HIP graph; the library allocates no device memory.  Pointers inside
@@ -165,6 +169,96 @@ typedef struct {
 int  tessel_weight_gradient_workspace_bytes(const tessel_weight_grad *a, size_t *bytes);
 /* Errors: INVALID_ARG, UNSUPPORTED (type), TOOBIG, WORKSPACE, HIP. */
 int  tessel_weight_gradient(const tessel_weight_grad *a, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* ---- dropout whose mask is never stored --------------------------------------------------------------------------
+ * Whether a value is kept is a function of where it stands and of three numbers, so that the backward pass, and a block that
+ * computes its activations again, find the same mask without one in memory.  Channel c of token t takes word c % 4 of Philox4x32-10
+ * (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) for
+ *     counter (c / 4, t, low and high 32 bits of number + *step),    key (low and high 32 bits of seed):
+ *     y = x / (1 - rate) where word >= floor(rate 2^32), else 0 (whatever x is).
+ * The factor is rounded to 32 bits, the product with it once.  dropout is linear: applied to the gradient of y it gives that of x. */
+typedef struct {
+    uint64_t seed;
+    uint64_t number;        /* which dropout of the program this is: a layer's, of a micro-batch           */
+    const uint64_t *step;   /* one number in device memory, added to `number` when the kernel runs (a captured graph that
+                               counts it up draws anew in every replay), or NULL                            */
+    float    rate;          /* 0 (no dropout: y = x) .. below 1                                            */
+} tessel_dropout;
+
+typedef struct {
+    int32_t  type;
+    int32_t  channels;
+    int64_t  tokens;
+    tessel_rows x;
+    tessel_rows y;          /* written                                                                     */
+    tessel_dropout drop;
+} tessel_dropout_rows;
+/* Errors: INVALID_ARG, UNSUPPORTED (type), TOOBIG, HIP. */
+int  tessel_dropout_apply(const tessel_dropout_rows *a, void *hip_stream);
+
+/* ---- the embedding -----------------------------------------------------------------------------------------------
+ * The table holds the rows first .. first + rows - 1 of a vocabulary (all of it, or the shard of one of the devices that an embedding is
+ * spread over).  With v = token_t - first, D the dropout of `drop` and sums over t in ascending order, in 32 bits:
+ *     out_t = D(scale table_v) where 0 <= v < rows, else 0;    dtable_v = scale sum of D(d_out_t) over all t with token_t - first = v.
+ * A token of another shard, or of none (any number below 0), so gets a row of zeros, which the shards add up to the whole, and no
+ * gradient; its row of d_out is not read. */
+enum { TESSEL_I32 = 0, TESSEL_I64 = 1 };
+typedef struct {
+    int32_t  type;          /* of table, out and d_out                                                     */
+    int32_t  index_type;    /* TESSEL_I32 or TESSEL_I64                                                    */
+    const void *token;      /* [tokens]                                                                    */
+    int64_t  tokens;
+    int64_t  first;         /* 0 .. 2^62                                                                   */
+    int32_t  rows;          /* at most 2^24                                                                */
+    int32_t  channels;
+    float    scale;
+    tessel_rows table;      /* forward: [rows][channels]                                                   */
+    tessel_rows out;        /* forward: written                                                            */
+    tessel_rows d_out;      /* backward: gradient of out                                                   */
+    float   *dtable;        /* backward: [rows][channels], written, or added to with `accumulate`          */
+    int64_t  dtable_stride;
+    int32_t  accumulate;    /* not 0: rows of tokens that do not occur are neither read nor written        */
+    tessel_dropout drop;
+} tessel_embedding;
+
+/* Errors: INVALID_ARG, UNSUPPORTED (types), TOOBIG, WORKSPACE (16-byte aligned, contents need not be kept between calls), HIP. */
+int  tessel_embedding_forward(const tessel_embedding *a, void *hip_stream);
+int  tessel_embedding_backward_workspace_bytes(const tessel_embedding *a, size_t *bytes);
+int  tessel_embedding_backward(const tessel_embedding *a, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* ---- the norms of queries and keys with the rotation by position ---------------------------------------------------
+ * For every head z of a token's queries and keys, with w = wq or wk (both NULL: no norm, n = z), over its dim channels:
+ *     n = w z / sqrt(mean(z^2) + eps);    of the first `turning` channels the i-th pair turns by the angle position frequency_i,
+ *     (a, b) -> (a cos - b sin, a sin + b cos),
+ * pair i being channels (i, i + turning / 2) or, with `neighbours`, (2 i, 2 i + 1); the others stay.  Angles are taken in 64 bits and reduced
+ * there, so that they are right at any position; all else in 32 bits, rounded once.  Backward from the gradients of the results and z:
+ * gradients of z, and of wq and wk, sums over tokens and heads in 32 bits.  Infinities and NaN of a head stay in that head (and
+ * reach the gradients of w). */
+typedef struct {
+    int32_t  type;
+    int32_t  index_type;    /* of position: TESSEL_I32 or TESSEL_I64                                       */
+    int32_t  heads;
+    int32_t  kv_heads;
+    int32_t  dim;           /* even, at most 256                                                           */
+    int32_t  turning;       /* even, 0 .. dim                                                              */
+    int32_t  neighbours;
+    float    eps;           /* not negative                                                                */
+    int64_t  tokens;
+    const void *position;   /* [tokens]                                                                    */
+    const double *frequency;/* [turning / 2]: radians a position                                           */
+    const float *wq, *wk;   /* [dim], or both NULL                                                         */
+    tessel_heads q, k;      /* strides here count elements and may be any that are not negative            */
+    tessel_heads q_out, k_out;      /* forward: written                                                    */
+    tessel_heads dq_out, dk_out;    /* backward: gradients of q_out and k_out                              */
+    tessel_heads dq, dk;    /* backward: written                                                           */
+    float   *dwq, *dwk;     /* backward, with norms: [dim], written, or added to with `accumulate`         */
+    int32_t  accumulate;
+} tessel_rotation;
+
+/* Errors: INVALID_ARG, UNSUPPORTED (types), TOOBIG, WORKSPACE, HIP. */
+int  tessel_rotation_forward(const tessel_rotation *a, void *hip_stream);
+int  tessel_rotation_backward_workspace_bytes(const tessel_rotation *a, size_t *bytes);
+int  tessel_rotation_backward(const tessel_rotation *a, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,6 +1,7 @@
 """Thin ctypes binding of include/tessel_block_ops.h: the operators that the blocks of a schedule run -- causal attention over
 packed sequences, the norms around a block with gate and residual scale, activation checkpoints in 8 bits and their use in
-the backward pass.
+the backward pass -- and what lies between the tokens and the attention: the embedding of a shard of the vocabulary, the norms of
+queries and keys with the rotation by position, dropout whose mask is never stored.
 
 Tensors are torch's, on the GPU; every call runs on torch's current stream and allocates its outputs and workspace there
 (a tensor that another stream wrote is the caller's to wait for, as with torch's own operators).  There is no CPU fallback.
@@ -18,6 +19,8 @@ EXPORTS = (
     "tessel_residual_norm_forward", "tessel_residual_norm_backward_workspace_bytes", "tessel_residual_norm_backward",
     "tessel_checkpoint_store", "tessel_checkpoint_restore", "tessel_gated_forward", "tessel_gated_backward",
     "tessel_weight_gradient_workspace_bytes", "tessel_weight_gradient",
+    "tessel_dropout_apply", "tessel_embedding_forward", "tessel_embedding_backward_workspace_bytes", "tessel_embedding_backward",
+    "tessel_rotation_forward", "tessel_rotation_backward_workspace_bytes", "tessel_rotation_backward",
 )
 
 E_INVALID_ARG = -1
@@ -59,6 +62,28 @@ class WeightGrad(C.Structure):
                 ("dw_stride", C.c_int64)]
 
 
+class Drop(C.Structure):
+    _fields_ = [("seed", C.c_uint64), ("number", C.c_uint64), ("step", C.c_void_p), ("rate", C.c_float)]
+
+
+class DropoutRows(C.Structure):
+    _fields_ = [("type", C.c_int32), ("channels", C.c_int32), ("tokens", C.c_int64), ("x", Rows), ("y", Rows), ("drop", Drop)]
+
+
+class Embedding(C.Structure):
+    _fields_ = [("type", C.c_int32), ("index_type", C.c_int32), ("token", C.c_void_p), ("tokens", C.c_int64), ("first", C.c_int64),
+                ("rows", C.c_int32), ("channels", C.c_int32), ("scale", C.c_float), ("table", Rows), ("out", Rows), ("d_out", Rows),
+                ("dtable", C.c_void_p), ("dtable_stride", C.c_int64), ("accumulate", C.c_int32), ("drop", Drop)]
+
+
+class Rotation(C.Structure):
+    _fields_ = [("type", C.c_int32), ("index_type", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
+                ("turning", C.c_int32), ("neighbours", C.c_int32), ("eps", C.c_float), ("tokens", C.c_int64), ("position", C.c_void_p),
+                ("frequency", C.c_void_p), ("wq", C.c_void_p), ("wk", C.c_void_p), ("q", Heads), ("k", Heads), ("q_out", Heads),
+                ("k_out", Heads), ("dq_out", Heads), ("dk_out", Heads), ("dq", Heads), ("dk", Heads), ("dwq", C.c_void_p),
+                ("dwk", C.c_void_p), ("accumulate", C.c_int32)]
+
+
 def _flat(struct):
     """The same layout with the fields of the structures inside side by side: one call fills it, which is most of what a small call costs
     on the host."""
@@ -71,6 +96,7 @@ def _flat(struct):
 
 
 _FlatAttention, _FlatNorm, _FlatWeight = _flat(Attention), _flat(ResidualNorm), _flat(WeightGrad)
+_FlatDropout, _FlatEmbedding, _FlatRotation = _flat(DropoutRows), _flat(Embedding), _flat(Rotation)
 _lib = None
 
 
@@ -98,6 +124,12 @@ def _library():
         lib.tessel_gated_backward.argtypes = [C.c_int] + [ptr] * 7
         lib.tessel_weight_gradient_workspace_bytes.argtypes = [ptr, size]
         lib.tessel_weight_gradient.argtypes = [ptr, ptr, C.c_size_t, ptr]
+        for f in (lib.tessel_dropout_apply, lib.tessel_embedding_forward, lib.tessel_rotation_forward):
+            f.argtypes = [ptr, ptr]
+        for f in (lib.tessel_embedding_backward_workspace_bytes, lib.tessel_rotation_backward_workspace_bytes):
+            f.argtypes = [ptr, size]
+        for f in (lib.tessel_embedding_backward, lib.tessel_rotation_backward):
+            f.argtypes = [ptr, ptr, C.c_size_t, ptr]
         _lib = lib
     return _lib
 
@@ -454,3 +486,173 @@ def weight_gradient(dy, x, into=None):
     ws = _workspace(need, dy) if need else None
     binding._check(lib.tessel_weight_gradient(C.byref(a), ws.data_ptr() if need else None, need, _stream(dy)))
     return dw
+
+
+class Dropout:
+    """A dropout: which values it keeps follows from `seed`, `number` (which dropout of the program this is: a layer's, of a micro-batch) and where
+    they stand, so the backward pass, and a block that computes its activations again, draw the same ones.  `step`: an int64 tensor of one
+    number on the GPU, added to `number` when a kernel runs (a captured graph that counts it up draws anew in every replay)."""
+
+    def __init__(self, rate, seed, number=0, step=None):
+        import torch
+        if not 0 <= rate < 1:
+            _refuse("a dropout rate of %r: from 0 to below 1" % (rate,))
+        for n in (seed, number):
+            if not 0 <= n < 1 << 64:
+                _refuse("%r is no number of 64 bits" % (n,))
+        if step is not None and (step.dtype is not torch.int64 or step.numel() != 1 or not step.is_cuda):
+            _refuse("step has to be one int64 number on the GPU")
+        self.rate, self.seed, self.number, self.step = float(rate), int(seed), int(number), step
+        self._words = (self.seed, self.number, None if step is None else step.data_ptr(), self.rate)
+
+    def _at(self, like):
+        if self.step is not None and self.step.get_device() != like.get_device():
+            _refuse("step on %s, the tensors on %s" % (self.step.device, like.device))
+        return self._words
+
+
+_NO_DROP = (0, 0, None, 0.0)
+
+
+def _on_gpu(t, dims):
+    if t.dim() != len(dims) or not t.is_cuda:
+        _refuse("expected [%s] on the GPU, got %s on %s" % (", ".join(dims), tuple(t.shape), t.device))
+    if max(t.shape) > MOST:
+        _too_big(max(t.shape))
+    if t.requires_grad:
+        _refuse_gradient(t)
+
+
+def _index(t, n, like):
+    """type and address of a whole number for each token"""
+    import torch
+    kind = 1 if t.dtype is torch.int64 else 0 if t.dtype is torch.int32 else None
+    if kind is None:
+        raise binding.TesselError(E_UNSUPPORTED, "tokens and positions are int32 or int64, not %s" % t.dtype)
+    if t.shape != (n,) or t.get_device() != like.get_device() or (n > 1 and t.stride(0) != 1):
+        _refuse("expected %d contiguous whole numbers on %s, got %s on %s" % (n, like.device, tuple(t.shape), t.device))
+    return kind, t.data_ptr()
+
+
+def dropout(x, drop):
+    """tessel_dropout_apply: x [tokens, channels] with what `drop` (a Dropout) drops as zeros and the rest by 1 / (1 - rate); the same call on the
+    gradient of what it gave is the backward pass"""
+    _on_gpu(x, ("tokens", "channels"))
+    y = _like(x)
+    n, c = x.shape
+    a = _FlatDropout(_type(x), c, n, *_rows(x), y.data_ptr(), c, *drop._at(x))
+    binding._check(_library().tessel_dropout_apply(C.byref(a), _stream(x)))
+    return y
+
+
+def _whole_first(first):
+    if not 0 <= first <= 1 << 62:
+        _refuse("the first row of a shard has to be 0 to 2^62, not %r" % (first,))
+    return int(first)
+
+
+def embed(tokens, table, scale=1.0, first=0, drop=None):
+    """tessel_embedding_forward: scale times the rows of table [rows, channels] that tokens (int32 or int64) ask for, after `drop` (a Dropout) if
+    there is one -> [tokens, channels].  The table holds the rows from `first` on of a vocabulary; tokens of other rows, and negative ones, get zeros."""
+    _on_gpu(table, ("rows", "channels"))
+    rows, c = table.shape
+    if tokens.dim() != 1 or tokens.shape[0] > MOST:
+        _refuse("expected at most 2^31 - 1 tokens in one dimension, got %s" % (tuple(tokens.shape),))
+    n = tokens.shape[0]
+    kind, at = _index(tokens, n, table)
+    out = table.new_empty((n, c))
+    a = _FlatEmbedding(_type(table), kind, at, n, _whole_first(first), rows, c, scale, *_rows(table), out.data_ptr(), c, None, 0, None, 0, 0,
+                       *(_NO_DROP if drop is None else drop._at(table)))
+    binding._check(_library().tessel_embedding_forward(C.byref(a), _stream(table)))
+    return out
+
+
+def embed_backward(d_out, tokens, rows, scale=1.0, first=0, drop=None, into=None):
+    """tessel_embedding_backward: the gradient [rows, channels] of the table in 32 bits from that of what embed() gave; added to `into` (and that
+    returned) if it is given, of which rows that no token asked for are neither read nor written"""
+    import torch
+    lib = _library()
+    _on_gpu(d_out, ("tokens", "channels"))
+    n, c = d_out.shape
+    if not 0 < rows <= MOST:
+        _refuse("a table of %r rows" % (rows,))
+    kind, at = _index(tokens, n, d_out)
+    if into is None:
+        dtable = d_out.new_empty((rows, c), dtype=torch.float32)
+    else:
+        dtable = into
+        if dtable.dtype is not torch.float32 or dtable.shape != (rows, c) or dtable.get_device() != d_out.get_device() or (c > 1 and dtable.stride(1) != 1):
+            _refuse("the sum has to be 32-bit %s on %s" % ((rows, c), d_out.device))
+        if dtable.requires_grad:
+            _refuse_gradient(dtable)
+    a = _FlatEmbedding(_type(d_out), kind, at, n, _whole_first(first), rows, c, scale, None, 0, None, 0, *_rows(d_out), dtable.data_ptr(),
+                       dtable.stride(0) if rows > 1 else c, 0 if into is None else 1, *(_NO_DROP if drop is None else drop._at(d_out)))
+    size = C.c_size_t()
+    binding._check(lib.tessel_embedding_backward_workspace_bytes(C.byref(a), C.byref(size)))
+    ws = _workspace(size.value, d_out)
+    binding._check(lib.tessel_embedding_backward(C.byref(a), ws.data_ptr(), ws.numel(), _stream(d_out)))
+    return dtable
+
+
+def frequencies(turning, base=10000.0, device=None):
+    """base^(-2 i / turning) for the pairs i of `turning` channels, in 64 bits: what rotate() takes"""
+    import torch
+    return torch.exp(torch.arange(0, turning, 2, dtype=torch.float64, device="cuda" if device is None else device) * (-math.log(base) / max(1, turning)))
+
+
+def _describe_rotation(q, k, positions, frequency, wq, wk, eps, neighbours):
+    import torch
+    _on_gpu(q, ("tokens", "heads", "dim"))
+    _on_gpu(k, ("tokens", "heads", "dim"))
+    n, heads, dim = q.shape
+    kv_heads = k.shape[1]
+    _same(q, (n, kv_heads, dim), k)
+    if frequency.dtype is not torch.float64 or frequency.dim() != 1 or not frequency.is_contiguous() or frequency.get_device() != q.get_device():
+        _refuse("frequencies are contiguous 64-bit numbers on %s" % q.device)
+    if 2 * frequency.shape[0] > dim:
+        _refuse("%d pairs of %d channels" % (frequency.shape[0], dim))
+    if (wq is None) != (wk is None):
+        _refuse("weights for both, queries and keys, or for neither")
+    kind, at = _index(positions, n, q)
+    return (_type(q), kind, heads, kv_heads, dim, 2 * frequency.shape[0], 1 if neighbours else 0, eps, n, at, frequency.data_ptr(),
+            None if wq is None else _vector(wq, dim, q), None if wk is None else _vector(wk, dim, q), *_heads(q), *_heads(k))
+
+
+def rotate(q, k, positions, frequency, wq=None, wk=None, eps=1e-6, neighbours=False):
+    """tessel_rotation_forward: q [tokens, heads, dim] and k [tokens, kv_heads, dim] -> both, each head normed with wq or wk [dim] (None: as it is) and its
+    first 2 len(frequency) channels turned pair by pair by the angles positions x frequency: channels i and i + len(frequency), or with `neighbours`
+    2 i and 2 i + 1.  positions: int32 or int64 [tokens] (Packing.positions: those of its sequences); frequency: 64-bit numbers (see frequencies)."""
+    described = _describe_rotation(q, k, positions, frequency, wq, wk, eps, neighbours)
+    qo, ko = _like(q), _like(k)
+    a = _FlatRotation(*described, *_heads(qo), *_heads(ko))
+    binding._check(_library().tessel_rotation_forward(C.byref(a), _stream(q)))
+    return qo, ko
+
+
+def rotate_backward(dq_out, dk_out, q, k, positions, frequency, wq=None, wk=None, eps=1e-6, neighbours=False, into=None, out=None):
+    """tessel_rotation_backward: (dq, dk, dwq, dwk) from the gradients of what rotate() gave and from what it took; dwq and dwk are None without norms, and
+    added to `into` = (dwq, dwk) if it is given.  `out` = (dq, dk): tensors to write the gradients to, of any strides (parts of the gradient of a
+    joint projection)."""
+    import torch
+    lib = _library()
+    described = _describe_rotation(q, k, positions, frequency, wq, wk, eps, neighbours)
+    _same(q, q.shape, dq_out)
+    _same(q, k.shape, dk_out)
+    dim = q.shape[2]
+    if out is None:
+        dq, dk = _like(q), _like(k)
+    else:
+        dq, dk = out
+        _same(q, q.shape, dq)
+        _same(q, k.shape, dk)
+    dwq = dwk = None
+    to = (None, None)
+    if wq is not None:
+        dwq, dwk = q.new_empty((2, dim), dtype=torch.float32).unbind(0) if into is None else into
+        to = (_vector(dwq, dim, q), _vector(dwk, dim, q))
+    a = _FlatRotation(*described, None, 0, 0, None, 0, 0, *_heads(dq_out), *_heads(dk_out), *_heads(dq), *_heads(dk), *to, 0 if into is None else 1)
+    size = C.c_size_t()
+    binding._check(lib.tessel_rotation_backward_workspace_bytes(C.byref(a), C.byref(size)))
+    ws = _workspace(size.value, q) if size.value else None
+    binding._check(lib.tessel_rotation_backward(C.byref(a), None if ws is None else ws.data_ptr(), size.value, _stream(q)))
+    return dq, dk, dwq, dwk

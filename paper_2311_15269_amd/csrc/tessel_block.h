@@ -48,4 +48,21 @@ int64_t weight_tiles(const tessel_weight_grad &a);
 int weight_parts(const tessel_weight_grad &a);
 int launch_weight_gradient(const tessel_weight_grad &a, float *parts, void *stream);
 
+// A dropout as kernels take it: words below `least` drop a value, the others multiply it.
+struct DropLaunch {
+    uint32_t least;              // 0: no dropout
+    float    by;
+    uint64_t seed, number;
+    const uint64_t *step;
+};
+int launch_dropout(const tessel_dropout_rows &a, const DropLaunch &d, void *stream);
+
+int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream);
+size_t embed_workspace(const tessel_embedding &a);
+int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *workspace, void *stream);
+
+int launch_rotate(const tessel_rotation &a, void *stream);
+int rotate_parts(const tessel_rotation &a);
+int launch_rotate_backward(const tessel_rotation &a, float *parts, void *stream);
+
 }  // namespace tessel

@@ -163,6 +163,80 @@ size_t weight_workspace(const tessel_weight_grad *a)
     return parts > 1 ? (size_t)parts * a->outputs * a->x.channels * sizeof(float) : 0;
 }
 
+// ---- between the tokens and the attention
+bool lanes_ok(int64_t lanes) { return lanes <= kMostThreads / 256 * 256; }       // (workgroups of 256)
+
+int drop_ok(const tessel_dropout &d, DropLaunch &l)
+{
+    if (!(d.rate >= 0.0f && d.rate < 1.0f) || !aligned(d.step, 8)) return TESSEL_E_INVALID_ARG;
+    // (exact: the largest rate below 1 is 1 - 2^-24)
+    l = {(uint32_t)((double)d.rate * 0x1p32), (float)(1.0 / (1.0 - (double)d.rate)), d.seed, d.number, d.step};
+    return TESSEL_OK;
+}
+
+int dropout_ok(const tessel_dropout_rows *a, DropLaunch &l)
+{
+    if (!a || a->tokens < 0 || a->channels < 1) return TESSEL_E_INVALID_ARG;
+    if (!is_type(a->type)) return TESSEL_E_UNSUPPORTED;
+    const int e = drop_ok(a->drop, l);
+    if (e) return e;
+    if (a->tokens > INT32_MAX || !lanes_ok(a->tokens * (((int64_t)a->channels + 7) / 8))) return TESSEL_E_TOOBIG;
+    return rows_ok(a->x, a->type, a->tokens, a->channels, false) && rows_ok(a->y, a->type, a->tokens, a->channels, true) ? TESSEL_OK : TESSEL_E_INVALID_ARG;
+}
+
+bool index_ok(const void *p, int type, int64_t tokens) { return tokens == 0 || (p && aligned(p, type == TESSEL_I64 ? 8 : 4)); }
+
+int embedding_sizes_ok(const tessel_embedding *a)
+{
+    if (!a || a->tokens < 0 || a->rows < 1 || a->channels < 1) return TESSEL_E_INVALID_ARG;
+    if (a->tokens > INT32_MAX || a->rows > 1 << 24 || !lanes_ok(a->tokens * (((int64_t)a->channels + 7) / 8))) return TESSEL_E_TOOBIG;
+    return TESSEL_OK;
+}
+
+int embedding_ok(const tessel_embedding *a, DropLaunch &l)
+{
+    int e = embedding_sizes_ok(a);
+    if (e) return e;
+    if (!is_type(a->type) || (a->index_type != TESSEL_I32 && a->index_type != TESSEL_I64)) return TESSEL_E_UNSUPPORTED;
+    if (a->first < 0 || a->first > (int64_t)1 << 62 || !std::isfinite(a->scale) || !index_ok(a->token, a->index_type, a->tokens)) return TESSEL_E_INVALID_ARG;
+    return drop_ok(a->drop, l);
+}
+
+// strides of any multiple; what is written must not lie on itself
+bool any_heads_ok(const tessel_heads &h, int type, bool written, int64_t tokens, int heads, int dim)
+{
+    if (!h.data || !aligned(h.data, size_of(type)) || h.token_stride < 0 || h.head_stride < 0) return false;
+    if (h.token_stride > kMostStride || h.head_stride > kMostStride) return false;
+    if (!written) return true;
+    const bool by_token = heads == 1 || (tokens > 1 && h.token_stride >= h.head_stride);       // heads lie inside a token
+    const int64_t near = by_token ? h.head_stride : h.token_stride, far = by_token ? h.token_stride : h.head_stride;
+    const int64_t inner = by_token ? heads : tokens, outer = by_token ? tokens : heads;
+    return (inner == 1 || near >= dim) && (outer == 1 || far >= (inner - 1) * near + dim);
+}
+
+int rotation_sizes_ok(const tessel_rotation *a)
+{
+    if (!a || a->tokens < 0 || a->heads < 1 || a->kv_heads < 1 || a->dim < 2 || a->dim % 2 || a->turning < 0 || a->turning > a->dim || a->turning % 2)
+        return TESSEL_E_INVALID_ARG;
+    // (a wave for each head of a token)
+    if (a->dim > 256 || a->tokens > INT32_MAX || ((int64_t)a->heads + a->kv_heads) * 64 > kMostThreads / 256 * 256 / std::max<int64_t>(1, a->tokens)) return TESSEL_E_TOOBIG;
+    return TESSEL_OK;
+}
+
+int rotation_ok(const tessel_rotation *a)
+{
+    const int e = rotation_sizes_ok(a);
+    if (e) return e;
+    if (!is_type(a->type) || (a->index_type != TESSEL_I32 && a->index_type != TESSEL_I64)) return TESSEL_E_UNSUPPORTED;
+    if (!(a->eps >= 0.0f) || !std::isfinite(a->eps) || !a->wq != !a->wk || !aligned(a->wq, 4) || !aligned(a->wk, 4)) return TESSEL_E_INVALID_ARG;
+    if (a->turning && (!a->frequency || !aligned(a->frequency, 8) || !index_ok(a->position, a->index_type, a->tokens))) return TESSEL_E_INVALID_ARG;
+    if (a->tokens && (!any_heads_ok(a->q, a->type, false, a->tokens, a->heads, a->dim) || !any_heads_ok(a->k, a->type, false, a->tokens, a->kv_heads, a->dim)))
+        return TESSEL_E_INVALID_ARG;
+    return TESSEL_OK;
+}
+
+size_t rotation_workspace(const tessel_rotation *a) { return a->wq ? (size_t)rotate_parts(*a) * 2 * a->dim * sizeof(float) : 0; }
+
 }  // namespace
 
 extern "C" {
@@ -382,6 +456,73 @@ int tessel_weight_gradient(const tessel_weight_grad *a, void *workspace_dev, siz
     if (e) return e;
     if (!workspace_ok(workspace_dev, workspace_bytes, weight_workspace(a))) return TESSEL_E_WORKSPACE;
     return hip_result(launch_weight_gradient(*a, (float *)workspace_dev, hip_stream));
+}
+
+int tessel_dropout_apply(const tessel_dropout_rows *a, void *hip_stream)
+{
+    DropLaunch l;
+    const int e = dropout_ok(a, l);
+    if (e) return e;
+    return a->tokens == 0 ? TESSEL_OK : hip_result(launch_dropout(*a, l, hip_stream));
+}
+
+int tessel_embedding_forward(const tessel_embedding *a, void *hip_stream)
+{
+    DropLaunch l;
+    const int e = embedding_ok(a, l);
+    if (e) return e;
+    if (!rows_ok(a->table, a->type, a->rows, a->channels, false) || !rows_ok(a->out, a->type, a->tokens, a->channels, true)) return TESSEL_E_INVALID_ARG;
+    return a->tokens == 0 ? TESSEL_OK : hip_result(launch_embed(*a, l, hip_stream));
+}
+
+int tessel_embedding_backward_workspace_bytes(const tessel_embedding *a, size_t *bytes)
+{
+    if (!bytes) return TESSEL_E_INVALID_ARG;
+    const int e = embedding_sizes_ok(a);
+    if (e) return e;
+    *bytes = embed_workspace(*a);
+    return TESSEL_OK;
+}
+
+int tessel_embedding_backward(const tessel_embedding *a, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    DropLaunch l;
+    const int e = embedding_ok(a, l);
+    if (e) return e;
+    if (!rows_ok(a->d_out, a->type, a->tokens, a->channels, false) || !a->dtable || !aligned(a->dtable, 4) || a->dtable_stride < a->channels ||
+        a->dtable_stride > kMostStride) return TESSEL_E_INVALID_ARG;
+    if (!workspace_ok(workspace_dev, workspace_bytes, embed_workspace(*a))) return TESSEL_E_WORKSPACE;
+    return hip_result(launch_embed_backward(*a, l, workspace_dev, hip_stream));
+}
+
+int tessel_rotation_forward(const tessel_rotation *a, void *hip_stream)
+{
+    const int e = rotation_ok(a);
+    if (e || a->tokens == 0) return e;
+    if (!any_heads_ok(a->q_out, a->type, true, a->tokens, a->heads, a->dim) || !any_heads_ok(a->k_out, a->type, true, a->tokens, a->kv_heads, a->dim))
+        return TESSEL_E_INVALID_ARG;
+    return hip_result(launch_rotate(*a, hip_stream));
+}
+
+int tessel_rotation_backward_workspace_bytes(const tessel_rotation *a, size_t *bytes)
+{
+    if (!bytes) return TESSEL_E_INVALID_ARG;
+    const int e = rotation_sizes_ok(a);
+    if (e) return e;
+    *bytes = rotation_workspace(a);
+    return TESSEL_OK;
+}
+
+int tessel_rotation_backward(const tessel_rotation *a, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    const int e = rotation_ok(a);
+    if (e) return e;
+    if (a->wq && (!a->dwq || !a->dwk || !aligned(a->dwq, 4) || !aligned(a->dwk, 4))) return TESSEL_E_INVALID_ARG;
+    if (a->tokens && (!any_heads_ok(a->dq_out, a->type, false, a->tokens, a->heads, a->dim) || !any_heads_ok(a->dk_out, a->type, false, a->tokens, a->kv_heads, a->dim) ||
+                      !any_heads_ok(a->dq, a->type, true, a->tokens, a->heads, a->dim) || !any_heads_ok(a->dk, a->type, true, a->tokens, a->kv_heads, a->dim)))
+        return TESSEL_E_INVALID_ARG;
+    if (!workspace_ok(workspace_dev, workspace_bytes, rotation_workspace(a))) return TESSEL_E_WORKSPACE;
+    return hip_result(launch_rotate_backward(*a, (float *)workspace_dev, hip_stream));
 }
 
 }  // extern "C"
