@@ -210,7 +210,7 @@ typedef struct {
     int64_t  tokens;
     int64_t  first;         /* 0 .. 2^62                                                                   */
     int32_t  rows;          /* at most 2^24                                                                */
-    int32_t  channels;
+    int32_t  channels;      /* at most 2^24                                                                */
     float    scale;
     tessel_rows table;      /* forward: [rows][channels]                                                   */
     tessel_rows out;        /* forward: written                                                            */

@@ -189,7 +189,7 @@ bool index_ok(const void *p, int type, int64_t tokens) { return tokens == 0 || (
 int embedding_sizes_ok(const tessel_embedding *a)
 {
     if (!a || a->tokens < 0 || a->rows < 1 || a->channels < 1) return TESSEL_E_INVALID_ARG;
-    if (a->tokens > INT32_MAX || a->rows > 1 << 24 || !lanes_ok(a->tokens * (((int64_t)a->channels + 7) / 8))) return TESSEL_E_TOOBIG;
+    if (a->tokens > INT32_MAX || a->rows > 1 << 24 || a->channels > 1 << 24 || !lanes_ok(a->tokens * (((int64_t)a->channels + 7) / 8))) return TESSEL_E_TOOBIG;
     return TESSEL_OK;
 }
 

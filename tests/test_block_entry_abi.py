@@ -43,7 +43,7 @@ def embedding(**change):
 
 
 @pytest.mark.parametrize("change, code", [
-    ({"tokens": -1}, INVALID), ({"rows": 0}, INVALID), ({"channels": 0}, INVALID), ({"tokens": 1 << 31}, TOOBIG), ({"rows": (1 << 24) + 1}, TOOBIG),
+    ({"tokens": -1}, INVALID), ({"rows": 0}, INVALID), ({"channels": 0}, INVALID), ({"tokens": 1 << 31}, TOOBIG), ({"rows": (1 << 24) + 1}, TOOBIG), ({"channels": (1 << 24) + 1}, TOOBIG),
     ({"tokens": (1 << 31) - 1, "channels": 17}, TOOBIG), ({"type": 3}, UNSUPPORTED), ({"index_type": 2}, UNSUPPORTED), ({"first": -1}, INVALID), ({"first": (1 << 62) + 1}, INVALID),
     ({"scale": NAN}, INVALID), ({"scale": INF}, INVALID), ({"token": None}, INVALID), ({"token": AT + 4}, INVALID), ({"drop": drop(rate=1.0)}, INVALID),
 ])
