@@ -1,32 +1,40 @@
-// Dropout whose mask is never stored (formulas: include/tessel_block_ops.h): eight channels a lane, two words' counters each.
+// Dropout whose mask is never stored (formulas: include/tessel_block_ops.h): one pass, eight channels a lane, four tokens one after the other.
 #include "tessel_draw.h"
 
 namespace tessel {
 
 constexpr int kThreads = 256;
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void dropout_kernel(tessel_dropout_rows a, DropLaunch d)
+template <typename T, bool WIDE, int ROWS>
+__global__ __launch_bounds__(kThreads) void dropout_kernel(tessel_dropout_rows a, DropLaunch l, int lanes)
 {
-    const uint32_t per = (uint32_t)(((int64_t)a.channels + 7) / 8);
-    const uint64_t n = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-    const uint32_t row = (uint32_t)(n / per);
-    const int col = (int)(n % per) * 8;
-    if ((int64_t)(n / per) >= a.tokens) return;
-    float v[8];
-    load8<T>(v, (const T *)a.x.data + row * a.x.stride, col, a.channels);
-    if (d.least) drop8(v, d, number_of(d), row, col);
-    store8<T>((T *)a.y.data + row * a.y.stride, v, col, a.channels);
+    const Span<WIDE, ROWS> at(a.channels, lanes);
+    typename Eight<T>::type x[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; r++) x[r] = take8<T, !WIDE>((const T *)a.x.data + min(at.token + r * at.step, a.tokens - 1) * a.x.stride, at.col, a.channels);
+    const Draw draw(l, at.col);
+#pragma unroll
+    for (int r = 0; r < ROWS; r++) {
+        const int64_t token = at.token + r * at.step;
+        if (token >= a.tokens) break;
+        float v[8];
+        settle8<T, !WIDE>(at.col, a.channels, x[r]);
+        widen8<T>(v, x[r]);
+        if (l.least) draw.apply(v, (uint32_t)token);
+        store8<T>((T *)a.y.data + token * a.y.stride, v, at.col, a.channels);
+    }
 }
 
 int launch_dropout(const tessel_dropout_rows &a, const DropLaunch &d, void *stream)
 {
     tessel_dropout_rows aa = a;
     DropLaunch dd = d;
-    void *args[] = {&aa, &dd};
-    const int64_t lanes = a.tokens * (((int64_t)a.channels + 7) / 8);
-#define KERNEL(T) ((const void *)dropout_kernel<T>)
-    return launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)((lanes + kThreads - 1) / kThreads)), dim3(kThreads), args, 0, (hipStream_t)stream));
+    const int rows = span_rows(a.type, a.tokens, a.channels, d);
+    SpanShape s = span_shape(a.tokens, a.channels, rows);
+    void *args[] = {&aa, &dd, &s.lanes};
+#define KERNEL(T) (s.wide ? rows == 4 ? (const void *)dropout_kernel<T, true, 4> : (const void *)dropout_kernel<T, true, 1> \
+                          : rows == 4 ? (const void *)dropout_kernel<T, false, 4> : (const void *)dropout_kernel<T, false, 1>)
+    return launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3(s.groups), dim3(kThreads), args, 0, (hipStream_t)stream));
 #undef KERNEL
 }
 

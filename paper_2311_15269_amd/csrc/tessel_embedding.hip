@@ -1,6 +1,8 @@
 // The embedding of a shard of the vocabulary, forward and backward (formulas: include/tessel_block_ops.h).
 //
 // Forward: eight channels of a token a lane.  Backward: a workgroup for every row of the table looks through all tokens for its own, in order.
+#include <algorithm>
+
 #include "tessel_draw.h"
 
 namespace tessel {
@@ -14,63 +16,92 @@ __device__ __forceinline__ int row_at(const tessel_embedding &a, int64_t t)
     return v >= a.first && v - a.first < a.rows ? (int)(v - a.first) : -1;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void embed_kernel(tessel_embedding a, DropLaunch d)
+template <typename T, bool WIDE, int ROWS>
+__global__ __launch_bounds__(kThreads) void embed_kernel(tessel_embedding a, DropLaunch d, int lanes)
 {
-    const uint32_t per = (uint32_t)(((int64_t)a.channels + 7) / 8);
-    const uint64_t n = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t t = (int64_t)(n / per);
-    const int col = (int)(n % per) * 8;
-    if (t >= a.tokens) return;
-    const int row = row_at(a, t);
-    float v[8] = {};
-    if (row >= 0) {
-        load8<T>(v, (const T *)a.table.data + row * a.table.stride, col, a.channels);
+    const Span<WIDE, ROWS> at(a.channels, lanes);
+    int row[ROWS];
+    typename Eight<T>::type x[ROWS];
 #pragma unroll
-        for (int j = 0; j < 8; j++) v[j] *= a.scale;
-        if (d.least) drop8(v, d, number_of(d), (uint32_t)t, col);
+    for (int r = 0; r < ROWS; r++) row[r] = row_at(a, min(at.token + r * at.step, a.tokens - 1));
+#pragma unroll
+    for (int r = 0; r < ROWS; r++) x[r] = take8<T, !WIDE>((const T *)a.table.data + max(row[r], 0) * a.table.stride, at.col, a.channels);
+    const Draw draw(d, at.col);
+#pragma unroll
+    for (int r = 0; r < ROWS; r++) {
+        const int64_t token = at.token + r * at.step;
+        if (token >= a.tokens) break;
+        float v[8];
+        settle8<T, !WIDE>(at.col, a.channels, x[r]);
+        widen8<T>(v, x[r]);
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = row[r] >= 0 ? v[j] * a.scale : 0.0f;
+        if (d.least) draw.apply(v, (uint32_t)token);
+        store8<T>((T *)a.out.data + token * a.out.stride, v, at.col, a.channels);
     }
-    store8<T>((T *)a.out.data + t * a.out.stride, v, col, a.channels);
 }
 
-// Backward: the places of a batch sorted by row, those of a row in ascending order (sort_kernel); sums over runs of so many sorted places
-// (sum_kernel); sums of what the runs left of rows that go on from one run into the next, and rows that no token asked for (join_kernel).
+// Backward: the places of a batch sorted by row, those of a row in ascending order (sort_kernel); sums over runs of so many sorted places, and zeros in the rows that no
+// token asked for (sum_kernel); sums of what the runs left of rows that go on from one run into the next (join_kernel).
 struct EmbedLaunch {
     tessel_embedding a;
     DropLaunch d;
     int32_t *place, *row;        // [tokens] sorted: place in the batch, row of the table
     int32_t *total;              // how many of them
-    int32_t *count;              // [buckets][bins]: tokens of row bin * buckets + bucket
-    float   *parts;              // [runs][2][channels]: of the row that a run begins within, and of the one that goes on behind it
+    int32_t *count;              // [buckets][bins], where the gradient is written: tokens of row bin * buckets + bucket
+    float   *parts;              // [runs][2][part]: of the row that a run begins within, and of the one that goes on behind it
+    int64_t  part;               // channels up to the next multiple of eight
     int32_t  bins, shift;        // buckets = 2^shift
     int32_t  run, runs;          // sorted places a run
-    int32_t  lanes;              // that hold a run's columns: a power of two up to 256, eight columns each
+    int32_t  lanes, tiles;       // that hold a run's columns: a power of two up to 256, eight columns each; of them, to the end of a row
+    uint32_t sum_groups;         // workgroups that add up
+    uint32_t fill_rows, fill_pieces, fill_lanes;      // and of one that fills: rows, or pieces of a row; lanes a row takes
 };
 
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kEach = 4, kTile = kSortThreads * kEach;
-constexpr int kMostBins = 4096;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kSubs = 4, kSub = 4 * kSortThreads, kTile = kSubs * kSub;          // a thread takes four places of each part of a tile
+constexpr int kMostBins = 2 * kSortThreads;        // (two workgroups have room on a compute unit)
 
-// rows of the table for tokens t .. t + 3, -1 where there is none
+// rows of the table for a thread's places of the tile at t0, -1 where there is none
 template <typename I>
-__device__ __forceinline__ void rows4(const tessel_embedding &a, int64_t t, int (&v)[kEach])
+__device__ __forceinline__ void tile_rows(const tessel_embedding &a, int64_t t0, int (&v)[kSubs][4])
 {
     typedef I V __attribute__((ext_vector_type(4), aligned(sizeof(I))));
     const I *p = (const I *)a.token;
-    V w;
-    if (t + kEach <= a.tokens) {
-        w = *(const V *)(p + t);
-    } else {
+    V w[kSubs];
 #pragma unroll
-        for (int j = 0; j < kEach; j++) w[j] = t + j < a.tokens ? p[t + j] : (I)-1;
+    for (int s = 0; s < kSubs; s++) {
+        const int64_t t = t0 + s * kSub + 4 * threadIdx.x;
+        w[s] = V{(I)-1, (I)-1, (I)-1, (I)-1};
+        if (t + 4 <= a.tokens) {
+            w[s] = *(const V *)(p + t);
+        } else if (t < a.tokens) {
+            w[s][0] = p[t];
+            if (t + 1 < a.tokens) w[s][1] = p[t + 1];
+            if (t + 2 < a.tokens) w[s][2] = p[t + 2];
+        }
     }
 #pragma unroll
-    for (int j = 0; j < kEach; j++) {
-        const int64_t n = w[j];
-        v[j] = n >= a.first && n - a.first < a.rows ? (int)(n - a.first) : -1;
-    }
+    for (int s = 0; s < kSubs; s++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int64_t n = w[s][j];
+            v[s][j] = n >= a.first && n - a.first < a.rows ? (int)(n - a.first) : -1;
+        }
 }
 
 __device__ __forceinline__ int below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u)); }
+
+// sums over the lanes up to and with this one
+__device__ __forceinline__ int sums_up_to(int x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        if ((int)(threadIdx.x & 63) >= d) x += y;
+    }
+    return x;
+}
 
 // A workgroup for each bucket of rows with the same low bits (frequent tokens are neighbours in a vocabulary).  It counts the places of its rows
 // and of the buckets before it, and then goes through the batch once more, a tile at a time, and puts its places where they belong.
@@ -78,24 +109,32 @@ template <typename I>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(EmbedLaunch l)
 {
     __shared__ int cursor[kMostBins];                            // counts, then the place where the next one of a row goes
-    __shared__ int list_row[kTile], list_place[kTile];           // this bucket's share of a tile, in order
-    __shared__ int sums[2][kSortWaves];
+    __shared__ int list[kTile];                                  // this bucket's share of a tile, in order: bin, and place in the tile
+    __shared__ int sums[2][kSortWaves], shares[kSubs * kSortWaves];
+    static_assert(kSubs * kSortWaves == 64 && kTile <= 1 << 14, "a lane for each wave's share of a part; 14 bits of a place");
     const tessel_embedding &a = l.a;
     const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, bucket = blockIdx.x, mask = (1 << l.shift) - 1;
     for (int b = thread; b < l.bins; b += kSortThreads) cursor[b] = 0;
-    __syncthreads();
-    int before = 0, own = 0;
-    for (int64_t t0 = 0; t0 < a.tokens; t0 += kTile) {
-        int v[kEach];
-        rows4<I>(a, t0 + kEach * thread, v);
+    int before = 0, own = 0, v[kSubs][4];
+    const auto count = [&](const int (&v)[kSubs][4]) {
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
-            before += v[j] >= 0 && (v[j] & mask) < bucket ? 1 : 0;
-            if (v[j] >= 0 && (v[j] & mask) == bucket) {
-                own++;
-                atomicAdd(&cursor[v[j] >> l.shift], 1);          // (whole numbers: the order does not matter)
+        for (int s = 0; s < kSubs; s++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                before += v[s][j] >= 0 && (v[s][j] & mask) < bucket ? 1 : 0;
+                if (v[s][j] >= 0 && (v[s][j] & mask) == bucket) {
+                    own++;
+                    atomicAdd(&cursor[v[s][j] >> l.shift], 1);   // (whole numbers: the order does not matter)
+                }
             }
-        }
+    };
+    tile_rows<I>(a, 0, v);
+    __syncthreads();
+    count(v);
+    for (int64_t t0 = kTile; t0 < a.tokens; t0 += kTile) {
+        int w[kSubs][4];
+        tile_rows<I>(a, t0, w);
+        count(w);
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
@@ -117,119 +156,137 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(EmbedLaunch l)
     if (!a.accumulate)
         for (int b = thread; b < l.bins; b += kSortThreads) l.count[(int64_t)bucket * l.bins + b] = cursor[b];
     if (own == 0) return;
-    // where each row's places begin: four bins a thread
-    __syncthreads();
-    int c[4], sum = 0;
+    // where each row's places begin: two bins a thread
+    int c[2], sum = 0;
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-        c[j] = 4 * thread + j < l.bins ? cursor[4 * thread + j] : 0;
+    for (int j = 0; j < 2; j++) {
+        c[j] = 2 * thread + j < l.bins ? cursor[2 * thread + j] : 0;
         sum += c[j];
     }
-    int up = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int x = __shfl_up(up, d);
-        if (lane >= d) up += x;
-    }
+    const int up = sums_up_to(sum);
+    __syncthreads();                                             // (all are done with the counts and sums)
     if (lane == 63) sums[0][wave] = up;
     __syncthreads();
     int at = before + up - sum;
     for (int w = 0; w < wave; w++) at += sums[0][w];
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-        if (4 * thread + j < l.bins) cursor[4 * thread + j] = at;
+    for (int j = 0; j < 2; j++) {
+        if (2 * thread + j < l.bins) cursor[2 * thread + j] = at;
         at += c[j];
     }
     for (int64_t t0 = 0; t0 < a.tokens; t0 += kTile) {
-        int v[kEach], n = 0;
-        rows4<I>(a, t0 + kEach * thread, v);
+        if (t0 > 0) tile_rows<I>(a, t0, v);                      // (a batch of one tile is read once)
+        // places before this thread's in its wave: none to four of each thread
+        int to[kSubs];
+        __syncthreads();                                         // (the list and the shares of the tile before are done with)
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
-            if (v[j] >= 0 && (v[j] & mask) != bucket) v[j] = -1;
-            n += v[j] >= 0 ? 1 : 0;
-        }
-        // places before this thread's: n is 0 to 4
-        const uint64_t one = __ballot(n & 1), two = __ballot(n & 2), four = __ballot(n & 4);
-        int to = below(one) + 2 * below(two) + 4 * below(four);
-        __syncthreads();                                         // (the list and the sums of the tile before are done with)
-        if (lane == 0) sums[0][wave] = __popcll(one) + 2 * __popcll(two) + 4 * __popcll(four);
-        __syncthreads();
-        int found = 0;
+        for (int s = 0; s < kSubs; s++) {
+            int n = 0;
 #pragma unroll
-        for (int w = 0; w < kSortWaves; w++) {
-            to += w < wave ? sums[0][w] : 0;
-            found += sums[0][w];
-        }
-#pragma unroll
-        for (int j = 0; j < kEach; j++)
-            if (v[j] >= 0) {
-                list_row[to] = v[j];
-                list_place[to] = (int)(t0 + kEach * thread + j);
-                to++;
+            for (int j = 0; j < 4; j++) {
+                if (v[s][j] >= 0 && (v[s][j] & mask) != bucket) v[s][j] = -1;
+                n += v[s][j] >= 0 ? 1 : 0;
             }
+            const uint64_t one = __ballot(n & 1), two = __ballot(n & 2), four = __ballot(n & 4);
+            to[s] = below(one) + 2 * below(two) + 4 * below(four);
+            if (lane == 0) shares[s * kSortWaves + wave] = __popcll(one) + 2 * __popcll(two) + 4 * __popcll(four);
+        }
+        __syncthreads();
+        const int share = shares[lane], through = sums_up_to(share), found = __shfl(through, 63);
+#pragma unroll
+        for (int s = 0; s < kSubs; s++) {
+            int i = to[s] + __shfl(through - share, s * kSortWaves + wave);
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                if (v[s][j] >= 0) list[i++] = (v[s][j] >> l.shift) << 14 | (s * kSub + 4 * thread + j);
+        }
         __syncthreads();
         for (int first = 0; first < found; first += kSortThreads) {
             // a wave's 64 places: how many of the same row come before, and which lane is the first of the row
-            const int i = first + thread, row = i < found ? list_row[i] : -1, bin = row >> l.shift;
-            uint64_t same = __ballot(row >= 0);
+            const int i = first + thread;
+            const bool there = i < found;
+            const int entry = there ? list[i] : 0, bin = entry >> 14;
+            uint64_t same = __ballot(there);
             for (int b = 0; 1 << b < l.bins; b++) {
                 const uint64_t bit = __ballot(bin >> b & 1);
                 same &= bin >> b & 1 ? bit : ~bit;
             }
-            const int rank = below(same), leader = __ffsll((unsigned long long)same) - 1;
+            const int rank = below(same), leader = max(0, __ffsll((unsigned long long)same) - 1);
             const int waves = min(kSortWaves, (found - first + 63) / 64);
             int start = 0;
             for (int w = 0; w < waves; w++) {                    // (the waves one after the other: places of a row stay in order)
-                if (wave == w && row >= 0 && rank == 0) {
+                if (wave == w && there && rank == 0) {
                     start = cursor[bin];
                     cursor[bin] = start + __popcll(same);
                 }
                 __syncthreads();
             }
-            start = __shfl(start, leader < 0 ? 0 : leader);
-            if (row >= 0) {
-                l.place[start + rank] = list_place[i];
-                l.row[start + rank] = row;
+            start = __shfl(start, leader);
+            if (there) {
+                l.place[start + rank] = (int)(t0 + (entry & (kTile - 1)));
+                l.row[start + rank] = bin << l.shift | bucket;
             }
         }
     }
 }
 
-// what a run left of a row, or all of it
-template <bool NARROW>
-__device__ __forceinline__ void put_sum(const EmbedLaunch &l, float *to, bool whole, const float *sum, int col)
+constexpr int kFill = 16384;     // values that a workgroup fills with zeros
+
+// Rows that no token asked for; neighbouring workgroups write neighbouring pieces.
+__device__ __forceinline__ void fill(const EmbedLaunch &l, uint32_t piece)
 {
+    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
     const tessel_embedding &a = l.a;
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; j++) v[j] = whole ? a.scale * sum[j] : sum[j];
-    if (whole && a.accumulate) {
-        float old[8];
-        load8<float>(old, to, col, a.channels);
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] += old[j];
+    const int lanes = l.fill_lanes, lane = threadIdx.x % lanes;
+    const int64_t first = (int64_t)(piece / l.fill_pieces) * l.fill_rows;
+    const int begin = piece % l.fill_pieces * kFill, end = (int)min((int64_t)a.channels, (int64_t)begin + kFill);
+    for (int r = threadIdx.x / lanes; r < (int)l.fill_rows; r += kThreads / lanes) {
+        const int64_t row = first + r;
+        if (row >= a.rows || l.count[(row & ((1 << l.shift) - 1)) * l.bins + (row >> l.shift)]) continue;
+        float *to = a.dtable + row * a.dtable_stride;
+        int col = begin + 4 * lane;
+        for (; col + 4 <= end; col += 4 * lanes) *(V *)(to + col) = V{};
+        for (int j = col; j < end; j++) to[j] = 0.0f;
     }
-    store8<float>(to, v, col, a.channels);
 }
 
-template <typename T, bool NARROW>
+// Sums over runs of sorted places, eight columns a lane.  Rows that lie inside a run are whole; of the row that it begins within and of the
+// one that goes on behind it, it leaves a part.  The workgroups
+// behind these fill the other rows, whose stores hide the way of the sums' reads.
+// WIDE: a run's columns take whole waves, which so read rows and places by the scalar unit
+template <typename T, bool WIDE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
 {
     constexpr int kAhead = 8;
     const tessel_embedding &a = l.a;
-    int run = blockIdx.x * (kThreads / l.lanes) + threadIdx.x / l.lanes;
-    if (l.lanes >= 64) run = __builtin_amdgcn_readfirstlane(run);
-    const int col = 8 * (blockIdx.y * l.lanes + threadIdx.x % l.lanes), total = *l.total;
+    if (blockIdx.x >= l.sum_groups) {
+        fill(l, blockIdx.x - l.sum_groups);
+        return;
+    }
+    const int group = blockIdx.x / l.tiles, tile = blockIdx.x % l.tiles;
+    int run = group * (kThreads / l.lanes) + threadIdx.x / l.lanes;
+    if constexpr (WIDE) run = __builtin_amdgcn_readfirstlane(run);
+    const int col = 8 * (tile * l.lanes + threadIdx.x % l.lanes), total = *l.total;
     const int64_t first = (int64_t)run * l.run;
     if (run >= l.runs || first >= total || col >= a.channels) return;
     const uint32_t begin = (uint32_t)first, end = (uint32_t)min(first + l.run, (int64_t)total);
-    const uint64_t number = number_of(l.d);
+    const Draw draw(l.d, col);
     int row = l.row[begin];
     bool starts = begin == 0 || l.row[begin - 1] != row;         // (the row's first place is in this run)
+    const bool goes_on = end < (uint32_t)total && l.row[end] == l.row[end - 1];
     float sum[8] = {};
     const auto flush = [&](bool ends) {
-        const bool whole = starts && ends;
-        put_sum<NARROW>(l, whole ? a.dtable + row * a.dtable_stride : l.parts + ((int64_t)run * 2 + (starts ? 1 : 0)) * a.channels, whole, sum, col);
+        if (starts && ends) {
+            float *to = a.dtable + row * a.dtable_stride, old[8] = {};
+            if (a.accumulate) load8<float>(old, to, col, a.channels);
+#pragma unroll
+            for (int j = 0; j < 8; j++) sum[j] = old[j] + a.scale * sum[j];
+            store8<float>(to, sum, col, a.channels);
+        } else {
+            float4v *to = (float4v *)(l.parts + ((int64_t)run * 2 + (starts ? 1 : 0)) * l.part + col);
+            to[0] = float4v{sum[0], sum[1], sum[2], sum[3]};
+            to[1] = float4v{sum[4], sum[5], sum[6], sum[7]};
+        }
     };
     for (uint32_t i = begin; i < end; i += kAhead) {
         int r[kAhead], t[kAhead];
@@ -254,68 +311,46 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
             float v[8];
             settle8<T, NARROW>(col, a.channels, x[j]);
             widen8<T>(v, x[j]);
-            if (l.d.least) drop8(v, l.d, number, (uint32_t)t[j], col);
+            if (l.d.least) draw.apply(v, (uint32_t)t[j]);
 #pragma unroll
             for (int k = 0; k < 8; k++) sum[k] += v[k];
         }
     }
-    flush(end == (uint32_t)total || l.row[end] != row);
+    flush(!goes_on);
 }
 
-// The first workgroups, one for each run and 4 lanes columns: where a row goes on behind the run that it starts in, the sum of what the runs left of it.
-// The others, rows that no token asked for.
-__global__ __launch_bounds__(kSortThreads) void join_kernel(EmbedLaunch l, int joins, int tiles)
+// Where a row goes on behind the run that it starts in: the sum of what the runs left of it, four columns a lane.  A workgroup for each run
+// and tile of columns; most runs have none.  All that the decision needs is read at once.
+__global__ __launch_bounds__(kSortThreads) void join_kernel(EmbedLaunch l, int lanes, int tiles)
 {
-    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
     __shared__ float4v sums[kSortThreads];
     const tessel_embedding &a = l.a;
-    if ((int)blockIdx.x >= joins) {                              // a wave for each row
-        const int step = (gridDim.x - joins) * kSortWaves, lane = threadIdx.x & 63;
-        for (int64_t row = (int64_t)(blockIdx.x - joins) * kSortWaves + (threadIdx.x >> 6); row < a.rows; row += step) {
-            if (l.count[(row & ((1 << l.shift) - 1)) * l.bins + (row >> l.shift)]) continue;
-            float *to = a.dtable + row * a.dtable_stride;
-            const float zero[8] = {};
-            for (int col = 8 * lane; col < a.channels; col += 512) store8<float>(to, zero, col, a.channels);
-        }
-        return;
-    }
-    const int run = blockIdx.x / tiles, total = *l.total;
-    const int64_t last = ((int64_t)run + 1) * l.run;
-    if (last >= total) return;
-    const int row = l.row[last - 1], lane = threadIdx.x & 63;
-    if (l.row[last] != row) return;
-    if (l.row[last - l.run] == row && run > 0 && l.row[last - l.run - 1] == row) return;       // (it does not start here)
-    int more = 0;                                                // runs that it goes on in
-    for (;;) {
-        const int64_t i = (int64_t)(run + 1 + more + lane) * l.run;
-        const uint64_t there = __ballot(i < total && l.row[min(i, (int64_t)total - 1)] == row);
+    const int run = blockIdx.x / tiles, tile = blockIdx.x % tiles, lane = threadIdx.x & 63, total = *l.total;
+    const int64_t first = (int64_t)run * l.run, next = first + l.run, end = a.tokens - 1;
+    const int row = l.row[min(next - 1, end)], behind = l.row[min(next, end)], begin = l.row[min(first, end)], before = l.row[max(first - 1, (int64_t)0)];
+    int64_t i = next + (int64_t)lane * l.run;
+    int more = 0, at = l.row[min(i, end)];
+    if (next >= total || behind != row || (begin == row && run > 0 && before == row)) return;
+    for (;;) {                                                   // runs that it goes on in
+        const uint64_t there = __ballot(i < total && at == row);
         const int n = there == ~0ull ? 64 : __ffsll((unsigned long long)~there) - 1;
         more += n;
         if (n < 64) break;
+        i += (int64_t)64 * l.run;
+        at = l.row[min(i, end)];
     }
-    const int lanes = 2 * l.lanes, groups = kSortThreads / lanes, group = threadIdx.x / lanes, at = threadIdx.x % lanes;
-    const int col = 4 * (blockIdx.x % tiles * lanes + at);
-    V sum = {};
+    const int groups = kSortThreads / lanes, group = threadIdx.x / lanes, place = threadIdx.x % lanes, col = 4 * (tile * lanes + place);
+    float4v sum = {};
     if (col < a.channels) {
-        const int whole = min(4, a.channels - col);
-        const auto part = [&](int p) {                           // the first of them is the run's own
-            const float *from = l.parts + ((int64_t)(run + p) * 2 + (p == 0 ? 1 : 0)) * a.channels + col;
-            V v = {};
-            if (whole == 4) v = *(const V *)from;
-            else
-                for (int j = 0; j < whole; j++) v[j] = from[j];
-            return v;
-        };
+        const float *own = l.parts + ((int64_t)run * 2 + 1) * l.part + col, *others = own + l.part;      // (behind a run's second part, the next one's first)
+        if (group == 0) sum = *(const float4v *)own;
 #pragma unroll 8
-        for (int p = group; p <= more; p += groups) sum += part(p);
+        for (int p = group; p < more; p += groups) sum += *(const float4v *)(others + (int64_t)p * 2 * l.part);
     }
-    sums[threadIdx.x] = float4v{sum[0], sum[1], sum[2], sum[3]};
+    sums[threadIdx.x] = sum;
     __syncthreads();
     if (group > 0 || col >= a.channels) return;
-    for (int g = 1; g < min(groups, more + 1); g++) {
-        const float4v v = sums[g * lanes + at];
-        sum += V{v[0], v[1], v[2], v[3]};
-    }
+    for (int g = 1; g < min(groups, more); g++) sum += sums[g * lanes + place];
     float *to = a.dtable + row * a.dtable_stride + col;
     for (int j = 0; j < min(4, a.channels - col); j++) to[j] = (a.accumulate ? to[j] : 0.0f) + a.scale * sum[j];
 }
@@ -324,10 +359,12 @@ int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream)
 {
     tessel_embedding aa = a;
     DropLaunch dd = d;
-    void *args[] = {&aa, &dd};
-    const int64_t lanes = a.tokens * (((int64_t)a.channels + 7) / 8);
-#define KERNEL(T) ((const void *)embed_kernel<T>)
-    return launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)((lanes + kThreads - 1) / kThreads)), dim3(kThreads), args, 0, (hipStream_t)stream));
+    const int rows = span_rows(a.type, a.tokens, a.channels, d);
+    SpanShape s = span_shape(a.tokens, a.channels, rows);
+    void *args[] = {&aa, &dd, &s.lanes};
+#define KERNEL(T) (s.wide ? rows == 4 ? (const void *)embed_kernel<T, true, 4> : (const void *)embed_kernel<T, true, 1> \
+                          : rows == 4 ? (const void *)embed_kernel<T, false, 4> : (const void *)embed_kernel<T, false, 1>)
+    return launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3(s.groups), dim3(kThreads), args, 0, (hipStream_t)stream));
 #undef KERNEL
 }
 
@@ -340,21 +377,34 @@ static EmbedLaunch embed_launch(const tessel_embedding &a)
     l.bins = (int)(((int64_t)a.rows + (1 << l.shift) - 1) >> l.shift);
     l.lanes = 8;
     while (l.lanes < 256 && 8 * l.lanes < a.channels) l.lanes *= 2;
-    // places a run: few enough that the runs fill the GPU, and that there are at most 2048 of them
-    const int64_t threads = a.tokens * (((int64_t)a.channels + 7) / 8);
+    l.tiles = (int)(((int64_t)a.channels + 8 * l.lanes - 1) / (8 * l.lanes));
+    l.part = ((int64_t)a.channels + 7) / 8 * 8;
+    // places a run: few enough that the runs fill the GPU, and that there are at most 1024 of them
+    const int64_t threads = a.tokens * (l.part / 8);
     l.run = 8;
-    while (l.run < threads >> 18 || (int64_t)l.run * 2048 < a.tokens) l.run *= 2;
+    while (l.run < threads >> 17 || (int64_t)l.run * 1024 < a.tokens) l.run *= 2;
     l.runs = (int)((a.tokens + l.run - 1) / l.run);
+    l.sum_groups = (uint32_t)((l.runs + kThreads / l.lanes - 1) / (kThreads / l.lanes) * l.tiles);
+    l.fill_lanes = 1;
+    while (l.fill_lanes < 64 && 4 * (int)l.fill_lanes < a.channels) l.fill_lanes *= 2;
+    l.fill_rows = (uint32_t)std::max(1, kFill / a.channels);
+    l.fill_pieces = (uint32_t)((a.channels + kFill - 1) / kFill);
     return l;
 }
 
 static size_t whole_chunks(int64_t words) { return (size_t)(words + 3) / 4 * 4; }
 static size_t counts_of(const tessel_embedding &a, const EmbedLaunch &l) { return a.accumulate ? 0 : whole_chunks((int64_t)l.bins << l.shift); }
+// workgroups of sum_kernel
+static int64_t sum_groups(const tessel_embedding &a, const EmbedLaunch &l)
+{
+    return l.sum_groups + (a.accumulate ? 0 : (a.rows + (int64_t)l.fill_rows - 1) / l.fill_rows * l.fill_pieces);
+}
+bool embed_launchable(const tessel_embedding &a) { return sum_groups(a, embed_launch(a)) <= UINT32_MAX / kThreads; }
 
 size_t embed_workspace(const tessel_embedding &a)
 {
     const EmbedLaunch l = embed_launch(a);
-    return 4 * (2 * whole_chunks(a.tokens) + 4 + counts_of(a, l) + whole_chunks((int64_t)l.runs * 2 * a.channels));
+    return 4 * (2 * whole_chunks(a.tokens) + 4 + counts_of(a, l) + (size_t)l.runs * 2 * l.part);
 }
 
 int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *workspace, void *stream)
@@ -369,18 +419,17 @@ int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *
     void *args[] = {&l};
     const void *sort = a.index_type == TESSEL_I64 ? (const void *)sort_kernel<int64_t> : (const void *)sort_kernel<int32_t>;
     int e = launched(hipLaunchKernel(sort, dim3(1u << l.shift), dim3(kSortThreads), args, 0, (hipStream_t)stream));
-    if (e == 0 && l.runs > 0) {
-        const int each = kThreads / l.lanes;
-#define KERNEL(T) (a.channels < 8 ? (const void *)sum_kernel<T, true> : (const void *)sum_kernel<T, false>)
-        const dim3 grid((unsigned)((l.runs + each - 1) / each), (unsigned)(((int64_t)a.channels + 8 * l.lanes - 1) / (8 * l.lanes)));
-        e = launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), grid, dim3(kThreads), args, 0, (hipStream_t)stream));
+    const int64_t groups = sum_groups(a, l);
+#define KERNEL(T) (l.lanes >= 64 ? (const void *)sum_kernel<T, true, false> : (const void *)sum_kernel<T, false, true>)
+    if (e == 0 && groups > 0) e = launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)groups), dim3(kThreads), args, 0, (hipStream_t)stream));
 #undef KERNEL
+    if (e == 0 && l.runs > 1) {
+        int lanes = 16, tiles;
+        while (lanes < 256 && 4 * lanes < a.channels) lanes *= 2;
+        tiles = (int)(((int64_t)a.channels + 4 * lanes - 1) / (4 * lanes));
+        void *more[] = {&l, &lanes, &tiles};
+        e = launched(hipLaunchKernel((const void *)join_kernel, dim3((unsigned)(l.runs * tiles)), dim3(kSortThreads), more, 0, (hipStream_t)stream));
     }
-    int tiles = (int)(((int64_t)a.channels + 8 * l.lanes - 1) / (8 * l.lanes)), joins = l.runs > 1 ? l.runs * tiles : 0;
-    const int fills = a.accumulate ? 0 : (int)(a.rows / kSortWaves + 1 < 4096 ? a.rows / kSortWaves + 1 : 4096);
-    void *more[] = {&l, &joins, &tiles};
-    if (e == 0 && joins + fills > 0)
-        e = launched(hipLaunchKernel((const void *)join_kernel, dim3((unsigned)(joins + fills)), dim3(kSortThreads), more, 0, (hipStream_t)stream));
     return e;
 }
 
