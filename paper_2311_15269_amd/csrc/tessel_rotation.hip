@@ -21,6 +21,7 @@ struct RotateLaunch {
     int32_t  steps_q, steps;     // of those, for the queries, and for all heads of a token
     int32_t  splits;             // waves that share a token's steps
     int64_t  units;              // waves' turns in all
+    float    share;              // 1 / dim
 };
 
 template <typename T, int V> struct Some {
@@ -30,14 +31,16 @@ template <typename T> struct Some<T, 1> {
     typedef T type;
 };
 
-// sum over the group of lanes; all of them get the same bits
+// sum over the group of lanes; all of them get the same bits.  GROUP: 2^GROUP lanes, or as many as `group` says
 template <int CTRL>
 __device__ __forceinline__ float plus_lane(float v)
 {
     return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 15, 15, true));
 }
+template <int GROUP>
 __device__ __forceinline__ float group_sum(float v, int group)
 {
+    if (GROUP >= 0) group = GROUP;
     if (group > 0) v = plus_lane<0xB1>(v);                       // neighbours
     if (group > 1) v = plus_lane<0x4E>(v);                       // pairs of a quad
     if (group > 2) v = plus_lane<0x141>(v);                      // quads of eight lanes, mirrored
@@ -45,6 +48,13 @@ __device__ __forceinline__ float group_sum(float v, int group)
     if (group > 4) v += __shfl_xor(v, 16);
     if (group > 5) v += __shfl_xor(v, 32);
     return v;
+}
+
+// 1 / sqrt(v) by the instruction (one step of rounding off), which takes subnormal numbers for nought
+__device__ __forceinline__ float over_root(float v)
+{
+    const bool small = v < 0x1p-96f;
+    return __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v) * (small ? 0x1p32f : 1.0f);
 }
 
 // sines and cosines of a wave's tokens, for all pairs of a head (those that do not turn: by no angle)
@@ -71,7 +81,7 @@ __device__ __forceinline__ void angles(const tessel_rotation &a, int64_t token, 
 template <int V, int CHUNKS>
 struct Mine {
     int  first[CHUNKS], second[CHUNKS], pair[CHUNKS];
-    bool on[CHUNKS];
+    bool on[CHUNKS], turns[CHUNKS];
     __device__ __forceinline__ Mine(const tessel_rotation &a, int lane, int lanes)
     {
         const int chunks = a.dim / (2 * V), half = a.turning / 2;
@@ -80,7 +90,8 @@ struct Mine {
             const int c = lane + k * lanes;
             on[k] = c < chunks;
             pair[k] = V * min(c, chunks - 1);
-            const bool apart = pair[k] < half && !a.neighbours;
+            turns[k] = pair[k] < half;
+            const bool apart = turns[k] && !a.neighbours;
             first[k] = apart ? pair[k] : 2 * pair[k];
             second[k] = apart ? pair[k] + half : 2 * pair[k] + V;
         }
@@ -146,11 +157,37 @@ struct Turn {
     }
 };
 
-// the pointer to a head of a token, and its stride, by element
-template <typename T>
-__device__ __forceinline__ T *head_at(const tessel_heads &h, int64_t token, int head) { return (T *)h.data + token * h.token_stride + head * h.head_stride; }
+// Where a lane's chunks of a tensor's heads are: those of its first head of a token, and the way from one step's to the next.  A lane that has no head in
+// the last step has the one before it again, or in the first the last head.
+template <typename T, int CHUNKS>
+struct Chunks {
+    T      *p[CHUNKS][2];
+    int64_t by;
+    template <int V>
+    __device__ __forceinline__ void set(const tessel_heads &h, int64_t token, int head, const Mine<V, CHUNKS> &mine, int heads)
+    {
+        T *z = (T *)h.data + token * h.token_stride + head * h.head_stride;
+        by = h.head_stride << heads;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; k++) {
+            p[k][0] = z + mine.first[k];
+            p[k][1] = z + mine.second[k];
+        }
+    }
+    // the way to step s; `full`: every lane has a head there
+    __device__ __forceinline__ int64_t way(int s, bool full, bool there) const { return full || there ? s * by : max(s - 1, 0) * by; }
+};
 
-template <typename T, int V, int CHUNKS>
+// eight values or fewer as they are in memory, noughts where they do not count
+template <typename T, int V>
+__device__ __forceinline__ void take(float *v, const typename Some<T, V>::type &x, bool counts)
+{
+    spread<T, V>(v, x);
+#pragma unroll
+    for (int j = 0; j < V; j++) v[j] = counts ? v[j] : 0.0f;
+}
+
+template <typename T, int V, int CHUNKS, int GROUP>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateLaunch l)
 {
     __shared__ __attribute__((aligned(16))) float table[kWaves][2][64 * V * CHUNKS];
@@ -170,36 +207,43 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateLaunch l)
         get<V>(c[k], table[wave][0] + which * (a.dim / 2) + mine.pair[k]);
         get<V>(s[k], table[wave][1] + which * (a.dim / 2) + mine.pair[k]);
     }
-    for (int step = at.begin; step < at.end; step++) {
-        const bool key = step >= l.steps_q;
-        const int n = ((key ? step - l.steps_q : step) << l.heads) + head, all = key ? a.kv_heads : a.heads;
-        const T *z = head_at<const T>(key ? a.k : a.q, token, min(n, all - 1));
+    Chunks<const T, CHUNKS> z;
+    Chunks<T, CHUNKS> o;
+    for (int i = at.begin; i < at.end; i++) {
+        const bool key = i >= l.steps_q;
+        const int step = key ? i - l.steps_q : i, all = key ? a.kv_heads : a.heads;
+        const bool full = (step + 1) << l.heads <= all, counts = full || (step << l.heads) + head < all;
+        if (i == at.begin || i == l.steps_q) {
+            z.template set<V>(key ? a.k : a.q, token, min(head, all - 1), mine, l.heads);
+            o.template set<V>(key ? a.k_out : a.q_out, token, min(head, all - 1), mine, l.heads);
+            if (a.wq) {
+                const float *from = key ? a.wk : a.wq;
+#pragma unroll
+                for (int k = 0; k < CHUNKS; k++) {
+                    get<V>(w[k][0], from + mine.first[k]);
+                    get<V>(w[k][1], from + mine.second[k]);
+                }
+            }
+        }
+        const int64_t way = z.way(step, full, counts), back = o.way(step, full, counts);
         float x[CHUNKS][V], y[CHUNKS][V], sum = 0;
         typename Some<T, V>::type rx[CHUNKS], ry[CHUNKS];
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            rx[k] = *(const typename Some<T, V>::type *)(z + mine.first[k]);
-            ry[k] = *(const typename Some<T, V>::type *)(z + mine.second[k]);
-        }
-        if (a.wq && (step == at.begin || step == l.steps_q)) {
-            const float *from = key ? a.wk : a.wq;
-#pragma unroll
-            for (int k = 0; k < CHUNKS; k++) {
-                get<V>(w[k][0], from + mine.first[k]);
-                get<V>(w[k][1], from + mine.second[k]);
-            }
+            rx[k] = *(const typename Some<T, V>::type *)(z.p[k][0] + way);
+            ry[k] = *(const typename Some<T, V>::type *)(z.p[k][1] + way);
         }
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            spread<T, V>(x[k], rx[k]);
-            spread<T, V>(y[k], ry[k]);
+            take<T, V>(x[k], rx[k], mine.on[k]);
+            take<T, V>(y[k], ry[k], mine.on[k]);
         }
         if (a.wq) {
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
-                for (int j = 0; j < V; j++) sum += mine.on[k] ? x[k][j] * x[k][j] + y[k][j] * y[k][j] : 0.0f;
-            const float over = 1.0f / sqrtf(group_sum(sum, l.group) / a.dim + a.eps);
+                for (int j = 0; j < V; j++) sum += x[k][j] * x[k][j] + y[k][j] * y[k][j];
+            const float over = over_root(group_sum<GROUP>(sum, l.group) * l.share + a.eps);
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
@@ -208,19 +252,18 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateLaunch l)
                     y[k][j] *= over * w[k][1][j];
                 }
         }
-        T *o = head_at<T>(key ? a.k_out : a.q_out, token, min(n, all - 1));
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            turn<V, 1>(x[k], y[k], c[k], s[k], a.neighbours && mine.pair[k] < a.turning / 2);
-            if (there && n < all && mine.on[k]) {
-                put<T, V>(o + mine.first[k], x[k]);
-                put<T, V>(o + mine.second[k], y[k]);
+            if (mine.turns[k]) turn<V, 1>(x[k], y[k], c[k], s[k], a.neighbours);
+            if (there && counts && mine.on[k]) {
+                put<T, V>(o.p[k][0] + back, x[k]);
+                put<T, V>(o.p[k][1] + back, y[k]);
             }
         }
     }
 }
 
-template <typename T, int V, int CHUNKS>
+template <typename T, int V, int CHUNKS, int GROUP>
 __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch l)
 {
     __shared__ __attribute__((aligned(16))) float table[kWaves][2][64 * V * CHUNKS];
@@ -241,44 +284,53 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
             get<V>(c[k], table[wave][0] + which * (a.dim / 2) + mine.pair[k]);
             get<V>(s[k], table[wave][1] + which * (a.dim / 2) + mine.pair[k]);
         }
-        for (int step = at.begin; step < at.end; step++) {
-            const bool key = step >= l.steps_q;
-            const int n = ((key ? step - l.steps_q : step) << l.heads) + head, all = key ? a.kv_heads : a.heads;
-            const bool mine_too = there && n < all;
-            const T *z = head_at<const T>(key ? a.k : a.q, token, min(n, all - 1)), *g = head_at<const T>(key ? a.dk_out : a.dq_out, token, min(n, all - 1));
+        Chunks<const T, CHUNKS> z, g;
+        Chunks<T, CHUNKS> o;
+        for (int i = at.begin; i < at.end; i++) {
+            const bool key = i >= l.steps_q;
+            const int step = key ? i - l.steps_q : i, all = key ? a.kv_heads : a.heads;
+            const bool full = (step + 1) << l.heads <= all, counts = full || (step << l.heads) + head < all;
+            if (i == at.begin || i == l.steps_q) {
+                z.template set<V>(key ? a.k : a.q, token, min(head, all - 1), mine, l.heads);
+                g.template set<V>(key ? a.dk_out : a.dq_out, token, min(head, all - 1), mine, l.heads);
+                o.template set<V>(key ? a.dk : a.dq, token, min(head, all - 1), mine, l.heads);
+                if (a.wq) {
+                    const float *from = key ? a.wk : a.wq;
+#pragma unroll
+                    for (int k = 0; k < CHUNKS; k++) {
+                        get<V>(w[k][0], from + mine.first[k]);
+                        get<V>(w[k][1], from + mine.second[k]);
+                    }
+                }
+            }
+            const int64_t way = z.way(step, full, counts), down = g.way(step, full, counts), back = o.way(step, full, counts);
             float x[CHUNKS][V], y[CHUNKS][V], dx[CHUNKS][V], dy[CHUNKS][V], sum = 0;
             typename Some<T, V>::type rx[CHUNKS], ry[CHUNKS], gx[CHUNKS], gy[CHUNKS];
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++) {
-                rx[k] = *(const typename Some<T, V>::type *)(z + mine.first[k]);
-                ry[k] = *(const typename Some<T, V>::type *)(z + mine.second[k]);
-                gx[k] = *(const typename Some<T, V>::type *)(g + mine.first[k]);
-                gy[k] = *(const typename Some<T, V>::type *)(g + mine.second[k]);
+                rx[k] = *(const typename Some<T, V>::type *)(z.p[k][0] + way);
+                ry[k] = *(const typename Some<T, V>::type *)(z.p[k][1] + way);
+                gx[k] = *(const typename Some<T, V>::type *)(g.p[k][0] + down);
+                gy[k] = *(const typename Some<T, V>::type *)(g.p[k][1] + down);
             }
-            if (a.wq && (step == at.begin || step == l.steps_q)) {
-                const float *from = key ? a.wk : a.wq;
-#pragma unroll
-                for (int k = 0; k < CHUNKS; k++) {
-                    get<V>(w[k][0], from + mine.first[k]);
-                    get<V>(w[k][1], from + mine.second[k]);
-                }
-            }
+            // (heads and channels that are not there are noughts, which add nothing to the gradients of w)
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++) {
-                spread<T, V>(x[k], rx[k]);
-                spread<T, V>(y[k], ry[k]);
-                spread<T, V>(dx[k], gx[k]);
-                spread<T, V>(dy[k], gy[k]);
-                turn<V, -1>(dx[k], dy[k], c[k], s[k], a.neighbours && mine.pair[k] < a.turning / 2);
+                const bool mine_too = there && counts && mine.on[k];
+                take<T, V>(x[k], rx[k], mine_too);
+                take<T, V>(y[k], ry[k], mine_too);
+                take<T, V>(dx[k], gx[k], mine_too);
+                take<T, V>(dy[k], gy[k], mine_too);
+                if (mine.turns[k]) turn<V, -1>(dx[k], dy[k], c[k], s[k], a.neighbours);
             }
             if (a.wq) {
 #pragma unroll
                 for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
-                    for (int j = 0; j < V; j++) sum += mine.on[k] ? x[k][j] * x[k][j] + y[k][j] * y[k][j] : 0.0f;
-                const float over = 1.0f / sqrtf(group_sum(sum, l.group) / a.dim + a.eps);
+                    for (int j = 0; j < V; j++) sum += x[k][j] * x[k][j] + y[k][j] * y[k][j];
+                float over = over_root(group_sum<GROUP>(sum, l.group) * l.share + a.eps);
+                over = there && counts ? over : 0.0f;
                 sum = 0;
-                // (heads and channels that are not there count nothing)
                 const auto add = [&](float (&to)[CHUNKS][2][V]) {
 #pragma unroll
                     for (int k = 0; k < CHUNKS; k++)
@@ -286,16 +338,16 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
                         for (int j = 0; j < V; j++) {
                             x[k][j] *= over;
                             y[k][j] *= over;
-                            to[k][0][j] += mine_too ? dx[k][j] * x[k][j] : 0.0f;
-                            to[k][1][j] += mine_too ? dy[k][j] * y[k][j] : 0.0f;
+                            to[k][0][j] += dx[k][j] * x[k][j];
+                            to[k][1][j] += dy[k][j] * y[k][j];
                             dx[k][j] *= w[k][0][j];
                             dy[k][j] *= w[k][1][j];
-                            sum += mine.on[k] ? dx[k][j] * x[k][j] + dy[k][j] * y[k][j] : 0.0f;
+                            sum += dx[k][j] * x[k][j] + dy[k][j] * y[k][j];
                         }
                 };
                 if (key) add(dw[1]);
                 else add(dw[0]);
-                const float mean = group_sum(sum, l.group) / a.dim;
+                const float mean = group_sum<GROUP>(sum, l.group) * l.share;
 #pragma unroll
                 for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
@@ -304,12 +356,11 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
                         dy[k][j] = over * (dy[k][j] - y[k][j] * mean);
                     }
             }
-            T *o = head_at<T>(key ? a.dk : a.dq, token, min(n, all - 1));
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++)
-                if (mine_too && mine.on[k]) {
-                    put<T, V>(o + mine.first[k], dx[k]);
-                    put<T, V>(o + mine.second[k], dy[k]);
+                if (there && counts && mine.on[k]) {
+                    put<T, V>(o.p[k][0] + back, dx[k]);
+                    put<T, V>(o.p[k][1] + back, dy[k]);
                 }
         }
     }
@@ -337,31 +388,34 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
     }
 }
 
-// sums of the workgroups' parts: 64 channels a workgroup, sixteen waves over every sixteenth part each
+// sums of the workgroups' parts: sixteen channels a workgroup, four parts a wave at a time
 __global__ __launch_bounds__(1024) void rotate_sum_kernel(RotateLaunch l)
 {
-    __shared__ float sums[16][64];
+    __shared__ float sums[16][16];
     const tessel_rotation &a = l.a;
-    const int which = blockIdx.y, lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane, group = threadIdx.x >> 6;
+    const int which = blockIdx.y, lane = threadIdx.x & 63, place = lane & 15, col = blockIdx.x * 16 + place, wave = threadIdx.x >> 6;
     float sum = 0;
     if (col < a.dim)
 #pragma unroll 8
-        for (int p = group; p < l.num_parts; p += 16) sum += l.parts[((int64_t)p * 2 + which) * a.dim + col];
-    sums[group][lane] = sum;
+        for (int p = wave * 4 + (lane >> 4); p < l.num_parts; p += 64) sum += l.parts[((int64_t)p * 2 + which) * a.dim + col];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (lane < 16) sums[wave][place] = sum;
     __syncthreads();
-    if (group != 0 || col >= a.dim) return;
+    if (threadIdx.x >= 16 || col >= a.dim) return;
     sum = 0;
 #pragma unroll
-    for (int g = 0; g < 16; g++) sum += sums[g][lane];
+    for (int w = 0; w < 16; w++) sum += sums[w][place];
     float *out = (which == 0 ? a.dwq : a.dwk) + col;
     *out = a.accumulate ? *out + sum : sum;
 }
 
-// pairs a lane: eight or four where no chunk of them lies across the end of those that turn, else one
+// Pairs a lane: four where no chunk of them lies across the end of those that turn, else one.  (Eight leave too few registers: 8192 tokens of 32 + 8 heads of
+// 128 bf16 66 instead of 56 us backward, 33 forward either way.)
 static int values_of(const tessel_rotation &a)
 {
     const int turns = a.turning / 2, stays = (a.dim - a.turning) / 2;
-    return turns % 8 == 0 && stays % 8 == 0 ? 8 : turns % 4 == 0 && stays % 4 == 0 ? 4 : 1;
+    return turns % 4 == 0 && stays % 4 == 0 ? 4 : 1;
 }
 
 static RotateLaunch rotate_launch(const tessel_rotation &a)
@@ -379,6 +433,7 @@ static RotateLaunch rotate_launch(const tessel_rotation &a)
     l.splits = (int)std::min<int64_t>(l.steps, std::max<int64_t>(1, 4096 / std::max<int64_t>(1, groups)));
     l.splits = (l.steps + (l.steps + l.splits - 1) / l.splits - 1) / ((l.steps + l.splits - 1) / l.splits);       // (none without a step)
     l.units = groups * l.splits;
+    l.share = 1.0f / a.dim;
     return l;
 }
 
@@ -387,9 +442,10 @@ int rotate_parts(const tessel_rotation &a) { return (int)std::min<int64_t>((rota
 template <typename T>
 static const void *rotate_of(const tessel_rotation &a, bool back)
 {
-#define PICK(V, K) (back ? (const void *)rotate_backward_kernel<T, V, K> : (const void *)rotate_kernel<T, V, K>)
-    const int v = values_of(a);
-    return v == 8 ? PICK(8, 1) : v == 4 ? PICK(4, 1) : a.dim > 128 ? PICK(1, 2) : PICK(1, 1);
+#define PICK(V, K, G) (back ? (const void *)rotate_backward_kernel<T, V, K, G> : (const void *)rotate_kernel<T, V, K, G>)
+    // (heads of 72 to 128 and of 40 to 64 channels in fours without a branch for each step of their sums)
+    if (values_of(a) == 4) return a.dim > 128 || a.dim <= 32 ? PICK(4, 1, -1) : a.dim > 64 ? PICK(4, 1, 4) : PICK(4, 1, 3);
+    return a.dim > 128 ? PICK(1, 2, -1) : PICK(1, 1, -1);
 #undef PICK
 }
 static const void *rotate_of(const tessel_rotation &a, bool back)
@@ -413,7 +469,7 @@ int launch_rotate_backward(const tessel_rotation &a, float *parts, void *stream)
     int e = 0;
     if (l.num_parts > 0) e = launched(hipLaunchKernel(rotate_of(a, true), dim3((unsigned)l.num_parts), dim3(kThreads), args, 0, (hipStream_t)stream));
     if (e == 0 && a.wq)
-        e = launched(hipLaunchKernel((const void *)rotate_sum_kernel, dim3((unsigned)((a.dim + 63) / 64), 2), dim3(1024), args, 0, (hipStream_t)stream));
+        e = launched(hipLaunchKernel((const void *)rotate_sum_kernel, dim3((unsigned)((a.dim + 15) / 16), 2), dim3(1024), args, 0, (hipStream_t)stream));
     return e;
 }
 
