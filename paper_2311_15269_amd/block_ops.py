@@ -241,7 +241,22 @@ class Packing:
         binding._check(lib.tessel_packing_table_bytes(h, C.byref(n)))
         self._table = torch.empty(n.value, dtype=torch.uint8, device="cuda" if device is None else device)
         self._made_on = _stream(self._table)
+        self._positions = None
         binding._check(lib.tessel_packing_bind(h, self._table.data_ptr(), n.value, self._made_on))
+
+    @property
+    def positions(self):
+        """each token's place in its sequence, as rotate() takes it: int32 [tokens], made at the first use, which so is not for a stream that is being
+        captured; noughts for tokens of no sequence"""
+        if self._positions is None:
+            import torch
+            places = torch.zeros(self.tokens, dtype=torch.int32)
+            begin = 0
+            for n in self.lengths:
+                places[begin:begin + n] = torch.arange(n, dtype=torch.int32)
+                begin += n
+            self._positions = places.to(self._table.device)
+        return self._positions
 
     def close(self):
         if getattr(self, "_h", None) and _lib is not None:
@@ -603,18 +618,19 @@ def frequencies(turning, base=10000.0, device=None):
 def _describe_rotation(q, k, positions, frequency, wq, wk, eps, neighbours):
     import torch
     _on_gpu(q, ("tokens", "heads", "dim"))
-    _on_gpu(k, ("tokens", "heads", "dim"))
+    if k.dim() != 3 or k.shape[1] > MOST:
+        _refuse("expected [tokens, heads, dim], got %s" % (tuple(k.shape),))
     n, heads, dim = q.shape
-    kv_heads = k.shape[1]
+    kv_heads, pairs = k.shape[1], frequency.numel()
     _same(q, (n, kv_heads, dim), k)
     if frequency.dtype is not torch.float64 or frequency.dim() != 1 or not frequency.is_contiguous() or frequency.get_device() != q.get_device():
         _refuse("frequencies are contiguous 64-bit numbers on %s" % q.device)
-    if 2 * frequency.shape[0] > dim:
-        _refuse("%d pairs of %d channels" % (frequency.shape[0], dim))
+    if 2 * pairs > dim:
+        _refuse("%d pairs of %d channels" % (pairs, dim))
     if (wq is None) != (wk is None):
         _refuse("weights for both, queries and keys, or for neither")
     kind, at = _index(positions, n, q)
-    return (_type(q), kind, heads, kv_heads, dim, 2 * frequency.shape[0], 1 if neighbours else 0, eps, n, at, frequency.data_ptr(),
+    return (_type(q), kind, heads, kv_heads, dim, 2 * pairs, 1 if neighbours else 0, eps, n, at, frequency.data_ptr(),
             None if wq is None else _vector(wq, dim, q), None if wk is None else _vector(wk, dim, q), *_heads(q), *_heads(k))
 
 
@@ -647,8 +663,12 @@ def rotate_backward(dq_out, dk_out, q, k, positions, frequency, wq=None, wk=None
         _same(q, k.shape, dk)
     dwq = dwk = None
     to = (None, None)
-    if wq is not None:
-        dwq, dwk = q.new_empty((2, dim), dtype=torch.float32).unbind(0) if into is None else into
+    if wq is not None and into is None:
+        new = q.new_empty((2, dim), dtype=torch.float32)
+        dwq, dwk = new.unbind(0)
+        to = (new.data_ptr(), new.data_ptr() + 4 * dim)
+    elif wq is not None:
+        dwq, dwk = into
         to = (_vector(dwq, dim, q), _vector(dwk, dim, q))
     a = _FlatRotation(*described, None, 0, 0, None, 0, 0, *_heads(dq_out), *_heads(dk_out), *_heads(dq), *_heads(dk), *to, 0 if into is None else 1)
     size = C.c_size_t()

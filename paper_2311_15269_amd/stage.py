@@ -1,7 +1,9 @@
 """A transformer stage of a pipeline, trained in the order that the schedule search finds for it.
 
 `Stage` is one layer -- attention over packed sequences and a gated block inside, each between the norms around it -- whose
-forward and backward passes are made of block_ops and plain matrix products.  It keeps its inputs to the products in 8 bits
+forward and backward passes are made of block_ops and plain matrix products.  With `turning`, its queries and keys have norms of
+their own and turn by position; with `rate`, dropout follows its attention and its gated part.  `Entry` is the block in front of the first stage, an embedding
+spread over devices by shards of the vocabulary.  A stage keeps its inputs to the products in 8 bits
 (or, for comparison, everything in 16, with the gated activation by torch's own operations), which is the activation memory m of its blocks.  `plan` measures t and m of its blocks,
 searches the best window under a memory cap and completes it; `run` executes the blocks of that schedule on one GPU, every
 simulated device holding a stage of its own, and sums the weights' gradients over the micro-batches.
@@ -30,9 +32,10 @@ def _activation(kind, z):
 
 class Stage:
     """Weights in 16 bits, parameters of the norms and all gradients in 32.  Micro-batches are told apart by a number; what a
-    forward pass keeps goes away with its backward pass.  `small`: 8-bit checkpoints."""
+    forward pass keeps goes away with its backward pass.  `small`: 8-bit checkpoints.  `turning`: channels of a head that turn by position (0: no
+    norms of queries and keys either).  `rate`: of dropout, whose masks go by `seed`, `layer` and the micro-batch's number."""
 
-    def __init__(self, channels, heads, kv_heads, inner, generator, dtype, small=True, scale=1.0, act="silu"):
+    def __init__(self, channels, heads, kv_heads, inner, generator, dtype, small=True, scale=1.0, act="silu", turning=0, rate=0.0, seed=0, layer=0):
         import torch
         self.heads, self.kv_heads, self.dim = heads, kv_heads, channels // heads
         self.small, self.scale, self.act = small, scale, act
@@ -49,7 +52,38 @@ class Stage:
         self.norms = [{"post": vector(1.0), "gate": vector(0.5), "pre": vector(1.0)} for _ in range(2)]
         self.gradients = {k: torch.zeros(w.shape, device="cuda") for k, w in self.weights.items()}
         self.norm_gradients = [{k: torch.zeros_like(v) for k, v in n.items()} for n in self.norms]
+        self.turning, self.rate, self.seed, self.layer = turning, rate, seed, layer
+        self.head_norms, self.head_gradients = None, None
+        if turning:
+            self.frequency = block_ops.frequencies(turning)
+            self.head_norms = tuple(torch.ones(self.dim, device="cuda") for _ in range(2))
+            self.head_gradients = tuple(torch.zeros(self.dim, device="cuda") for _ in range(2))
         self.kept = {}
+
+    def _drop(self, y, number, which):
+        """dropout of what the attention (which 0) or the gated part (1) put out for a micro-batch, and of its gradient"""
+        if not self.rate:
+            return y
+        return block_ops.dropout(y, block_ops.Dropout(self.rate, self.seed, (number & 0xFFFFFFFF) << 32 | self.layer << 1 | which))
+
+    def _turn(self, packing, qkv):
+        """queries, keys and values as the attention takes them"""
+        q, k, v = qkv.split((self.heads, self.kv_heads, self.kv_heads), 1)
+        if self.turning:
+            q, k = block_ops.rotate(q, k, packing.positions, self.frequency, *self.head_norms)
+        return q, k, v
+
+    def _turn_backward(self, packing, qkv, dq, dk, dv):
+        """the gradient of qkv from those of what _turn gave"""
+        import torch
+        if not self.turning:
+            return torch.cat((dq, dk, dv), 1)
+        q, k, _ = qkv.split((self.heads, self.kv_heads, self.kv_heads), 1)
+        d = torch.empty_like(qkv)
+        to = d.split((self.heads, self.kv_heads, self.kv_heads), 1)
+        block_ops.rotate_backward(dq, dk, q, k, packing.positions, self.frequency, *self.head_norms, into=self.head_gradients, out=to[:2])
+        to[2].copy_(dv)
+        return d
 
     # -- one product and the two of its backward pass
     def _add(self, name, dy, x):
@@ -90,12 +124,11 @@ class Stage:
         """the residual stream x and its norm h [tokens, channels] -> the next stage's"""
         w, n = self.weights, x.shape[0]
         qkv = (h @ w["qkv"].t()).view(n, self.heads + 2 * self.kv_heads, self.dim)
-        q, k, v = qkv.split((self.heads, self.kv_heads, self.kv_heads), 1)
-        o, lse = packing.attention(q, k, v)
-        y = o.view(n, -1) @ w["out"].t()
+        o, lse = packing.attention(*self._turn(packing, qkv))
+        y = self._drop(o.view(n, -1) @ w["out"].t(), number, 0)
         r, hr, stats = self._norm(0, x, y)
         a, g, u = self._gated(hr @ w["gate"].t(), hr @ w["up"].t())
-        z = a @ w["down"].t()
+        z = self._drop(a @ w["down"].t(), number, 1)
         r2, h2, stats2 = self._norm(1, r, z)
         self.kept[number] = (packing, x, self._keep(h), qkv, o, lse, y, stats, r, self._keep(hr), g, u, z, stats2)
         return r2, h2
@@ -105,17 +138,17 @@ class Stage:
         packing, x, h, qkv, o, lse, y, stats, r, hr, g, u, z, stats2 = self.kept.pop(number)
         w, n = self.weights, x.shape[0]
         dr, dz = self._norm_backward(1, dr, dh, r, z, stats2)
+        dz = self._drop(dz, number, 1)
         da = dz @ w["down"]
         dg, du, a = self._gated_backward(da, g, u)
         self._add("down", dz, a)
         self._add("gate", dg, hr)
         self._add("up", du, hr)
         dx, dy = self._norm_backward(0, dr, dg @ w["gate"] + du @ w["up"], x, y, stats)
+        dy = self._drop(dy, number, 0)
         self._add("out", dy, o.view(n, -1))
-        q, k, v = qkv.split((self.heads, self.kv_heads, self.kv_heads), 1)
-        import torch
-        dq, dk, dv = packing.attention_backward((dy @ w["out"]).view(o.shape), q, k, v, o, lse)
-        dqkv = torch.cat((dq, dk, dv), 1).view(n, -1)
+        q, k, v = self._turn(packing, qkv)                      # (turned again: less than what keeping them would cost in memory)
+        dqkv = self._turn_backward(packing, qkv, *packing.attention_backward((dy @ w["out"]).view(o.shape), q, k, v, o, lse)).view(n, -1)
         self._add("qkv", dqkv, h)
         return dx, dqkv @ w["qkv"]
 
@@ -123,6 +156,43 @@ class Stage:
         """what a forward pass keeps until its backward pass: m of its block.  (The residual stream that it was given too: the stage that made it does not
         keep it.)"""
         return sum(t.nbytes for t in self.kept[number] if hasattr(t, "nbytes"))
+
+
+class Entry:
+    """The block in front of the first stage: an embedding spread over devices, each of which holds a shard of the vocabulary, dropout, and the norm that the stage
+    reads.  (All shards are on this GPU: what their devices would add up in an all-reduce is added here.)  Gradients are sums in 32 bits."""
+
+    def __init__(self, vocabulary, shards, channels, generator, dtype, rate=0.0, seed=0):
+        import torch
+        self.rows, self.scale, self.rate, self.seed = -(-vocabulary // shards), math.sqrt(channels), rate, seed
+        self.first = list(range(0, vocabulary, self.rows))
+        self.tables = [(torch.randn(min(self.rows, vocabulary - f), channels, generator=generator, device="cuda") * channels ** -0.5).to(dtype) for f in self.first]
+        self.pre = torch.ones(channels, device="cuda")
+        self.gradients = [torch.zeros(t.shape, device="cuda") for t in self.tables]
+        self.pre_gradient = torch.zeros_like(self.pre)
+        self.kept = {}
+
+    def _drop(self, number):
+        return block_ops.Dropout(self.rate, self.seed, (number & 0xFFFFFFFF) << 32 | 0xFFFFFFFF) if self.rate else None
+
+    def forward(self, number, tokens):
+        """tokens [tokens] -> the residual stream and its norm"""
+        drop = self._drop(number)
+        x = None
+        for f, t in zip(self.first, self.tables):
+            part = block_ops.embed(tokens, t, self.scale, f, drop)          # (noughts for the tokens of other shards, with dropout as without)
+            x = part if x is None else x + part
+        _, h, stats = block_ops.residual_norm(x, x, self.pre, scale=0.0)
+        self.kept[number] = (tokens, x, stats)
+        return x, h
+
+    def backward(self, number, dx, dh):
+        """the tables' gradients from those of what forward() gave"""
+        tokens, x, stats = self.kept.pop(number)
+        d = block_ops.residual_norm_backward(dx, dh, x, x, stats, self.pre, scale=0.0, into=(self.pre_gradient, None, None))[1]
+        drop = self._drop(number)
+        for f, g in zip(self.first, self.gradients):
+            block_ops.embed_backward(d, tokens, g.shape[0], self.scale, f, drop, into=g)
 
 
 def measure(stage, packing, x, h):
@@ -141,7 +211,7 @@ def measure(stage, packing, x, h):
         if turn:                                                # (the first pass loads the kernels)
             took[0] += t1 - t0
             took[1] += time.perf_counter() - t1
-    for g in list(stage.gradients.values()) + [v for n in stage.norm_gradients for v in n.values()]:
+    for g in list(stage.gradients.values()) + [v for n in stage.norm_gradients for v in n.values()] + list(stage.head_gradients or ()):
         g.zero_()
     return took[0] / 5, took[1] / 5, size
 
@@ -161,20 +231,23 @@ def plan(devices, seconds, kept, cap, microbatches, max_nr=4):
     return found, done, best.instantiate(microbatches, done["start"])
 
 
-def run(stages, packings, xs, hs, gradient, operations):
-    """Executes a schedule's operations: micro-batch mu of xs, hs through all stages, gradient(mu, r, h) -> (dr, dh) behind the last one, and
-    back.  Returns the gradients of xs and hs.  (All devices share this GPU: a tensor that would be sent is there already.)"""
-    n, last = len(xs), len(stages) - 1
+def run(stages, packings, xs, hs, gradient, operations, entry=None, tokens=None):
+    """Executes a schedule's operations: micro-batch mu of xs, hs (or, with an `entry`, of tokens) through all stages, gradient(mu, r, h) -> (dr, dh) behind
+    the last one, and back.  Returns the gradients of xs and hs.  (All devices share this GPU: a tensor that would be sent is there already.)"""
+    n, last = len(packings), len(stages) - 1
     there, back = {}, {}
     for kind, block, *_ in operations:
         if kind != 0:
             continue
         i, mu = divmod(block, n)
         if i <= last:
-            there[i, mu] = stages[i].forward(mu, packings[mu], *(there.pop((i - 1, mu)) if i else (xs[mu], hs[mu])))
+            first = there.pop((i - 1, mu)) if i else entry.forward(mu, tokens[mu]) if entry else (xs[mu], hs[mu])
+            there[i, mu] = stages[i].forward(mu, packings[mu], *first)
         else:
             i = 2 * last + 1 - i
             back[i, mu] = stages[i].backward(mu, *(back.pop((i + 1, mu)) if i < last else gradient(mu, *there.pop((last, mu)))))
+            if entry and i == 0:
+                entry.backward(mu, *back[i, mu])
     return [back[0, mu] for mu in range(n)]
 
 
@@ -183,18 +256,27 @@ def in_turn(devices, microbatches):
     return [(0, i * microbatches + mu, 0, 0, 0) for mu in range(microbatches) for i in range(2 * devices)]
 
 
-def make(devices, microbatches, lengths, channels, heads, kv_heads, inner, small, seed=0, dtype=None):
+def make(devices, microbatches, lengths, channels, heads, kv_heads, inner, small, seed=0, dtype=None, turning=0, rate=0.0):
     """stages, packings and inputs, the same for the same seed"""
     import torch
     dtype = dtype or torch.bfloat16
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
-    stages = [Stage(channels, heads, kv_heads, inner, gen, dtype, small) for _ in range(devices)]
+    stages = [Stage(channels, heads, kv_heads, inner, gen, dtype, small, turning=turning, rate=rate, seed=seed, layer=i) for i in range(devices)]
     packings = [block_ops.Packing(lengths) for _ in range(microbatches)]
     xs = [torch.randn(sum(lengths), channels, generator=gen, device="cuda").to(dtype) for _ in range(microbatches)]
     one = torch.ones(channels, device="cuda")
     hs = [block_ops.residual_norm(x, torch.zeros_like(x), one)[1] for x in xs]
     return stages, packings, xs, hs
+
+
+def make_entry(microbatches, lengths, channels, vocabulary, shards, seed=0, dtype=None, rate=0.0):
+    """an entry and the tokens of its micro-batches, the same for the same seed"""
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed + 1)
+    entry = Entry(vocabulary, shards, channels, gen, dtype or torch.bfloat16, rate, seed)
+    return entry, [torch.randint(0, vocabulary, (sum(lengths),), generator=gen, device="cuda") for _ in range(microbatches)]
 
 
 def main():
@@ -206,13 +288,17 @@ def main():
     ap.add_argument("--heads", type=int, default=16)
     ap.add_argument("--kv-heads", type=int, default=4)
     ap.add_argument("--lengths", default="1000,37,500,511")
+    ap.add_argument("--turning", type=int, default=0, help="channels of a head that turn by position, behind norms of queries and keys")
+    ap.add_argument("--rate", type=float, default=0.0, help="of dropout")
+    ap.add_argument("--vocabulary", type=int, default=0, help="an embedding of so many tokens in front, a shard on each device")
     a = ap.parse_args()
     lengths = [int(n) for n in a.lengths.split(",")]
     sizes = (a.devices, a.microbatches, lengths, a.channels, a.heads, a.kv_heads, 4 * a.channels)
     unit = sum(lengths) * a.channels                            # a byte a channel
+    more = {"turning": a.turning, "rate": a.rate}
     cap = None
     for small in (False, True):
-        stages, packings, xs, hs = make(*sizes, small)
+        stages, packings, xs, hs = make(*sizes, small, **more)
         forward, backward, kept = measure(stages[0], packings[0], xs[0], hs[0])
         m = -(-kept // unit)
         if cap is None:
@@ -225,11 +311,14 @@ def main():
 
     def gradient(mu, r, h):
         return dr, dr
-    got = run(stages, packings, xs, hs, gradient, operations)
-    again, packings, xs, hs = make(*sizes, True)
-    want = run(again, packings, xs, hs, gradient, in_turn(a.devices, a.microbatches))
+    front = [make_entry(a.microbatches, lengths, a.channels, a.vocabulary, a.devices, rate=a.rate) if a.vocabulary else (None, None) for _ in range(2)]
+    got = run(stages, packings, xs, hs, gradient, operations, *front[0])
+    again, packings, xs, hs = make(*sizes, True, **more)
+    want = run(again, packings, xs, hs, gradient, in_turn(a.devices, a.microbatches), *front[1])
     same = all(torch.equal(p, q) for x, y in zip(got, want) for p, q in zip(x, y))
     same = same and all(torch.equal(s.gradients[k], t.gradients[k]) for s, t in zip(stages, again) for k in s.gradients)
+    if a.vocabulary:
+        same = same and all(torch.equal(p, q) for p, q in zip(front[0][0].gradients, front[1][0].gradients))
     print("%d micro-batches in the order of the schedule (%d operations, makespan %d): gradients %s those of one after the other" % (
         a.microbatches, len(operations), done["makespan"], "equal" if same else "DIFFER from"))
     return 0 if same else 1
