@@ -9,11 +9,15 @@ namespace tessel {
 
 constexpr int kThreads = 256;
 
-// the row of the table that token t takes, -1 if there is none
+// the row of the table that a token takes, -1 if there is none (one comparison: what is below `first` wraps around)
+__device__ __forceinline__ int row_of(const tessel_embedding &a, int64_t token)
+{
+    const uint64_t row = (uint64_t)token - (uint64_t)a.first;
+    return row < (uint64_t)a.rows ? (int)row : -1;
+}
 __device__ __forceinline__ int row_at(const tessel_embedding &a, int64_t t)
 {
-    const int64_t v = a.index_type == TESSEL_I64 ? ((const int64_t *)a.token)[t] : ((const int32_t *)a.token)[t];
-    return v >= a.first && v - a.first < a.rows ? (int)(v - a.first) : -1;
+    return row_of(a, a.index_type == TESSEL_I64 ? ((const int64_t *)a.token)[t] : ((const int32_t *)a.token)[t]);
 }
 
 template <typename T, bool WIDE, int ROWS>
@@ -46,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(tessel_embedding a, Dro
 struct EmbedLaunch {
     tessel_embedding a;
     DropLaunch d;
-    int32_t *place, *row;        // [tokens] sorted: place in the batch, row of the table
+    int32_t *place, *row;        // [tokens + 8] sorted: place in the batch, row of the table
     int32_t *total;              // how many of them
     int32_t *count;              // [buckets][bins], where the gradient is written: tokens of row bin * buckets + bucket
     float   *parts;              // [runs][2][part]: of the row that a run begins within, and of the one that goes on behind it
@@ -61,151 +65,197 @@ struct EmbedLaunch {
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kSubs = 4, kSub = 4 * kSortThreads, kTile = kSubs * kSub;          // a thread takes four places of each part of a tile
 constexpr int kMostBins = 2 * kSortThreads;        // (two workgroups have room on a compute unit)
-
-// rows of the table for a thread's places of the tile at t0, -1 where there is none
-template <typename I>
-__device__ __forceinline__ void tile_rows(const tessel_embedding &a, int64_t t0, int (&v)[kSubs][4])
-{
-    typedef I V __attribute__((ext_vector_type(4), aligned(sizeof(I))));
-    const I *p = (const I *)a.token;
-    V w[kSubs];
-#pragma unroll
-    for (int s = 0; s < kSubs; s++) {
-        const int64_t t = t0 + s * kSub + 4 * threadIdx.x;
-        w[s] = V{(I)-1, (I)-1, (I)-1, (I)-1};
-        if (t + 4 <= a.tokens) {
-            w[s] = *(const V *)(p + t);
-        } else if (t < a.tokens) {
-            w[s][0] = p[t];
-            if (t + 1 < a.tokens) w[s][1] = p[t + 1];
-            if (t + 2 < a.tokens) w[s][2] = p[t + 2];
-        }
-    }
-#pragma unroll
-    for (int s = 0; s < kSubs; s++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int64_t n = w[s][j];
-            v[s][j] = n >= a.first && n - a.first < a.rows ? (int)(n - a.first) : -1;
-        }
-}
+constexpr int kOften = 256;
 
 __device__ __forceinline__ int below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u)); }
 
-// sums over the lanes up to and with this one
-__device__ __forceinline__ int sums_up_to(int x)
+// sums over the lanes up to and with this one, and their largest value so far (whole numbers from 0 on)
+template <typename F>
+__device__ __forceinline__ int up_to(int x, F &&f)
 {
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 15, 15, false));         // of sixteen lanes: one, two, four and eight back
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 15, 15, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 15, 15, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 15, 15, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 10, 15, false));         // the last lane of the sixteen before, to the second and fourth
+    return f(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 12, 15, false));      // of the first half, to the second
+}
+__device__ __forceinline__ int sums_up_to(int x) { return up_to(x, [](int a, int b) { return a + b; }); }
+__device__ __forceinline__ int most_up_to(int x) { return up_to(x, [](int a, int b) { return max(a, b); }); }
+
+// A thread's places of the tile at t0, sixteen bits: those whose row is in the bucket.  `before`: how many are in the buckets before it, added up.  (No read stands in a
+// branch, behind which the compiler would wait for it: behind the last place the last four are read again.)
+template <typename I>
+__device__ __forceinline__ uint32_t tile_places(const EmbedLaunch &l, int64_t t0, uint32_t bucket, int &before)
+{
+    typedef I V __attribute__((ext_vector_type(4), aligned(sizeof(I))));
+    const tessel_embedding &a = l.a;
+    const uint32_t buckets = 1u << l.shift;
+    V w[kSubs];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d);
-        if ((int)(threadIdx.x & 63) >= d) x += y;
+    for (int s = 0; s < kSubs; s++) {
+        const int64_t t = t0 + s * kSub + 4 * (int)threadIdx.x;
+        const I *p = (const I *)a.token + min(t, max(a.tokens - 4, (int64_t)0));
+        if (a.tokens >= 4) w[s] = *(const V *)p;
+        else w[s] = V{p[0], p[min(1, (int)a.tokens - 1)], p[min(2, (int)a.tokens - 1)], (I)-1};
     }
-    return x;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int s = 0; s < kSubs; s++) {
+        const int64_t t = t0 + s * kSub + 4 * (int)threadIdx.x;
+        if (t0 + s * kSub >= a.tokens) break;
+        uint32_t here = 0;
+        int less = 0;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint64_t row = (uint64_t)(int64_t)w[s][j] - (uint64_t)a.first;
+            const uint32_t b = row < (uint64_t)a.rows ? (uint32_t)row & (buckets - 1) : buckets;
+            here |= b == bucket ? 1u << j : 0u;
+            less |= b < bucket ? 1 << j : 0;
+        }
+        if (__any(t + 4 > a.tokens)) {                           // the last places: of those read again, what is not there
+            const int by = a.tokens >= 4 ? (int)min(t - min(t, a.tokens - 4), (int64_t)4) : (int)(t > 0 ? 4 : 0), left = (int)min(max(a.tokens - t, (int64_t)0), (int64_t)4);
+            here = here >> by & ((1u << left) - 1);
+            less = less >> by & ((1 << left) - 1);
+        }
+        before += __popc(less);
+        mine |= here << (4 * s);
+    }
+    return mine;
 }
 
-// A workgroup for each bucket of rows with the same low bits (frequent tokens are neighbours in a vocabulary).  It counts the places of its rows
-// and of the buckets before it, and then goes through the batch once more, a tile at a time, and puts its places where they belong.
+// A workgroup for each bucket of rows with the same low bits (frequent tokens are neighbours in a vocabulary).  It goes through the batch a tile at a time and lists its
+// places in order.  Once to count them by row, and those of the buckets before it; once more to put them where they belong, if not all of them fit the list.
 template <typename I>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(EmbedLaunch l)
 {
     __shared__ int cursor[kMostBins];                            // counts, then the place where the next one of a row goes
-    __shared__ int list[kTile];                                  // this bucket's share of a tile, in order: bin, and place in the tile
+    __shared__ uint16_t list[2][kTile];                          // places behind `base`
     __shared__ int sums[2][kSortWaves], shares[kSubs * kSortWaves];
-    static_assert(kSubs * kSortWaves == 64 && kTile <= 1 << 14, "a lane for each wave's share of a part; 14 bits of a place");
+    static_assert(kSubs * kSortWaves == 64 && kTile <= 1 << 16 && kMostBins <= 1 << 11, "a lane for each wave's share of a part; 16 bits of a place, 11 of a bin");
     const tessel_embedding &a = l.a;
-    const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, bucket = blockIdx.x, mask = (1 << l.shift) - 1;
-    for (int b = thread; b < l.bins; b += kSortThreads) cursor[b] = 0;
-    int before = 0, own = 0, v[kSubs][4];
-    const auto count = [&](const int (&v)[kSubs][4]) {
-#pragma unroll
-        for (int s = 0; s < kSubs; s++)
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                before += v[s][j] >= 0 && (v[s][j] & mask) < bucket ? 1 : 0;
-                if (v[s][j] >= 0 && (v[s][j] & mask) == bucket) {
-                    own++;
-                    atomicAdd(&cursor[v[s][j] >> l.shift], 1);   // (whole numbers: the order does not matter)
-                }
-            }
-    };
-    tile_rows<I>(a, 0, v);
-    __syncthreads();
-    count(v);
-    for (int64_t t0 = kTile; t0 < a.tokens; t0 += kTile) {
-        int w[kSubs][4];
-        tile_rows<I>(a, t0, w);
-        count(w);
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        before += __shfl_xor(before, d);
-        own += __shfl_xor(own, d);
-    }
-    if (lane == 0) {
-        sums[0][wave] = before;
-        sums[1][wave] = own;
-    }
-    __syncthreads();
-    before = own = 0;
-#pragma unroll
-    for (int w = 0; w < kSortWaves; w++) {
-        before += sums[0][w];
-        own += sums[1][w];
-    }
-    if (bucket == mask && thread == 0) *l.total = before + own;
-    if (!a.accumulate)
-        for (int b = thread; b < l.bins; b += kSortThreads) l.count[(int64_t)bucket * l.bins + b] = cursor[b];
-    if (own == 0) return;
-    // where each row's places begin: two bins a thread
-    int c[2], sum = 0;
-#pragma unroll
-    for (int j = 0; j < 2; j++) {
-        c[j] = 2 * thread + j < l.bins ? cursor[2 * thread + j] : 0;
-        sum += c[j];
-    }
-    const int up = sums_up_to(sum);
-    __syncthreads();                                             // (all are done with the counts and sums)
-    if (lane == 63) sums[0][wave] = up;
-    __syncthreads();
-    int at = before + up - sum;
-    for (int w = 0; w < wave; w++) at += sums[0][w];
-#pragma unroll
-    for (int j = 0; j < 2; j++) {
-        if (2 * thread + j < l.bins) cursor[2 * thread + j] = at;
-        at += c[j];
-    }
-    for (int64_t t0 = 0; t0 < a.tokens; t0 += kTile) {
-        if (t0 > 0) tile_rows<I>(a, t0, v);                      // (a batch of one tile is read once)
-        // places before this thread's in its wave: none to four of each thread
+    const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, bucket = blockIdx.x;
+    const bool near = a.tokens <= 1 << 16;                       // (16 bits hold any place)
+    const auto row_in = [&](int64_t base, int place) { return row_of(a, ((const I *)a.token)[base + place]); };
+    // The tile's places of this bucket to list[0] behind its first `listed`, or in place of these if they would not fit; how many there are.  Through barriers:
+    // all are done with an earlier list before it is written, and it is there when this returns.
+    const auto find = [&](int64_t t0, int64_t base, int &listed, int &before) {
+        uint32_t mine = tile_places<I>(l, t0, (uint32_t)bucket, before);
         int to[kSubs];
-        __syncthreads();                                         // (the list and the shares of the tile before are done with)
 #pragma unroll
-        for (int s = 0; s < kSubs; s++) {
-            int n = 0;
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                if (v[s][j] >= 0 && (v[s][j] & mask) != bucket) v[s][j] = -1;
-                n += v[s][j] >= 0 ? 1 : 0;
-            }
+        for (int s = 0; s < kSubs; s++) {                        // none to four of each thread
+            const int n = __popc(mine >> 4 * s & 15u);
             const uint64_t one = __ballot(n & 1), two = __ballot(n & 2), four = __ballot(n & 4);
             to[s] = below(one) + 2 * below(two) + 4 * below(four);
             if (lane == 0) shares[s * kSortWaves + wave] = __popcll(one) + 2 * __popcll(two) + 4 * __popcll(four);
         }
         __syncthreads();
         const int share = shares[lane], through = sums_up_to(share), found = __shfl(through, 63);
+        listed = listed + found <= kTile ? listed : 0;
 #pragma unroll
         for (int s = 0; s < kSubs; s++) {
-            int i = to[s] + __shfl(through - share, s * kSortWaves + wave);
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-                if (v[s][j] >= 0) list[i++] = (v[s][j] >> l.shift) << 14 | (s * kSub + 4 * thread + j);
+            int i = listed + to[s] + __shfl(through - share, s * kSortWaves + wave);
+            for (uint32_t m = mine >> 4 * s & 15u; m; m &= m - 1) list[0][i++] = (uint16_t)(t0 - base + s * kSub + 4 * thread + __builtin_ctz(m));
         }
         __syncthreads();
+        return found;
+    };
+    for (int b = thread; b < l.bins; b += kSortThreads) cursor[b] = 0;
+    int before = 0, own = 0, listed = 0;
+    for (int64_t t0 = 0; t0 < a.tokens; t0 += kTile) {
+        const int64_t base = near ? 0 : t0;
+        if (!near) listed = 0;
+        const int found = find(t0, base, listed, before);
+        for (int first = 0; first < found; first += kSortThreads) {
+            // (whole numbers: the order does not matter.  The first lane's row at once: those of a frequent one would wait for each other at its count)
+            const int i = first + thread, row = i < found ? row_in(base, list[0][listed + i]) : -1, one = __builtin_amdgcn_readfirstlane(row);
+            const int n = __popcll(__ballot(row == one));
+            if (row >= 0 && (row != one || lane == 0)) atomicAdd(&cursor[row >> l.shift], row == one ? n : 1);
+        }
+        own += found;
+        listed += found;
+    }
+    const bool all = near && listed == own;                      // the list holds every place
+    before = sums_up_to(before);
+    if (lane == 63) sums[0][wave] = before;
+    __syncthreads();
+    before = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; w++) before += sums[0][w];
+    if (bucket == (1 << l.shift) - 1 && thread == 0) *l.total = before + own;
+    if (!a.accumulate)
+        for (int b = thread; b < l.bins; b += kSortThreads) l.count[(int64_t)bucket * l.bins + b] = cursor[b];
+    if (own == 0) return;
+    // where each row's places begin: two bins a thread; and the most frequent row
+    int c[2], sum = 0, top = 0;
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+        c[j] = 2 * thread + j < l.bins ? cursor[2 * thread + j] : 0;
+        sum += c[j];
+        top = max(top, min(c[j], (1 << 20) - 1) << 11 | (2 * thread + j));
+    }
+    const int up = sums_up_to(sum);
+    top = most_up_to(top);
+    __syncthreads();                                             // (all are done with the counts and sums)
+    if (lane == 63) {
+        sums[0][wave] = up;
+        sums[1][wave] = top;
+    }
+    __syncthreads();
+    int at = before + up - sum;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; w++) {
+        at += w < wave ? sums[0][w] : 0;
+        top = max(top, sums[1][w]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+        if (2 * thread + j < l.bins) cursor[2 * thread + j] = at;
+        at += c[j];
+    }
+    __syncthreads();
+    // A row of many places: they are put in place by counting alone, and only the others go through the steps below, wave by wave.
+    const int often = top >> 11 >= kOften ? (top & 2047) << l.shift | bucket : -2;
+    int often_at = often >= 0 ? cursor[often >> l.shift] : 0;
+    for (int64_t t0 = 0; t0 < a.tokens; t0 += kTile) {
+        const int64_t base = all ? 0 : t0;
+        int found = own, none = 0, from = 0;
+        if (!all) found = find(t0, base, from, none);
+        int which = 0;
+        if (often >= 0) {
+            int others = 0;
+            for (int first = 0; first < found; first += kSortThreads) {
+                const int i = first + thread, place = i < found ? list[0][i] : 0, row = i < found ? row_in(base, place) : -1;
+                const uint64_t same = __ballot(row == often), rest = __ballot(row >= 0 && row != often);
+                if (lane == 0) {
+                    sums[0][wave] = __popcll(same);
+                    sums[1][wave] = __popcll(rest);
+                }
+                __syncthreads();
+                int to = often_at + below(same), rest_to = others + below(rest);
+#pragma unroll
+                for (int w = 0; w < kSortWaves; w++) {
+                    to += w < wave ? sums[0][w] : 0;
+                    rest_to += w < wave ? sums[1][w] : 0;
+                    often_at += sums[0][w];
+                    others += sums[1][w];
+                }
+                if (row == often) {
+                    l.place[to] = (int)(base + place);
+                    l.row[to] = often;
+                } else if (row >= 0) {
+                    list[1][rest_to] = (uint16_t)place;
+                }
+                __syncthreads();
+            }
+            which = 1;
+            found = others;
+        }
         for (int first = 0; first < found; first += kSortThreads) {
             // a wave's 64 places: how many of the same row come before, and which lane is the first of the row
             const int i = first + thread;
             const bool there = i < found;
-            const int entry = there ? list[i] : 0, bin = entry >> 14;
+            const int place = there ? list[which][i] : 0, row = there ? row_in(base, place) : bucket, bin = row >> l.shift;
             uint64_t same = __ballot(there);
             for (int b = 0; 1 << b < l.bins; b++) {
                 const uint64_t bit = __ballot(bin >> b & 1);
@@ -223,10 +273,11 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(EmbedLaunch l)
             }
             start = __shfl(start, leader);
             if (there) {
-                l.place[start + rank] = (int)(t0 + (entry & (kTile - 1)));
-                l.row[start + rank] = bin << l.shift | bucket;
+                l.place[start + rank] = (int)(base + place);
+                l.row[start + rank] = row;
             }
         }
+        if (all) break;
     }
 }
 
@@ -268,12 +319,24 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
     if constexpr (WIDE) run = __builtin_amdgcn_readfirstlane(run);
     const int col = 8 * (tile * l.lanes + threadIdx.x % l.lanes), total = *l.total;
     const int64_t first = (int64_t)run * l.run;
-    if (run >= l.runs || first >= total || col >= a.channels) return;
+    // eight sorted places at once; behind the last one whatever is there, as some place
+    int r[kAhead], t[kAhead];
+    const auto look = [&](uint32_t i) {
+#pragma unroll
+        for (int j = 0; j < kAhead; j++) {
+            r[j] = l.row[i + j];
+            t[j] = (int)min((uint32_t)l.place[i + j], (uint32_t)a.tokens - 1u);
+        }
+    };
+    if (run >= l.runs) return;
     const uint32_t begin = (uint32_t)first, end = (uint32_t)min(first + l.run, (int64_t)total);
+    look(begin);
+    const int last = l.row[min(first + l.run, a.tokens) - 1], behind = l.row[min(first + l.run, a.tokens - 1)], before = l.row[max(first - 1, (int64_t)0)];
+    if (first >= total || col >= a.channels) return;
     const Draw draw(l.d, col);
-    int row = l.row[begin];
-    bool starts = begin == 0 || l.row[begin - 1] != row;         // (the row's first place is in this run)
-    const bool goes_on = end < (uint32_t)total && l.row[end] == l.row[end - 1];
+    int row = r[0];
+    bool starts = begin == 0 || before != row;                   // (the row's first place is in this run)
+    const bool goes_on = first + l.run < total && behind == last;
     float sum[8] = {};
     const auto flush = [&](bool ends) {
         if (starts && ends) {
@@ -289,13 +352,8 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
         }
     };
     for (uint32_t i = begin; i < end; i += kAhead) {
-        int r[kAhead], t[kAhead];
         typename Eight<T>::type x[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; j++) {
-            r[j] = l.row[min(i + j, end - 1)];
-            t[j] = l.place[min(i + j, end - 1)];
-        }
+        if (i > begin) look(i);
 #pragma unroll
         for (int j = 0; j < kAhead; j++) x[j] = take8<T, NARROW>((const T *)a.d_out.data + t[j] * a.d_out.stride, col, a.channels);
 #pragma unroll
@@ -340,8 +398,13 @@ __global__ __launch_bounds__(kSortThreads) void join_kernel(EmbedLaunch l, int l
         at = l.row[min(i, end)];
     }
     const int groups = kSortThreads / lanes, group = threadIdx.x / lanes, place = threadIdx.x % lanes, col = 4 * (tile * lanes + place);
-    float4v sum = {};
+    float4v sum = {}, old = {};
+    float *to = a.dtable + row * a.dtable_stride + col;
     if (col < a.channels) {
+        if (a.accumulate && group == 0) {                        // (under way beside the parts)
+#pragma unroll
+            for (int j = 0; j < 4; j++) old[j] = to[min(j, a.channels - 1 - col)];
+        }
         const float *own = l.parts + ((int64_t)run * 2 + 1) * l.part + col, *others = own + l.part;      // (behind a run's second part, the next one's first)
         if (group == 0) sum = *(const float4v *)own;
 #pragma unroll 8
@@ -351,8 +414,9 @@ __global__ __launch_bounds__(kSortThreads) void join_kernel(EmbedLaunch l, int l
     __syncthreads();
     if (group > 0 || col >= a.channels) return;
     for (int g = 1; g < min(groups, more); g++) sum += sums[g * lanes + place];
-    float *to = a.dtable + row * a.dtable_stride + col;
-    for (int j = 0; j < min(4, a.channels - col); j++) to[j] = (a.accumulate ? to[j] : 0.0f) + a.scale * sum[j];
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+        if (col + j < a.channels) to[j] = old[j] + a.scale * sum[j];
 }
 
 int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream)
@@ -393,6 +457,7 @@ static EmbedLaunch embed_launch(const tessel_embedding &a)
 }
 
 static size_t whole_chunks(int64_t words) { return (size_t)(words + 3) / 4 * 4; }
+static size_t sorted_of(const tessel_embedding &a) { return whole_chunks(a.tokens + 8); }      // (sum_kernel reads eight at once)
 static size_t counts_of(const tessel_embedding &a, const EmbedLaunch &l) { return a.accumulate ? 0 : whole_chunks((int64_t)l.bins << l.shift); }
 // workgroups of sum_kernel
 static int64_t sum_groups(const tessel_embedding &a, const EmbedLaunch &l)
@@ -404,7 +469,7 @@ bool embed_launchable(const tessel_embedding &a) { return sum_groups(a, embed_la
 size_t embed_workspace(const tessel_embedding &a)
 {
     const EmbedLaunch l = embed_launch(a);
-    return 4 * (2 * whole_chunks(a.tokens) + 4 + counts_of(a, l) + (size_t)l.runs * 2 * l.part);
+    return 4 * (2 * sorted_of(a) + 4 + counts_of(a, l) + (size_t)l.runs * 2 * l.part);
 }
 
 int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *workspace, void *stream)
@@ -412,8 +477,8 @@ int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *
     EmbedLaunch l = embed_launch(a);
     l.d = d;
     l.place = (int32_t *)workspace;
-    l.row = l.place + whole_chunks(a.tokens);
-    l.total = l.row + whole_chunks(a.tokens);
+    l.row = l.place + sorted_of(a);
+    l.total = l.row + sorted_of(a);
     l.count = l.total + 4;
     l.parts = (float *)(l.count + counts_of(a, l));
     void *args[] = {&l};

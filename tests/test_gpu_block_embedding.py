@@ -248,3 +248,16 @@ def test_refusals(ops):
     for call in bad:
         with pytest.raises(TesselError):
             call()
+
+
+@pytest.mark.parametrize("n", [16383, 16384, 16385, 32768, 40001, 65536, 65537, 100003])
+@pytest.mark.parametrize("hot", [0.0, 0.2, 0.97])
+def test_long_batches(ops, n, hot):
+    """batches of several tiles, of which a bucket's places fit its list, and do not"""
+    gen = torch.Generator().manual_seed(n)
+    token = torch.randint(-3, 1000, (n,), generator=gen)
+    token[torch.rand(n, generator=gen) < hot] = 300
+    d = torch.randn(n, 8, generator=gen).to(torch.bfloat16)
+    for kind in (torch.int64, torch.int32):
+        got = ops.embed_backward(d.cuda(), token.to(kind).cuda(), 990)
+        R.close(got, *R.embedding_gradient(d, token, 990, 1.0, 0), "dtable")
