@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -10,6 +11,17 @@ if ROOT not in sys.path:
 
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
+
+
+def pytest_collection_finish(session):
+    gc.collect()
+    gc.freeze()                                                 # (what lives for the whole run is not looked through again)
+
+
+def pytest_runtest_setup(item):
+    """What earlier tests left in cycles goes away before a test of the GPU, not in the middle of one that counts what is allocated."""
+    if item.get_closest_marker("gpu"):
+        gc.collect()
 
 
 @pytest.fixture(scope="session")
