@@ -619,8 +619,8 @@ def embed_backward(d_out, tokens, rows, scale=1.0, first=0, drop=None, into=None
                         dtable.stride(0) if rows > 1 else c, 0 if into is None else 1, *(_NO_DROP if drop is None else drop._at(d_out)))
     size = C.c_size_t()
     binding._check(lib.tessel_embedding_backward_workspace_bytes(a, C.byref(size)))
-    ws = _workspace(size.value, d_out)
-    binding._check(lib.tessel_embedding_backward(a, ws.data_ptr(), ws.numel(), _stream(d_out)))
+    ws = _workspace(size.value, d_out) if size.value else None
+    binding._check(lib.tessel_embedding_backward(a, 0 if ws is None else ws.data_ptr(), size.value, _stream(d_out)))
     return dtable
 
 

@@ -283,22 +283,112 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(EmbedLaunch l)
 
 constexpr int kFill = 16384;     // values that a workgroup fills with zeros
 
-// Rows that no token asked for; neighbouring workgroups write neighbouring pieces.
-__device__ __forceinline__ void fill(const EmbedLaunch &l, uint32_t piece)
+// Zeros in the rows of a piece that no token asked for; neighbouring workgroups write neighbouring pieces.
+struct Piece {
+    int64_t row;                 // the first of fill_rows
+    int     begin, end;          // columns
+    __device__ __forceinline__ Piece(const EmbedLaunch &l, uint32_t piece) : row((int64_t)(piece / l.fill_pieces) * l.fill_rows), begin(piece % l.fill_pieces * kFill)
+    {
+        end = (int)min((int64_t)l.a.channels, (int64_t)begin + kFill);
+    }
+};
+template <typename F>
+__device__ __forceinline__ void fill(const EmbedLaunch &l, const Piece &p, F &&asked)
 {
     typedef float V __attribute__((ext_vector_type(4), aligned(4)));
     const tessel_embedding &a = l.a;
     const int lanes = l.fill_lanes, lane = threadIdx.x % lanes;
-    const int64_t first = (int64_t)(piece / l.fill_pieces) * l.fill_rows;
-    const int begin = piece % l.fill_pieces * kFill, end = (int)min((int64_t)a.channels, (int64_t)begin + kFill);
     for (int r = threadIdx.x / lanes; r < (int)l.fill_rows; r += kThreads / lanes) {
-        const int64_t row = first + r;
-        if (row >= a.rows || l.count[(row & ((1 << l.shift) - 1)) * l.bins + (row >> l.shift)]) continue;
-        float *to = a.dtable + row * a.dtable_stride;
-        int col = begin + 4 * lane;
-        for (; col + 4 <= end; col += 4 * lanes) *(V *)(to + col) = V{};
-        for (int j = col; j < end; j++) to[j] = 0.0f;
+        if (p.row + r >= a.rows || asked(r)) continue;
+        float *to = a.dtable + (p.row + r) * a.dtable_stride;
+        int col = p.begin + 4 * lane;
+        for (; col + 4 <= p.end; col += 4 * lanes) *(V *)(to + col) = V{};
+        for (int j = col; j < p.end; j++) to[j] = 0.0f;
     }
+}
+
+// a row's whole sum
+__device__ __forceinline__ void put_row(const tessel_embedding &a, int row, float (&sum)[8], int col)
+{
+    float *to = a.dtable + row * a.dtable_stride, old[8] = {};
+    if (a.accumulate) load8<float>(old, to, col, a.channels);
+#pragma unroll
+    for (int j = 0; j < 8; j++) sum[j] = old[j] + a.scale * sum[j];
+    store8<float>(to, sum, col, a.channels);
+}
+
+// A batch of few tokens in one launch.  A workgroup for each token and 512 columns: all four waves look which tokens have the same row, 64 each; that of the first of these adds
+// them up, a wave its share of the tokens, and the waves' sums in order.  Behind them workgroups that fill the other rows.
+constexpr int kFew = 256;
+
+template <typename T, bool NARROW>
+__global__ __launch_bounds__(kThreads) void few_kernel(EmbedLaunch l)
+{
+    __shared__ uint64_t found[kThreads / 64];
+    __shared__ uint32_t seen[kFill / 32];
+    __shared__ float4v sums[kThreads / 64][2][64];
+    static_assert(kFew == kThreads, "a token a thread");
+    const tessel_embedding &a = l.a;
+    const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    const int mine = thread < a.tokens ? row_at(a, thread) : -1;
+    if (blockIdx.x >= l.sum_groups) {
+        const Piece p(l, blockIdx.x - l.sum_groups);
+        for (int n = thread; n < kFill / 32; n += kThreads) seen[n] = 0;
+        __syncthreads();
+        if (mine >= p.row && mine < p.row + l.fill_rows) atomicOr(&seen[(mine - p.row) / 32], 1u << (mine - p.row) % 32);
+        __syncthreads();
+        fill(l, p, [&](int r) { return seen[r / 32] >> r % 32 & 1; });
+        return;
+    }
+    const int token = blockIdx.x / l.tiles, col = 8 * (blockIdx.x % l.tiles * 64 + lane), row = row_at(a, token);
+    if (row < 0) return;
+    uint64_t same = __ballot(mine == row);
+    if (lane == 0) found[wave] = same;
+    __syncthreads();
+    int first = 0;
+    while (found[first] == 0) first++;                           // (one of them is this token)
+    if (64 * first + __builtin_ctzll(found[first]) != token) return;
+    const Draw draw(l.d, col);
+    float sum[8] = {};
+    while (same) {
+        constexpr int kAhead = 8;
+        int t[kAhead], n = 0;
+        typename Eight<T>::type x[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; j++) {                       // (behind the last one, that again)
+            t[j] = same ? 64 * wave + __builtin_ctzll(same) : t[max(j - 1, 0)];
+            n += same ? 1 : 0;
+            same &= same - 1;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; j++) x[j] = take8<T, NARROW>((const T *)a.d_out.data + t[j] * a.d_out.stride, col, a.channels);
+#pragma unroll
+        for (int j = 0; j < kAhead; j++) {
+            if (j >= n) break;
+            float v[8];
+            settle8<T, NARROW>(col, a.channels, x[j]);
+            widen8<T>(v, x[j]);
+            if (l.d.least) draw.apply(v, (uint32_t)t[j]);
+#pragma unroll
+            for (int k = 0; k < 8; k++) sum[k] += v[k];
+        }
+    }
+    if (wave != first) {
+        sums[wave][0][lane] = float4v{sum[0], sum[1], sum[2], sum[3]};
+        sums[wave][1][lane] = float4v{sum[4], sum[5], sum[6], sum[7]};
+    }
+    __syncthreads();
+    if (wave != first) return;
+    for (int w = first + 1; w < kThreads / 64; w++)
+        if (found[w]) {
+            const float4v x = sums[w][0][lane], y = sums[w][1][lane];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                sum[k] += x[k];
+                sum[4 + k] += y[k];
+            }
+        }
+    put_row(a, row, sum, col);
 }
 
 // Sums over runs of sorted places, eight columns a lane.  Rows that lie inside a run are whole; of the row that it begins within and of the
@@ -311,7 +401,8 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
     constexpr int kAhead = 8;
     const tessel_embedding &a = l.a;
     if (blockIdx.x >= l.sum_groups) {
-        fill(l, blockIdx.x - l.sum_groups);
+        const Piece p(l, blockIdx.x - l.sum_groups);
+        fill(l, p, [&](int r) { return l.count[((p.row + r) & ((1 << l.shift) - 1)) * l.bins + ((p.row + r) >> l.shift)] != 0; });
         return;
     }
     const int group = blockIdx.x / l.tiles, tile = blockIdx.x % l.tiles;
@@ -340,11 +431,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
     float sum[8] = {};
     const auto flush = [&](bool ends) {
         if (starts && ends) {
-            float *to = a.dtable + row * a.dtable_stride, old[8] = {};
-            if (a.accumulate) load8<float>(old, to, col, a.channels);
-#pragma unroll
-            for (int j = 0; j < 8; j++) sum[j] = old[j] + a.scale * sum[j];
-            store8<float>(to, sum, col, a.channels);
+            put_row(a, row, sum, col);
         } else {
             float4v *to = (float4v *)(l.parts + ((int64_t)run * 2 + (starts ? 1 : 0)) * l.part + col);
             to[0] = float4v{sum[0], sum[1], sum[2], sum[3]};
@@ -432,6 +519,8 @@ int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream)
 #undef KERNEL
 }
 
+static bool few(const tessel_embedding &a) { return a.tokens <= kFew; }
+
 static EmbedLaunch embed_launch(const tessel_embedding &a)
 {
     EmbedLaunch l = {};
@@ -453,6 +542,10 @@ static EmbedLaunch embed_launch(const tessel_embedding &a)
     while (l.fill_lanes < 64 && 4 * (int)l.fill_lanes < a.channels) l.fill_lanes *= 2;
     l.fill_rows = (uint32_t)std::max(1, kFill / a.channels);
     l.fill_pieces = (uint32_t)((a.channels + kFill - 1) / kFill);
+    if (few(a)) {
+        l.tiles = (int)(((int64_t)a.channels + 511) / 512);
+        l.sum_groups = (uint32_t)(a.tokens * l.tiles);
+    }
     return l;
 }
 
@@ -468,6 +561,7 @@ bool embed_launchable(const tessel_embedding &a) { return sum_groups(a, embed_la
 
 size_t embed_workspace(const tessel_embedding &a)
 {
+    if (few(a)) return 0;
     const EmbedLaunch l = embed_launch(a);
     return 4 * (2 * sorted_of(a) + 4 + counts_of(a, l) + (size_t)l.runs * 2 * l.part);
 }
@@ -476,15 +570,20 @@ int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *
 {
     EmbedLaunch l = embed_launch(a);
     l.d = d;
+    void *args[] = {&l};
+    const int64_t groups = sum_groups(a, l);
+    if (few(a)) {
+#define KERNEL(T) (a.channels < 8 ? (const void *)few_kernel<T, true> : (const void *)few_kernel<T, false>)
+        return groups ? launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)groups), dim3(kThreads), args, 0, (hipStream_t)stream)) : 0;
+#undef KERNEL
+    }
     l.place = (int32_t *)workspace;
     l.row = l.place + sorted_of(a);
     l.total = l.row + sorted_of(a);
     l.count = l.total + 4;
     l.parts = (float *)(l.count + counts_of(a, l));
-    void *args[] = {&l};
     const void *sort = a.index_type == TESSEL_I64 ? (const void *)sort_kernel<int64_t> : (const void *)sort_kernel<int32_t>;
     int e = launched(hipLaunchKernel(sort, dim3(1u << l.shift), dim3(kSortThreads), args, 0, (hipStream_t)stream));
-    const int64_t groups = sum_groups(a, l);
 #define KERNEL(T) (l.lanes >= 64 ? (const void *)sum_kernel<T, true, false> : (const void *)sum_kernel<T, false, true>)
     if (e == 0 && groups > 0) e = launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)groups), dim3(kThreads), args, 0, (hipStream_t)stream));
 #undef KERNEL
