@@ -187,7 +187,7 @@ typedef struct {
 
 typedef struct {
     int32_t  type;
-    int32_t  channels;
+    int32_t  channels;      /* at most 2^30                                                                */
     int64_t  tokens;
     tessel_rows x;
     tessel_rows y;          /* written                                                                     */

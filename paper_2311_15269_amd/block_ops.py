@@ -10,6 +10,7 @@ refused while torch records (under torch.no_grad(), and in the passes of a torch
 """
 import ctypes as C
 import math
+import operator
 import struct
 
 from . import binding
@@ -515,23 +516,30 @@ def weight_gradient(dy, x, into=None):
 class Dropout:
     """A dropout: which values it keeps follows from `seed`, `number` (which dropout of the program this is: a layer's, of a micro-batch) and where
     they stand, so the backward pass, and a block that computes its activations again, draw the same ones.  `step`: an int64 tensor of one
-    number on the GPU, added to `number` when a kernel runs (a captured graph that counts it up draws anew in every replay)."""
+    number on the GPU, added to `number` when a kernel runs (a captured graph that counts it up draws anew in every replay).  An object
+    stays what it was made as."""
 
     def __init__(self, rate, seed, number=0, step=None):
         import torch
         if not 0 <= rate < 1:
             _refuse("a dropout rate of %r: from 0 to below 1" % (rate,))
+        seed, number = operator.index(seed), operator.index(number)
         for n in (seed, number):
             if not 0 <= n < 1 << 64:
                 _refuse("%r is no number of 64 bits" % (n,))
         if step is not None and (step.dtype is not torch.int64 or step.numel() != 1 or not step.is_cuda):
             _refuse("step has to be one int64 number on the GPU")
-        self.rate, self.seed, self.number, self.step = float(rate), int(seed), int(number), step
-        self._words = (self.seed, self.number, 0 if step is None else step.data_ptr(), self.rate)
+        self._step = step
+        self._words = (seed, number, 0 if step is None else step.data_ptr(), float(rate))
+
+    rate = property(lambda self: self._words[3])
+    seed = property(lambda self: self._words[0])
+    number = property(lambda self: self._words[1])
+    step = property(lambda self: self._step)
 
     def _at(self, like):
-        if self.step is not None and self.step.get_device() != like.get_device():
-            _refuse("step on %s, the tensors on %s" % (self.step.device, like.device))
+        if self._step is not None and self._step.get_device() != like.get_device():
+            _refuse("step on %s, the tensors on %s" % (self._step.device, like.device))
         return self._words
 
 
@@ -576,9 +584,10 @@ def _number(n):
 
 
 def _whole_first(first):
+    first = operator.index(first)
     if not 0 <= first <= 1 << 62:
         _refuse("the first row of a shard has to be 0 to 2^62, not %r" % (first,))
-    return int(first)
+    return first
 
 
 def embed(tokens, table, scale=1.0, first=0, drop=None):
@@ -604,6 +613,7 @@ def embed_backward(d_out, tokens, rows, scale=1.0, first=0, drop=None, into=None
     lib = _library()
     _on_gpu(d_out, ("tokens", "channels"))
     n, c = d_out.shape
+    rows = operator.index(rows)
     if not 0 < rows <= MOST:
         _refuse("a table of %r rows" % (rows,))
     kind, at = _index(tokens, n, d_out)
@@ -627,6 +637,8 @@ def embed_backward(d_out, tokens, rows, scale=1.0, first=0, drop=None, into=None
 def frequencies(turning, base=10000.0, device=None):
     """base^(-2 i / turning) for the pairs i of `turning` channels, in 64 bits: what rotate() takes"""
     import torch
+    if turning < 0 or turning % 2:
+        _refuse("%r channels are no pairs" % (turning,))
     return torch.exp(torch.arange(0, turning, 2, dtype=torch.float64, device="cuda" if device is None else device) * (-math.log(base) / max(1, turning)))
 
 

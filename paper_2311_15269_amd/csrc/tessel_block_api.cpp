@@ -180,7 +180,7 @@ int dropout_ok(const tessel_dropout_rows *a, DropLaunch &l)
     if (!is_type(a->type)) return TESSEL_E_UNSUPPORTED;
     const int e = drop_ok(a->drop, l);
     if (e) return e;
-    if (a->tokens > INT32_MAX || !lanes_ok(a->tokens * (((int64_t)a->channels + 7) / 8))) return TESSEL_E_TOOBIG;
+    if (a->tokens > INT32_MAX || a->channels > 1 << 30 || !lanes_ok(a->tokens * (((int64_t)a->channels + 7) / 8))) return TESSEL_E_TOOBIG;
     return rows_ok(a->x, a->type, a->tokens, a->channels, false) && rows_ok(a->y, a->type, a->tokens, a->channels, true) ? TESSEL_OK : TESSEL_E_INVALID_ARG;
 }
 

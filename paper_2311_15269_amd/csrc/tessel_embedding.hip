@@ -1,6 +1,13 @@
 // The embedding of a shard of the vocabulary, forward and backward (formulas: include/tessel_block_ops.h).
 //
-// Forward: eight channels of a token a lane.  Backward: a workgroup for every row of the table looks through all tokens for its own, in order.
+// Forward: a gather, eight channels of a token a lane, scaled and dropped on its way.  Backward: a sum over the tokens of each row.  Adding them up with atomics would
+// make their order, and with it the bits, chance; so the places of the batch are sorted by row first, stably, and every sum goes over its places in ascending
+// order, in pieces whose bounds do not depend on what runs when.  The sort is by buckets of rows with the same low bits, a workgroup each, which all read the
+// whole batch (T tokens 256 times, from the caches) and need nothing from each other: one launch, where a sort by digits takes three a digit.
+//
+// Bound by memory but for the way through the launches.  Forward, 8192 tokens of 4096 bf16: 17 us (100 MB, 5.8 TB/s), with dropout 23; 16384 of 1024 f16 10.  Backward,
+// the same 8192 tokens into 50000 rows of which some 3700 occur: sort 8.8 us, sums and zeros 165 (886 MB, 5.4 TB/s; zeros alone 5.8), join 8; 16384 tokens added
+// to 62500 rows of 1024: 10, 18 and 7 us.  512 tokens and fewer in one launch, 2.5 to 13 us.
 #include <algorithm>
 
 #include "tessel_draw.h"
@@ -65,7 +72,7 @@ struct EmbedLaunch {
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kSubs = 4, kSub = 4 * kSortThreads, kTile = kSubs * kSub;          // a thread takes four places of each part of a tile
 constexpr int kMostBins = 2 * kSortThreads;        // (two workgroups have room on a compute unit)
-constexpr int kOften = 256;
+constexpr int kOften = 256;      // places of a row that is put in place by counting (32768 tokens, nearly all of them one: sort 54 us, without this 74)
 
 __device__ __forceinline__ int below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u)); }
 
@@ -292,13 +299,13 @@ struct Piece {
         end = (int)min((int64_t)l.a.channels, (int64_t)begin + kFill);
     }
 };
-template <typename F>
+template <int THREADS, typename F>
 __device__ __forceinline__ void fill(const EmbedLaunch &l, const Piece &p, F &&asked)
 {
     typedef float V __attribute__((ext_vector_type(4), aligned(4)));
     const tessel_embedding &a = l.a;
     const int lanes = l.fill_lanes, lane = threadIdx.x % lanes;
-    for (int r = threadIdx.x / lanes; r < (int)l.fill_rows; r += kThreads / lanes) {
+    for (int r = threadIdx.x / lanes; r < (int)l.fill_rows; r += THREADS / lanes) {
         if (p.row + r >= a.rows || asked(r)) continue;
         float *to = a.dtable + (p.row + r) * a.dtable_stride;
         int col = p.begin + 4 * lane;
@@ -317,27 +324,24 @@ __device__ __forceinline__ void put_row(const tessel_embedding &a, int row, floa
     store8<float>(to, sum, col, a.channels);
 }
 
-// A batch of few tokens in one launch.  A workgroup for each token and 512 columns: all four waves look which tokens have the same row, 64 each; that of the first of these adds
-// them up, a wave its share of the tokens, and the waves' sums in order.  Behind them workgroups that fill the other rows.
-constexpr int kFew = 256;
-
-template <typename T, bool NARROW>
-__global__ __launch_bounds__(kThreads) void few_kernel(EmbedLaunch l)
+// A batch of few tokens in one launch.  A workgroup for each token and 512 columns: its waves look which tokens have the same row, 64 each; that of the first of these adds
+// them up, a wave its share of the tokens, and the waves' sums in order.  Behind them workgroups that fill the other rows.  WAVES: as many as the tokens take
+template <typename T, int WAVES, bool NARROW>
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(EmbedLaunch l)
 {
-    __shared__ uint64_t found[kThreads / 64];
+    __shared__ uint64_t found[WAVES];
     __shared__ uint32_t seen[kFill / 32];
-    __shared__ float4v sums[kThreads / 64][2][64];
-    static_assert(kFew == kThreads, "a token a thread");
+    __shared__ float4v sums[WAVES][2][64];
     const tessel_embedding &a = l.a;
     const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int mine = thread < a.tokens ? row_at(a, thread) : -1;
     if (blockIdx.x >= l.sum_groups) {
         const Piece p(l, blockIdx.x - l.sum_groups);
-        for (int n = thread; n < kFill / 32; n += kThreads) seen[n] = 0;
+        for (int n = thread; n < kFill / 32; n += 64 * WAVES) seen[n] = 0;
         __syncthreads();
         if (mine >= p.row && mine < p.row + l.fill_rows) atomicOr(&seen[(mine - p.row) / 32], 1u << (mine - p.row) % 32);
         __syncthreads();
-        fill(l, p, [&](int r) { return seen[r / 32] >> r % 32 & 1; });
+        fill<64 * WAVES>(l, p, [&](int r) { return seen[r / 32] >> r % 32 & 1; });
         return;
     }
     const int token = blockIdx.x / l.tiles, col = 8 * (blockIdx.x % l.tiles * 64 + lane), row = row_at(a, token);
@@ -379,7 +383,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(EmbedLaunch l)
     }
     __syncthreads();
     if (wave != first) return;
-    for (int w = first + 1; w < kThreads / 64; w++)
+    for (int w = first + 1; w < WAVES; w++)
         if (found[w]) {
             const float4v x = sums[w][0][lane], y = sums[w][1][lane];
 #pragma unroll
@@ -402,7 +406,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
     const tessel_embedding &a = l.a;
     if (blockIdx.x >= l.sum_groups) {
         const Piece p(l, blockIdx.x - l.sum_groups);
-        fill(l, p, [&](int r) { return l.count[((p.row + r) & ((1 << l.shift) - 1)) * l.bins + ((p.row + r) >> l.shift)] != 0; });
+        fill<kThreads>(l, p, [&](int r) { return l.count[((p.row + r) & ((1 << l.shift) - 1)) * l.bins + ((p.row + r) >> l.shift)] != 0; });
         return;
     }
     const int group = blockIdx.x / l.tiles, tile = blockIdx.x % l.tiles;
@@ -519,7 +523,9 @@ int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream)
 #undef KERNEL
 }
 
-static bool few(const tessel_embedding &a) { return a.tokens <= kFew; }
+// Batches that few_kernel takes.  Tokens all different, 1024 channels added to: 256 tokens 3.1 us (13.2 by sort, sums and join), 512 5.2 (13.2), 1024 16.5 (15.2); 4096 channels:
+// 256 5.0 (14.8), 512 13.5 (15), 1024 57 (17.7).  One token everywhere: 256 10.3 (13.0), 512 12.4 (13.7), 1024 19 (18.8).
+static bool few(const tessel_embedding &a) { return a.tokens <= 256 || (a.tokens <= 512 && a.channels <= 4096); }
 
 static EmbedLaunch embed_launch(const tessel_embedding &a)
 {
@@ -532,7 +538,8 @@ static EmbedLaunch embed_launch(const tessel_embedding &a)
     while (l.lanes < 256 && 8 * l.lanes < a.channels) l.lanes *= 2;
     l.tiles = (int)(((int64_t)a.channels + 8 * l.lanes - 1) / (8 * l.lanes));
     l.part = ((int64_t)a.channels + 7) / 8 * 8;
-    // places a run: few enough that the runs fill the GPU, and that there are at most 1024 of them
+    // Places a run: few enough that the runs fill the GPU, and that there are at most 1024 of them, whose parts are read again (8192 tokens of 4096: 32 a run, sums
+    // and zeros 164 us and join 8; 16 a run 165 and 11).
     const int64_t threads = a.tokens * (l.part / 8);
     l.run = 8;
     while (l.run < threads >> 17 || (int64_t)l.run * 1024 < a.tokens) l.run *= 2;
@@ -573,9 +580,12 @@ int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *
     void *args[] = {&l};
     const int64_t groups = sum_groups(a, l);
     if (few(a)) {
-#define KERNEL(T) (a.channels < 8 ? (const void *)few_kernel<T, true> : (const void *)few_kernel<T, false>)
-        return groups ? launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)groups), dim3(kThreads), args, 0, (hipStream_t)stream)) : 0;
+        const int waves = a.tokens <= 64 ? 1 : a.tokens <= 256 ? 4 : 8;
+#define PICK(T, W) (a.channels < 8 ? (const void *)few_kernel<T, W, true> : (const void *)few_kernel<T, W, false>)
+#define KERNEL(T) (waves == 1 ? PICK(T, 1) : waves == 4 ? PICK(T, 4) : PICK(T, 8))
+        return groups ? launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)groups), dim3(64 * waves), args, 0, (hipStream_t)stream)) : 0;
 #undef KERNEL
+#undef PICK
     }
     l.place = (int32_t *)workspace;
     l.row = l.place + sorted_of(a);

@@ -29,6 +29,7 @@ def change_of(a, change):
     ({"tokens": -1}, INVALID), ({"channels": 0}, INVALID), ({"type": 3}, UNSUPPORTED), ({"x": B.Rows(None, 64)}, INVALID), ({"x": B.Rows(AT + 1, 64)}, INVALID),
     ({"x": B.Rows(AT, -1)}, INVALID), ({"y": B.Rows(AT, 63)}, INVALID), ({"y": B.Rows(None, 64)}, INVALID), ({"tokens": 1 << 31}, TOOBIG),
     ({"tokens": (1 << 31) - 1, "channels": 17}, TOOBIG), ({"tokens": 1 << 24, "channels": (1 << 31) - 1}, TOOBIG),
+    ({"tokens": 1, "channels": (1 << 30) + 1}, TOOBIG),
     ({"drop": drop(rate=1.0)}, INVALID), ({"drop": drop(rate=-0.5)}, INVALID), ({"drop": drop(rate=NAN)}, INVALID), ({"drop": drop(rate=INF)}, INVALID),
     ({"drop": drop(step=AT + 4)}, INVALID), ({"tokens": 0, "drop": drop(step=AT)}, OK),
 ])
@@ -133,3 +134,19 @@ def test_numbers_that_are_none_of_64_bits_are_refused():
     for first in (-1, (1 << 62) + 1):
         with pytest.raises(binding.TesselError):
             B._whole_first(first)
+    for call in (lambda: B.Dropout(0.5, 1.5), lambda: B.Dropout(0.5, 1, 2.5), lambda: B._whole_first(1.5)):
+        with pytest.raises(TypeError):
+            call()
+    for n in (1e39, -1e39, NAN, INF):
+        with pytest.raises(binding.TesselError):
+            B._number(n)
+    for turning in (-2, 5):
+        with pytest.raises(binding.TesselError):
+            B.frequencies(turning, device="cpu")
+
+
+def test_a_dropout_stays_what_it_is():
+    drop = B.Dropout(0.25, 7, 8)
+    assert (drop.rate, drop.seed, drop.number, drop.step) == (0.25, 7, 8, None)
+    with pytest.raises(AttributeError):
+        drop.number = 9

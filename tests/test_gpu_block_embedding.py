@@ -53,6 +53,16 @@ def test_tokens_and_rows(ops, n, rows):
     check(ops, *inputs(n, rows, 24 if rows < 100000 else 8, torch.bfloat16, seed=n + rows))
 
 
+@pytest.mark.parametrize("n", [2, 4, 64, 65, 255, 256, 257, 300, 511, 512, 513])
+@pytest.mark.parametrize("c", [3, 520, 4096, 4104])
+def test_few_tokens(ops, n, c):
+    """batches of one launch and of three, tokens of waves that have none in common and some"""
+    token, table, d = inputs(n, 40, c, torch.bfloat16, seed=n + c, low=-2)
+    check(ops, token, table, d)
+    if c < 4000:
+        check(ops, torch.full((n,), 39), table, d, drop=(0.3, 4, 5))
+
+
 @pytest.mark.parametrize("kind", [torch.int32, torch.int64])
 @pytest.mark.parametrize("first", [0, 37, 1000])
 def test_shards(ops, first, kind):

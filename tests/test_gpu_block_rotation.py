@@ -105,6 +105,34 @@ def test_position_nought_turns_nothing(ops):
     assert torch.equal(q, v["q"]) and torch.equal(k, v["k"])
 
 
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_channels_that_do_not_turn_stay_as_they_are(ops, neighbours):
+    """bit by bit, infinities among them, and next to these too"""
+    v = inputs(6, 2, 1, 64, torch.bfloat16, False)
+    for n in ("q", "k", "dq", "dk"):
+        v[n][1, 0, 40], v[n][2, 0, 63], v[n][3, 0, 16] = float("inf"), float("-inf"), float("nan")
+    g = cuda(v)
+    args = (g["q"], g["k"], positions(6).cuda(), frequency(16).cuda(), None, None, 1e-6, neighbours)
+    for got, name in zip(ops.rotate(*args) + ops.rotate_backward(g["dq"], g["dk"], *args)[:2], ("q", "k", "dq", "dk")):
+        assert torch.equal(got[..., 16:].view(torch.int16), g[name][..., 16:].view(torch.int16))
+        assert bool(torch.isfinite(got[..., :16]).all())
+
+
+def test_small_and_large_values(ops):
+    """heads whose squares are subnormal numbers of 32 bits, with and without eps, and heads near the largest whose squares are numbers"""
+    for size, eps in ((1e-20, 0.0), (3e-20, 0.0), (1e-19, 1e-37), (1e-12, 0.0), (1e18, 1e-6)):
+        v = inputs(4, 2, 2, 64, torch.float32)
+        for n in ("q", "k"):
+            v[n] *= size
+        g = cuda(v)
+        at, f = positions(4), frequency(64)
+        got = ops.rotate(g["q"], g["k"], at.cuda(), f.cuda(), g["wq"], g["wk"], eps)
+        for x, n in zip(got, ("q", "k")):
+            want, bound = R.rotation(v[n], at, f, v["w" + n], eps, False)[0]
+            # squares of numbers around 2^-66 lose bits below 2^-149: 2^-17 of the mean of 64 of them, half that of its root
+            R.close(x, want, bound + (2.0 ** -16 * R.both(want, 64, 64, False) if size < 1e-19 else 0.0), (n, size))
+
+
 def test_heads_of_noughts(ops):
     """a head whose channels are all nought, of which eps is the whole norm"""
     v = inputs(4, 2, 2, 64, torch.float32)
