@@ -62,64 +62,85 @@ __device__ __forceinline__ float over_root(float v)
     return __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v) * (small ? 0x1p32f : 1.0f);
 }
 
-// sines and cosines of a wave's tokens, for all pairs of a head (those that do not turn: by no angle)
+// sines and cosines of a wave's tokens
 __device__ __forceinline__ void angles(const tessel_rotation &a, int64_t token, int tokens, float *cosine, float *sine)
 {
-    const int pairs = a.dim / 2, half = a.turning / 2;
-    for (int i = threadIdx.x & 63; i < tokens * pairs; i += 64) {
-        const int t = i / pairs, p = i - t * pairs;
-        float s = 0.0f, c = 1.0f;
-        if (p < half) {
-            const int64_t n = min(token + t, a.tokens - 1);
-            const double position = a.index_type == TESSEL_I64 ? (double)((const int64_t *)a.position)[n] : (double)((const int32_t *)a.position)[n];
-            const double turns = position * a.frequency[p] * 0.15915494309189535;        // angle / (2 pi)
-            sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-        }
+    const int half = a.turning / 2;
+    for (int i = threadIdx.x & 63; i < tokens * half; i += 64) {
+        const int t = i / half, p = i - t * half;
+        const int64_t n = min(token + t, a.tokens - 1);
+        const double position = a.index_type == TESSEL_I64 ? (double)((const int64_t *)a.position)[n] : (double)((const int32_t *)a.position)[n];
+        const double turns = position * a.frequency[p] * 0.15915494309189535;            // angle / (2 pi)
+        float s, c;
+        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
         cosine[i] = c;
         sine[i] = s;
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // (the wave's own LDS: no barrier)
 }
 
-// What a lane has of a head: channels first[k] .. + V - 1 and second[k] .. + V - 1 of chunk k.  Pairs are the j-th of both; with `neighbours`, of which a chunk's
-// channels are 2 V in a row, two in a row.
-template <int V, int CHUNKS>
+// What a lane has of a head: channels first[k] .. + V - 1 and second[k] .. + V - 1 of chunk k, V pairs, first those that turn, then the others.  Pair j are the j-th of both; where
+// neighbours are paired (NEAR), of which a chunk's channels are 2 V in a row, two in a row.  Channels that do not turn are paired alike.  A chunk that would pass the last of
+// its pairs starts before it, at what other lanes have too (RAGGED): its first `skip` pairs count nothing, and both lanes write the same.
+template <int V, int CHUNKS, bool NEAR, bool RAGGED>
 struct Mine {
-    int  first[CHUNKS], second[CHUNKS], pair[CHUNKS];
+    int  first[CHUNKS], second[CHUNKS], pair[CHUNKS], skip[CHUNKS];
     bool on[CHUNKS], turns[CHUNKS];
     __device__ __forceinline__ Mine(const tessel_rotation &a, int lane, int lanes)
     {
-        const int chunks = a.dim / (2 * V), half = a.turning / 2;
+        const int half = a.turning / 2, rest = a.dim / 2 - half, turning = (half + V - 1) / V, chunks = turning + (rest + V - 1) / V;
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            const int c = lane + k * lanes;
-            on[k] = c < chunks;
-            pair[k] = V * min(c, chunks - 1);
-            turns[k] = pair[k] < half;
-            const bool apart = turns[k] && !a.neighbours;
-            first[k] = apart ? pair[k] : 2 * pair[k];
-            second[k] = apart ? pair[k] + half : 2 * pair[k] + V;
+            const int c = min(lane + k * lanes, chunks - 1);
+            on[k] = lane + k * lanes < chunks;
+            turns[k] = c < turning;
+            const int at = V * (turns[k] ? c : c - turning), pairs = turns[k] ? half : rest, start = RAGGED ? min(at, pairs - V) : at;
+            skip[k] = at - start;
+            pair[k] = turns[k] ? start : 0;
+            first[k] = (turns[k] ? 0 : a.turning) + (NEAR ? 2 * start : start);
+            second[k] = first[k] + (NEAR ? V : pairs);
+        }
+    }
+    // does value j of the first V or of the second (h) count
+    __device__ __forceinline__ bool counts(int k, int h, int j) const { return !RAGGED || (NEAR ? (h * V + j) / 2 : j) >= skip[k]; }
+};
+
+// a chunk as it is in memory, in one piece where it lies in one
+template <typename T, int V, bool NEAR>
+struct Raw {
+    static constexpr int kPieces = NEAR ? 1 : 2, kEach = NEAR ? 2 * V : V;
+    typedef typename Some<T, kEach>::type Piece;
+    Piece v[kPieces];
+    __device__ __forceinline__ void read(const T *first, const T *second)
+    {
+        v[0] = *(const Piece *)first;
+        if constexpr (!NEAR) v[1] = *(const Piece *)second;
+    }
+    __device__ __forceinline__ void write(T *first, T *second) const
+    {
+        *(Piece *)first = v[0];
+        if constexpr (!NEAR) *(Piece *)second = v[1];
+    }
+    // in 32 bits, noughts where they do not count
+    __device__ __forceinline__ void take(float (&x)[2][V], bool counts) const
+    {
+#pragma unroll
+        for (int e = 0; e < 2 * V; e++) {
+            float f;
+            if constexpr (kEach == 1) f = (float)v[e];
+            else f = (float)v[e / kEach][e % kEach];
+            x[e / V][e % V] = counts ? f : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void round(const float (&x)[2][V])
+    {
+#pragma unroll
+        for (int e = 0; e < 2 * V; e++) {
+            if constexpr (kEach == 1) v[e] = (T)x[e / V][e % V];
+            else v[e / kEach][e % kEach] = (T)x[e / V][e % V];
         }
     }
 };
-template <typename T, int V>
-__device__ __forceinline__ void spread(float *v, const typename Some<T, V>::type &x)
-{
-    if constexpr (V == 1) v[0] = (float)x;
-    else
-#pragma unroll
-        for (int j = 0; j < V; j++) v[j] = (float)x[j];
-}
-template <typename T, int V>
-__device__ __forceinline__ void put(T *to, const float *v)
-{
-    typename Some<T, V>::type x;
-    if constexpr (V == 1) x = (T)v[0];
-    else
-#pragma unroll
-        for (int j = 0; j < V; j++) x[j] = (T)v[j];
-    *(typename Some<T, V>::type *)to = x;
-}
 template <int V>
 __device__ __forceinline__ void get(float *v, const float *from)
 {
@@ -127,24 +148,16 @@ __device__ __forceinline__ void get(float *v, const float *from)
     for (int j = 0; j < V; j++) v[j] = from[j];
 }
 
-// x and y turned by the angles, or with SIGN -1 back
-template <int V, int SIGN>
-__device__ __forceinline__ void turn(float *x, float *y, const float *c, const float *s, bool neighbours)
+// a chunk turned by its angles, or with SIGN -1 back
+template <int V, bool NEAR, int SIGN>
+__device__ __forceinline__ void turn(float (&x)[2][V], const float *c, const float *s)
 {
-    const auto pair = [](float &a, float &b, float c, float s) {
+#pragma unroll
+    for (int j = 0; j < V; j++) {
+        float &a = NEAR ? x[2 * j / V][2 * j % V] : x[0][j], &b = NEAR ? x[(2 * j + 1) / V][(2 * j + 1) % V] : x[1][j];
         const float p = a, q = b;
-        a = SIGN > 0 ? p * c - q * s : p * c + q * s;
-        b = SIGN > 0 ? p * s + q * c : q * c - p * s;
-    };
-    if (V > 1 && neighbours) {
-#pragma unroll
-        for (int j = 0; j < V; j++) {
-            float *z = j < V / 2 ? x + 2 * j : y + 2 * j - V;
-            pair(z[0], z[1], c[j], s[j]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; j++) pair(x[j], y[j], c[j], s[j]);
+        a = SIGN > 0 ? p * c[j] - q * s[j] : p * c[j] + q * s[j];
+        b = SIGN > 0 ? p * s[j] + q * c[j] : q * c[j] - p * s[j];
     }
 }
 
@@ -168,8 +181,8 @@ template <typename T, int CHUNKS>
 struct Chunks {
     T      *p[CHUNKS][2];
     int64_t by;
-    template <int V>
-    __device__ __forceinline__ void set(const tessel_heads &h, int64_t token, int head, const Mine<V, CHUNKS> &mine, int heads)
+    template <typename M>
+    __device__ __forceinline__ void set(const tessel_heads &h, int64_t token, int head, const M &mine, int heads)
     {
         T *z = (T *)h.data + token * h.token_stride + head * h.head_stride;
         by = h.head_stride << heads;
@@ -183,16 +196,18 @@ struct Chunks {
     __device__ __forceinline__ int64_t way(int s, bool full, bool there) const { return full || there ? s * by : max(s - 1, 0) * by; }
 };
 
-// eight values or fewer as they are in memory, noughts where they do not count
-template <typename T, int V>
-__device__ __forceinline__ void take(float *v, const typename Some<T, V>::type &x, bool counts)
+// the weights of a lane's channels
+template <int V, int CHUNKS, typename M>
+__device__ __forceinline__ void weights(float (&w)[CHUNKS][2][V], const float *from, const M &mine)
 {
-    spread<T, V>(v, x);
 #pragma unroll
-    for (int j = 0; j < V; j++) v[j] = counts ? v[j] : 0.0f;
+    for (int k = 0; k < CHUNKS; k++) {
+        get<V>(w[k][0], from + mine.first[k]);
+        get<V>(w[k][1], from + mine.second[k]);
+    }
 }
 
-template <typename T, int V, int CHUNKS, int GROUP>
+template <typename T, int V, int CHUNKS, int GROUP, bool NEAR, bool RAGGED>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateLaunch l)
 {
     __shared__ __attribute__((aligned(16))) float table[kWaves][2][64 * V * CHUNKS];
@@ -201,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateLaunch l)
     const int64_t unit = (int64_t)blockIdx.x * kWaves + wave;
     if (unit >= l.units) return;
     const Turn at(l, unit, tokens);
-    const Mine<V, CHUNKS> mine(a, lane & ((1 << l.group) - 1), 1 << l.group);
+    const Mine<V, CHUNKS, NEAR, RAGGED> mine(a, lane & ((1 << l.group) - 1), 1 << l.group);
     const int slot = lane >> l.group, head = slot & ((1 << l.heads) - 1), which = slot >> l.heads;
     const bool there = at.token + which < a.tokens;
     const int64_t token = min(at.token + which, a.tokens - 1);
@@ -209,8 +224,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateLaunch l)
     float c[CHUNKS][V], s[CHUNKS][V], w[CHUNKS][2][V];
 #pragma unroll
     for (int k = 0; k < CHUNKS; k++) {
-        get<V>(c[k], table[wave][0] + which * (a.dim / 2) + mine.pair[k]);
-        get<V>(s[k], table[wave][1] + which * (a.dim / 2) + mine.pair[k]);
+        get<V>(c[k], table[wave][0] + which * (a.turning / 2) + mine.pair[k]);
+        get<V>(s[k], table[wave][1] + which * (a.turning / 2) + mine.pair[k]);
     }
     Chunks<const T, CHUNKS> z;
     Chunks<T, CHUNKS> o;
@@ -219,63 +234,51 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateLaunch l)
         const int step = key ? i - l.steps_q : i, all = key ? a.kv_heads : a.heads;
         const bool full = (step + 1) << l.heads <= all, counts = full || (step << l.heads) + head < all;
         if (i == at.begin || i == l.steps_q) {
-            z.template set<V>(key ? a.k : a.q, token, min(head, all - 1), mine, l.heads);
-            o.template set<V>(key ? a.k_out : a.q_out, token, min(head, all - 1), mine, l.heads);
-            if (a.wq) {
-                const float *from = key ? a.wk : a.wq;
-#pragma unroll
-                for (int k = 0; k < CHUNKS; k++) {
-                    get<V>(w[k][0], from + mine.first[k]);
-                    get<V>(w[k][1], from + mine.second[k]);
-                }
-            }
+            z.set(key ? a.k : a.q, token, min(head, all - 1), mine, l.heads);
+            o.set(key ? a.k_out : a.q_out, token, min(head, all - 1), mine, l.heads);
+            if (a.wq) weights(w, key ? a.wk : a.wq, mine);
         }
         const int64_t way = z.way(step, full, counts), back = o.way(step, full, counts);
-        float x[CHUNKS][V], y[CHUNKS][V], sum = 0;
-        typename Some<T, V>::type rx[CHUNKS], ry[CHUNKS];
+        Raw<T, V, NEAR> raw[CHUNKS];
 #pragma unroll
-        for (int k = 0; k < CHUNKS; k++) {
-            rx[k] = *(const typename Some<T, V>::type *)(z.p[k][0] + way);
-            ry[k] = *(const typename Some<T, V>::type *)(z.p[k][1] + way);
-        }
+        for (int k = 0; k < CHUNKS; k++) raw[k].read(z.p[k][0] + way, z.p[k][1] + way);
+        float x[CHUNKS][2][V], sum = 0;
 #pragma unroll
-        for (int k = 0; k < CHUNKS; k++) {
-            take<T, V>(x[k], rx[k], mine.on[k]);
-            take<T, V>(y[k], ry[k], mine.on[k]);
-        }
+        for (int k = 0; k < CHUNKS; k++) raw[k].take(x[k], mine.on[k]);
         if (a.wq) {
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
-                for (int j = 0; j < V; j++) sum += x[k][j] * x[k][j] + y[k][j] * y[k][j];
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int j = 0; j < V; j++) sum += mine.counts(k, h, j) ? x[k][h][j] * x[k][h][j] : 0.0f;
             const float over = over_root(group_sum<GROUP>(sum, l.group) * l.share + a.eps);
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
-                for (int j = 0; j < V; j++) {
-                    x[k][j] *= over * w[k][0][j];
-                    y[k][j] *= over * w[k][1][j];
-                }
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int j = 0; j < V; j++) x[k][h][j] *= over * w[k][h][j];
         }
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            if (mine.turns[k]) turn<V, 1>(x[k], y[k], c[k], s[k], a.neighbours);
+            if (mine.turns[k]) turn<V, NEAR, 1>(x[k], c[k], s[k]);
             if (there && counts && mine.on[k]) {
-                put<T, V>(o.p[k][0] + back, x[k]);
-                put<T, V>(o.p[k][1] + back, y[k]);
+                raw[k].round(x[k]);
+                raw[k].write(o.p[k][0] + back, o.p[k][1] + back);
             }
         }
     }
 }
 
-template <typename T, int V, int CHUNKS, int GROUP>
+template <typename T, int V, int CHUNKS, int GROUP, bool NEAR, bool RAGGED>
 __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch l)
 {
     __shared__ __attribute__((aligned(16))) float table[kWaves][2][64 * V * CHUNKS];
     __shared__ float sums[kWaves][2][256];
     const tessel_rotation &a = l.a;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, tokens = 64 >> l.group >> l.heads;
-    const Mine<V, CHUNKS> mine(a, lane & ((1 << l.group) - 1), 1 << l.group);
+    const Mine<V, CHUNKS, NEAR, RAGGED> mine(a, lane & ((1 << l.group) - 1), 1 << l.group);
     const int slot = lane >> l.group, head = slot & ((1 << l.heads) - 1), which = slot >> l.heads;
     float dw[2][CHUNKS][2][V] = {}, w[CHUNKS][2][V];
     for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < l.units; unit += (int64_t)gridDim.x * kWaves) {
@@ -286,8 +289,8 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
         float c[CHUNKS][V], s[CHUNKS][V];
 #pragma unroll
         for (int k = 0; k < CHUNKS; k++) {
-            get<V>(c[k], table[wave][0] + which * (a.dim / 2) + mine.pair[k]);
-            get<V>(s[k], table[wave][1] + which * (a.dim / 2) + mine.pair[k]);
+            get<V>(c[k], table[wave][0] + which * (a.turning / 2) + mine.pair[k]);
+            get<V>(s[k], table[wave][1] + which * (a.turning / 2) + mine.pair[k]);
         }
         Chunks<const T, CHUNKS> z, g;
         Chunks<T, CHUNKS> o;
@@ -296,43 +299,33 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
             const int step = key ? i - l.steps_q : i, all = key ? a.kv_heads : a.heads;
             const bool full = (step + 1) << l.heads <= all, counts = full || (step << l.heads) + head < all;
             if (i == at.begin || i == l.steps_q) {
-                z.template set<V>(key ? a.k : a.q, token, min(head, all - 1), mine, l.heads);
-                g.template set<V>(key ? a.dk_out : a.dq_out, token, min(head, all - 1), mine, l.heads);
-                o.template set<V>(key ? a.dk : a.dq, token, min(head, all - 1), mine, l.heads);
-                if (a.wq) {
-                    const float *from = key ? a.wk : a.wq;
-#pragma unroll
-                    for (int k = 0; k < CHUNKS; k++) {
-                        get<V>(w[k][0], from + mine.first[k]);
-                        get<V>(w[k][1], from + mine.second[k]);
-                    }
-                }
+                z.set(key ? a.k : a.q, token, min(head, all - 1), mine, l.heads);
+                g.set(key ? a.dk_out : a.dq_out, token, min(head, all - 1), mine, l.heads);
+                o.set(key ? a.dk : a.dq, token, min(head, all - 1), mine, l.heads);
+                if (a.wq) weights(w, key ? a.wk : a.wq, mine);
             }
             const int64_t way = z.way(step, full, counts), down = g.way(step, full, counts), back = o.way(step, full, counts);
-            float x[CHUNKS][V], y[CHUNKS][V], dx[CHUNKS][V], dy[CHUNKS][V], sum = 0;
-            typename Some<T, V>::type rx[CHUNKS], ry[CHUNKS], gx[CHUNKS], gy[CHUNKS];
+            Raw<T, V, NEAR> raw[CHUNKS], grad[CHUNKS];
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++) {
-                rx[k] = *(const typename Some<T, V>::type *)(z.p[k][0] + way);
-                ry[k] = *(const typename Some<T, V>::type *)(z.p[k][1] + way);
-                gx[k] = *(const typename Some<T, V>::type *)(g.p[k][0] + down);
-                gy[k] = *(const typename Some<T, V>::type *)(g.p[k][1] + down);
+                raw[k].read(z.p[k][0] + way, z.p[k][1] + way);
+                grad[k].read(g.p[k][0] + down, g.p[k][1] + down);
             }
             // (heads and channels that are not there are noughts, which add nothing to the gradients of w)
+            float x[CHUNKS][2][V], d[CHUNKS][2][V], sum = 0;
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++) {
-                const bool mine_too = there && counts && mine.on[k];
-                take<T, V>(x[k], rx[k], mine_too);
-                take<T, V>(y[k], ry[k], mine_too);
-                take<T, V>(dx[k], gx[k], mine_too);
-                take<T, V>(dy[k], gy[k], mine_too);
-                if (mine.turns[k]) turn<V, -1>(dx[k], dy[k], c[k], s[k], a.neighbours);
+                raw[k].take(x[k], there && counts && mine.on[k]);
+                grad[k].take(d[k], there && counts && mine.on[k]);
+                if (mine.turns[k]) turn<V, NEAR, -1>(d[k], c[k], s[k]);
             }
             if (a.wq) {
 #pragma unroll
                 for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
-                    for (int j = 0; j < V; j++) sum += x[k][j] * x[k][j] + y[k][j] * y[k][j];
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int j = 0; j < V; j++) sum += mine.counts(k, h, j) ? x[k][h][j] * x[k][h][j] : 0.0f;
                 float over = over_root(group_sum<GROUP>(sum, l.group) * l.share + a.eps);
                 over = there && counts ? over : 0.0f;
                 sum = 0;
@@ -340,15 +333,14 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
 #pragma unroll
                     for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
-                        for (int j = 0; j < V; j++) {
-                            x[k][j] *= over;
-                            y[k][j] *= over;
-                            to[k][0][j] += dx[k][j] * x[k][j];
-                            to[k][1][j] += dy[k][j] * y[k][j];
-                            dx[k][j] *= w[k][0][j];
-                            dy[k][j] *= w[k][1][j];
-                            sum += dx[k][j] * x[k][j] + dy[k][j] * y[k][j];
-                        }
+                        for (int h = 0; h < 2; h++)
+#pragma unroll
+                            for (int j = 0; j < V; j++) {
+                                x[k][h][j] *= over;
+                                to[k][h][j] += d[k][h][j] * x[k][h][j];
+                                d[k][h][j] *= w[k][h][j];
+                                sum += mine.counts(k, h, j) ? d[k][h][j] * x[k][h][j] : 0.0f;
+                            }
                 };
                 if (key) add(dw[1]);
                 else add(dw[0]);
@@ -356,16 +348,15 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
 #pragma unroll
                 for (int k = 0; k < CHUNKS; k++)
 #pragma unroll
-                    for (int j = 0; j < V; j++) {
-                        dx[k][j] = over * (dx[k][j] - x[k][j] * mean);
-                        dy[k][j] = over * (dy[k][j] - y[k][j] * mean);
-                    }
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int j = 0; j < V; j++) d[k][h][j] = over * (d[k][h][j] - x[k][h][j] * mean);
             }
 #pragma unroll
             for (int k = 0; k < CHUNKS; k++)
                 if (there && counts && mine.on[k]) {
-                    put<T, V>(o.p[k][0] + back, dx[k]);
-                    put<T, V>(o.p[k][1] + back, dy[k]);
+                    raw[k].round(d[k]);
+                    raw[k].write(o.p[k][0] + back, o.p[k][1] + back);
                 }
         }
     }
@@ -381,7 +372,7 @@ __global__ __launch_bounds__(kThreads) void rotate_backward_kernel(RotateLaunch 
                 for (int j = 0; j < V; j++) {
                     float v = dw[i][k][h][j];
                     for (int d = 1 << l.group; d < 64; d <<= 1) v += __shfl_xor(v, d);
-                    if (slot == 0 && mine.on[k]) sums[wave][i][(h ? mine.second[k] : mine.first[k]) + j] = v;
+                    if (slot == 0 && mine.on[k] && mine.counts(k, h, j)) sums[wave][i][(h ? mine.second[k] : mine.first[k]) + j] = v;
                 }
     __syncthreads();
     for (int n = threadIdx.x; n < 2 * a.dim; n += kThreads) {
@@ -415,19 +406,25 @@ __global__ __launch_bounds__(1024) void rotate_sum_kernel(RotateLaunch l)
     *out = a.accumulate ? *out + sum : sum;
 }
 
-// Pairs a lane: four where no chunk of them lies across the end of those that turn, else one.  (Eight leave too few registers: 8192 tokens of 32 + 8 heads of
-// 128 bf16 66 instead of 56 us backward, 33 forward either way.)
+// Pairs a lane: four where those that turn and those that do not are each none or four at least, else one.  (Eight leave too few registers: 8192 tokens of
+// 32 + 8 heads of 128 bf16 66 instead of 56 us backward, 33 forward either way.)
 static int values_of(const tessel_rotation &a)
 {
-    const int turns = a.turning / 2, stays = (a.dim - a.turning) / 2;
-    return turns % 4 == 0 && stays % 4 == 0 ? 4 : 1;
+    const int turns = a.turning / 2, rest = (a.dim - a.turning) / 2;
+    return (turns == 0 || turns >= 4) && (rest == 0 || rest >= 4) ? 4 : 1;
+}
+static int chunks_of(const tessel_rotation &a)
+{
+    const int v = values_of(a), turns = a.turning / 2, rest = (a.dim - a.turning) / 2;
+    return (turns + v - 1) / v + (rest + v - 1) / v;
 }
 
 static RotateLaunch rotate_launch(const tessel_rotation &a)
 {
     RotateLaunch l = {};
     l.a = a;
-    const int chunks = a.dim / (2 * values_of(a));
+    if (a.turning == 0) l.a.neighbours = 1;                      // (in one piece; there is no pair that turns)
+    const int chunks = chunks_of(a);
     while (l.group < 6 && 1 << l.group < chunks) l.group++;
     while (l.heads < 6 - l.group && 1 << l.heads < a.heads) l.heads++;
     const int each = 1 << l.heads, tokens = 64 >> l.group >> l.heads;
@@ -444,14 +441,20 @@ static RotateLaunch rotate_launch(const tessel_rotation &a)
 
 int rotate_parts(const tessel_rotation &a) { return (int)std::min<int64_t>((rotate_launch(a).units + kWaves - 1) / kWaves, 1024); }
 
+template <typename T, bool NEAR>
+static const void *rotate_of(const tessel_rotation &a, bool back)
+{
+#define PICK(V, K, G, R) (back ? (const void *)rotate_backward_kernel<T, V, K, G, NEAR, R> : (const void *)rotate_kernel<T, V, K, G, NEAR, R>)
+    if (values_of(a) == 1) return a.dim > 128 ? PICK(1, 2, -1, false) : PICK(1, 1, -1, false);
+    if (a.turning % 8 || (a.dim - a.turning) % 8) return PICK(4, 1, -1, true);
+    // (heads of 72 to 128 and of 40 to 64 channels without a branch for each step of their sums)
+    return a.dim > 128 || a.dim <= 32 ? PICK(4, 1, -1, false) : a.dim > 64 ? PICK(4, 1, 4, false) : PICK(4, 1, 3, false);
+#undef PICK
+}
 template <typename T>
 static const void *rotate_of(const tessel_rotation &a, bool back)
 {
-#define PICK(V, K, G) (back ? (const void *)rotate_backward_kernel<T, V, K, G> : (const void *)rotate_kernel<T, V, K, G>)
-    // (heads of 72 to 128 and of 40 to 64 channels in fours without a branch for each step of their sums)
-    if (values_of(a) == 4) return a.dim > 128 || a.dim <= 32 ? PICK(4, 1, -1) : a.dim > 64 ? PICK(4, 1, 4) : PICK(4, 1, 3);
-    return a.dim > 128 ? PICK(1, 2, -1) : PICK(1, 1, -1);
-#undef PICK
+    return a.neighbours || a.turning == 0 ? rotate_of<T, true>(a, back) : rotate_of<T, false>(a, back);
 }
 static const void *rotate_of(const tessel_rotation &a, bool back)
 {

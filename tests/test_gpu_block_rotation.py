@@ -71,7 +71,7 @@ def test_heads(ops, dim, turning, dtype, normed, neighbours):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("dim, turning", [(2, 2), (2, 0), (4, 2), (6, 6), (6, 4), (10, 8), (12, 12), (16, 16), (16, 8), (18, 2), (24, 24), (32, 32), (48, 16), (50, 50), (66, 66), (72, 72),
                                           (100, 50), (112, 112), (120, 40), (126, 124), (128, 0), (128, 2), (128, 126), (136, 136), (160, 80), (192, 192), (200, 200), (224, 32), (254, 254),
-                                          (254, 100), (256, 64), (256, 0), (256, 240)])
+                                          (254, 100), (256, 64), (256, 0), (256, 240), (128, 120), (80, 60), (256, 130), (256, 250), (22, 10), (20, 8), (40, 32), (18, 10)])
 def test_dims_of_every_kind(ops, dim, turning, dtype):
     for neighbours in (False, True):
         check(ops, inputs(5, 3, 2, dim, dtype, True, seed=dim + turning), positions(5), turning, neighbours)
