@@ -67,6 +67,7 @@ struct EmbedLaunch {
     int32_t  lanes, tiles;       // that hold a run's columns: a power of two up to 256, eight columns each; of them, to the end of a row
     uint32_t sum_groups;         // workgroups that add up
     uint32_t fill_rows, fill_pieces, fill_lanes;      // and of one that fills: rows, or pieces of a row; lanes a row takes
+    int32_t  fill_size;          // values it fills at most
 };
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
@@ -288,15 +289,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(EmbedLaunch l)
     }
 }
 
-constexpr int kFill = 16384;     // values that a workgroup fills with zeros
+constexpr int kFill = 16384, kFillFew = 4096;     // values that a workgroup fills with zeros, beside sums of a sorted batch and of few tokens (whose launch is short)
 
 // Zeros in the rows of a piece that no token asked for; neighbouring workgroups write neighbouring pieces.
 struct Piece {
     int64_t row;                 // the first of fill_rows
     int     begin, end;          // columns
-    __device__ __forceinline__ Piece(const EmbedLaunch &l, uint32_t piece) : row((int64_t)(piece / l.fill_pieces) * l.fill_rows), begin(piece % l.fill_pieces * kFill)
+    __device__ __forceinline__ Piece(const EmbedLaunch &l, uint32_t piece) : row((int64_t)(piece / l.fill_pieces) * l.fill_rows), begin(piece % l.fill_pieces * l.fill_size)
     {
-        end = (int)min((int64_t)l.a.channels, (int64_t)begin + kFill);
+        end = (int)min((int64_t)l.a.channels, (int64_t)begin + l.fill_size);
     }
 };
 template <int THREADS, typename F>
@@ -330,14 +331,14 @@ template <typename T, int WAVES, bool NARROW>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(EmbedLaunch l)
 {
     __shared__ uint64_t found[WAVES];
-    __shared__ uint32_t seen[kFill / 32];
+    __shared__ uint32_t seen[kFillFew / 32];
     __shared__ float4v sums[WAVES][2][64];
     const tessel_embedding &a = l.a;
     const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int mine = thread < a.tokens ? row_at(a, thread) : -1;
     if (blockIdx.x >= l.sum_groups) {
         const Piece p(l, blockIdx.x - l.sum_groups);
-        for (int n = thread; n < kFill / 32; n += 64 * WAVES) seen[n] = 0;
+        for (int n = thread; n < kFillFew / 32; n += 64 * WAVES) seen[n] = 0;
         __syncthreads();
         if (mine >= p.row && mine < p.row + l.fill_rows) atomicOr(&seen[(mine - p.row) / 32], 1u << (mine - p.row) % 32);
         __syncthreads();
@@ -547,8 +548,9 @@ static EmbedLaunch embed_launch(const tessel_embedding &a)
     l.sum_groups = (uint32_t)((l.runs + kThreads / l.lanes - 1) / (kThreads / l.lanes) * l.tiles);
     l.fill_lanes = 1;
     while (l.fill_lanes < 64 && 4 * (int)l.fill_lanes < a.channels) l.fill_lanes *= 2;
-    l.fill_rows = (uint32_t)std::max(1, kFill / a.channels);
-    l.fill_pieces = (uint32_t)((a.channels + kFill - 1) / kFill);
+    l.fill_size = few(a) ? kFillFew : kFill;
+    l.fill_rows = (uint32_t)std::max(1, l.fill_size / a.channels);
+    l.fill_pieces = (uint32_t)(((int64_t)a.channels + l.fill_size - 1) / l.fill_size);
     if (few(a)) {
         l.tiles = (int)(((int64_t)a.channels + 511) / 512);
         l.sum_groups = (uint32_t)(a.tokens * l.tiles);
@@ -580,9 +582,9 @@ int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *
     void *args[] = {&l};
     const int64_t groups = sum_groups(a, l);
     if (few(a)) {
-        const int waves = a.tokens <= 64 ? 1 : a.tokens <= 256 ? 4 : 8;
+        const int waves = a.tokens <= 256 ? 4 : 8;
 #define PICK(T, W) (a.channels < 8 ? (const void *)few_kernel<T, W, true> : (const void *)few_kernel<T, W, false>)
-#define KERNEL(T) (waves == 1 ? PICK(T, 1) : waves == 4 ? PICK(T, 4) : PICK(T, 8))
+#define KERNEL(T) (waves == 4 ? PICK(T, 4) : PICK(T, 8))
         return groups ? launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)groups), dim3(64 * waves), args, 0, (hipStream_t)stream)) : 0;
 #undef KERNEL
 #undef PICK
