@@ -67,7 +67,6 @@ struct EmbedLaunch {
     int32_t  lanes, tiles;       // that hold a run's columns: a power of two up to 256, eight columns each; of them, to the end of a row
     uint32_t sum_groups;         // workgroups that add up
     uint32_t fill_rows, fill_pieces, fill_lanes;      // and of one that fills: rows, or pieces of a row; lanes a row takes
-    int32_t  fill_size;          // values it fills at most
 };
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
@@ -289,15 +288,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(EmbedLaunch l)
     }
 }
 
-constexpr int kFill = 16384, kFillFew = 4096;     // values that a workgroup fills with zeros, beside sums of a sorted batch and of few tokens (whose launch is short)
+constexpr int kFill = 4096;      // values that a workgroup fills with zeros at most (100000 rows of 264 channels 18 us, 200000 of 40 10.6; four times as many a workgroup 19 and 14)
 
 // Zeros in the rows of a piece that no token asked for; neighbouring workgroups write neighbouring pieces.
 struct Piece {
     int64_t row;                 // the first of fill_rows
     int     begin, end;          // columns
-    __device__ __forceinline__ Piece(const EmbedLaunch &l, uint32_t piece) : row((int64_t)(piece / l.fill_pieces) * l.fill_rows), begin(piece % l.fill_pieces * l.fill_size)
+    __device__ __forceinline__ Piece(const EmbedLaunch &l, uint32_t piece) : row((int64_t)(piece / l.fill_pieces) * l.fill_rows), begin(piece % l.fill_pieces * kFill)
     {
-        end = (int)min((int64_t)l.a.channels, (int64_t)begin + l.fill_size);
+        end = (int)min((int64_t)l.a.channels, (int64_t)begin + kFill);
     }
 };
 template <int THREADS, typename F>
@@ -331,14 +330,14 @@ template <typename T, int WAVES, bool NARROW>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(EmbedLaunch l)
 {
     __shared__ uint64_t found[WAVES];
-    __shared__ uint32_t seen[kFillFew / 32];
+    __shared__ uint32_t seen[kFill / 32];
     __shared__ float4v sums[WAVES][2][64];
     const tessel_embedding &a = l.a;
     const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int mine = thread < a.tokens ? row_at(a, thread) : -1;
     if (blockIdx.x >= l.sum_groups) {
         const Piece p(l, blockIdx.x - l.sum_groups);
-        for (int n = thread; n < kFillFew / 32; n += 64 * WAVES) seen[n] = 0;
+        for (int n = thread; n < kFill / 32; n += 64 * WAVES) seen[n] = 0;
         __syncthreads();
         if (mine >= p.row && mine < p.row + l.fill_rows) atomicOr(&seen[(mine - p.row) / 32], 1u << (mine - p.row) % 32);
         __syncthreads();
@@ -548,9 +547,8 @@ static EmbedLaunch embed_launch(const tessel_embedding &a)
     l.sum_groups = (uint32_t)((l.runs + kThreads / l.lanes - 1) / (kThreads / l.lanes) * l.tiles);
     l.fill_lanes = 1;
     while (l.fill_lanes < 64 && 4 * (int)l.fill_lanes < a.channels) l.fill_lanes *= 2;
-    l.fill_size = few(a) ? kFillFew : kFill;
-    l.fill_rows = (uint32_t)std::max(1, l.fill_size / a.channels);
-    l.fill_pieces = (uint32_t)(((int64_t)a.channels + l.fill_size - 1) / l.fill_size);
+    l.fill_rows = (uint32_t)std::max(1, kFill / a.channels);
+    l.fill_pieces = (uint32_t)(((int64_t)a.channels + kFill - 1) / kFill);
     if (few(a)) {
         l.tiles = (int)(((int64_t)a.channels + 511) / 512);
         l.sum_groups = (uint32_t)(a.tokens * l.tiles);
