@@ -22,8 +22,10 @@ struct Draw {
     static constexpr uint32_t kA = 0xD2511F53u, kC = 0xCD9E8D57u, kK = 0x9E3779B9u, kM = 0xBB67AE85u;
     uint32_t least, k, m, first;                                 // (the same for all lanes)
     float    by;
+    int      counters;           // one where a row has no more than four channels
     uint32_t b[2], c[2], d[2], e[2];                             // of the two counters, behind the second and third round
-    __device__ __forceinline__ Draw(const DropLaunch &l, int col) : least(l.least), k((uint32_t)l.seed), m((uint32_t)(l.seed >> 32)), first(0), by(l.by)
+    __device__ __forceinline__ Draw(const DropLaunch &l, int channels, int col)
+        : least(l.least), k((uint32_t)l.seed), m((uint32_t)(l.seed >> 32)), first(0), by(l.by), counters(channels > 4 ? 2 : 1)
     {
         if (least == 0) return;
         const uint64_t number = l.number + (l.step ? *l.step : 0), q = (uint64_t)(uint32_t)number * kC;
@@ -45,6 +47,7 @@ struct Draw {
         const uint64_t p = (uint64_t)(first ^ token) * kA;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
+            if (h >= counters) break;
             const uint64_t q = wide_product((uint32_t)(p >> 32) ^ b[h], kC);
             uint32_t w[4] = {(uint32_t)(q >> 32) ^ c[h], (uint32_t)q, d[h] ^ (uint32_t)p, e[h]};
 #pragma unroll
@@ -60,6 +63,20 @@ struct Draw {
         }
     }
 };
+
+// Eight values of a row without a branch around the read, and put in their places behind all reads (tessel_rows.h); rows of fewer than eight, which a
+// NARROW kernel may have, in pieces of four, two and one.
+template <typename T, bool NARROW>
+__device__ __forceinline__ typename Eight<T>::type read8(const T *row, int col, int channels)
+{
+    if (NARROW && channels < 8) return raw8<T>(row, col, channels);
+    return take8<T, false>(row, col, channels);
+}
+template <typename T, bool NARROW>
+__device__ __forceinline__ void place8(int col, int channels, typename Eight<T>::type &x)
+{
+    if (!NARROW || channels >= 8) settle8<T, false>(col, channels, x);
+}
 
 // The places of a wave in [tokens][channels], ROWS tokens a lane: WIDE, 64 chunks of eight channels of the same tokens (a wave for each tile of 512 channels);
 // else 64 / lanes tokens at a time, `lanes` a power of two.

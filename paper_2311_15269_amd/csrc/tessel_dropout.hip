@@ -15,14 +15,14 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(tessel_dropout_rows a
     const Span<WIDE, ROWS> at(a.channels, lanes);
     typename Eight<T>::type x[ROWS];
 #pragma unroll
-    for (int r = 0; r < ROWS; r++) x[r] = take8<T, !WIDE>((const T *)a.x.data + min(at.token + r * at.step, a.tokens - 1) * a.x.stride, at.col, a.channels);
-    const Draw draw(l, at.col);
+    for (int r = 0; r < ROWS; r++) x[r] = read8<T, !WIDE>((const T *)a.x.data + min(at.token + r * at.step, a.tokens - 1) * a.x.stride, at.col, a.channels);
+    const Draw draw(l, a.channels, at.col);
 #pragma unroll
     for (int r = 0; r < ROWS; r++) {
         const int64_t token = at.token + r * at.step;
         if (token >= a.tokens) break;
         float v[8];
-        settle8<T, !WIDE>(at.col, a.channels, x[r]);
+        place8<T, !WIDE>(at.col, a.channels, x[r]);
         widen8<T>(v, x[r]);
         if (l.least) draw.apply(v, (uint32_t)token);
         store8<T>((T *)a.y.data + token * a.y.stride, v, at.col, a.channels);

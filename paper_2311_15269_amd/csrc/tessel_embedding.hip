@@ -36,14 +36,14 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(tessel_embedding a, Dro
 #pragma unroll
     for (int r = 0; r < ROWS; r++) row[r] = row_at(a, min(at.token + r * at.step, a.tokens - 1));
 #pragma unroll
-    for (int r = 0; r < ROWS; r++) x[r] = take8<T, !WIDE>((const T *)a.table.data + max(row[r], 0) * a.table.stride, at.col, a.channels);
-    const Draw draw(d, at.col);
+    for (int r = 0; r < ROWS; r++) x[r] = read8<T, !WIDE>((const T *)a.table.data + max(row[r], 0) * a.table.stride, at.col, a.channels);
+    const Draw draw(d, a.channels, at.col);
 #pragma unroll
     for (int r = 0; r < ROWS; r++) {
         const int64_t token = at.token + r * at.step;
         if (token >= a.tokens) break;
         float v[8];
-        settle8<T, !WIDE>(at.col, a.channels, x[r]);
+        place8<T, !WIDE>(at.col, a.channels, x[r]);
         widen8<T>(v, x[r]);
 #pragma unroll
         for (int j = 0; j < 8; j++) v[j] = row[r] >= 0 ? v[j] * a.scale : 0.0f;
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(EmbedLaunch l)
     int first = 0;
     while (found[first] == 0) first++;                           // (one of them is this token)
     if (64 * first + __builtin_ctzll(found[first]) != token) return;
-    const Draw draw(l.d, col);
+    const Draw draw(l.d, a.channels, col);
     float sum[8] = {};
     while (same) {
         constexpr int kAhead = 8;
@@ -365,12 +365,12 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(EmbedLaunch l)
             same &= same - 1;
         }
 #pragma unroll
-        for (int j = 0; j < kAhead; j++) x[j] = take8<T, NARROW>((const T *)a.d_out.data + t[j] * a.d_out.stride, col, a.channels);
+        for (int j = 0; j < kAhead; j++) x[j] = read8<T, NARROW>((const T *)a.d_out.data + t[j] * a.d_out.stride, col, a.channels);
 #pragma unroll
         for (int j = 0; j < kAhead; j++) {
             if (j >= n) break;
             float v[8];
-            settle8<T, NARROW>(col, a.channels, x[j]);
+            place8<T, NARROW>(col, a.channels, x[j]);
             widen8<T>(v, x[j]);
             if (l.d.least) draw.apply(v, (uint32_t)t[j]);
 #pragma unroll
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
     look(begin);
     const int last = l.row[min(first + l.run, a.tokens) - 1], behind = l.row[min(first + l.run, a.tokens - 1)], before = l.row[max(first - 1, (int64_t)0)];
     if (first >= total || col >= a.channels) return;
-    const Draw draw(l.d, col);
+    const Draw draw(l.d, a.channels, col);
     int row = r[0];
     bool starts = begin == 0 || before != row;                   // (the row's first place is in this run)
     const bool goes_on = first + l.run < total && behind == last;
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
         typename Eight<T>::type x[kAhead];
         if (i > begin) look(i);
 #pragma unroll
-        for (int j = 0; j < kAhead; j++) x[j] = take8<T, NARROW>((const T *)a.d_out.data + t[j] * a.d_out.stride, col, a.channels);
+        for (int j = 0; j < kAhead; j++) x[j] = read8<T, NARROW>((const T *)a.d_out.data + t[j] * a.d_out.stride, col, a.channels);
 #pragma unroll
         for (int j = 0; j < kAhead; j++) {
             if (i + j >= end) break;
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
                 for (int k = 0; k < 8; k++) sum[k] = 0;
             }
             float v[8];
-            settle8<T, NARROW>(col, a.channels, x[j]);
+            place8<T, NARROW>(col, a.channels, x[j]);
             widen8<T>(v, x[j]);
             if (l.d.least) draw.apply(v, (uint32_t)t[j]);
 #pragma unroll
