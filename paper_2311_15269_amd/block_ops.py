@@ -644,21 +644,28 @@ def frequencies(turning, base=10000.0, device=None):
 
 def _describe_rotation(q, k, positions, frequency, wq, wk, eps, neighbours):
     import torch
-    _on_gpu(q, ("tokens", "heads", "dim"))
-    if k.dim() != 3 or k.shape[1] > MOST:
-        _refuse("expected [tokens, heads, dim], got %s" % (tuple(k.shape),))
-    n, heads, dim = q.shape
+    at, shape = q.get_device(), q.shape
+    if len(shape) != 3 or k.dim() != 3 or at < 0:
+        _refuse("expected [tokens, heads, dim] on the GPU, got %s and %s on %s" % (tuple(shape), tuple(k.shape), q.device))
+    n, heads, dim = shape
     kv_heads, pairs = k.shape[1], frequency.numel()
+    if max(n, heads, kv_heads, dim) > MOST:
+        _too_big(max(n, heads, kv_heads, dim))
+    if q.requires_grad:
+        _refuse_gradient(q)
     _same(q, (n, kv_heads, dim), k)
-    if frequency.dtype is not torch.float64 or frequency.dim() != 1 or not frequency.is_contiguous() or frequency.get_device() != q.get_device():
+    if frequency.dtype is not torch.float64 or frequency.dim() != 1 or not frequency.is_contiguous() or frequency.get_device() != at:
         _refuse("frequencies are contiguous 64-bit numbers on %s" % q.device)
     if 2 * pairs > dim:
         _refuse("%d pairs of %d channels" % (pairs, dim))
-    if (wq is None) != (wk is None):
+    kind, where = _index(positions, n, q)
+    if wq is None and wk is None:
+        weights = (0, 0)
+    elif wq is None or wk is None:
         _refuse("weights for both, queries and keys, or for neither")
-    kind, at = _index(positions, n, q)
-    return (_type(q), kind, heads, kv_heads, dim, 2 * pairs, 1 if neighbours else 0, _number(eps), n, at, frequency.data_ptr(),
-            0 if wq is None else _vector(wq, dim, q), 0 if wk is None else _vector(wk, dim, q), *_heads(q), *_heads(k))
+    else:
+        weights = (_vector(wq, dim, q), _vector(wk, dim, q))
+    return (_type(q), kind, heads, kv_heads, dim, 2 * pairs, 1 if neighbours else 0, _number(eps), n, where, frequency.data_ptr(), *weights, *_heads(q), *_heads(k))
 
 
 def rotate(q, k, positions, frequency, wq=None, wk=None, eps=1e-6, neighbours=False):
