@@ -58,7 +58,6 @@ struct DropLaunch {
 int launch_dropout(const tessel_dropout_rows &a, const DropLaunch &d, void *stream);
 
 int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream);
-bool embed_launchable(const tessel_embedding &a);        // backward
 size_t embed_workspace(const tessel_embedding &a);
 int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *workspace, void *stream);
 

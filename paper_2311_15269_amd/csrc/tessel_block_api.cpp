@@ -480,7 +480,6 @@ int tessel_embedding_backward_workspace_bytes(const tessel_embedding *a, size_t 
     if (!bytes) return TESSEL_E_INVALID_ARG;
     const int e = embedding_sizes_ok(a);
     if (e) return e;
-    if (!embed_launchable(*a)) return TESSEL_E_TOOBIG;
     *bytes = embed_workspace(*a);
     return TESSEL_OK;
 }
@@ -490,7 +489,6 @@ int tessel_embedding_backward(const tessel_embedding *a, void *workspace_dev, si
     DropLaunch l;
     const int e = embedding_ok(a, l);
     if (e) return e;
-    if (!embed_launchable(*a)) return TESSEL_E_TOOBIG;
     if (!rows_ok(a->d_out, a->type, a->tokens, a->channels, false) || !a->dtable || !aligned(a->dtable, 4) || a->dtable_stride < a->channels ||
         a->dtable_stride > kMostStride) return TESSEL_E_INVALID_ARG;
     if (!workspace_ok(workspace_dev, workspace_bytes, embed_workspace(*a))) return TESSEL_E_WORKSPACE;

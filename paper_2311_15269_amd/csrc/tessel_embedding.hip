@@ -66,7 +66,8 @@ struct EmbedLaunch {
     int32_t  run, runs;          // sorted places a run
     int32_t  lanes, tiles;       // that hold a run's columns: a power of two up to 256, eight columns each; of them, to the end of a row
     uint32_t sum_groups;         // workgroups that add up
-    uint32_t fill_rows, fill_pieces, fill_lanes;      // and of one that fills: rows, or pieces of a row; lanes a row takes
+    uint32_t fill_rows, fill_pieces, fill_lanes;      // zeros: rows a piece, pieces a row (one of the two is one); lanes a row takes
+    int64_t  fills;              // pieces in all
 };
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
@@ -294,7 +295,7 @@ constexpr int kFill = 4096;      // values that a workgroup fills with zeros at 
 struct Piece {
     int64_t row;                 // the first of fill_rows
     int     begin, end;          // columns
-    __device__ __forceinline__ Piece(const EmbedLaunch &l, uint32_t piece) : row((int64_t)(piece / l.fill_pieces) * l.fill_rows), begin(piece % l.fill_pieces * kFill)
+    __device__ __forceinline__ Piece(const EmbedLaunch &l, int64_t piece) : row(piece / l.fill_pieces * l.fill_rows), begin((int)(piece % l.fill_pieces) * kFill)
     {
         end = (int)min((int64_t)l.a.channels, (int64_t)begin + kFill);
     }
@@ -336,12 +337,15 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(EmbedLaunch l)
     const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int mine = thread < a.tokens ? row_at(a, thread) : -1;
     if (blockIdx.x >= l.sum_groups) {
-        const Piece p(l, blockIdx.x - l.sum_groups);
-        for (int n = thread; n < kFill / 32; n += 64 * WAVES) seen[n] = 0;
-        __syncthreads();
-        if (mine >= p.row && mine < p.row + l.fill_rows) atomicOr(&seen[(mine - p.row) / 32], 1u << (mine - p.row) % 32);
-        __syncthreads();
-        fill<64 * WAVES>(l, p, [&](int r) { return seen[r / 32] >> r % 32 & 1; });
+        for (int64_t piece = blockIdx.x - l.sum_groups; piece < l.fills; piece += gridDim.x - l.sum_groups) {
+            const Piece p(l, piece);
+            for (int n = thread; n < kFill / 32; n += 64 * WAVES) seen[n] = 0;
+            __syncthreads();
+            if (mine >= p.row && mine < p.row + l.fill_rows) atomicOr(&seen[(mine - p.row) / 32], 1u << (mine - p.row) % 32);
+            __syncthreads();
+            fill<64 * WAVES>(l, p, [&](int r) { return seen[r / 32] >> r % 32 & 1; });
+            __syncthreads();
+        }
         return;
     }
     const int token = blockIdx.x / l.tiles, col = 8 * (blockIdx.x % l.tiles * 64 + lane), row = row_at(a, token);
@@ -396,17 +400,18 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(EmbedLaunch l)
 }
 
 // Sums over runs of sorted places, eight columns a lane.  Rows that lie inside a run are whole; of the row that it begins within and of the
-// one that goes on behind it, it leaves a part.  The workgroups
-// behind these fill the other rows, whose stores hide the way of the sums' reads.
-// WIDE: a run's columns take whole waves, which so read rows and places by the scalar unit
+// one that goes on behind it, it leaves a part.  The workgroups behind these fill the other rows, whose stores hide the way of the sums' reads.  WIDE: a run's columns
+// take whole waves, which so read rows and places by the scalar unit
 template <typename T, bool WIDE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void sum_kernel(EmbedLaunch l)
 {
     constexpr int kAhead = 8;
     const tessel_embedding &a = l.a;
     if (blockIdx.x >= l.sum_groups) {
-        const Piece p(l, blockIdx.x - l.sum_groups);
-        fill<kThreads>(l, p, [&](int r) { return l.count[((p.row + r) & ((1 << l.shift) - 1)) * l.bins + ((p.row + r) >> l.shift)] != 0; });
+        for (int64_t piece = blockIdx.x - l.sum_groups; piece < l.fills; piece += gridDim.x - l.sum_groups) {
+            const Piece p(l, piece);
+            fill<kThreads>(l, p, [&](int r) { return l.count[((p.row + r) & ((1 << l.shift) - 1)) * l.bins + ((p.row + r) >> l.shift)] != 0; });
+        }
         return;
     }
     const int group = blockIdx.x / l.tiles, tile = blockIdx.x % l.tiles;
@@ -549,6 +554,7 @@ static EmbedLaunch embed_launch(const tessel_embedding &a)
     while (l.fill_lanes < 64 && 4 * (int)l.fill_lanes < a.channels) l.fill_lanes *= 2;
     l.fill_rows = (uint32_t)std::max(1, kFill / a.channels);
     l.fill_pieces = (uint32_t)(((int64_t)a.channels + kFill - 1) / kFill);
+    l.fills = a.accumulate ? 0 : (a.rows + (int64_t)l.fill_rows - 1) / l.fill_rows * l.fill_pieces;
     if (few(a)) {
         l.tiles = (int)(((int64_t)a.channels + 511) / 512);
         l.sum_groups = (uint32_t)(a.tokens * l.tiles);
@@ -559,12 +565,6 @@ static EmbedLaunch embed_launch(const tessel_embedding &a)
 static size_t whole_chunks(int64_t words) { return (size_t)(words + 3) / 4 * 4; }
 static size_t sorted_of(const tessel_embedding &a) { return whole_chunks(a.tokens + 8); }      // (sum_kernel reads eight at once)
 static size_t counts_of(const tessel_embedding &a, const EmbedLaunch &l) { return a.accumulate ? 0 : whole_chunks((int64_t)l.bins << l.shift); }
-// workgroups of sum_kernel
-static int64_t sum_groups(const tessel_embedding &a, const EmbedLaunch &l)
-{
-    return l.sum_groups + (a.accumulate ? 0 : (a.rows + (int64_t)l.fill_rows - 1) / l.fill_rows * l.fill_pieces);
-}
-bool embed_launchable(const tessel_embedding &a) { return sum_groups(a, embed_launch(a)) <= UINT32_MAX / kThreads; }
 
 size_t embed_workspace(const tessel_embedding &a)
 {
@@ -578,7 +578,7 @@ int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *
     EmbedLaunch l = embed_launch(a);
     l.d = d;
     void *args[] = {&l};
-    const int64_t groups = sum_groups(a, l);
+    const int64_t groups = l.sum_groups + std::min(l.fills, (int64_t)1 << 20);
     if (few(a)) {
         const int waves = a.tokens <= 256 ? 4 : 8;
 #define PICK(T, W) (a.channels < 8 ? (const void *)few_kernel<T, W, true> : (const void *)few_kernel<T, W, false>)

@@ -271,3 +271,16 @@ def test_long_batches(ops, n, hot):
     for kind in (torch.int64, torch.int32):
         got = ops.embed_backward(d.cuda(), token.to(kind).cuda(), 990)
         R.close(got, *R.embedding_gradient(d, token, 990, 1.0, 0), "dtable")
+
+
+def test_more_pieces_of_zeros_than_workgroups(ops):
+    """2.2 million rows of 2050 channels, a workgroup a row and more than 2^20 of them, for few tokens and for many"""
+    rows, c = 2200000, 2050
+    for n in (5, 600):
+        token = torch.randint(0, rows, (n,), generator=torch.Generator().manual_seed(n))
+        token[0], token[1] = 0, rows - 1
+        got = torch.full((rows, c), float("nan"), device="cuda")
+        del got                                                     # (the memory that the call below is likely to get)
+        got = ops.embed_backward(torch.ones(n, c, dtype=torch.bfloat16, device="cuda"), token.cuda(), rows)
+        assert torch.equal(got.sum(1, dtype=torch.float64).cpu(), c * torch.bincount(token, minlength=rows).double())
+        del got
