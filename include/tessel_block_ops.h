@@ -237,7 +237,7 @@ int  tessel_embedding_backward(const tessel_embedding *a, void *workspace_dev, s
 typedef struct {
     int32_t  type;
     int32_t  index_type;    /* of position: TESSEL_I32 or TESSEL_I64                                       */
-    int32_t  heads;
+    int32_t  heads;         /* at most 2^24, as kv_heads                                                   */
     int32_t  kv_heads;
     int32_t  dim;           /* even, at most 256                                                           */
     int32_t  turning;       /* even, 0 .. dim                                                              */

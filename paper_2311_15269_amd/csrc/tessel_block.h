@@ -61,6 +61,7 @@ int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream);
 size_t embed_workspace(const tessel_embedding &a);
 int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *workspace, void *stream);
 
+int64_t rotate_waves(const tessel_rotation &a);   // forward
 int launch_rotate(const tessel_rotation &a, void *stream);
 int rotate_parts(const tessel_rotation &a);
 int launch_rotate_backward(const tessel_rotation &a, float *parts, void *stream);

@@ -218,8 +218,8 @@ int rotation_sizes_ok(const tessel_rotation *a)
 {
     if (!a || a->tokens < 0 || a->heads < 1 || a->kv_heads < 1 || a->dim < 2 || a->dim % 2 || a->turning < 0 || a->turning > a->dim || a->turning % 2)
         return TESSEL_E_INVALID_ARG;
-    // (a wave for each head of a token)
-    if (a->dim > 256 || a->tokens > INT32_MAX || ((int64_t)a->heads + a->kv_heads) * 64 > kMostThreads / 256 * 256 / std::max<int64_t>(1, a->tokens)) return TESSEL_E_TOOBIG;
+    if (a->dim > 256 || a->tokens > INT32_MAX || a->heads > 1 << 24 || a->kv_heads > 1 << 24) return TESSEL_E_TOOBIG;
+    if (rotate_waves(*a) > kMostThreads / 256 * 4) return TESSEL_E_TOOBIG;       // (workgroups of four waves)
     return TESSEL_OK;
 }
 

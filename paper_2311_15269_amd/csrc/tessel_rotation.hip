@@ -439,6 +439,7 @@ static RotateLaunch rotate_launch(const tessel_rotation &a)
     return l;
 }
 
+int64_t rotate_waves(const tessel_rotation &a) { return rotate_launch(a).units; }
 int rotate_parts(const tessel_rotation &a) { return (int)std::min<int64_t>((rotate_launch(a).units + kWaves - 1) / kWaves, 1024); }
 
 template <typename T, bool NEAR>

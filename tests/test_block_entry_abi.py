@@ -82,7 +82,7 @@ def rotation(**change):
 
 @pytest.mark.parametrize("change, code", [
     ({"tokens": -1}, INVALID), ({"heads": 0}, INVALID), ({"kv_heads": 0}, INVALID), ({"dim": 0}, INVALID), ({"dim": 63}, INVALID), ({"turning": 66}, INVALID), ({"turning": 3}, INVALID),
-    ({"turning": -2}, INVALID), ({"dim": 258}, TOOBIG), ({"tokens": 1 << 31}, TOOBIG), ({"tokens": 1 << 20, "heads": 64}, TOOBIG), ({"heads": (1 << 31) - 1, "kv_heads": (1 << 31) - 1}, TOOBIG),
+    ({"turning": -2}, INVALID), ({"dim": 258}, TOOBIG), ({"tokens": 1 << 31}, TOOBIG), ({"tokens": (1 << 26) + 64, "heads": 64}, TOOBIG), ({"heads": (1 << 24) + 1}, TOOBIG), ({"kv_heads": (1 << 31) - 1}, TOOBIG),
     ({"type": 3}, UNSUPPORTED), ({"index_type": 5}, UNSUPPORTED), ({"eps": -1.0}, INVALID), ({"eps": NAN}, INVALID), ({"eps": INF}, INVALID), ({"wq": None}, INVALID), ({"wk": None}, INVALID),
     ({"wq": AT + 2}, INVALID), ({"frequency": None}, INVALID), ({"frequency": AT + 4}, INVALID), ({"position": None}, INVALID), ({"position": AT + 4}, INVALID),
     ({"q": B.Heads(None, 256, 64)}, INVALID), ({"q": B.Heads(AT + 1, 256, 64)}, INVALID), ({"k": B.Heads(AT, -2, 64)}, INVALID), ({"k": B.Heads(AT, 1 << 41, 64)}, INVALID),
@@ -91,6 +91,14 @@ def test_rotation_refuses(change, code):
     lib, a = B._library(), rotation(**change)
     assert lib.tessel_rotation_forward(C.byref(a), None) == code
     assert lib.tessel_rotation_backward(C.byref(a), AT, 1 << 50, None) == code
+
+
+def test_rotation_of_many_tokens():
+    """a wave for all heads of a token where there are many: 2^26 waves are the threads of a launch"""
+    n = C.c_size_t()
+    for tokens, heads, code in (((1 << 26) - 4, 64, OK), (1 << 26, 64, TOOBIG), ((1 << 31) - 1, 1, OK), (1 << 20, 1 << 20, OK), (1, 1 << 24, OK)):
+        a = rotation(tokens=tokens, heads=heads, kv_heads=heads, dim=128 if heads > 1 else 2, turning=0)
+        assert B._library().tessel_rotation_backward_workspace_bytes(C.byref(a), C.byref(n)) == code, (tokens, heads)
 
 
 def test_rotation_passes_refuse_their_own():

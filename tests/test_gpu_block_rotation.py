@@ -229,6 +229,44 @@ def test_a_token_alone_is_what_it_is_among_others(ops):
         assert torch.equal(a, q[part]) and torch.equal(b, k[part])
 
 
+def test_more_heads_in_all_than_waves_of_a_launch(ops):
+    """2^21 tokens of 32 + 8 heads: the first tokens, some and the last against the definition; only their gradients add to those of w"""
+    n, dim = (1 << 21) + 3, 8
+    part = torch.tensor([0, 1, 2, 5, 1 << 20, (1 << 20) + 1, n - 4, n - 2, n - 1])
+    v, at, f = inputs(len(part), 32, 8, dim, torch.bfloat16), positions(len(part)), frequency(dim)
+    g = {}
+    for name, heads in (("q", 32), ("k", 8), ("dq", 32), ("dk", 8)):
+        g[name] = torch.full((n, heads, dim), 0.0 if name[0] == "d" else 1.0, dtype=torch.bfloat16, device="cuda")
+        g[name][part.cuda()] = v[name].cuda()
+    where = torch.zeros(n, dtype=torch.int64)
+    where[part] = at
+    args = (g["q"], g["k"], where.cuda(), f.cuda(), v["wq"].cuda(), v["wk"].cuda(), 1e-5)
+    out = ops.rotate(*args)
+    grad = ops.rotate_backward(g["dq"], g["dk"], *args)
+    want = wanted(v, at, f, 1e-5, False)
+    for i, name in enumerate(("q", "k")):
+        for what, x, (value, bound) in zip(("result", "gradient", "gradient of w"), (out[i][part.cuda()], grad[i][part.cuda()], grad[2 + i]), want[name]):
+            R.close(x, value, bound, (what, name))
+        assert int(grad[i].ne(0).any(-1).any(-1).sum()) <= len(part)
+
+
+def test_strides_beyond_32_bits(ops):
+    """tokens, and heads, further apart than 32 bits count, read and written there"""
+    v = cuda(inputs(3, 2, 2, 64, torch.bfloat16))
+    far, at, f = (1 << 32) + 8, positions(3).cuda(), frequency(64).cuda()
+    big = torch.empty(2 * far + 4096, dtype=torch.bfloat16, device="cuda")
+    want = ops.rotate(v["q"], v["k"], at, f, v["wq"], v["wk"])
+    back = ops.rotate_backward(v["dq"], v["dk"], v["q"], v["k"], at, f, v["wq"], v["wk"])
+    for strides in ((far, 64, 1), (64, far, 1)):
+        q, k, dq, dk = (big.as_strided((3, 2, 64), strides, 256 * i) for i in range(4))
+        q.copy_(v["q"])
+        k.copy_(v["k"])
+        got = ops.rotate(q, k, at, f, v["wq"], v["wk"])
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        got = ops.rotate_backward(v["dq"], v["dk"], q, k, at, f, v["wq"], v["wk"], out=(dq, dk))
+        assert got[0] is dq and all(torch.equal(a, b) for a, b in zip(got, back))
+
+
 def test_a_graph_with_other_positions(ops):
     v = inputs(50, 4, 2, 64, torch.bfloat16)
     g, f = cuda(v), frequency(64).cuda()
