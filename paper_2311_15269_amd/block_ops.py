@@ -257,15 +257,18 @@ class Packing:
     @property
     def positions(self):
         """each token's place in its sequence, as rotate() takes it: int32 [tokens], made at the first use, which so is not for a stream that is being
-        captured; noughts for tokens of no sequence"""
+        captured; noughts for tokens of no sequence.  To be read on the stream that is current now, also when the packing is gone by then."""
+        import torch
+        stream = torch.cuda.current_stream(self._table.device)
         if self._positions is None:
-            import torch
             places = torch.zeros(self.tokens, dtype=torch.int32)
             begin = 0
             for n in self.lengths:
                 places[begin:begin + n] = torch.arange(n, dtype=torch.int32)
                 begin += n
-            self._positions = places.to(self._table.device)
+            self._positions, self._placed_on = places.to(self._table.device), stream
+        elif stream != self._placed_on:                     # (as with the table: not given away while that stream still reads it)
+            self._positions.record_stream(stream)
         return self._positions
 
     def close(self):

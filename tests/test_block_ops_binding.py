@@ -79,3 +79,18 @@ def test_heads_that_do_not_fit_32_bits_are_refused():
     with pytest.raises(binding.TesselError) as error:
         B.Packing._describe(types.SimpleNamespace(_table=q, tokens=1), q, q, q, None, 0)
     assert error.value.code == TOOBIG
+
+
+def test_positions_stay_until_the_streams_that_read_them_are_done(monkeypatch):
+    """made on one stream and read on another, they are recorded there: else the first one's next tensor may get their memory while the other still reads them"""
+    now, recorded = ["first"], []
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[0])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: recorded.append((t.data_ptr(), stream)))
+    p = object.__new__(B.Packing)
+    p.lengths, p.tokens, p._table, p._positions, p._h = [2, 0, 3], 6, torch.empty(0), None, None
+    at = p.positions
+    assert at.tolist() == [0, 1, 0, 1, 2, 0] and p.positions is at and not recorded
+    now[0] = "second"
+    assert p.positions is at and recorded == [(at.data_ptr(), "second")]
+    now[0] = "first"
+    assert p.positions is at and len(recorded) == 1

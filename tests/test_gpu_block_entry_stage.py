@@ -127,6 +127,33 @@ def test_positions_of_a_packing(stage):
     assert block_ops.Packing([]).positions.shape == (0,)
 
 
+def test_positions_of_a_packing_that_is_gone(stage):
+    """made on one stream, read on another that is busy, and the packing dropped: the first stream's next tensors do not get their memory"""
+    from paper_2311_15269_amd import block_ops
+    n, gen = 5000, torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    q, k = (torch.randn(n, h, 64, generator=gen, device="cuda").bfloat16() for h in (4, 2))
+    f, (busy, product) = block_ops.frequencies(64), (torch.zeros(8192, 8192, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    want = block_ops.rotate(q, k, torch.arange(n, device="cuda"), f)
+    torch.mm(busy, busy, out=product)
+    torch.cuda.synchronize()
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(first):
+        packing = block_ops.Packing([n])
+        at = packing.positions.data_ptr()
+    with torch.cuda.stream(second):
+        for _ in range(100):
+            torch.mm(busy, busy, out=product)
+        got = block_ops.rotate(q, k, packing.positions, f)
+    del packing
+    with torch.cuda.stream(first):
+        others = [torch.full((n,), 7, dtype=torch.int32, device="cuda") for _ in range(8)]
+    if not second.query():                                      # (once it is done the memory is anyone's)
+        assert at not in [t.data_ptr() for t in others]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_a_captured_step(stage):
     """lookup, dropout, norms, rotation, attention and back to the table's gradient in one graph, with other tokens and other masks in each replay"""
     from paper_2311_15269_amd import block_ops
