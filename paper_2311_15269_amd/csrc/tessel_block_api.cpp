@@ -164,7 +164,9 @@ size_t weight_workspace(const tessel_weight_grad *a)
 }
 
 // ---- between the tokens and the attention
-bool lanes_ok(int64_t lanes) { return lanes <= kMostThreads / 256 * 256; }       // (workgroups of 256)
+bool groups_ok(int64_t groups) { return groups <= kMostThreads / 256; }          // (workgroups of 256)
+// chunks of eight channels, of which a kernel has no more at once than its launch has threads
+bool chunks_ok(int64_t tokens, int channels) { return tokens * (((int64_t)channels + 7) / 8) <= kMostThreads / 256 * 256; }
 
 int drop_ok(const tessel_dropout &d, DropLaunch &l)
 {
@@ -180,7 +182,7 @@ int dropout_ok(const tessel_dropout_rows *a, DropLaunch &l)
     if (!is_type(a->type)) return TESSEL_E_UNSUPPORTED;
     const int e = drop_ok(a->drop, l);
     if (e) return e;
-    if (a->tokens > INT32_MAX || a->channels > 1 << 30 || !lanes_ok(a->tokens * (((int64_t)a->channels + 7) / 8))) return TESSEL_E_TOOBIG;
+    if (a->tokens > INT32_MAX || a->channels > 1 << 30 || !chunks_ok(a->tokens, a->channels) || !groups_ok(dropout_groups(*a, l))) return TESSEL_E_TOOBIG;
     return rows_ok(a->x, a->type, a->tokens, a->channels, false) && rows_ok(a->y, a->type, a->tokens, a->channels, true) ? TESSEL_OK : TESSEL_E_INVALID_ARG;
 }
 
@@ -189,7 +191,7 @@ bool index_ok(const void *p, int type, int64_t tokens) { return tokens == 0 || (
 int embedding_sizes_ok(const tessel_embedding *a)
 {
     if (!a || a->tokens < 0 || a->rows < 1 || a->channels < 1) return TESSEL_E_INVALID_ARG;
-    if (a->tokens > INT32_MAX || a->rows > 1 << 24 || a->channels > 1 << 24 || !lanes_ok(a->tokens * (((int64_t)a->channels + 7) / 8))) return TESSEL_E_TOOBIG;
+    if (a->tokens > INT32_MAX || a->rows > 1 << 24 || a->channels > 1 << 24 || !chunks_ok(a->tokens, a->channels)) return TESSEL_E_TOOBIG;
     return TESSEL_OK;
 }
 
@@ -471,6 +473,7 @@ int tessel_embedding_forward(const tessel_embedding *a, void *hip_stream)
     DropLaunch l;
     const int e = embedding_ok(a, l);
     if (e) return e;
+    if (!groups_ok(embed_groups(*a, l))) return TESSEL_E_TOOBIG;
     if (!rows_ok(a->table, a->type, a->rows, a->channels, false) || !rows_ok(a->out, a->type, a->tokens, a->channels, true)) return TESSEL_E_INVALID_ARG;
     return a->tokens == 0 ? TESSEL_OK : hip_result(launch_embed(*a, l, hip_stream));
 }

@@ -100,18 +100,19 @@ struct Span {
         }
     }
 };
-// chunks of eight channels that a row takes up to 64 lanes for, and the workgroups of 256 of such a launch
+// chunks of eight channels that a row takes up to 64 lanes for, and the workgroups of 256 of such a launch (lanes that a row leaves over are threads too: up to
+// twice the chunks; in 64 bits for 2^31 tokens of 2^30 channels)
 struct SpanShape {
-    bool wide;
-    int  lanes;
-    unsigned groups;
+    bool    wide;
+    int     lanes;
+    int64_t groups;
 };
 inline SpanShape span_shape(int64_t tokens, int channels, int rows)
 {
     SpanShape s = {channels > 256, 1, 0};
     while (s.lanes < 64 && 8 * s.lanes < channels) s.lanes *= 2;
     const int64_t at_once = (int64_t)(64 / s.lanes) * rows, tiles = s.wide ? ((int64_t)channels + 511) / 512 : 1;
-    s.groups = (unsigned)(((tokens + at_once - 1) / at_once * tiles + 3) / 4);
+    s.groups = ((tokens + at_once - 1) / at_once * tiles + 3) / 4;
     return s;
 }
 // Tokens a lane: four, of which a lane's columns are worked out once, where dropout of 16-bit values would else hold memory up (8192 x 4096 bf16: 23.7 us, one

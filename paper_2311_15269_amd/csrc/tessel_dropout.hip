@@ -29,6 +29,11 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(tessel_dropout_rows a
     }
 }
 
+int64_t dropout_groups(const tessel_dropout_rows &a, const DropLaunch &d)
+{
+    return span_shape(a.tokens, a.channels, span_rows(a.type, a.tokens, a.channels, d)).groups;
+}
+
 int launch_dropout(const tessel_dropout_rows &a, const DropLaunch &d, void *stream)
 {
     tessel_dropout_rows aa = a;
@@ -38,7 +43,7 @@ int launch_dropout(const tessel_dropout_rows &a, const DropLaunch &d, void *stre
     void *args[] = {&aa, &dd, &s.lanes};
 #define KERNEL(T) (s.wide ? rows == 4 ? (const void *)dropout_kernel<T, true, 4> : (const void *)dropout_kernel<T, true, 1> \
                           : rows == 4 ? (const void *)dropout_kernel<T, false, 4> : (const void *)dropout_kernel<T, false, 1>)
-    return launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3(s.groups), dim3(kThreads), args, 0, (hipStream_t)stream));
+    return launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)s.groups), dim3(kThreads), args, 0, (hipStream_t)stream));
 #undef KERNEL
 }
 

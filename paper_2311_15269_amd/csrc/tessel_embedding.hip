@@ -515,6 +515,11 @@ __global__ __launch_bounds__(kSortThreads) void join_kernel(EmbedLaunch l, int l
         if (col + j < a.channels) to[j] = old[j] + a.scale * sum[j];
 }
 
+int64_t embed_groups(const tessel_embedding &a, const DropLaunch &d)
+{
+    return span_shape(a.tokens, a.channels, span_rows(a.type, a.tokens, a.channels, d)).groups;
+}
+
 int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream)
 {
     tessel_embedding aa = a;
@@ -524,7 +529,7 @@ int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream)
     void *args[] = {&aa, &dd, &s.lanes};
 #define KERNEL(T) (s.wide ? rows == 4 ? (const void *)embed_kernel<T, true, 4> : (const void *)embed_kernel<T, true, 1> \
                           : rows == 4 ? (const void *)embed_kernel<T, false, 4> : (const void *)embed_kernel<T, false, 1>)
-    return launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3(s.groups), dim3(kThreads), args, 0, (hipStream_t)stream));
+    return launched(hipLaunchKernel(BY_TYPE(a.type, KERNEL), dim3((unsigned)s.groups), dim3(kThreads), args, 0, (hipStream_t)stream));
 #undef KERNEL
 }
 

@@ -54,6 +54,24 @@ def test_embedding_refuses(change, code):
     assert lib.tessel_embedding_backward(C.byref(a), AT, 1 << 50, None) == code
 
 
+@pytest.mark.parametrize("tokens, channels, rate, kind, code", [
+    # rows of more than 256 channels take whole waves, four in a workgroup of which a launch holds 2^24 - 1; others the next power of two of their chunks of eight
+    ((1 << 26) - 4, 257, 0.0, 0, INVALID), ((1 << 26) - 3, 257, 0.0, 0, TOOBIG), (80000000, 257, 0.0, 0, TOOBIG), (100000000, 257, 0.5, 2, TOOBIG), ((1 << 26) - 4, 512, 0.0, 0, INVALID),
+    ((1 << 25) - 2, 513, 0.5, 2, INVALID), ((1 << 25) - 1, 513, 0.5, 2, TOOBIG), ((1 << 30) - 64, 17, 0.0, 1, INVALID), ((1 << 30) - 63, 17, 0.0, 1, TOOBIG),
+    (1200000000, 17, 0.0, 1, TOOBIG), (1200000000, 24, 0.5, 2, TOOBIG), ((1 << 31) - 1, 9, 0.0, 0, TOOBIG), ((1 << 31) - 128, 9, 0.0, 0, INVALID), ((1 << 31) - 1, 8, 0.0, 0, INVALID),
+    # four tokens a lane
+    (100000000, 257, 0.5, 0, INVALID), (1200000000, 17, 0.5, 1, INVALID),
+])
+def test_rows_of_more_lanes_than_a_launch_holds(tokens, channels, rate, kind, code):
+    """TOOBIG is counted by the threads that a launch takes, not by the chunks of eight channels that there are.  (INVALID: a table and rows that are not there, looked for behind
+    the sizes.)"""
+    none = B.Rows(None, 0)
+    a = B.DropoutRows(type=kind, channels=channels, tokens=tokens, x=none, y=none, drop=drop(rate=rate))
+    assert B._library().tessel_dropout_apply(C.byref(a), None) == code
+    a = embedding(type=kind, channels=channels, tokens=tokens, table=none, out=none, drop=drop(rate=rate))
+    assert B._library().tessel_embedding_forward(C.byref(a), None) == code
+
+
 def test_embedding_passes_refuse_their_own():
     lib, n = B._library(), C.c_size_t()
     for change, code in (({"tokens": 0}, OK), ({"tokens": 0, "token": None, "out": B.Rows(None, 0)}, OK), ({"table": B.Rows(None, 64)}, INVALID), ({"table": B.Rows(AT + 1, 64)}, INVALID),
