@@ -659,6 +659,8 @@ def _describe_rotation(q, k, positions, frequency, wq, wk, eps, neighbours):
     _same(q, (n, kv_heads, dim), k)
     if frequency.dtype is not torch.float64 or frequency.dim() != 1 or not frequency.is_contiguous() or frequency.get_device() != at:
         _refuse("frequencies are contiguous 64-bit numbers on %s" % q.device)
+    if frequency.requires_grad:
+        _refuse_gradient(frequency)
     if 2 * pairs > dim:
         _refuse("%d pairs of %d channels" % (pairs, dim))
     kind, where = _index(positions, n, q)

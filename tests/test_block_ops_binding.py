@@ -94,3 +94,32 @@ def test_positions_stay_until_the_streams_that_read_them_are_done(monkeypatch):
     assert p.positions is at and recorded == [(at.data_ptr(), "second")]
     now[0] = "first"
     assert p.positions is at and len(recorded) == 1
+
+
+class OnGpu(torch.Tensor):
+    """a tensor that says it is on GPU number 0"""
+    is_cuda = True
+
+    def get_device(self):
+        return 0
+
+
+@pytest.mark.parametrize("which", range(7))
+def test_rotations_refuse_whatever_requires_a_gradient(which):
+    """while torch records: queries, keys, frequencies and weights alike, and what a backward call takes"""
+    q, k = (torch.zeros(5, h, 8, dtype=BF16).as_subclass(OnGpu) for h in (2, 1))
+    all_of = [q, k, torch.ones(4, dtype=torch.float64).as_subclass(OnGpu), *(torch.ones(8).as_subclass(OnGpu) for _ in range(2)), q.clone(), k.clone()]
+    at = torch.zeros(5, dtype=torch.int64).as_subclass(OnGpu)
+
+    def call():
+        q, k, f, wq, wk, dq, dk = all_of
+        B._same(q, q.shape, dq)
+        B._same(q, k.shape, dk)
+        return B._describe_rotation(q, k, at, f, wq, wk, 1e-6, False)
+    call()
+    all_of[which].requires_grad_()
+    with pytest.raises(binding.TesselError) as error:
+        call()
+    assert error.value.code == INVALID and "gradient" in str(error.value)
+    with torch.no_grad():
+        call()

@@ -311,3 +311,15 @@ def test_refusals(ops):
         ops.rotate_backward(v["dk"], v["dk"], *args[2:])
     with pytest.raises(TesselError):
         ops.rotate_backward(*args, into=(w, w[:60]))
+
+
+def test_frequencies_that_require_a_gradient_are_refused(ops):
+    """while torch records; they get none"""
+    from paper_2311_15269_amd.binding import TesselError
+    v = cuda(inputs(6, 4, 2, 64, torch.bfloat16))
+    at, f = positions(6).cuda(), frequency(64).cuda().requires_grad_()
+    for call in (lambda: ops.rotate(v["q"], v["k"], at, f), lambda: ops.rotate_backward(v["dq"], v["dk"], v["q"], v["k"], at, f, v["wq"], v["wk"])):
+        with pytest.raises(TesselError):
+            call()
+        with torch.no_grad():
+            call()
