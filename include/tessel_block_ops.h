@@ -230,8 +230,9 @@ int  tessel_embedding_backward(const tessel_embedding *a, void *workspace_dev, s
  * For every head z of a token's queries and keys, with w = wq or wk (both NULL: no norm, n = z), over its dim channels:
  *     n = w z / sqrt(mean(z^2) + eps);    of the first `turning` channels the i-th pair turns by the angle position frequency_i,
  *     (a, b) -> (a cos - b sin, a sin + b cos),
- * pair i being channels (i, i + turning / 2) or, with `neighbours`, (2 i, 2 i + 1); the others stay.  Angles are taken in 64 bits and reduced
- * there, so that they are right at any position; all else in 32 bits, rounded once.  Backward from the gradients of the results and z:
+ * pair i being channels (i, i + turning / 2) or, with `neighbours`, (2 i, 2 i + 1); the others stay.  Angles are reduced in
+ * 64 bits, far ones in two parts of 64, so that up to 2^70 radians (a frequency of 100 at the last position) no more than their fraction of a turn is rounded, to
+ * 32 bits; all else in 32 bits, rounded once.  Backward from the gradients of the results and z:
  * gradients of z, and of wq and wk, sums over tokens and heads in 32 bits.  Infinities and NaN of a head stay in that head (and
  * reach the gradients of w). */
 typedef struct {

@@ -62,6 +62,18 @@ __device__ __forceinline__ float over_root(float v)
     return __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v) * (small ? 0x1p32f : 1.0f);
 }
 
+// An angle in turns, less whole ones, for such as are far: product and quotient are taken in two parts of 64 bits each, what the first rounds off in the second.  Up to 2^70
+// radians that is off by less than 2^-30 of a turn, where the product alone is by 2^-53 of the angle, an eighth of a radian at 2^50.  (A product that were contracted
+// with what is taken from it would count its rounding twice.)
+__device__ __forceinline__ double far_turns(double position, double frequency)
+{
+#pragma clang fp contract(off)
+    constexpr double kOver = 0x1.45f306dc9c883p-3, kMore = -0x1.6b01ec5417056p-57;            // 1 / (2 pi), to 2^-107 of it
+    const double angle = position * frequency, rest = fma(position, frequency, -angle), turns = angle * kOver;
+    const double more = fma(angle, kOver, -turns) + (angle * kMore + rest * kOver), part = (turns - rint(turns)) + (more - rint(more));
+    return part - rint(part);
+}
+
 // sines and cosines of a wave's tokens
 __device__ __forceinline__ void angles(const tessel_rotation &a, int64_t token, int tokens, float *cosine, float *sine)
 {
@@ -70,9 +82,17 @@ __device__ __forceinline__ void angles(const tessel_rotation &a, int64_t token, 
         const int t = i / half, p = i - t * half;
         const int64_t n = min(token + t, a.tokens - 1);
         const double position = a.index_type == TESSEL_I64 ? (double)((const int64_t *)a.position)[n] : (double)((const int32_t *)a.position)[n];
-        const double turns = position * a.frequency[p] * 0.15915494309189535;            // angle / (2 pi)
+        double turns = position * a.frequency[p] * 0.15915494309189535;                  // angle / (2 pi), off by 2^-52 of it: less than 2^-30 where it is near
+        const double whole = rint(turns);
+        if (__builtin_expect(fabs(turns) < 0x1p22, 1)) {
+            turns -= whole;
+        } else {                                                 // the position in two parts, which 64 bits hold as they are
+            const int64_t far = a.index_type == TESSEL_I64 ? ((const int64_t *)a.position)[n] : ((const int32_t *)a.position)[n];
+            turns = far_turns((double)(far >> 32) * 0x1p32, a.frequency[p]) + far_turns((double)(uint32_t)far, a.frequency[p]);
+            turns -= rint(turns);
+        }
         float s, c;
-        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+        sincospif((float)(2.0 * turns), &s, &c);
         cosine[i] = c;
         sine[i] = s;
     }

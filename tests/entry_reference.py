@@ -3,6 +3,8 @@
 H is half a step of a 32-bit number as a share of its value.  A sum of n terms in 32 bits, in any order, is at most n H times the sum of the
 terms' sizes off (to first order; every bound below leaves room for the second).
 """
+from fractions import Fraction
+
 import numpy as np
 import torch
 
@@ -138,3 +140,20 @@ def close(got, want, bound, what):
     assert got.shape == want.shape, (what, got.shape, want.shape)
     off = (got - want).abs() - bound
     assert bool((off <= 0).all()), (what, float(off.max()), "of", float(want.abs().max()))
+
+
+def reduced_angles(position, frequency):
+    """position x frequency less whole turns, rounded once to 64 bits, from whole numbers of any length: [tokens, pairs] for lists of whole numbers and of 64-bit ones"""
+    bits = 300                                                  # pi = 16 atan(1 / 5) - 4 atan(1 / 239) (Machin 1706)
+    pi, power = 0, [0, 0]
+    for i, (by, n) in enumerate(((16, 5), (-4, 239))):
+        power[i], k = (1 << bits) // n, 0
+        while power[i]:
+            pi += (-1) ** k * by * (power[i] // (2 * k + 1))
+            power[i], k = power[i] // n ** 2, k + 1
+    turn = Fraction(2 * pi, 1 << bits)
+    out = []
+    for n in position:
+        angles = [n * Fraction(f) for f in frequency]
+        out.append([float(a - turn * round(a / turn)) for a in angles])
+    return torch.tensor(out, dtype=torch.float64)

@@ -66,3 +66,13 @@ def test_gradient_of_the_embedding_by_differences():
         up.view(-1)[i] += 1e-3
         down.view(-1)[i] -= 1e-3
         assert abs((value(up) - value(down)) / 2e-3 - float(want.view(-1)[i])) < 1e-9
+
+
+def test_angles_less_whole_turns():
+    import math
+    position, frequency = [0, 1, -1, 12, 1 << 30, 710], [1.0, 0.37, 1e-4]
+    got = R.reduced_angles(position, frequency)
+    want = torch.tensor([[math.remainder(n * f, 2 * math.pi) for f in frequency] for n in position], dtype=torch.float64)
+    # (2 pi rounds by 2^-53 a turn, the product by 2^-53 of itself)
+    assert float((got - want).abs().max()) < 2.0 ** -50 * (1 << 30) and float((got - want).abs()[[0, 1, 2, 3, 5]].max()) < 1e-12
+    assert abs(math.sin(float(R.reduced_angles([1 << 62], [1.0])[0, 0])) - math.sin(1 << 62)) < 1e-15        # (the library's own reduction of a whole number of 64 bits)

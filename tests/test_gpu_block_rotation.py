@@ -323,3 +323,19 @@ def test_frequencies_that_require_a_gradient_are_refused(ops):
             call()
         with torch.no_grad():
             call()
+
+
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_positions_up_to_the_last_of_64_bits(ops, neighbours):
+    """angles of 2^40 radians and more.  Of the angle there is what rounding its fraction of half a turn, the sine and cosine to 32 bits costs, 2^-21 with what the products add,
+    and nothing that grows with it"""
+    at = [0, 3, 1 << 40, -(1 << 45) - 1, (1 << 50) + 1, 1 << 53, (1 << 53) + 1, -(1 << 53) - 1, 12345678901234567, (1 << 62) + 3, (1 << 63) - 1, -(1 << 63)]
+    f = torch.cat((frequency(56), torch.tensor([100.0, -0.37, 2.5, 1e-12], dtype=torch.float64)))
+    v = inputs(len(at), 4, 2, 64, torch.float32, False)
+    g, args = cuda(v), (torch.tensor(at).cuda(), f.cuda(), None, None, 1e-6, neighbours)
+    angle = R.reduced_angles(at, f.tolist())
+    got = dict(zip(("q", "k"), ops.rotate(g["q"], g["k"], *args))) | dict(zip(("dq", "dk"), ops.rotate_backward(g["dq"], g["dk"], g["q"], g["k"], *args)))
+    for name, x in got.items():
+        z = v[name].double()
+        want = R.turned(z, -angle if name[0] == "d" else angle, 64, 64, neighbours)
+        R.close(x, want, R.H * want.abs() * (1 + 1e-3) + (2.0 ** -21 + 6 * R.H) * R.both(z, 64, 64, neighbours), name)
