@@ -30,13 +30,28 @@ def _activation(kind, z):
     return 0.5 * z * (1 + t), 0.5 * (1 + t) + 0.5 * (1 - t * t) * z * root * (1 + 3 * cube * (z * z).clamp(max=1e6))
 
 
+_ENTRY = 0xFFFFFFFF             # the entry's place among a program's dropouts; a stage's are 2 layer and 2 layer + 1
+
+
+def _dropout(rate, seed, number, place, step):
+    """the dropout at a place of the program for a micro-batch.  With a `step` its numbers are 20 bits of the micro-batch's, 12 of the place and 32 that the step counts through; else
+    32 bits of each of the first two."""
+    if step is None:
+        return block_ops.Dropout(rate, seed, (number & 0xFFFFFFFF) << 32 | place)
+    return block_ops.Dropout(rate, seed, (number & 0xFFFFF) << 44 | (place & 0xFFF) << 32, step)
+
+
 class Stage:
     """Weights in 16 bits, parameters of the norms and all gradients in 32.  Micro-batches are told apart by a number; what a
     forward pass keeps goes away with its backward pass.  `small`: 8-bit checkpoints.  `turning`: channels of a head that turn by position (0: no
-    norms of queries and keys either).  `rate`: of dropout, whose masks go by `seed`, `layer` and the micro-batch's number."""
+    norms of queries and keys either).  `rate`: of dropout, whose masks go by `seed`, `layer`, the micro-batch's number and `step`: one int64 number on the GPU, which the
+    program counts up between training steps (behind the last backward pass of one, on the GPU or in its graph), so that each draws anew.  Without a step, a
+    micro-batch's number has the same masks each time."""
 
-    def __init__(self, channels, heads, kv_heads, inner, generator, dtype, small=True, scale=1.0, act="silu", turning=0, rate=0.0, seed=0, layer=0):
+    def __init__(self, channels, heads, kv_heads, inner, generator, dtype, small=True, scale=1.0, act="silu", turning=0, rate=0.0, seed=0, layer=0, step=None):
         import torch
+        if step is not None and layer >= 2047:
+            raise ValueError("layer %d: dropout with a step tells 2047 layers apart" % layer)
         self.heads, self.kv_heads, self.dim = heads, kv_heads, channels // heads
         self.small, self.scale, self.act = small, scale, act
         wide = (heads + 2 * kv_heads) * self.dim
@@ -52,7 +67,7 @@ class Stage:
         self.norms = [{"post": vector(1.0), "gate": vector(0.5), "pre": vector(1.0)} for _ in range(2)]
         self.gradients = {k: torch.zeros(w.shape, device="cuda") for k, w in self.weights.items()}
         self.norm_gradients = [{k: torch.zeros_like(v) for k, v in n.items()} for n in self.norms]
-        self.turning, self.rate, self.seed, self.layer = turning, rate, seed, layer
+        self.turning, self.rate, self.seed, self.layer, self.step = turning, rate, seed, layer, step
         self.head_norms, self.head_gradients = None, None
         if turning:
             self.frequency = block_ops.frequencies(turning)
@@ -64,7 +79,7 @@ class Stage:
         """dropout of what the attention (which 0) or the gated part (1) put out for a micro-batch, and of its gradient"""
         if not self.rate:
             return y
-        return block_ops.dropout(y, block_ops.Dropout(self.rate, self.seed, (number & 0xFFFFFFFF) << 32 | self.layer << 1 | which))
+        return block_ops.dropout(y, _dropout(self.rate, self.seed, number, self.layer << 1 | which, self.step))
 
     def _turn(self, packing, qkv):
         """queries, keys and values as the attention takes them"""
@@ -160,11 +175,12 @@ class Stage:
 
 class Entry:
     """The block in front of the first stage: an embedding spread over devices, each of which holds a shard of the vocabulary, dropout, and the norm that the stage
-    reads.  (All shards are on this GPU: what their devices would add up in an all-reduce is added here.)  Gradients are sums in 32 bits."""
+    reads.  (All shards are on this GPU: what their devices would add up in an all-reduce is added here.)  Gradients are sums in 32 bits.  `rate`, `seed`, `step`: as a
+    stage's."""
 
-    def __init__(self, vocabulary, shards, channels, generator, dtype, rate=0.0, seed=0):
+    def __init__(self, vocabulary, shards, channels, generator, dtype, rate=0.0, seed=0, step=None):
         import torch
-        self.rows, self.scale, self.rate, self.seed = -(-vocabulary // shards), math.sqrt(channels), rate, seed
+        self.rows, self.scale, self.rate, self.seed, self.step = -(-vocabulary // shards), math.sqrt(channels), rate, seed, step
         self.first = list(range(0, vocabulary, self.rows))
         self.tables = [(torch.randn(min(self.rows, vocabulary - f), channels, generator=generator, device="cuda") * channels ** -0.5).to(dtype) for f in self.first]
         self.pre = torch.ones(channels, device="cuda")
@@ -173,7 +189,7 @@ class Entry:
         self.kept = {}
 
     def _drop(self, number):
-        return block_ops.Dropout(self.rate, self.seed, (number & 0xFFFFFFFF) << 32 | 0xFFFFFFFF) if self.rate else None
+        return _dropout(self.rate, self.seed, number, _ENTRY, self.step) if self.rate else None
 
     def forward(self, number, tokens):
         """tokens [tokens] -> the residual stream and its norm"""
@@ -256,13 +272,13 @@ def in_turn(devices, microbatches):
     return [(0, i * microbatches + mu, 0, 0, 0) for mu in range(microbatches) for i in range(2 * devices)]
 
 
-def make(devices, microbatches, lengths, channels, heads, kv_heads, inner, small, seed=0, dtype=None, turning=0, rate=0.0):
+def make(devices, microbatches, lengths, channels, heads, kv_heads, inner, small, seed=0, dtype=None, turning=0, rate=0.0, step=None):
     """stages, packings and inputs, the same for the same seed"""
     import torch
     dtype = dtype or torch.bfloat16
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed)
-    stages = [Stage(channels, heads, kv_heads, inner, gen, dtype, small, turning=turning, rate=rate, seed=seed, layer=i) for i in range(devices)]
+    stages = [Stage(channels, heads, kv_heads, inner, gen, dtype, small, turning=turning, rate=rate, seed=seed, layer=i, step=step) for i in range(devices)]
     packings = [block_ops.Packing(lengths) for _ in range(microbatches)]
     xs = [torch.randn(sum(lengths), channels, generator=gen, device="cuda").to(dtype) for _ in range(microbatches)]
     one = torch.ones(channels, device="cuda")
@@ -270,12 +286,12 @@ def make(devices, microbatches, lengths, channels, heads, kv_heads, inner, small
     return stages, packings, xs, hs
 
 
-def make_entry(microbatches, lengths, channels, vocabulary, shards, seed=0, dtype=None, rate=0.0):
+def make_entry(microbatches, lengths, channels, vocabulary, shards, seed=0, dtype=None, rate=0.0, step=None):
     """an entry and the tokens of its micro-batches, the same for the same seed"""
     import torch
     gen = torch.Generator(device="cuda")
     gen.manual_seed(seed + 1)
-    entry = Entry(vocabulary, shards, channels, gen, dtype or torch.bfloat16, rate, seed)
+    entry = Entry(vocabulary, shards, channels, gen, dtype or torch.bfloat16, rate, seed, step)
     return entry, [torch.randint(0, vocabulary, (sum(lengths),), generator=gen, device="cuda") for _ in range(microbatches)]
 
 
@@ -290,6 +306,7 @@ def main():
     ap.add_argument("--lengths", default="1000,37,500,511")
     ap.add_argument("--turning", type=int, default=0, help="channels of a head that turn by position, behind norms of queries and keys")
     ap.add_argument("--rate", type=float, default=0.0, help="of dropout")
+    ap.add_argument("--steps", type=int, default=1, help="training steps, each with masks of its own")
     ap.add_argument("--vocabulary", type=int, default=0, help="an embedding of so many tokens in front, a shard on each device")
     a = ap.parse_args()
     lengths = [int(n) for n in a.lengths.split(",")]
@@ -311,14 +328,20 @@ def main():
 
     def gradient(mu, r, h):
         return dr, dr
-    front = [make_entry(a.microbatches, lengths, a.channels, a.vocabulary, a.devices, rate=a.rate) if a.vocabulary else (None, None) for _ in range(2)]
-    got = run(stages, packings, xs, hs, gradient, operations, *front[0])
-    again, packings, xs, hs = make(*sizes, True, **more)
-    want = run(again, packings, xs, hs, gradient, in_turn(a.devices, a.microbatches), *front[1])
+    sides = []
+    for order in (operations, in_turn(a.devices, a.microbatches)):
+        step = torch.zeros(1, dtype=torch.int64, device="cuda")
+        stages, packings, xs, hs = make(*sizes, True, **more, step=step)
+        front = make_entry(a.microbatches, lengths, a.channels, a.vocabulary, a.devices, rate=a.rate, step=step) if a.vocabulary else (None, None)
+        for _ in range(max(1, a.steps)):
+            back = run(stages, packings, xs, hs, gradient, order, *front)
+            step += 1
+        sides.append((back, stages, front[0]))
+    (got, stages, entry), (want, again, other) = sides
     same = all(torch.equal(p, q) for x, y in zip(got, want) for p, q in zip(x, y))
     same = same and all(torch.equal(s.gradients[k], t.gradients[k]) for s, t in zip(stages, again) for k in s.gradients)
     if a.vocabulary:
-        same = same and all(torch.equal(p, q) for p, q in zip(front[0][0].gradients, front[1][0].gradients))
+        same = same and all(torch.equal(p, q) for p, q in zip(entry.gradients, other.gradients))
     print("%d micro-batches in the order of the schedule (%d operations, makespan %d): gradients %s those of one after the other" % (
         a.microbatches, len(operations), done["makespan"], "equal" if same else "DIFFER from"))
     return 0 if same else 1
