@@ -167,6 +167,10 @@ class Stage:
         self._add("qkv", dqkv, h)
         return dx, dqkv @ w["qkv"]
 
+    def sums(self):
+        """the gradients of all weights and norms"""
+        return list(self.gradients.values()) + [v for n in self.norm_gradients for v in n.values()] + list(self.head_gradients or ())
+
     def kept_bytes(self, number):
         """what a forward pass keeps until its backward pass: m of its block.  (The residual stream that it was given too: the stage that made it does not
         keep it.)"""
@@ -210,6 +214,10 @@ class Entry:
         for f, g in zip(self.first, self.gradients):
             block_ops.embed_backward(d, tokens, g.shape[0], self.scale, f, drop, into=g)
 
+    def sums(self):
+        """the gradients of all shards and of the norm"""
+        return self.gradients + [self.pre_gradient]
+
 
 def measure(stage, packing, x, h):
     """(seconds forward, seconds backward, bytes kept) of a stage's blocks for a micro-batch"""
@@ -227,7 +235,7 @@ def measure(stage, packing, x, h):
         if turn:                                                # (the first pass loads the kernels)
             took[0] += t1 - t0
             took[1] += time.perf_counter() - t1
-    for g in list(stage.gradients.values()) + [v for n in stage.norm_gradients for v in n.values()] + list(stage.head_gradients or ()):
+    for g in stage.sums():
         g.zero_()
     return took[0] / 5, took[1] / 5, size
 
@@ -336,12 +344,9 @@ def main():
         for _ in range(max(1, a.steps)):
             back = run(stages, packings, xs, hs, gradient, order, *front)
             step += 1
-        sides.append((back, stages, front[0]))
-    (got, stages, entry), (want, again, other) = sides
-    same = all(torch.equal(p, q) for x, y in zip(got, want) for p, q in zip(x, y))
-    same = same and all(torch.equal(s.gradients[k], t.gradients[k]) for s, t in zip(stages, again) for k in s.gradients)
-    if a.vocabulary:
-        same = same and all(torch.equal(p, q) for p, q in zip(entry.gradients, other.gradients))
+        blocks = stages + ([front[0]] if a.vocabulary else [])
+        sides.append([t for pair in back for t in pair] + [t for block in blocks for t in block.sums()])
+    same = all(torch.equal(p, q) for p, q in zip(*sides))
     print("%d micro-batches in the order of the schedule (%d operations, makespan %d): gradients %s those of one after the other" % (
         a.microbatches, len(operations), done["makespan"], "equal" if same else "DIFFER from"))
     return 0 if same else 1

@@ -116,3 +116,30 @@ def test_steps_in_the_order_of_a_schedule(stage):
         assert not torch.equal(out[0][0], out[1][0])
         result.append(out[0] + out[1] + entry.gradients + [entry.pre_gradient] + [t for s in stages for t in (*s.gradients.values(), *s.head_gradients)])
     assert all(torch.equal(a, b) for a, b in zip(*result))
+
+
+@pytest.mark.parametrize("which", [None, "weights", "norms", "heads", "shards", "entry"])
+def test_the_command_compares_all_gradients(stage, which, monkeypatch, capsys):
+    """one number of one of them changed on one side is a difference"""
+    import sys
+    monkeypatch.setattr(sys, "argv", ["stage", "--devices", "2", "--microbatches", "4", "--channels", "128", "--heads", "4", "--kv-heads", "2", "--lengths", "60,1,5", "--turning", "16",
+                                      "--rate", "0.1", "--vocabulary", "300", "--steps", "2"])
+    run, calls = stage.run, []
+
+    def changed(stages, packings, xs, hs, gradient, operations, entry=None, tokens=None):
+        back = run(stages, packings, xs, hs, gradient, operations, entry, tokens)
+        calls.append(1)
+        if which and len(calls) == 4:
+            {"weights": stages[1].gradients["up"], "norms": stages[0].norm_gradients[1]["gate"], "heads": stages[1].head_gradients[0], "shards": entry.gradients[1],
+             "entry": entry.pre_gradient}[which].view(-1)[3] += 1.0
+        return back
+    monkeypatch.setattr(stage, "run", changed)
+    assert stage.main() == (1 if which else 0) and len(calls) == 4
+    assert ("DIFFER" if which else "equal") in capsys.readouterr().out
+
+
+def test_measuring_leaves_no_gradients(stage):
+    s, packing, entry, tokens, _ = made(stage)
+    x, h = entry.forward(MU, tokens)
+    stage.measure(s, packing, x, h)
+    assert not any(bool(g.any()) for g in s.sums()) and len(s.sums()) == len(s.gradients) + 6 + 2 and len(entry.sums()) == 4
