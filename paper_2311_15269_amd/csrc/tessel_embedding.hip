@@ -92,7 +92,7 @@ __device__ __forceinline__ int sums_up_to(int x) { return up_to(x, [](int a, int
 __device__ __forceinline__ int most_up_to(int x) { return up_to(x, [](int a, int b) { return max(a, b); }); }
 
 // A thread's places of the tile at t0, sixteen bits: those whose row is in the bucket.  `before`: how many are in the buckets before it, added up.  (No read stands in a
-// branch, behind which the compiler would wait for it: behind the last place the last four are read again.)
+// branch, behind which the compiler would wait for it: behind the last place the last four are read again.  Of four tokens there are more: few_kernel takes batches of up to 256.)
 template <typename I>
 __device__ __forceinline__ uint32_t tile_places(const EmbedLaunch &l, int64_t t0, uint32_t bucket, int &before)
 {
@@ -103,9 +103,7 @@ __device__ __forceinline__ uint32_t tile_places(const EmbedLaunch &l, int64_t t0
 #pragma unroll
     for (int s = 0; s < kSubs; s++) {
         const int64_t t = t0 + s * kSub + 4 * (int)threadIdx.x;
-        const I *p = (const I *)a.token + min(t, max(a.tokens - 4, (int64_t)0));
-        if (a.tokens >= 4) w[s] = *(const V *)p;
-        else w[s] = V{p[0], p[min(1, (int)a.tokens - 1)], p[min(2, (int)a.tokens - 1)], (I)-1};
+        w[s] = *(const V *)((const I *)a.token + min(t, a.tokens - 4));
     }
     uint32_t mine = 0;
 #pragma unroll
@@ -122,7 +120,7 @@ __device__ __forceinline__ uint32_t tile_places(const EmbedLaunch &l, int64_t t0
             less |= b < bucket ? 1 << j : 0;
         }
         if (__any(t + 4 > a.tokens)) {                           // the last places: of those read again, what is not there
-            const int by = a.tokens >= 4 ? (int)min(t - min(t, a.tokens - 4), (int64_t)4) : (int)(t > 0 ? 4 : 0), left = (int)min(max(a.tokens - t, (int64_t)0), (int64_t)4);
+            const int by = (int)min(t - min(t, a.tokens - 4), (int64_t)4), left = (int)min(max(a.tokens - t, (int64_t)0), (int64_t)4);
             here = here >> by & ((1u << left) - 1);
             less = less >> by & ((1 << left) - 1);
         }

@@ -443,7 +443,6 @@ static RotateLaunch rotate_launch(const tessel_rotation &a)
 {
     RotateLaunch l = {};
     l.a = a;
-    if (a.turning == 0) l.a.neighbours = 1;                      // (in one piece; there is no pair that turns)
     const int chunks = chunks_of(a);
     while (l.group < 6 && 1 << l.group < chunks) l.group++;
     while (l.heads < 6 - l.group && 1 << l.heads < a.heads) l.heads++;
@@ -475,7 +474,7 @@ static const void *rotate_of(const tessel_rotation &a, bool back)
 template <typename T>
 static const void *rotate_of(const tessel_rotation &a, bool back)
 {
-    return a.neighbours || a.turning == 0 ? rotate_of<T, true>(a, back) : rotate_of<T, false>(a, back);
+    return a.neighbours || a.turning == 0 ? rotate_of<T, true>(a, back) : rotate_of<T, false>(a, back);      // (where none turns, in one piece)
 }
 static const void *rotate_of(const tessel_rotation &a, bool back)
 {
