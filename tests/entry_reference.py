@@ -25,10 +25,15 @@ def philox(counter, key):
 
 def words(tokens, channels, seed, number):
     """the random words of [tokens, channels]"""
-    n, groups = tokens, -(-channels // 4)
+    return words_of(np.arange(tokens), channels, seed, number)
+
+
+def words_of(places, channels, seed, number):
+    """those of the tokens at these places"""
+    n, groups = len(places), -(-channels // 4)
     x = np.zeros((4, n, groups), np.uint64)
     x[0] += np.arange(groups, dtype=np.uint64)
-    x[1] += np.arange(n, dtype=np.uint64)[:, None]
+    x[1] += np.asarray(places, dtype=np.uint64)[:, None]
     x[2] += np.uint64(number % 2 ** 32)
     x[3] += np.uint64(number >> 32)
     k = [seed % 2 ** 32, seed >> 32]
