@@ -55,10 +55,8 @@ struct DropLaunch {
     uint64_t seed, number;
     const uint64_t *step;
 };
-int64_t dropout_groups(const tessel_dropout_rows &a, const DropLaunch &d);      // workgroups of 256
 int launch_dropout(const tessel_dropout_rows &a, const DropLaunch &d, void *stream);
 
-int64_t embed_groups(const tessel_embedding &a, const DropLaunch &d);           // forward, of 256
 int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream);
 size_t embed_workspace(const tessel_embedding &a);
 int launch_embed_backward(const tessel_embedding &a, const DropLaunch &d, void *workspace, void *stream);

@@ -164,8 +164,7 @@ size_t weight_workspace(const tessel_weight_grad *a)
 }
 
 // ---- between the tokens and the attention
-bool groups_ok(int64_t groups) { return groups <= kMostThreads / 256; }          // (workgroups of 256)
-// chunks of eight channels, of which a kernel has no more at once than its launch has threads
+// chunks of eight channels: of as many as a launch has threads, by workgroups of 256, the kernels take several a lane where rows leave lanes over
 bool chunks_ok(int64_t tokens, int channels) { return tokens * (((int64_t)channels + 7) / 8) <= kMostThreads / 256 * 256; }
 
 int drop_ok(const tessel_dropout &d, DropLaunch &l)
@@ -182,7 +181,7 @@ int dropout_ok(const tessel_dropout_rows *a, DropLaunch &l)
     if (!is_type(a->type)) return TESSEL_E_UNSUPPORTED;
     const int e = drop_ok(a->drop, l);
     if (e) return e;
-    if (a->tokens > INT32_MAX || a->channels > 1 << 30 || !chunks_ok(a->tokens, a->channels) || !groups_ok(dropout_groups(*a, l))) return TESSEL_E_TOOBIG;
+    if (a->tokens > INT32_MAX || a->channels > 1 << 30 || !chunks_ok(a->tokens, a->channels)) return TESSEL_E_TOOBIG;
     return rows_ok(a->x, a->type, a->tokens, a->channels, false) && rows_ok(a->y, a->type, a->tokens, a->channels, true) ? TESSEL_OK : TESSEL_E_INVALID_ARG;
 }
 
@@ -473,7 +472,6 @@ int tessel_embedding_forward(const tessel_embedding *a, void *hip_stream)
     DropLaunch l;
     const int e = embedding_ok(a, l);
     if (e) return e;
-    if (!groups_ok(embed_groups(*a, l))) return TESSEL_E_TOOBIG;
     if (!rows_ok(a->table, a->type, a->rows, a->channels, false) || !rows_ok(a->out, a->type, a->tokens, a->channels, true)) return TESSEL_E_INVALID_ARG;
     return a->tokens == 0 ? TESSEL_OK : hip_result(launch_embed(*a, l, hip_stream));
 }

@@ -100,8 +100,7 @@ struct Span {
         }
     }
 };
-// chunks of eight channels that a row takes up to 64 lanes for, and the workgroups of 256 of such a launch (lanes that a row leaves over are threads too: up to
-// twice the chunks; in 64 bits for 2^31 tokens of 2^30 channels)
+// chunks of eight channels that a row takes up to 64 lanes for, and the workgroups of 256 of such a launch
 struct SpanShape {
     bool    wide;
     int     lanes;
@@ -115,12 +114,8 @@ inline SpanShape span_shape(int64_t tokens, int channels, int rows)
     s.groups = ((tokens + at_once - 1) / at_once * tiles + 3) / 4;
     return s;
 }
-// Tokens a lane: four, of which a lane's columns are worked out once, where dropout of 16-bit values would else hold memory up (8192 x 4096 bf16: 23.7 us, one
-// by one 24.9, without dropout 22; in 32 bits 45 and 44, 16384 x 1024 13.2 and 12.8; the embedding's 22.8 and 25.2)
-inline int span_rows(int type, int64_t tokens, int channels, const DropLaunch &d)
-{
-    return d.least && type != TESSEL_F32 && tokens * (((int64_t)channels + 7) / 8) >= 1 << 22 ? 4 : 1;
-}
+// Tokens a lane: one, and four where a launch does not hold the threads for one (a row's lanes are up to twice its chunks, of which there are at most 2^32)
+inline int span_rows(int64_t tokens, int channels) { return span_shape(tokens, channels, 1).groups <= UINT32_MAX / 256 ? 1 : 4; }
 
 #define BY_TYPE(type, call) ((type) == TESSEL_BF16 ? call(bf16) : (type) == TESSEL_F16 ? call(f16) : call(float))
 

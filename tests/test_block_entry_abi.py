@@ -54,22 +54,20 @@ def test_embedding_refuses(change, code):
     assert lib.tessel_embedding_backward(C.byref(a), AT, 1 << 50, None) == code
 
 
-@pytest.mark.parametrize("tokens, channels, rate, kind, code", [
-    # rows of more than 256 channels take whole waves, four in a workgroup of which a launch holds 2^24 - 1; others the next power of two of their chunks of eight
-    ((1 << 26) - 4, 257, 0.0, 0, INVALID), ((1 << 26) - 3, 257, 0.0, 0, TOOBIG), (80000000, 257, 0.0, 0, TOOBIG), (100000000, 257, 0.5, 2, TOOBIG), ((1 << 26) - 4, 512, 0.0, 0, INVALID),
-    ((1 << 25) - 2, 513, 0.5, 2, INVALID), ((1 << 25) - 1, 513, 0.5, 2, TOOBIG), ((1 << 30) - 64, 17, 0.0, 1, INVALID), ((1 << 30) - 63, 17, 0.0, 1, TOOBIG),
-    (1200000000, 17, 0.0, 1, TOOBIG), (1200000000, 24, 0.5, 2, TOOBIG), ((1 << 31) - 1, 9, 0.0, 0, TOOBIG), ((1 << 31) - 128, 9, 0.0, 0, INVALID), ((1 << 31) - 1, 8, 0.0, 0, INVALID),
-    # four tokens a lane
-    (100000000, 257, 0.5, 0, INVALID), (1200000000, 17, 0.5, 1, INVALID),
+@pytest.mark.parametrize("rate", [0.0, 0.5])
+@pytest.mark.parametrize("tokens, channels, code", [
+    # 2^32 - 256 chunks of eight channels, in rows that leave none, and nearly half, of their lanes over
+    ((1 << 31) - 128, 16, INVALID), ((1 << 31) - 127, 16, TOOBIG), (1431655680, 17, INVALID), (1431655681, 17, TOOBIG), (1200000000, 24, INVALID), (80000000, 257, INVALID), (130150516, 257, INVALID),
+    (130150517, 257, TOOBIG), ((1 << 26) - 4, 512, INVALID), (1 << 26, 512, TOOBIG), (66076416, 513, INVALID), (66076417, 513, TOOBIG), ((1 << 31) - 128, 9, INVALID),
 ])
-def test_rows_of_more_lanes_than_a_launch_holds(tokens, channels, rate, kind, code):
-    """TOOBIG is counted by the threads that a launch takes, not by the chunks of eight channels that there are.  (INVALID: a table and rows that are not there, looked for behind
-    the sizes.)"""
+def test_rows_of_as_many_chunks_as_a_launch_has_threads(tokens, channels, rate, code):
+    """(INVALID: a table and rows that are not there, looked for behind the sizes.)"""
     none = B.Rows(None, 0)
-    a = B.DropoutRows(type=kind, channels=channels, tokens=tokens, x=none, y=none, drop=drop(rate=rate))
-    assert B._library().tessel_dropout_apply(C.byref(a), None) == code
-    a = embedding(type=kind, channels=channels, tokens=tokens, table=none, out=none, drop=drop(rate=rate))
-    assert B._library().tessel_embedding_forward(C.byref(a), None) == code
+    for kind in range(3):
+        a = B.DropoutRows(type=kind, channels=channels, tokens=tokens, x=none, y=none, drop=drop(rate=rate))
+        assert B._library().tessel_dropout_apply(C.byref(a), None) == code
+        a = embedding(type=kind, channels=channels, tokens=tokens, table=none, out=none, drop=drop(rate=rate))
+        assert B._library().tessel_embedding_forward(C.byref(a), None) == code
 
 
 def test_embedding_passes_refuse_their_own():

@@ -1,5 +1,6 @@
-"""Dropout and the embedding of batches so large that a lane takes four tokens (16 bits, 2^22 chunks of eight channels and more), whose numbers of tokens are no multiples of what
-a lane or a wave takes; and gradients of shards whose rows go on over many runs, with factors that 32 bits round."""
+"""Dropout and the embedding of batches so large that a lane takes four tokens -- the lookup with dropout in 16 bits from 2^22 chunks of eight channels on, both where rows take more
+lanes than a launch has -- whose numbers of tokens are no multiples of what a lane or a wave takes; and gradients of shards whose rows go on over many runs, with
+factors that 32 bits round."""
 import numpy as np
 import pytest
 import torch
@@ -58,6 +59,35 @@ def test_lookup(ops, n, c, dtype):
     there = (rows >= 0) & (rows < 50)
     want = torch.where(there[:, None], table.cpu().float()[rows.clamp(0, 49)] * torch.tensor(1.7), torch.zeros(()))
     assert torch.equal(got[at].cpu(), dropped_at(at, want, 0.3, 99, 1 << 40).to(dtype))
+
+
+# a workgroup more than a launch holds with a token a lane, and some tokens more
+FARTHEST = [((1 << 26) + 1, 257), ((1 << 26) + 1030, 264), ((1 << 30) + 67, 17)]
+
+
+@pytest.mark.parametrize("n, c", FARTHEST)
+def test_dropout_of_more_lanes_than_a_launch_has(ops, n, c):
+    """all values with nothing dropped; with dropout the first and the last rows, and what is kept of all"""
+    gen = torch.Generator(device="cuda").manual_seed(c)
+    x = torch.empty(n, c, dtype=torch.bfloat16, device="cuda").uniform_(1, 2, generator=gen)
+    y = ops.dropout(x, ops.Dropout(0.0, 1))
+    step = 1 << 24
+    assert all(torch.equal(x[t:t + step], y[t:t + step]) for t in range(0, n, step))
+    del y
+    at, y = some(n), ops.dropout(x, ops.Dropout(0.3, 5, 6))
+    assert torch.equal(y[at].cpu(), dropped_at(at, x[at].cpu().float(), 0.3, 5, 6).bfloat16())
+    kept = [(int((y[t:t + step] != 0).sum()), y[t:t + step].numel()) for t in range(0, n, step)]
+    # (each a sum of m draws of 0.7: more than eight deviations off once in 10^15)
+    assert all(abs(k - 0.7 * m) < 8 * (0.21 * m) ** 0.5 for k, m in kept)
+
+
+@pytest.mark.parametrize("n, c", FARTHEST)
+def test_lookup_of_more_lanes_than_a_launch_has(ops, n, c):
+    table = torch.randn(7, c, generator=torch.Generator().manual_seed(c)).bfloat16()
+    token = torch.randint(0, 9, (n,), dtype=torch.int32, device="cuda")
+    out, step, g = ops.embed(token, table.cuda(), 0.5), 1 << 24, table.cuda()
+    rows = torch.cat((g * 0.5, torch.zeros(2, c, dtype=torch.bfloat16, device="cuda")))
+    assert all(torch.equal(out[t:t + step], rows[token[t:t + step]]) for t in range(0, n, step))
 
 
 @pytest.mark.parametrize("n, c", [(700, 64), (3000, 1003), (20000, 40)])
