@@ -114,8 +114,16 @@ inline SpanShape span_shape(int64_t tokens, int channels, int rows)
     s.groups = ((tokens + at_once - 1) / at_once * tiles + 3) / 4;
     return s;
 }
-// Tokens a lane: one, and four where a launch does not hold the threads for one (a row's lanes are up to twice its chunks, of which there are at most 2^32)
-inline int span_rows(int64_t tokens, int channels) { return span_shape(tokens, channels, 1).groups <= UINT32_MAX / 256 ? 1 : 4; }
+// Tokens a lane: four where dropout of 16-bit values would else hold memory up, as their columns are worked out once for all, or where a launch does not hold the threads for one
+// (a row's lanes are up to twice its chunks, of which there are at most 2^32); else one.  A dropout's reads wait for nothing, so that this is so for rows of up to 256 channels alone
+// (`widest`); the lookup's wait for its tokens.  Four and one, every call on other memory: dropout of 2^22 chunks in rows of 1 channel 17.2 and 20.9 us, 9: 27.8 and 30.4, 256: 27.3 and
+// 28.0, 4096: 27.7 and 26.6; of 2^24 x 1 57 and 74; lookup with dropout of 2^22 in rows of 64 27.6 and 32.3, 4096: 28.7 and 30.4.  2^20 chunks the same or up to 14 % slower by fours, 2^21 between -15 and
+// +13 % by width and operator; 32 bits 5 % slower.
+inline int span_rows(int type, int64_t tokens, int channels, const DropLaunch &d, int widest)
+{
+    const bool held_up = d.least && type != TESSEL_F32 && channels <= widest && tokens * (((int64_t)channels + 7) / 8) >= 1 << 22;
+    return held_up || span_shape(tokens, channels, 1).groups > UINT32_MAX / 256 ? 4 : 1;
+}
 
 #define BY_TYPE(type, call) ((type) == TESSEL_BF16 ? call(bf16) : (type) == TESSEL_F16 ? call(f16) : call(float))
 

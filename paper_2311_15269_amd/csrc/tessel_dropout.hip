@@ -1,8 +1,8 @@
 // Dropout whose mask is never stored (formulas: include/tessel_block_ops.h): one pass, eight channels a lane.
 //
 // Bound by memory: 8192 x 4096 bf16 in 21.2 us (134 MB, 6.3 TB/s), 26.6 where every call is on other memory than the last (5.0 TB/s, a large copy's rate); 4999 x 1003 in 32 bits
-// in 7.7 (5.2 TB/s, 2.3 of them the launch and the first reads).  A token a lane: four, of which a lane's columns are worked out once, take 23 and 27.7 us.  Philox's two counters for eight values are 64 instructions behind what their columns share, half of the time that
-// memory leaves.
+// in 7.7 (5.2 TB/s, 2.3 of them the launch and the first reads).  Philox's two counters for eight values are 64 instructions behind what their columns share, half of the time
+// that memory leaves; rows of few channels, of which a counter of four words serves one to four values, are bound by it (2^24 x 1 in 57 us, 1.2 TB/s).
 #include "tessel_draw.h"
 
 namespace tessel {
@@ -33,7 +33,7 @@ int launch_dropout(const tessel_dropout_rows &a, const DropLaunch &d, void *stre
 {
     tessel_dropout_rows aa = a;
     DropLaunch dd = d;
-    const int rows = span_rows(a.tokens, a.channels);
+    const int rows = span_rows(a.type, a.tokens, a.channels, d, 256);
     SpanShape s = span_shape(a.tokens, a.channels, rows);
     void *args[] = {&aa, &dd, &s.lanes};
 #define KERNEL(T) (s.wide ? rows == 4 ? (const void *)dropout_kernel<T, true, 4> : (const void *)dropout_kernel<T, true, 1> \

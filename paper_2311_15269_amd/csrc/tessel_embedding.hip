@@ -513,19 +513,11 @@ __global__ __launch_bounds__(kSortThreads) void join_kernel(EmbedLaunch l, int l
         if (col + j < a.channels) to[j] = old[j] + a.scale * sum[j];
 }
 
-// Tokens a lane: four, of which a lane's columns are worked out once, also where dropout of 16-bit values would else hold a large lookup up.  Every call on other memory, four and one:
-// 16384 x 1024 (2^21 chunks) 16.0 and 16.9 us, 8192 x 4096 (2^22) 28.7 and 30.4, 16384 x 4096 (2^23) 51 and 57; 2^20 chunks 10.7 and 10.3.  (A dropout by itself is 2 to 5 % slower
-// by fours: its reads wait for nothing.)
-static int lookup_rows(const tessel_embedding &a, const DropLaunch &d)
-{
-    return d.least && a.type != TESSEL_F32 && a.tokens * (((int64_t)a.channels + 7) / 8) >= 1 << 22 ? 4 : span_rows(a.tokens, a.channels);
-}
-
 int launch_embed(const tessel_embedding &a, const DropLaunch &d, void *stream)
 {
     tessel_embedding aa = a;
     DropLaunch dd = d;
-    const int rows = lookup_rows(a, d);
+    const int rows = span_rows(a.type, a.tokens, a.channels, d, INT32_MAX);
     SpanShape s = span_shape(a.tokens, a.channels, rows);
     void *args[] = {&aa, &dd, &s.lanes};
 #define KERNEL(T) (s.wide ? rows == 4 ? (const void *)embed_kernel<T, true, 4> : (const void *)embed_kernel<T, true, 1> \

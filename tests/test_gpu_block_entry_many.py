@@ -1,5 +1,5 @@
-"""Dropout and the embedding of batches so large that a lane takes four tokens -- the lookup with dropout in 16 bits from 2^22 chunks of eight channels on, both where rows take more
-lanes than a launch has -- whose numbers of tokens are no multiples of what a lane or a wave takes; and gradients of shards whose rows go on over many runs, with
+"""Dropout and the embedding of batches so large that a lane takes four tokens -- in 16 bits with dropout from 2^22 chunks of eight channels on, a dropout by itself in rows of up to 256 channels, and
+wherever rows take more lanes than a launch has -- whose numbers of tokens are no multiples of what a lane or a wave takes; and gradients of shards whose rows go on over many runs, with
 factors that 32 bits round."""
 import numpy as np
 import pytest
