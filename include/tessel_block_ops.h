@@ -198,10 +198,11 @@ int  tessel_dropout_apply(const tessel_dropout_rows *a, void *hip_stream);
 
 /* ---- the embedding -----------------------------------------------------------------------------------------------
  * The table holds the rows first .. first + rows - 1 of a vocabulary (all of it, or the shard of one of the devices that an embedding is
- * spread over).  With v = token_t - first, D the dropout of `drop` and sums over t in ascending order, in 32 bits:
+ * spread over).  With v = token_t - first, D the dropout of `drop` and sums over t in 32 bits, in an order that follows from tokens, shard and channels alone
+ * (ascending in pieces, and these in a fixed order: the same bits each time, but not those of another shard that holds the row):
  *     out_t = D(scale table_v) where 0 <= v < rows, else 0;    dtable_v = scale sum of D(d_out_t) over all t with token_t - first = v.
  * A token of another shard, or of none (any number below 0), so gets a row of zeros, which the shards add up to the whole, and no
- * gradient; its row of d_out is not read. */
+ * gradient; its row of d_out counts for nothing, whatever it holds. */
 enum { TESSEL_I32 = 0, TESSEL_I64 = 1 };
 typedef struct {
     int32_t  type;          /* of table, out and d_out                                                     */
@@ -232,7 +233,7 @@ int  tessel_embedding_backward(const tessel_embedding *a, void *workspace_dev, s
  *     (a, b) -> (a cos - b sin, a sin + b cos),
  * pair i being channels (i, i + turning / 2) or, with `neighbours`, (2 i, 2 i + 1); the others stay.  Angles are reduced in
  * 64 bits, far ones in two parts of 64, so that up to 2^70 radians (a frequency of 100 at the last position) no more than their fraction of a turn is rounded, to
- * 32 bits; all else in 32 bits, rounded once.  Backward from the gradients of the results and z:
+ * 32 bits; all else in 32 bits, rounded once (a head whose squares add up to 2^128 or more is divided by infinity).  Backward from the gradients of the results and z:
  * gradients of z, and of wq and wk, sums over tokens and heads in 32 bits.  Infinities and NaN of a head stay in that head (and
  * reach the gradients of w). */
 typedef struct {

@@ -194,8 +194,8 @@ def _same(like, shape, *tensors):
 
 
 def _heads(t):
-    """a [tokens, heads, dim] tensor: start and strides.  One whose last dimension is not contiguous, or whose strides or start are not
-    multiples of 16 bytes, is refused."""
+    """a [tokens, heads, dim] tensor: start and strides.  One whose last dimension is not contiguous is refused (by the attention in the library also one whose strides or
+    start are not multiples of 16 bytes)."""
     n, heads, dim = t.shape
     token, head, last = t.stride()
     if last != 1 and dim > 1:
@@ -611,7 +611,8 @@ def embed(tokens, table, scale=1.0, first=0, drop=None):
 
 def embed_backward(d_out, tokens, rows, scale=1.0, first=0, drop=None, into=None):
     """tessel_embedding_backward: the gradient [rows, channels] of the table in 32 bits from that of what embed() gave; added to `into` (and that
-    returned) if it is given, of which rows that no token asked for are neither read nor written"""
+    returned) if it is given, of which rows that no token asked for are neither read nor written.  The same bits each time; the rows of one shard are not
+    added up in the order of another that holds them."""
     import torch
     lib = _library()
     _on_gpu(d_out, ("tokens", "channels"))

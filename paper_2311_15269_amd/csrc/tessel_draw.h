@@ -118,7 +118,8 @@ inline SpanShape span_shape(int64_t tokens, int channels, int rows)
 // (a row's lanes are up to twice its chunks, of which there are at most 2^32); else one.  A dropout's reads wait for nothing, so that this is so for rows of up to 256 channels alone
 // (`widest`); the lookup's wait for its tokens.  Four and one, every call on other memory: dropout of 2^22 chunks in rows of 1 channel 17.2 and 20.9 us, 9: 27.8 and 30.4, 256: 27.3 and
 // 28.0, 4096: 27.7 and 26.6; of 2^24 x 1 57 and 74; lookup with dropout of 2^22 in rows of 64 27.6 and 32.3, 4096: 28.7 and 30.4.  2^20 chunks the same or up to 14 % slower by fours, 2^21 between -15 and
-// +13 % by width and operator; 32 bits 5 % slower.
+// +13 % by width and operator; 32 bits 5 % slower.  (8192 x 4096 twice, waited for behind both: 62.7 and 63.4, in a row
+// 51.2 and 49.9.)
 inline int span_rows(int type, int64_t tokens, int channels, const DropLaunch &d, int widest)
 {
     const bool held_up = d.least && type != TESSEL_F32 && channels <= widest && tokens * (((int64_t)channels + 7) / 8) >= 1 << 22;

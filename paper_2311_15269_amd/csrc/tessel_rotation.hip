@@ -5,7 +5,7 @@
 // it works out first, one a lane, and passes them around through LDS: all heads of a token share them.  Backward, a lane adds up the
 // gradients of w for its channels over all that its wave goes over; then groups, waves and, by a second kernel, workgroups, in order.
 //
-// Bound by memory: 8192 tokens of 32 + 8 heads of 128 bf16 forward 32 us (168 MB, 5.2 TB/s; a copy of as much by the dropout's kernel 26, by the library's 29.5, and this kernel's
+// Bound by memory: 8192 tokens of 32 + 8 heads of 128 bf16 forward 33 us (168 MB, 5.1 TB/s; a copy of as much by the dropout's kernel 26, by the library's 29.5, and this kernel's
 // own without norms and angles 32: the way it goes through memory, not its arithmetic), backward 54 (252 MB, 4.7 TB/s: 16 waves a compute unit have too little
 // under way; registers allow no more, and reads a step ahead cost more registers than they give, 67 us) and 4.6 for the second kernel.  One token
 // takes 3.4 us, a launch.
