@@ -115,11 +115,10 @@ inline SpanShape span_shape(int64_t tokens, int channels, int rows)
     return s;
 }
 // Tokens a lane: four where dropout of 16-bit values would else hold memory up, as their columns are worked out once for all, or where a launch does not hold the threads for one
-// (a row's lanes are up to twice its chunks, of which there are at most 2^32); else one.  A dropout's reads wait for nothing, so that this is so for rows of up to 256 channels alone
-// (`widest`); the lookup's wait for its tokens.  Four and one, every call on other memory: dropout of 2^22 chunks in rows of 1 channel 17.2 and 20.9 us, 9: 27.8 and 30.4, 256: 27.3 and
-// 28.0, 4096: 27.7 and 26.6; of 2^24 x 1 57 and 74; lookup with dropout of 2^22 in rows of 64 27.6 and 32.3, 4096: 28.7 and 30.4.  2^20 chunks the same or up to 14 % slower by fours, 2^21 between -15 and
-// +13 % by width and operator; 32 bits 5 % slower.  (8192 x 4096 twice, waited for behind both: 62.7 and 63.4, in a row
-// 51.2 and 49.9.)
+// (a row's lanes are up to twice its chunks, of which there are at most 2^32); else one.  The lookup's reads wait for its tokens, a dropout's for nothing, which so gains in rows of up
+// to 256 channels alone (`widest`).  By fours and by ones, every call on other memory, 2^22 chunks of bf16: dropout of rows of 1 channel 17.2 and 20.9 us, 9: 27.8 and 30.4, 256: 27.3
+// and 28.0, 4096: 27.7 and 26.6 (a pass of two, waited for: 62.7 and 63.4); lookup with dropout of rows of 64 27.6 and 32.3, 4096: 28.7 and 30.4.  2^24 x 1: 57 and 74.  Of 2^20 chunks fours are the
+// same or up to 14 % slower, of 2^21 15 % faster to 13 % slower by width and operator, in 32 bits some 5 % slower.
 inline int span_rows(int type, int64_t tokens, int channels, const DropLaunch &d, int widest)
 {
     const bool held_up = d.least && type != TESSEL_F32 && channels <= widest && tokens * (((int64_t)channels + 7) / 8) >= 1 << 22;

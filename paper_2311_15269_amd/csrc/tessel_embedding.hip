@@ -2,8 +2,9 @@
 //
 // Forward: a gather, eight channels of a token a lane, scaled and dropped on its way.  Backward: a sum over the tokens of each row.  Adding them up with atomics would
 // make their order, and with it the bits, chance; so the places of the batch are sorted by row first, stably, and every sum goes over its places in ascending
-// order, in pieces whose bounds, and the order in which they are joined, do not depend on what runs when (but on where the row lies among the shard's others).  The sort is by buckets of rows with the same low bits, a workgroup each, which all read the
-// whole batch (T tokens 256 times, from the caches) and need nothing from each other: one launch, where a sort by digits takes three a digit.
+// order, in pieces whose bounds, and the order in which they are joined, do not depend on what runs when (but on where the row lies among the shard's others).  The
+// sort is by buckets of rows with the same low bits, a workgroup each, which all read the whole batch (T tokens 256 times, from the caches) and need nothing from
+// each other: one launch, where a sort by digits takes three a digit.
 //
 // Bound by memory but for the way through the launches.  Forward, 8192 tokens of 4096 bf16: 17 us (100 MB, 5.8 TB/s), with dropout 21; 16384 of 1024 f16 10.  Backward,
 // the same 8192 tokens into 50000 rows of which some 3700 occur: sort 8.8 us, sums and zeros 165 (886 MB, 5.4 TB/s; zeros alone 5.8), join 8; 16384 tokens added

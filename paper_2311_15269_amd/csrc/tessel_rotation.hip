@@ -82,7 +82,7 @@ __device__ __forceinline__ void angles(const tessel_rotation &a, int64_t token, 
         const int t = i / half, p = i - t * half;
         const int64_t n = min(token + t, a.tokens - 1);
         const double position = a.index_type == TESSEL_I64 ? (double)((const int64_t *)a.position)[n] : (double)((const int32_t *)a.position)[n];
-        double turns = position * a.frequency[p] * 0.15915494309189535;                  // angle / (2 pi), off by 2^-52 of it: less than 2^-30 where it is near
+        double turns = position * a.frequency[p] * 0.15915494309189535;                  // angle / (2 pi), off by up to 2^-51 of it: 2^-29 where it is near
         const double whole = rint(turns);
         if (__builtin_expect(fabs(turns) < 0x1p22, 1)) {
             turns -= whole;
